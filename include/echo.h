@@ -12,10 +12,14 @@
  *   echo_compose               timeline composer (Sec. 4.2) + validator adjustment (Sec. 3, 6)
  *   echo_read_*                per-op start/finish, step makespan, CC estimates
  *
+ * Beside it, echo_embed, echo_layer_norm, echo_orthogonalize and their gradients run
+ * operators of a training step on the device, whose measured times are such durations.
+ *
  * Conventions for every call:
  *   - The return value is an echo_status; ECHO_OK (0) on success.  On failure the
  *     context keeps its previous state and echo_last_error() describes the cause.
- *   - Array arguments are caller-owned HOST memory unless stated otherwise.  They
+ *   - Array arguments are caller-owned HOST memory unless stated otherwise (the
+ *     operators' are device memory).  They
  *     are read (or written) during the call only; nothing keeps a pointer to them.
  *     Pinned (page-locked) host memory makes the copies faster but is not required,
  *     and neither is any alignment.
@@ -343,6 +347,125 @@ int echo_read_profile(echo_ctx *ctx, echo_kernel_stat *out, int cap, int *n);
  * setting of the device; the calling thread's current device is restored.
  * Allocates and frees 8 bytes. */
 int echo_measure_fp64(int device, double *rates);
+
+/*
+ * Operators of a rank's training step.  An execution graph's compute ops stand for
+ * kernels whose durations a tracer measures on one device (Sec. 4.1); these calls run
+ * the memory-bound and optimizer ones among them on this device, so that their times
+ * (echo_set_profiling, echo_read_profile) can go into echo_load_scenarios.
+ *   - Arrays are DEVICE memory of the context's device, owned by the caller, each at a
+ *     multiple of its element size.  Matrices are rows of contiguous elements, `stride`
+ *     elements apart: at least the row's length for outputs, any value >= 0 for inputs.
+ *   - Work is enqueued on the context's stream and is not waited for.  Scratch memory
+ *     belongs to the context and grows on the first call of a size (that call allocates,
+ *     so make it before a stream capture); calls on one context share it in stream order.
+ *   - They need no graph or scenarios and leave those of the context as they are.
+ *   - Outputs overlap no other array, except where a call says so.
+ *   - Sums, statistics and products accumulate in fp32; results are rounded once, to the
+ *     type of the output.  Every call gives the same bits for the same inputs.
+ *   - NULL or misplaced pointers, unknown types, bad sizes or strides:
+ *     ECHO_E_INVALID_ARG, with nothing enqueued; sizes beyond what a call states:
+ *     ECHO_E_UNSUPPORTED.
+ */
+enum { ECHO_F32 = 0, ECHO_BF16 = 1, ECHO_F16 = 2 };
+
+/* The stream the context enqueues on (its own, or the one given to echo_create), for
+ * ordering other work with the operators'. */
+int echo_stream_get(echo_ctx *ctx, void **cuda_stream);
+
+/* Embedding lookup (kernel class of the first pipeline stage) in a vocabulary shard:
+ *   out[t][:] = scale * table[ids[t] - vocab_start][:]
+ * for the ids of the shard's rows [vocab_start, vocab_start + vocab_rows), and zeros for
+ * every other id: a tensor-parallel rank's part of the sum over ranks, or padding.
+ * n_tokens and vocab_rows may be 0; hidden is 1 to 2^30. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start;
+  const void *ids;   /* [n_tokens] int32 or int64                                       */
+  const void *table; /* [vocab_rows][hidden]                                            */
+  void *out;         /* [n_tokens][hidden]                                              */
+  int64_t table_stride, out_stride;
+  int32_t id_bits;   /* 32 or 64                                                        */
+  int32_t table_type, out_type; /* ECHO_F32, ECHO_BF16, ECHO_F16                        */
+  float scale;
+} echo_embed_desc;
+int echo_embed(echo_ctx *ctx, const echo_embed_desc *d);
+
+/* Gradient of echo_embed for its table:
+ *   dtable[v][:] = scale * sum of dy[t][:] over the tokens t with ids[t] - vocab_start = v,
+ * summed in an order that the sizes alone fix.  accumulate = 0 writes every row (zeros
+ * where no token has it); accumulate = 1 adds to dtable and touches only rows that a token
+ * has (a main gradient over micro-batches).  n_tokens at most 2^31 - 1, vocab_rows at most
+ * 2^31 - 2. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start;
+  const void *ids; /* [n_tokens] int32 or int64                                         */
+  const void *dy;  /* [n_tokens][hidden]                                                */
+  void *dtable;    /* [vocab_rows][hidden]                                              */
+  int64_t dy_stride, dtable_stride;
+  int32_t id_bits;
+  int32_t dy_type, dtable_type;
+  int32_t accumulate;
+  float scale;
+} echo_embed_grad_desc;
+int echo_embed_grad(echo_ctx *ctx, const echo_embed_grad_desc *d);
+
+/* Layer norm over rows of `hidden` elements:
+ *   mean = sum(x) / hidden, rstd = 1 / sqrt(sum((x - mean)^2) / hidden + eps),
+ *   y = (x - mean) * rstd * weight + bias.
+ * y has x's type and may be x itself (same address and stride).  weight and bias may be
+ * NULL (1 and 0); mean and rstd (fp32, [rows], what the gradient needs) may be NULL. */
+typedef struct {
+  int64_t rows, hidden; /* rows >= 0, hidden 1 to 2^30                                  */
+  const void *x;
+  void *y;
+  const void *weight, *bias; /* [hidden] of param_type, or NULL                         */
+  float *mean, *rstd;        /* [rows] or NULL                                          */
+  int64_t x_stride, y_stride;
+  int32_t x_type, param_type;
+  float eps; /* >= 0                                                                    */
+} echo_layer_norm_desc;
+int echo_layer_norm(echo_ctx *ctx, const echo_layer_norm_desc *d);
+
+/* Gradients of echo_layer_norm.  With xh = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - sum(g) / hidden - xh * sum(g * xh) / hidden)   (per row),
+ *   dweight = sum of dy * xh over the rows, dbias = sum of dy over the rows,
+ * the last two written (accumulate = 0; zeros when rows is 0) or added to (1).  dx has
+ * x's type and may be dy or x itself.  Each of dx, dweight and dbias may be NULL: then it
+ * is not computed. */
+typedef struct {
+  int64_t rows, hidden;
+  const void *dy, *x;
+  const void *weight;       /* [hidden] of param_type, or NULL (1)                      */
+  const float *mean, *rstd; /* [rows], of the forward pass                              */
+  void *dx;
+  void *dweight, *dbias;    /* [hidden] of param_type                                   */
+  int64_t dy_stride, x_stride, dx_stride;
+  int32_t x_type;           /* of dy, x and dx                                          */
+  int32_t param_type;
+  int32_t accumulate;
+} echo_layer_norm_grad_desc;
+int echo_layer_norm_grad(echo_ctx *ctx, const echo_layer_norm_grad_desc *d);
+
+/* Orthogonalised update of a matrix optimizer (kernel class of the optimizer step), by
+ * Newton-Schulz products.  For each matrix G of the batch, taken transposed when it has
+ * more rows than columns:
+ *   X = G / (|G| + eps), |G| the Frobenius norm;
+ *   `steps` times: A = X X^T, X = a X + (b A + c A A) X;
+ *   O = scale * X (transposed back).
+ * fp32 matrices are multiplied as sums of two fp16 numbers (22 bits), 16-bit ones as fp16
+ * (11 bits); sums are in fp32.  (a, b, c) has to keep singular values in [0, 1] within
+ * [0, 2] over the steps, as the usual quintics do; a matrix with an infinite or NaN element gives NaN.
+ * rows and cols are 1 to 65536, steps 0 to 64. */
+typedef struct {
+  int64_t batch, rows, cols;
+  const void *g;                   /* matrix i begins at g + i * g_batch_stride         */
+  void *o;                         /* of g's type; may be g itself (same strides)       */
+  int64_t g_stride, g_batch_stride, o_stride, o_batch_stride;
+  int32_t type;
+  int32_t steps;
+  float a, b, c, eps, scale;
+} echo_orthogonalize_desc;
+int echo_orthogonalize(echo_ctx *ctx, const echo_orthogonalize_desc *d);
 
 const char *echo_strerror(int status);
 /* Copies the context's last error message (NUL-terminated) into buf. */

@@ -20,6 +20,7 @@
 #include "echo.h"
 #include "echo_align.h"
 #include "echo_internal.h"
+#include "echo_ops.h"
 
 using echo::CcSig;
 using echo::ChunkTable;
@@ -1580,6 +1581,9 @@ struct echo_ctx {
   // scratch for readback / queries
   void *stage = nullptr;
   size_t stage_bytes = 0;
+  // scratch of the operators (echo_ops.cpp)
+  void *ops = nullptr;
+  size_t ops_bytes = 0;
   // profiling
   bool prof = false;
   std::vector<std::pair<std::string, std::pair<cudaEvent_t, cudaEvent_t>>> recs;
@@ -1874,6 +1878,49 @@ int activate_fold(echo_ctx *c, bool want) {
 
 }  // namespace
 
+// -- what the operators use of a context (echo_ops.h) ----------------------------------------
+namespace echo {
+
+int op_begin(echo_ctx *c, OpContext *o) {
+  const int rc = check_ctx(c);
+  if (!rc) *o = {c->device, c->sms, c->stream};
+  return rc;
+}
+int op_error(echo_ctx *c, int code, const std::string &msg) { return set_err(c, code, msg); }
+int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what) { return cuda_fail(c, e, what); }
+
+int op_scratch(echo_ctx *c, size_t bytes, void **p) {
+  if (c->ops_bytes < bytes) {
+    if (c->ops) {
+      CK(cudaStreamSynchronize(c->stream), "waiting for the work that uses the scratch");
+      cudaFree(c->ops);
+    }
+    c->ops = nullptr;
+    c->ops_bytes = 0;
+    if (cudaMalloc(&c->ops, bytes) != cudaSuccess) {
+      (void)cudaGetLastError();
+      c->ops = nullptr;
+      return set_err(c, ECHO_E_OOM, "cudaMalloc of " + std::to_string(bytes) + " bytes of scratch failed");
+    }
+    c->ops_bytes = bytes;
+  }
+  *p = c->ops;
+  return ECHO_OK;
+}
+
+bool op_device_memory(echo_ctx *c, const void *p) {
+  cudaPointerAttributes at{};
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == c->device);
+}
+
+cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch) { return timed(c, name, launch); }
+
+}  // namespace echo
+
 extern "C" {
 
 const char *echo_strerror(int s) {
@@ -1959,6 +2006,7 @@ int echo_destroy(echo_ctx *c) {
   free_all(c->fold_allocs);
   free_all(c->raw_allocs);
   if (c->stage) cudaFree(c->stage);
+  if (c->ops) cudaFree(c->ops);
   for (auto &r : c->recs) {
     cudaEventDestroy(r.second.first);
     cudaEventDestroy(r.second.second);

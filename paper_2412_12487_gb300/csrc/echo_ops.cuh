@@ -1,0 +1,96 @@
+// echo_ops.cuh -- element types, pieces of rows and sums over threads, for the operators'
+// kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+#include "echo.h"
+
+namespace echo {
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f(float x);
+template <>
+__device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+
+// A piece: W consecutive elements of a row, at a multiple of the piece's size (16 bytes at
+// most: a larger one is several loads).  Rows that cannot be cut into wide pieces (an odd
+// length, stride or address) are cut into narrower ones; neighbouring threads always take
+// neighbouring pieces.
+template <typename T, int W>
+struct alignas(sizeof(T) * W <= 16 ? sizeof(T) * W : 16) Pack {
+  T v[W];
+};
+template <typename T, int W>
+__device__ __forceinline__ void unpack(const Pack<T, W> &p, float *f) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) f[i] = to_f(p.v[i]);
+}
+template <typename T, int W>
+__device__ __forceinline__ Pack<T, W> pack(const float *f) {
+  Pack<T, W> p;
+#pragma unroll
+  for (int i = 0; i < W; ++i) p.v[i] = from_f<T>(f[i]);
+  return p;
+}
+template <int W, typename T>
+__device__ __forceinline__ void load_piece(const T *at, float *f) {
+  unpack<T, W>(*reinterpret_cast<const Pack<T, W> *>(at), f);
+}
+template <int W, typename T>
+__device__ __forceinline__ void store_piece(T *at, const float *f) {
+  *reinterpret_cast<Pack<T, W> *>(at) = pack<T, W>(f);
+}
+
+// Piece of a vector of parameters whose type is known at run time; `none` without one.
+template <int W>
+__device__ __forceinline__ void load_param(const void *p, int type, int64_t j, float none, float *f) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[i] = none;
+  } else if (type == ECHO_F32) {
+    load_piece<W>(static_cast<const float *>(p) + j, f);
+  } else if (type == ECHO_BF16) {
+    load_piece<W>(static_cast<const __nv_bfloat16 *>(p) + j, f);
+  } else {
+    load_piece<W>(static_cast<const __half *>(p) + j, f);
+  }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+constexpr int type_bytes(int type) { return type == ECHO_F32 ? 4 : 2; }
+
+// Whether rows `stride` elements apart can be read in pieces of W elements.
+inline bool fits_pieces(const void *p, int64_t stride, int type, int W) {
+  const int64_t a = std::min<int64_t>(16, (int64_t)type_bytes(type) * W);
+  return reinterpret_cast<uintptr_t>(p) % a == 0 && stride * type_bytes(type) % a == 0;
+}
+
+// f(an element of the type)
+template <typename F>
+auto with_type(int type, F &&f) {
+  if (type == ECHO_F32) return f(float{});
+  if (type == ECHO_BF16) return f(__nv_bfloat16{});
+  return f(__half{});
+}
+template <int I>
+struct Int {
+  static constexpr int value = I;
+};
+
+}  // namespace echo

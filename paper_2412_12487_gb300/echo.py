@@ -24,7 +24,8 @@ EXPORTS = ["echo_create", "echo_destroy", "echo_check_graph", "echo_check_replic
            "echo_estimate_collectives", "echo_compose", "echo_read_times", "echo_read_makespan",
            "echo_read_cc", "echo_read_overlap", "echo_cc_query", "echo_cc_query_noalloc",
            "echo_graph_info_get", "echo_set_cc_model",
-           "echo_set_profiling", "echo_read_profile", "echo_measure_fp64", "echo_strerror", "echo_last_error"]
+           "echo_set_profiling", "echo_read_profile", "echo_measure_fp64", "echo_strerror", "echo_last_error",
+           "echo_stream_get", "echo_embed", "echo_embed_grad", "echo_layer_norm", "echo_layer_norm_grad", "echo_orthogonalize"]
 
 
 class EchoError(RuntimeError):
@@ -85,6 +86,44 @@ class KernelStat(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("total_ms", C.c_double)]
 
 
+class EmbedDesc(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("hidden", C.c_int64), ("vocab_rows", C.c_int64), ("vocab_start", C.c_int64),
+                ("ids", C.c_void_p), ("table", C.c_void_p), ("out", C.c_void_p),
+                ("table_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("id_bits", C.c_int32), ("table_type", C.c_int32), ("out_type", C.c_int32), ("scale", C.c_float)]
+
+
+class EmbedGradDesc(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("hidden", C.c_int64), ("vocab_rows", C.c_int64), ("vocab_start", C.c_int64),
+                ("ids", C.c_void_p), ("dy", C.c_void_p), ("dtable", C.c_void_p),
+                ("dy_stride", C.c_int64), ("dtable_stride", C.c_int64),
+                ("id_bits", C.c_int32), ("dy_type", C.c_int32), ("dtable_type", C.c_int32),
+                ("accumulate", C.c_int32), ("scale", C.c_float)]
+
+
+class LayerNormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("hidden", C.c_int64), ("x", C.c_void_p), ("y", C.c_void_p),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("x_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("x_type", C.c_int32), ("param_type", C.c_int32), ("eps", C.c_float)]
+
+
+class LayerNormGradDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("hidden", C.c_int64), ("dy", C.c_void_p), ("x", C.c_void_p),
+                ("weight", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("dx", C.c_void_p),
+                ("dweight", C.c_void_p), ("dbias", C.c_void_p),
+                ("dy_stride", C.c_int64), ("x_stride", C.c_int64), ("dx_stride", C.c_int64),
+                ("x_type", C.c_int32), ("param_type", C.c_int32), ("accumulate", C.c_int32)]
+
+
+class OrthogonalizeDesc(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("g", C.c_void_p), ("o", C.c_void_p),
+                ("g_stride", C.c_int64), ("g_batch_stride", C.c_int64),
+                ("o_stride", C.c_int64), ("o_batch_stride", C.c_int64),
+                ("type", C.c_int32), ("steps", C.c_int32),
+                ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -126,6 +165,12 @@ def load_library(path: Optional[str] = None):
         "echo_measure_fp64": ([C.c_int, vp], C.c_int),
         "echo_strerror": ([C.c_int], C.c_char_p),
         "echo_last_error": ([vp, C.c_char_p, C.c_size_t], C.c_int),
+        "echo_stream_get": ([vp, C.POINTER(vp)], C.c_int),
+        "echo_embed": ([vp, C.POINTER(EmbedDesc)], C.c_int),
+        "echo_embed_grad": ([vp, C.POINTER(EmbedGradDesc)], C.c_int),
+        "echo_layer_norm": ([vp, C.POINTER(LayerNormDesc)], C.c_int),
+        "echo_layer_norm_grad": ([vp, C.POINTER(LayerNormGradDesc)], C.c_int),
+        "echo_orthogonalize": ([vp, C.POINTER(OrthogonalizeDesc)], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -215,6 +260,59 @@ def measure_fp64(device: int = 0) -> Dict[str, float]:
     return {"dadd": float(r[0]), "dmul": float(r[1]), "ddiv": float(r[2])}
 
 
+_types: Dict[object, int] = {}  # torch dtype -> element type of the C ABI (F32, BF16, F16)
+
+
+def _type(dtype) -> int:
+    if not _types:
+        import torch
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise EchoError(1, f"elements of {dtype} are not float32, bfloat16 or float16") from None
+
+
+def _dptr(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _need(ok: bool, msg: str):
+    if not ok:
+        raise EchoError(1, msg)
+
+
+def _matrix(t, out: bool = False):
+    """``t`` as rows of its last dimension: (tensor, rows, row stride).  An input whose rows
+    are not a fixed distance apart, or not contiguous, is copied; an output is refused."""
+    if t.is_contiguous():
+        h = t.shape[-1]
+        return t, t.numel() // h if h else 0, h
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t, t.shape[0], t.stride(0)
+    if t.dim() > 2 and t.stride(-1) == 1:
+        try:
+            v = t.view(-1, t.shape[-1])
+            return v, v.shape[0], v.stride(0)
+        except RuntimeError:
+            pass
+    _need(not out, "an output's rows are not contiguous and a fixed distance apart")
+    return _matrix(t.contiguous())
+
+
+def _batch(t, out: bool = False):
+    """``t`` [..., rows, cols] as a batch of matrices: (tensor, batch, row stride, batch stride)."""
+    if t.is_contiguous():
+        r, c = t.shape[-2:]
+        return t, t.numel() // (r * c) if r * c else 0, c, r * c
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t, 1, t.stride(0), 0
+    if t.dim() == 3 and t.stride(2) == 1:
+        return t, t.shape[0], t.stride(1), t.stride(0)
+    _need(not out, "an output's matrices have no contiguous rows")
+    return _batch(t.contiguous())
+
+
 class Echo:
     """One composer context on one device (see include/echo.h for the semantics)."""
 
@@ -234,8 +332,12 @@ class Echo:
         if rc:
             raise EchoError(rc, "echo_create failed")
         self.h = h
+        self.device = int(device)
         self.n_ops = 0
         self.n_scen = 0
+        s = C.c_void_p()
+        self._check(self.lib.echo_stream_get(h, C.byref(s)))
+        self._stream = int(s.value or 0)
 
     def _check(self, rc: int):
         if rc:
@@ -370,3 +472,127 @@ class Echo:
         n = C.c_int(0)
         self._check(self.lib.echo_read_profile(self.h, buf, 32, C.byref(n)))
         return {buf[i].name.decode(): (int(buf[i].launches), float(buf[i].total_ms)) for i in range(n.value)}
+
+    # -- operators of a training step, on torch tensors of the context's device -----------
+    def _op(self, call, desc):
+        """Enqueues an operator in the order of torch's current stream: where that is not
+        the context's, the context's stream waits for it and it for the operator."""
+        import torch
+        cur = torch.cuda.current_stream(self.device)
+        if (cur.cuda_stream or CUDA_STREAM_LEGACY) == self._stream:
+            self._check(call(self.h, C.byref(desc)))
+            return
+        own = (torch.cuda.default_stream(self.device) if self._stream == CUDA_STREAM_LEGACY
+               else torch.cuda.ExternalStream(self._stream, device=self.device))
+        own.wait_stream(cur)
+        self._check(call(self.h, C.byref(desc)))
+        cur.wait_stream(own)
+
+    @staticmethod
+    def _ids(ids) -> int:
+        bits = {"torch.int64": 64, "torch.int32": 32}.get(str(ids.dtype), 0)
+        _need(bits > 0, "ids are neither int32 nor int64")
+        return bits
+
+    def embed(self, ids, table, scale: float = 1.0, vocab_start: int = 0, dtype=None, out=None):
+        """``scale * table[ids - vocab_start]`` ([..., hidden] for ids [...]), zeros for ids
+        outside the shard of ``table.shape[0]`` rows from ``vocab_start``.  ``dtype`` (the
+        table's by default) is the result's, unless ``out`` takes it."""
+        bits = self._ids(ids)
+        _need(table.dim() == 2, "the table is not a matrix")
+        ids = ids.contiguous()
+        v, h = table.shape
+        if out is None:
+            out = table.new_empty((*ids.shape, h), dtype=dtype or table.dtype)
+        _need(tuple(out.shape) == (*ids.shape, h), "out has another shape than ids and the table's rows")
+        table, _, ts = _matrix(table)
+        o, n, os_ = _matrix(out, out=True)
+        self._op(self.lib.echo_embed, EmbedDesc(n, h, v, vocab_start, ids.data_ptr(), table.data_ptr(), o.data_ptr(), ts, os_, bits,
+                                                _type(table.dtype), _type(o.dtype), scale))
+        return out
+
+    def embed_grad(self, ids, dy, vocab_rows: int, scale: float = 1.0, vocab_start: int = 0, dtype=None, out=None,
+                   accumulate: bool = False):
+        """Gradient of ``embed`` for its table, from ``dy`` [..., hidden]: [vocab_rows, hidden]
+        in ``dtype`` (float32 by default), or in ``out``, which ``accumulate`` adds to."""
+        import torch
+        bits = self._ids(ids)
+        h = dy.shape[-1]
+        _need(tuple(dy.shape[:-1]) == tuple(ids.shape), "dy has another shape than ids and a row")
+        _need(vocab_rows >= 0, "negative sizes")
+        _need(out is not None or not accumulate, "accumulate needs out")
+        if out is None:
+            out = dy.new_empty((vocab_rows, h), dtype=dtype or torch.float32)
+        _need(tuple(out.shape) == (vocab_rows, h), "out has another shape than vocab_rows and a row")
+        ids = ids.contiguous()
+        g, n, gs = _matrix(dy)
+        o, _, os_ = _matrix(out, out=True)
+        self._op(self.lib.echo_embed_grad, EmbedGradDesc(n, h, vocab_rows, vocab_start, ids.data_ptr(), g.data_ptr(), o.data_ptr(), gs, os_, bits,
+                                                         _type(g.dtype), _type(o.dtype), 1 if accumulate else 0, scale))
+        return out
+
+    def layer_norm(self, x, weight=None, bias=None, eps: float = 1e-5, out=None):
+        """(y, mean, rstd) of the rows of ``x`` [..., hidden]; mean and rstd are what
+        ``layer_norm_grad`` needs (float32 [...]).  ``out`` may be ``x``."""
+        import torch
+        h = x.shape[-1]
+        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
+        _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than x")
+        ptype = self._params(h, weight, bias)
+        mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
+        xm, n, xs = _matrix(x)
+        ym, _, ys = _matrix(y, out=True)
+        self._op(self.lib.echo_layer_norm, LayerNormDesc(n, h, xm.data_ptr(), ym.data_ptr(), _dptr(weight), _dptr(bias), mean.data_ptr(),
+                                                         rstd.data_ptr(), xs, ys, _type(x.dtype), ptype, eps))
+        return y, mean, rstd
+
+    def layer_norm_grad(self, dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, accumulate: bool = False):
+        """(dx, dweight, dbias) of ``layer_norm``.  dx may be ``dy`` or ``x``.  dweight and
+        dbias have the weight's type (float32 without one); ``accumulate`` adds to those
+        given."""
+        import torch
+        h = x.shape[-1]
+        _need(dy.shape == x.shape and dy.dtype == x.dtype, "dy has another shape or type than x")
+        _need(not accumulate or (dweight is not None and dbias is not None), "accumulate needs dweight and dbias")
+        if dx is None:
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        _need(dx.shape == x.shape and dx.dtype == x.dtype, "dx has another shape or type than x")
+        ptype = weight.dtype if weight is not None else dweight.dtype if dweight is not None else dbias.dtype if dbias is not None else torch.float32
+        dweight = torch.empty(h, dtype=ptype, device=x.device) if dweight is None else dweight
+        dbias = torch.empty(h, dtype=ptype, device=x.device) if dbias is None else dbias
+        ptype = self._params(h, weight, dweight, dbias)
+        for s in (mean, rstd):
+            _need(s.shape == x.shape[:-1] and s.dtype == torch.float32 and s.is_contiguous(), "mean and rstd are float32, one of each a row")
+        xm, n, xs = _matrix(x)
+        gm, _, gs = _matrix(dy)
+        om, _, os_ = _matrix(dx, out=True)
+        self._op(self.lib.echo_layer_norm_grad, LayerNormGradDesc(n, h, gm.data_ptr(), xm.data_ptr(), _dptr(weight), mean.data_ptr(), rstd.data_ptr(),
+                                                                  om.data_ptr(), dweight.data_ptr(), dbias.data_ptr(), gs, xs, os_,
+                                                                  _type(x.dtype), ptype, 1 if accumulate else 0))
+        return dx, dweight, dbias
+
+    @staticmethod
+    def _params(h: int, *params) -> int:
+        """Common type of the parameter vectors given."""
+        types = set()
+        for p in params:
+            if p is not None:
+                _need(p.dim() == 1 and p.shape[0] == h and (h == 1 or p.stride(0) == 1), "a parameter is not a contiguous vector of a row's length")
+                types.add(_type(p.dtype))
+        _need(len(types) <= 1, "the parameters and their gradients have different types")
+        return types.pop() if types else 0
+
+    def orthogonalize(self, g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0, out=None):
+        """Newton-Schulz orthogonalisation of the matrices ``g`` [..., rows, cols], times
+        ``scale``; ``coefficients`` are the quintic's (x, x^3, x^5).  ``out`` may be ``g``."""
+        import torch
+        _need(g.dim() >= 2, "g is not a matrix")
+        o = torch.empty_like(g, memory_format=torch.contiguous_format) if out is None else out
+        _need(o.shape == g.shape and o.dtype == g.dtype, "out has another shape or type than g")
+        r, c = g.shape[-2:]
+        gm, n, gs, gb = _batch(g)
+        om, _, os_, ob = _batch(o, out=True)
+        a, b, cc = coefficients
+        self._op(self.lib.echo_orthogonalize, OrthogonalizeDesc(n, r, c, gm.data_ptr(), om.data_ptr(), gs, gb, os_, ob, _type(g.dtype), steps,
+                                                                a, b, cc, eps, scale))
+        return o
