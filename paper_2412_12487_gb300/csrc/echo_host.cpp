@@ -1584,6 +1584,7 @@ struct echo_ctx {
   // scratch of the operators (echo_ops.cpp)
   void *ops = nullptr;
   size_t ops_bytes = 0;
+  int32_t *ops_status = nullptr;  // host memory: set by a kernel whose wait gave up
   // profiling
   bool prof = false;
   std::vector<std::pair<std::string, std::pair<cudaEvent_t, cudaEvent_t>>> recs;
@@ -1883,8 +1884,23 @@ namespace echo {
 
 int op_begin(echo_ctx *c, OpContext *o) {
   const int rc = check_ctx(c);
-  if (!rc) *o = {c->device, c->sms, c->stream};
-  return rc;
+  if (rc) return rc;
+  if (c->ops_status && *(volatile int32_t *)c->ops_status) {
+    *(volatile int32_t *)c->ops_status = 0;
+    return set_err(c, ECHO_E_TIMEOUT, "a device-side wait of an earlier operator gave up: its result is incomplete");
+  }
+  *o = {c->device, c->sms, c->stream, c->wait_limit_cycles, c->skip_level};
+  return ECHO_OK;
+}
+int op_status(echo_ctx *c, int32_t **p) {
+  if (!c->ops_status) {
+    void *q = nullptr;
+    CK(cudaHostAlloc(&q, sizeof(int32_t), cudaHostAllocMapped), "allocating the operators' status");
+    c->ops_status = static_cast<int32_t *>(q);
+    *c->ops_status = 0;
+  }
+  *p = c->ops_status;
+  return ECHO_OK;
 }
 int op_error(echo_ctx *c, int code, const std::string &msg) { return set_err(c, code, msg); }
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what) { return cuda_fail(c, e, what); }
@@ -2007,6 +2023,7 @@ int echo_destroy(echo_ctx *c) {
   free_all(c->raw_allocs);
   if (c->stage) cudaFree(c->stage);
   if (c->ops) cudaFree(c->ops);
+  if (c->ops_status) cudaFreeHost(c->ops_status);
   for (auto &r : c->recs) {
     cudaEventDestroy(r.second.first);
     cudaEventDestroy(r.second.second);

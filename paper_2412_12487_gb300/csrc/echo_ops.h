@@ -16,8 +16,11 @@ namespace echo {
 struct OpContext {
   int device, sms;
   cudaStream_t stream;
+  long long wait_limit;  // bound of every device-side wait, in SM clock cycles
+  int skip;              // failure injection for tests (-1: none)
 };
-// Makes the context's device current; an echo_status.
+// Makes the context's device current; an echo_status: ECHO_E_TIMEOUT where a kernel of an
+// earlier call gave up.
 int op_begin(echo_ctx *c, OpContext *o);
 int op_error(echo_ctx *c, int code, const std::string &msg);
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what);
@@ -25,6 +28,8 @@ int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what);
 int op_scratch(echo_ctx *c, size_t bytes, void **p);
 // Whether p is memory of the context's device.
 bool op_device_memory(echo_ctx *c, const void *p);
+// Word of the context in host memory that kernels set when a wait gives up.
+int op_status(echo_ctx *c, int32_t **p);
 // Runs a launch, between two events while the context is profiled.
 cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch);
 
@@ -102,8 +107,11 @@ struct OrthoArgs {
   int type, steps;
   float a, b, c, eps, scale;
   void *scratch;
+  int32_t *status;          // of op_status
+  long long wait_limit;     // bound of every wait of the kernels, in SM clock cycles
+  int skip;                 // failure injection for tests (ProductArgs)
 };
-size_t ortho_scratch_bytes(const OrthoArgs &a, int sms);
+size_t ortho_scratch_bytes(const OrthoArgs &a);
 using OpTimer = std::function<cudaError_t(const char *, const std::function<cudaError_t()> &)>;
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
 

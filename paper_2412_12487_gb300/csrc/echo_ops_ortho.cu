@@ -1,5 +1,20 @@
 // echo_ops_ortho.cu -- orthogonalised updates by Newton-Schulz products.
+//
+// A step is three products P Q^T of matrices whose rows run along the sum (K-major), so that
+// both operands of the tensor core come the same way from memory:
+//   A = X X^T,  B = b A + c A A^T (A is symmetric),  X' = a X + B (X^T)^T.
+// The last needs X^T, which every product's epilogue can write beside its result at little
+// cost: a thread holds one row of the tile, so a column of it is contiguous over the warp.
+// The two symmetric products compute the tiles that reach the lower triangle and write each
+// element to both places.
+//
+// Elements are fp16 numbers times a power of two (the iterate's singular values stay near 1,
+// so its elements are at most that): one for 16-bit matrices, the sum of two for fp32 ones
+// (22 bits), multiplied as high * high + high * low + low * high with sums in fp32.
+#include <cuda.h>
+
 #include <algorithm>
+#include <cstring>
 
 #include "echo_ops.cuh"
 #include "echo_ops.h"
@@ -8,25 +23,40 @@ namespace echo {
 
 namespace {
 
+// What is stored of X, A and B: the true value times this.  fp16 holds 2^-24 to 65504, so
+// elements up to 16 fit, and 22 bits remain of elements down to 2^-25.
+constexpr float kScaleX = 0x1p12f, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
+
 // -- Frobenius norm ------------------------------------------------------------------------------
 // Sums of squares of x, of 2^-60 x and of 2^60 x: one of them neither overflows nor underflows,
-// whatever the size of the elements.  A block sums a part of one matrix.
-constexpr int kNormParts = 64;
-
-template <typename T>
+// whatever the size of the elements.  A block sums a part of the rows of one matrix.
+template <typename T, int W>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t rows, int64_t cols, float *part) {
   __shared__ float sh[3][8];
   const float up = 0x1p60f, down = 0x1p-60f;
+  const int64_t pieces = cols / W, all = rows * pieces;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     float s[3] = {0.f, 0.f, 0.f};
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-      const T *g = static_cast<const T *>(a.g) + z * a.g_batch_stride + r * a.g_stride;
-      for (int64_t j = threadIdx.x; j < cols; j += blockDim.x) {
-        const float v = to_f(g[j]), lo = v * up, hi = v * down;
-        s[0] += v * v;
-        s[1] += hi * hi;
-        s[2] += lo * lo;
+    const T *g = static_cast<const T *>(a.g) + z * a.g_batch_stride;
+    constexpr int kFlight = 4;
+    for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
+      float v[kFlight][W];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        const int64_t i = i0 + k * 256;
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[k][e] = 0.f;
+        if (i < all) load_piece<W>(g + i / pieces * a.g_stride + i % pieces * W, v[k]);
       }
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k)
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float x = v[k][e], lo = x * up, hi = x * down;
+          s[0] += x * x;
+          s[1] += hi * hi;
+          s[2] += lo * lo;
+        }
     }
     for (int q = 0; q < 3; ++q) {
       s[q] = warp_sum(s[q]);
@@ -36,133 +66,703 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t ro
     if (threadIdx.x < 3) {
       float t = 0.f;
       for (int w = 0; w < 8; ++w) t += sh[threadIdx.x][w];
-      part[(z * kNormParts + blockIdx.x) * 3 + threadIdx.x] = t;
+      part[(z * gridDim.x + blockIdx.x) * 3 + threadIdx.x] = t;
     }
     __syncthreads();
   }
 }
 
-// 1 / (|G| + eps) of a matrix, from the parts of its sums of squares.
-__device__ double inverse_norm(const float *part, int64_t z, float eps) {
+// 1 / (|G| + eps) of matrix z, by a warp, from the parts of its sums of squares.
+__device__ __forceinline__ double inverse_norm(const float *part, int parts, int64_t z, float eps) {
   double s[3] = {0., 0., 0.};
-  for (int p = 0; p < kNormParts; ++p)
-    for (int q = 0; q < 3; ++q) s[q] += part[(z * kNormParts + p) * 3 + q];
+  for (int p = threadIdx.x & 31; p < parts; p += 32)
+#pragma unroll
+    for (int q = 0; q < 3; ++q) s[q] += part[(z * parts + p) * 3 + q];
+#pragma unroll
+  for (int q = 0; q < 3; ++q)
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s[q] += __shfl_xor_sync(0xFFFFFFFFu, s[q], d);
   // (the plain sum unless it is near the ends of the fp32 range; a NaN stays one)
   const double norm = s[0] > 1e30 ? sqrt(s[1]) * 0x1p60 : s[0] < 1e-24 ? sqrt(s[2]) * 0x1p-60 : sqrt(s[0]);
   return 1. / (norm + (double)eps);
 }
 
-// X = G / (|G| + eps) in fp32, [m][n]
-template <typename T>
-__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, const float *part, float *X) {
-  __shared__ double inv;
+// x times a factor that may be outside fp32's range while the product is not: two powers of
+// two, each exact, and a number between 1/2 and 1.
+struct Factor {
+  float p1, p2, f;
+  __device__ __forceinline__ void set(double v) {
+    int e = 0;
+    f = (float)frexp(v, &e);
+    const int half = e / 2;
+    p1 = ldexpf(1.f, half);
+    p2 = ldexpf(1.f, e - half);
+  }
+  __device__ __forceinline__ float operator()(float x) const { return x * p1 * p2 * f; }
+};
+
+// -- matrices of the iteration --------------------------------------------------------------------
+// [plane][batch][rows][ld] fp16; plane 1 (fp32 matrices) is what plane 0 leaves of an element.
+struct Planes {
+  __half *p;
+  int64_t ld, matrix, plane;  // elements of a row, of a matrix, of a plane
+};
+
+template <int PLANES>
+__device__ __forceinline__ void split(float v, __half (&h)[PLANES]) {
+  h[0] = __float2half_rn(v);
+  if constexpr (PLANES == 2) h[1] = __float2half_rn(v - __half2float(h[0]));
+}
+
+// X = G / (|G| + eps), and its transpose: `same` has G's orientation, `other` the other one.
+// A block takes 64 x 64 tiles; G and both results go in runs of at least 64 bytes.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes same, Planes other) {
+  __shared__ Factor factor;
+  __shared__ __half tile[PLANES][64][66];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int64_t tiles_c = (cols + 63) / 64, tiles = (rows + 63) / 64 * tiles_c;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
+    if (threadIdx.x < 32) {
+      const double v = inverse_norm(part, parts, z, a.eps) * (double)kScaleX;
+      if (threadIdx.x == 0) factor.set(v);
+    }
     __syncthreads();
-    if (threadIdx.x == 0) inv = inverse_norm(part, z, a.eps);
-    __syncthreads();
+    const Factor f = factor;
     const T *g = static_cast<const T *>(a.g) + z * a.g_batch_stride;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < a.m * a.n; i += (int64_t)gridDim.x * blockDim.x) {
-      const int64_t r = i / a.n, c = i % a.n;
-      X[z * a.m * a.n + i] = (float)((double)to_f(a.tall ? g[c * a.g_stride + r] : g[r * a.g_stride + c]) * inv);
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+      const int64_t r0 = t / tiles_c * 64, c0 = t % tiles_c * 64;
+      float v[8][2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int64_t r = r0 + ty + 8 * i, c = c0 + tx + 32 * e;
+          v[i][e] = r < rows && c < cols ? f(to_f(g[r * a.g_stride + c])) : 0.f;
+        }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          __half h[PLANES];
+          split<PLANES>(v[i][e], h);
+#pragma unroll
+          for (int q = 0; q < PLANES; ++q) tile[q][ty + 8 * i][tx + 32 * e] = h[q];
+        }
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = ty + 8 * i;  // two elements of a row: in both results the padding takes an odd end
+          if (r0 + at < rows && c0 + 2 * tx < cols)
+            *reinterpret_cast<__half2 *>(same.p + q * same.plane + z * same.matrix + (r0 + at) * same.ld + c0 + 2 * tx) =
+                *reinterpret_cast<const __half2 *>(&tile[q][at][2 * tx]);
+          if (c0 + at < cols && r0 + 2 * tx < rows)
+            *reinterpret_cast<__half2 *>(other.p + q * other.plane + z * other.matrix + (c0 + at) * other.ld + r0 + 2 * tx) =
+                __halves2half2(tile[q][2 * tx][at], tile[q][2 * tx + 1][at]);
+        }
+      __syncthreads();
     }
+    __syncthreads();
   }
 }
 
+// No steps: O = scale G / (|G| + eps).
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_finish_kernel(OrthoArgs a, const float *X) {
+__global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts) {
+  __shared__ Factor factor;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
-    T *o = static_cast<T *>(a.o) + z * a.o_batch_stride;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < a.m * a.n; i += (int64_t)gridDim.x * blockDim.x) {
-      const int64_t r = i / a.n, c = i % a.n;
-      o[a.tall ? c * a.o_stride + r : r * a.o_stride + c] = from_f<T>(a.scale * X[z * a.m * a.n + i]);
+    if (threadIdx.x < 32) {
+      const double v = inverse_norm(part, parts, z, a.eps);
+      if (threadIdx.x == 0) factor.set(v);
     }
+    __syncthreads();
+    const Factor f = factor;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * blockDim.x) {
+      const float v = to_f(static_cast<const T *>(a.g)[z * a.g_batch_stride + i / cols * a.g_stride + i % cols]);
+      static_cast<T *>(a.o)[z * a.o_batch_stride + i / cols * a.o_stride + i % cols] = from_f<T>(f(v) * a.scale);
+    }
+    __syncthreads();
   }
 }
 
-// D = alpha P Q + beta C of [M][K] and [K][N] (or Q transposed) matrices without gaps, 64 x 64 a block.
-__global__ void __launch_bounds__(256) ortho_product_kernel(int64_t batch, int M, int N, int K, const float *P, const float *Q, bool q_transposed,
-                                                            const float *C, float alpha, float beta, float *D) {
-  __shared__ float sp[16][65], sq[16][65];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-  for (int64_t z = blockIdx.z; z < batch; z += gridDim.z) {
-    const float *p = P + z * M * K, *q = Q + z * N * K;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < K; k0 += 16) {
-      for (int i = threadIdx.x; i < 1024; i += 256) {
-        const int r = i >> 4, k = i & 15;
-        sp[k][r] = r0 + r < M && k0 + k < K ? p[(int64_t)(r0 + r) * K + k0 + k] : 0.f;
-        if (q_transposed) {
-          sq[k][r] = c0 + r < N && k0 + k < K ? q[(int64_t)(c0 + r) * K + k0 + k] : 0.f;
-        } else {
-          const int kk = i >> 6, c = i & 63;
-          sq[kk][c] = c0 + c < N && k0 + kk < K ? q[(int64_t)(k0 + kk) * N + c0 + c] : 0.f;
+// -- products --------------------------------------------------------------------------------------
+// D = alpha P Q^T + beta C on tiles of 256 x BN, by persistent pairs of blocks that share a
+// tile (cta_group::2): each holds 128 rows of P and of the sums, and half of Q's rows, so that
+// a pair reads each operand once.  In each block one thread copies 64 columns of its operands
+// at a time with the TMA engine (128-byte swizzle) into a ring of stages; a thread of the
+// pair's first block issues tcgen05.mma on both blocks' stages; eight warps take the sums out
+// of tensor memory, which holds two sets of them.
+//
+// The tensor core adds to its fp32 sums with truncation: over 12288 columns of fp32 matrices
+// (2304 additions an element) the result was 8e-5 off.  So for them a set of sums covers 256
+// columns (48 additions) and the eight warps add the sets up in registers, rounding to
+// nearest; they do it while the next set is summed.
+constexpr int kBM = 256, kBK = 64, kRows = 128;  // of a tile, of a stage; rows of P a block holds
+constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
+// Registers of a thread of warps 0-3 and of 4-11, which hold 128 sums each; together no more
+// than the 168 a thread that the block is launched with (65536 / 384, in units of 8).
+constexpr int kFewRegs = 56, kManyRegs = 216;
+static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
+constexpr int kChunk = 4;                        // stages of a set of sums of fp32 matrices
+constexpr int stage_bytes(int planes, int bn) { return planes * (kRows + bn / 2) * kBK * 2; }
+constexpr int stages(int planes, int bn) { return 196608 / stage_bytes(planes, bn); }
+constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out: 32 x 32 elements of D and of D^T
+constexpr size_t smem_bytes(int planes, int bn) {
+  return (size_t)stages(planes, bn) * stage_bytes(planes, bn) + 8 * kOutBytes + 256 + 1024;
+}
+
+struct ProductArgs {
+  int64_t batch;
+  int M, N, K;
+  int tiles_n;          // tiles of a row of tiles (not symmetric)
+  int64_t tiles;        // of a matrix
+  int symmetric;        // D is symmetric: tiles of the lower triangle, each element written twice
+  float alpha, beta;
+  Planes c;             // C (p may be null)
+  void *o;              // the last product: the result instead of D
+  int64_t o_stride, o_batch_stride;
+  int o_transposed;
+  int32_t *status;      // host memory: set when a wait gave up
+  long long wait_limit;
+  int skip;             // failure injection for tests: this 64-column step is never copied (-1: none)
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// The same place in the pair's first block.
+__device__ __forceinline__ uint32_t in_first(uint32_t at) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;\n" : "=r"(r) : "r"(at));
+  return r;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return ok;
+}
+// Waits until the phase of that parity has completed; false if the block gives up (another
+// wait did, or this one's limit has passed).
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort, const ProductArgs &a) {
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity)) {
+    if (*abort) return false;
+    if (clock64() - t0 > a.wait_limit) {
+      *abort = 1;
+      *(volatile int32_t *)a.status = 1;
+      __threadfence_system();
+      return false;
+    }
+  }
+  return true;
+}
+
+// 64 columns from k (a multiple of 64) of a box of rows from `row`.
+__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap *map, int k, int row, int z, int plane, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n" ::"r"(to),
+      "l"(map), "r"(bar), "r"(k), "r"(row), "r"(z), "r"(plane)
+      : "memory");
+}
+
+// Descriptor of an operand tile: rows of 128 bytes, swizzled in groups of 8 rows (1024 bytes).
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// fp16 operands, fp32 sums, both along K, `bn` columns, kBM rows
+constexpr uint32_t instruction(int bn) { return 1u << 4 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(kBM >> 4) << 24; }
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t p, uint64_t q, uint32_t instr, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(p),
+               "l"(q), "r"(instr), "r"((uint32_t)add)
+               : "memory");
+}
+// The barriers of both blocks (or of this one) complete once the products issued so far have.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar), "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_sums(uint32_t at, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+      "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+
+// First row and column of a tile.  Symmetric: row i of tiles has (i + 1) kBM / BN of them.
+// Otherwise in bands of 8 rows of tiles, column by column, so that the tiles in work share
+// operands in L2.
+template <int BN>
+__device__ __forceinline__ void tile_place(const ProductArgs &a, int64_t t, int &r0, int &c0) {
+  constexpr int F = kBM / BN;
+  int64_t i, j;
+  if (a.symmetric) {
+    i = (int64_t)((sqrt(1. + 8. / F * (double)t) - 1.) * 0.5);
+    while (i > 0 && F * i * (i + 1) / 2 > t) --i;
+    while (F * (i + 1) * (i + 2) / 2 <= t) ++i;
+    j = t - F * i * (i + 1) / 2;
+  } else {
+    const int64_t rows = (a.M + kBM - 1) / kBM, band = t / (8 * a.tiles_n), in = t % (8 * a.tiles_n), high = min((int64_t)8, rows - band * 8);
+    i = band * 8 + in % high;
+    j = in / high;
+  }
+  r0 = (int)i * kBM;
+  c0 = (int)j * BN;
+}
+
+// 32 x 32 elements from a warp's buffer to a matrix of the iteration, by one thread; what is
+// outside the matrix is dropped.
+__device__ __forceinline__ void store_tile(const CUtensorMap *map, uint32_t from, int col, int row, int z, int plane) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];\ncp.async.bulk.commit_group;\n" ::"l"(map),
+               "r"(from), "r"(col), "r"(row), "r"(z), "r"(plane)
+               : "memory");
+}
+// All but the last store of this thread have read their buffer (or, at the end, all are done).
+__device__ __forceinline__ void stores_but_one_read() { asm volatile("cp.async.bulk.wait_group.read 1;\n" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
+
+// 32 x 32 elements of a tile out, by a warp: lane r has those of row row0 + r in v, from column
+// c.  A symmetric product writes the blocks of the lower triangle and, transposed, those of the
+// upper one.  The two halves of the buffer take turns, D's with 16-byte pieces exchanged as the
+// map's 64-byte swizzle has it (rows of 64 bytes would meet in the same banks).
+template <int PLANES>
+__device__ __forceinline__ void block_out(const CUtensorMap *dmap, const CUtensorMap *tmap, bool symmetric, int z, int row0, int c, int lane,
+                                          const float (&v)[32], unsigned char *buffer) {
+  if (symmetric && c > row0) return;
+  const bool mirror = !symmetric || c < row0;
+  const uint32_t buf = smem_u32(buffer);
+#pragma unroll
+  for (int q = 0; q < PLANES; ++q) {
+    __half h[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      __half e[PLANES];
+      split<PLANES>(v[i], e);
+      h[i] = e[q];
+    }
+    if (lane == 0) stores_but_one_read();
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      Pack<__half, 8> w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w.v[e] = h[8 * i + e];
+      *reinterpret_cast<Pack<__half, 8> *>(buffer + lane * 64 + (i ^ ((lane >> 1) & 3)) * 16) = w;
+    }
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      store_tile(dmap, buf, c, row0, z, q);
+      if (mirror) stores_but_one_read();
+      else stores_done();  // (the next block's first half is this one's)
+    }
+    if (!mirror) continue;
+    __syncwarp();
+    __half *t = reinterpret_cast<__half *>(buffer + 2048) + lane;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t[i * 32] = h[i];
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    __syncwarp();
+    if (lane == 0) store_tile(tmap, buf + 2048, row0, c, z, q);
+  }
+}
+
+// The same for the result: through the buffer where its rows are the tile's, so that
+// neighbouring lanes write neighbouring elements.
+template <typename OUT>
+__device__ __forceinline__ void result_out(const ProductArgs &a, int64_t z, int row0, int c, int lane, const float (&v)[32], unsigned char *buffer) {
+  OUT *o = static_cast<OUT *>(a.o) + z * a.o_batch_stride;
+  if (a.o_transposed) {
+    if (row0 + lane < a.M) {
+      o += (int64_t)c * a.o_stride + row0 + lane;
+#pragma unroll
+      for (int i = 0; i < 32; ++i, o += a.o_stride)
+        if (c + i < a.N) *o = from_f<OUT>(v[i]);
+    }
+    return;
+  }
+  float *f = reinterpret_cast<float *>(buffer);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[lane * 32 + (i ^ lane)] = v[i];
+  __syncwarp();
+  if (c + lane < a.N) {
+    o += (int64_t)row0 * a.o_stride + c + lane;
+    const int rows = min(32, a.M - row0);
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r, o += a.o_stride) *o = from_f<OUT>(f[r * 32 + (lane ^ r)]);
+  }
+}
+
+// OUT: void for a product whose result goes on in planes, else the type of the result.
+template <int PLANES, int BN, typename OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    ortho_product_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap dmap,
+                         const __grid_constant__ CUtensorMap tmap, const __grid_constant__ ProductArgs a) {
+  constexpr int S = stages(PLANES, BN), kStage = stage_bytes(PLANES, BN), kP = kRows * kBK * 2, kQ = BN / 2 * kBK * 2, kCols = BN / 2;
+  extern __shared__ unsigned char raw[];
+  unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
+  unsigned char *buffers = base + S * kStage;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(buffers + 8 * kOutBytes);
+  __shared__ uint32_t tmem_base;
+  __shared__ int give_up;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;  // (clusters of two along x)
+  // `full` and `sums_empty` are used in the first block alone, the others in both
+  const uint32_t ring = smem_u32(base), full = smem_u32(bars), empty = full + 8 * S, sums_full = empty + 8 * S, sums_empty = sums_full + 16,
+                 done = sums_empty + 16;
+  volatile int *abort = &give_up;
+  if (threadIdx.x == 0) {
+    give_up = 0;
+    for (int s = 0; s < S; ++s) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(sums_full + 8 * b, 1);
+      bar_init(sums_empty + 8 * b, 16);
+    }
+    bar_init(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base)), "r"(2u * BN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  const uint32_t tmem = tmem_base;
+  const int64_t all = a.tiles * a.batch;
+  const int steps = (a.K + kBK - 1) / kBK, chunk = PLANES == 2 ? kChunk : steps;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kFewRegs));
+    if (warp == 0 && lane == 0) {
+      int64_t it = 0;
+      bool ok = true;
+      for (int64_t t = pair; t < all && ok; t += pairs) {
+        int r0, c0;
+        tile_place<BN>(a, t % a.tiles, r0, c0);
+        const int z = (int)(t / a.tiles);
+        for (int k = 0; k < steps; ++k, ++it) {
+          const int s = (int)(it % S);
+          ok = k != a.skip && bar_wait(empty + 8 * s, (uint32_t)(it / S + 1) & 1, abort, a);
+          if (!ok) break;
+          const uint32_t at = ring + s * kStage, bar = in_first(full + 8 * s);
+          if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);  // both blocks' copies
+#pragma unroll
+          for (int q = 0; q < PLANES; ++q) {
+            copy_tile(at + q * kP, &pmap, k * kBK, r0 + rank * kRows, z, q, bar);
+            copy_tile(at + PLANES * kP + q * kQ, &qmap, k * kBK, c0 + rank * kCols, z, q, bar);
+          }
         }
       }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 16; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] += sp[k][ty + 16 * i] * sq[k][tx + 16 * j];
-      __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const int r = r0 + ty + 16 * i, c = c0 + tx + 16 * j;
-        if (r >= M || c >= N) continue;
-        const int64_t at = z * M * N + (int64_t)r * N + c;
-        D[at] = alpha * acc[i][j] + (C ? beta * C[at] : 0.f);
+      if (!ok) {  // what is still being copied lands long before this
+        const long long t0 = clock64();
+        while (clock64() - t0 < 1000000) {
+        }
       }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      int64_t it = 0, n = 0;
+      bool ok = true;
+      for (int64_t t = pair; t < all && ok; t += pairs) {
+        for (int k0 = 0; k0 < steps && ok; k0 += chunk, ++n) {
+          const int b = (int)(n & 1);
+          ok = bar_wait(sums_empty + 8 * b, (uint32_t)(n / 2 + 1) & 1, abort, a);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const uint32_t d = tmem + b * BN;
+          for (int k = k0; k < min(steps, k0 + chunk); ++k, ++it) {
+            const int s = (int)(it % S);
+            ok = bar_wait(full + 8 * s, (uint32_t)(it / S) & 1, abort, a);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            const uint64_t p = operand(ring + s * kStage), q = operand(ring + s * kStage + PLANES * kP);
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk) {  // 16 columns: 32 bytes on
+              mma(d, p + 2 * kk, q + 2 * kk, instruction(BN), k > k0 || kk > 0);
+              if constexpr (PLANES == 2) {
+                mma(d, p + 2 * kk, q + 2 * kk + (kQ >> 4), instruction(BN), true);
+                mma(d, p + 2 * kk + (kP >> 4), q + 2 * kk, instruction(BN), true);
+              }
+            }
+            commit_pair(empty + 8 * s);
+          }
+          if (ok) commit_pair(sums_full + 8 * b);
+        }
+      }
+      commit(done);  // nothing is in flight when the block ends
+      const long long t0 = clock64();
+      while (!bar_try(done, 0) && clock64() - t0 <= a.wait_limit) {
+      }
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kManyRegs));
+    const int quarter = warp & 3, side = (warp - 4) >> 2;  // (a warp reaches the 32 rows of tensor memory of its number modulo 4)
+    unsigned char *buffer = buffers + (warp - 4) * kOutBytes;
+    const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + side * kCols;
+    int64_t n = 0;
+    bool ok = true;
+    for (int64_t t = pair; t < all && ok; t += pairs) {
+      int r0, c0;
+      tile_place<BN>(a, t % a.tiles, r0, c0);
+      const int z = (int)(t / a.tiles), row0 = r0 + rank * kRows + quarter * 32;
+      const bool live = row0 < a.M;
+      c0 += side * kCols;
+      // C's part of the tile comes to L2 during the sums, and to registers one block ahead
+      const __half *from_c = a.c.p && row0 + lane < a.M ? a.c.p + z * a.c.matrix + (int64_t)(row0 + lane) * a.c.ld : nullptr;
+      if (from_c) {
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+          for (int i = 0; i < kCols; i += 64)
+            if (c0 + i < a.N) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(from_c + q * a.c.plane + c0 + i));
+      }
+      float acc[kCols / 32][32];
+      for (int k0 = 0; k0 < steps; k0 += chunk, ++n) {
+        const int b = (int)(n & 1);
+        ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+#pragma unroll
+        for (int part = 0; part < kCols / 32; ++part) {
+          __syncwarp();
+          if (k0 == 0) {
+            load_sums(from + b * BN + part * 32, acc[part]);
+          } else {
+            float v[32];
+            load_sums(from + b * BN + part * 32, v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[part][i] += v[i];
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(in_first(sums_empty + 8 * b));
+      }
+      if (!ok) break;
+      if (!live) continue;
+      Pack<__half, 8> ahead[PLANES][4] = {};
+      auto fetch = [&](int c) {
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (from_c && c + 8 * i < a.N)  // (to the end of a piece: within the padding of the row)
+              ahead[q][i] = *reinterpret_cast<const Pack<__half, 8> *>(from_c + q * a.c.plane + c + 8 * i);
+      };
+      fetch(c0);
+#pragma unroll
+      for (int part = 0; part < kCols / 32; ++part) {
+        const int c = c0 + part * 32;
+        if (c >= a.N) continue;
+        float (&v)[32] = acc[part];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= a.alpha;
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[8];
+            unpack<__half, 8>(ahead[q][i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[8 * i + e] += a.beta * f[e];
+          }
+        if (part + 1 < kCols / 32) fetch(c + 32);
+        if constexpr (std::is_void_v<OUT>)
+          block_out<PLANES>(&dmap, &tmap, a.symmetric, z, row0, c, lane, v, buffer);
+        else
+          result_out<OUT>(a, z, row0, c, lane, v, buffer);
+      }
+    }
+    if (lane == 0) stores_done();
+    __syncwarp();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  cluster_sync();  // (the other block's products read this one's stages, and signal its barriers)
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * BN) : "memory");
   }
 }
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+  static const EncodeTiled f = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
+}
+
+// Boxes of a matrix of the iteration; zeros outside it.
+cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows, int box_cols,
+                     CUtensorMapSwizzle swizzle) {
+  if (!encoder()) return cudaErrorNotSupported;
+  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)planes};
+  const cuuint64_t strides[3] = {(cuuint64_t)p.ld * 2, (cuuint64_t)p.matrix * 2, (cuuint64_t)p.plane * 2};
+  const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p.p, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+int64_t padded(int64_t x) { return (x + 63) / 64 * 64; }
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+Planes planes_of(char *&at, int64_t rows, int64_t cols, int64_t batch, int planes) {
+  Planes p{reinterpret_cast<__half *>(at), padded(cols), rows * padded(cols), batch * rows * padded(cols)};
+  at += up256((size_t)planes * p.plane * sizeof(__half));
+  return p;
+}
+int planes_for(int type) { return type == ECHO_F32 ? 2 : 1; }
 
 }  // namespace
 
-// norm parts; X, the next X, A, B in fp32
-size_t ortho_scratch_bytes(const OrthoArgs &a, int) {
-  return (size_t)a.batch * (kNormParts * 3 + 2 * a.m * a.n + 2 * a.m * a.m) * sizeof(float);
+// blocks that sum a matrix for its norm
+int norm_parts(const OrthoArgs &a) { return (int)std::clamp<int64_t>(a.m * a.n / 8192, 1, 608); }
+
+// parts of the norm; X, X^T twice (a product reads one while it writes the other), A, B
+size_t ortho_scratch_bytes(const OrthoArgs &a) {
+  char *at = nullptr;
+  const int planes = planes_for(a.type);
+  planes_of(at, a.m, a.n, a.batch, planes);
+  for (int i = 0; i < 2; ++i) planes_of(at, a.n, a.m, a.batch, planes);
+  for (int i = 0; i < 2; ++i) planes_of(at, a.m, a.m, a.batch, planes);
+  return (a.steps ? reinterpret_cast<uintptr_t>(at) : 0) + up256((size_t)a.batch * norm_parts(a) * 3 * sizeof(float));
 }
 
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
-  float *X = static_cast<float *>(a.scratch), *X2 = X + a.batch * a.m * a.n, *A = X2 + a.batch * a.m * a.n, *B = A + a.batch * a.m * a.m;
-  float *part = B + a.batch * a.m * a.m;
+  const int planes = planes_for(a.type), parts = norm_parts(a);
+  char *at = static_cast<char *>(a.scratch);
+  float *part = reinterpret_cast<float *>(at);
+  at += up256((size_t)a.batch * parts * 3 * sizeof(float));
   const unsigned gz = (unsigned)std::min<int64_t>(a.batch, 65535);
   const int64_t rows = a.tall ? a.n : a.m, cols = a.tall ? a.m : a.n;
   cudaError_t e = timed("ortho_norm", [&] {
     return with_type(a.type, [&](auto t) {
-      ortho_norm_kernel<decltype(t)><<<dim3(kNormParts, gz), 256, 0, st>>>(a, rows, cols, part);
+      using T = decltype(t);
+      constexpr int N = 16 / sizeof(T);
+      if (cols % N == 0 && fits_pieces(a.g, a.g_stride, a.type, N) && fits_pieces(a.g, a.g_batch_stride, a.type, N))
+        ortho_norm_kernel<T, N><<<dim3(parts, gz), 256, 0, st>>>(a, rows, cols, part);
+      else
+        ortho_norm_kernel<T, 1><<<dim3(parts, gz), 256, 0, st>>>(a, rows, cols, part);
       return cudaGetLastError();
     });
   });
   if (e != cudaSuccess) return e;
-  const dim3 flat((unsigned)std::min<int64_t>((a.m * a.n + 255) / 256, sms * 8), gz);
+  if (a.steps == 0)
+    return timed("ortho_scale", [&] {
+      return with_type(a.type, [&](auto t) {
+        ortho_scale_kernel<decltype(t)>
+            <<<dim3((unsigned)std::min<int64_t>((rows * cols + 255) / 256, sms * 8), gz), 256, 0, st>>>(a, rows, cols, part, parts);
+        return cudaGetLastError();
+      });
+    });
+  const Planes X = planes_of(at, a.m, a.n, a.batch, planes);
+  const Planes XT[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
+  const Planes A = planes_of(at, a.m, a.m, a.batch, planes), B = planes_of(at, a.m, a.m, a.batch, planes);
   e = timed("ortho_start", [&] {
+    const dim3 grid((unsigned)std::min<int64_t>((rows + 63) / 64 * ((cols + 63) / 64), sms * 8), gz);
+    const Planes &same = a.tall ? XT[0] : X, &other = a.tall ? X : XT[0];
     return with_type(a.type, [&](auto t) {
-      ortho_start_kernel<decltype(t)><<<flat, 256, 0, st>>>(a, part, X);
+      using T = decltype(t);
+      ortho_start_kernel<T, std::is_same_v<T, float> ? 2 : 1><<<grid, 256, 0, st>>>(a, rows, cols, part, parts, same, other);
       return cudaGetLastError();
     });
   });
-  const int m = (int)a.m, n = (int)a.n;
-  auto product = [&](int N, int K, const float *P, const float *Q, bool qt, const float *C, float alpha, float beta, float *D) {
-    return timed("ortho_product", [&] {
-      ortho_product_kernel<<<dim3((N + 63) / 64, (m + 63) / 64, gz), 256, 0, st>>>(a.batch, m, N, K, P, Q, qt, C, alpha, beta, D);
-      return cudaGetLastError();
-    });
-  };
-  for (int s = 0; s < a.steps && e == cudaSuccess; ++s) {
-    e = product(m, n, X, X, true, nullptr, 1.f, 0.f, A);
-    if (e == cudaSuccess) e = product(m, m, A, A, true, A, a.c, a.b, B);
-    if (e == cudaSuccess) e = product(n, m, B, X, false, X, 1.f, a.a, X2);
-    std::swap(X, X2);
-  }
   if (e != cudaSuccess) return e;
-  return timed("ortho_finish", [&] {
-    return with_type(a.type, [&](auto t) {
-      ortho_finish_kernel<decltype(t)><<<flat, 256, 0, st>>>(a, X);
+
+  const int pairs = sms / 2;
+  const int64_t tm = (a.m + kBM - 1) / kBM;
+  auto tiles_of = [&](int64_t N, bool symmetric, int bn) { return symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn); };
+  struct Operand {
+    const Planes &p;
+    int64_t rows, cols;
+  };
+  const Operand x{X, a.m, a.n}, xt[2] = {{XT[0], a.n, a.m}, {XT[1], a.n, a.m}}, sa{A, a.m, a.m}, sb{B, a.m, a.m};
+  auto product = [&](const char *name, const Operand &p, const Operand &q, bool symmetric, float alpha, float beta, const Planes *c, const Operand *d,
+                     const Operand *dt) -> cudaError_t {
+    ProductArgs g{};
+    g.batch = a.batch, g.M = (int)a.m, g.N = (int)q.rows, g.K = (int)p.cols;
+    g.symmetric = symmetric;
+    g.alpha = alpha, g.beta = beta;
+    if (c) g.c = *c;
+    g.o = a.o, g.o_stride = a.o_stride, g.o_batch_stride = a.o_batch_stride, g.o_transposed = a.tall;
+    g.status = a.status, g.wait_limit = a.wait_limit, g.skip = a.skip;
+    auto go = [&](auto planes_c, auto cols_c, auto out) -> cudaError_t {
+      constexpr int P = decltype(planes_c)::value, BN = decltype(cols_c)::value;
+      using O = std::remove_pointer_t<decltype(out)>;
+      g.tiles_n = (int)((g.N + BN - 1) / BN);
+      g.tiles = tiles_of(g.N, symmetric, BN);
+      CUtensorMap pm, qm, dm{}, tm{};
+      cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, planes, kRows, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
+      if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, planes, BN / 2, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
+      if (r == cudaSuccess && d) r = tile_map(&dm, d->p, d->rows, d->cols, a.batch, planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+      if (r == cudaSuccess && d) r = tile_map(&tm, dt->p, dt->rows, dt->cols, a.batch, planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
+      auto kernel = ortho_product_kernel<P, BN, O>;
+      if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(P, BN));
+      if (r != cudaSuccess) return r;
+      kernel<<<(unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2, kThreads, smem_bytes(P, BN), st>>>(pm, qm, dm, tm, g);
       return cudaGetLastError();
-    });
-  });
+    };
+    auto with_out = [&](auto cols_c) -> cudaError_t {
+      if (d) return planes == 2 ? go(Int<2>{}, cols_c, (void *)nullptr) : go(Int<1>{}, cols_c, (void *)nullptr);
+      return planes == 2 ? go(Int<2>{}, cols_c, (float *)nullptr)
+             : a.type == ECHO_BF16 ? go(Int<1>{}, cols_c, (__nv_bfloat16 *)nullptr)
+                                   : go(Int<1>{}, cols_c, (__half *)nullptr);
+    };
+    // narrower tiles where the wide ones would not occupy every pair
+    const bool narrow = tiles_of(q.rows, symmetric, 256) * a.batch < pairs;
+    return timed(name, [&] { return narrow ? with_out(Int<128>{}) : with_out(Int<256>{}); });
+  };
+  for (int s = 0; s < a.steps; ++s) {
+    const bool last = s == a.steps - 1;
+    if ((e = product("ortho_xxt", x, x, true, kScaleA / (kScaleX * kScaleX), 0.f, nullptr, &sa, &sa)) != cudaSuccess) return e;
+    if ((e = product("ortho_aa", sa, sa, true, a.c * (kScaleB / (kScaleA * kScaleA)), a.b * (kScaleB / kScaleA), &A, &sb, &sb)) != cudaSuccess) return e;
+    const float out = last ? a.scale / kScaleX : 1.f;
+    if ((e = product("ortho_bx", sb, xt[s & 1], false, out / kScaleB, out * a.a, &X, last ? nullptr : &x, &xt[(s + 1) & 1])) != cudaSuccess)
+      return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace echo
