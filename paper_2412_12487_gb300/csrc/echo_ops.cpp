@@ -215,7 +215,7 @@ int echo_orthogonalize(echo_ctx *c, const echo_orthogonalize_desc *d) {
            "a batch stride is negative, or the output's less than a matrix");
     k.need(d->batch == 1 || std::max(d->g_batch_stride, d->o_batch_stride) <= ((int64_t)1 << 58) / (d->batch - 1), "a batch does not fit the address space");
     if (k.rc) return k.rc;
-    echo::OrthoArgs a{d->batch, std::min(d->rows, d->cols), std::max(d->rows, d->cols), d->rows > d->cols, d->g, d->o,
+    echo::OrthoArgs a{d->batch, std::min(d->rows, d->cols), std::max(d->rows, d->cols), d->rows >= d->cols, d->g, d->o,
                       d->g_stride, d->g_batch_stride, d->o_stride, d->o_batch_stride, d->type, d->steps,
                       d->a, d->b, d->c, d->eps, d->scale, nullptr, nullptr, o.wait_limit, o.skip};
     if (const int rc = echo::op_status(c, &a.status)) return rc;

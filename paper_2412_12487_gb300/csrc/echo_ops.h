@@ -97,7 +97,7 @@ cudaError_t launch_layer_norm_grad_columns(const NormGradArgs &a, cudaStream_t s
 cudaError_t launch_layer_norm_grad_join(const NormGradArgs &a, cudaStream_t st);
 
 // Orthogonalised update: m <= n are the smaller and the larger side, `tall` whether the
-// matrices have m columns (they are taken transposed).
+// matrices have n rows (the others are taken transposed).
 struct OrthoArgs {
   int64_t batch, m, n;
   bool tall;

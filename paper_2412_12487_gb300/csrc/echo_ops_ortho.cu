@@ -1,16 +1,18 @@
 // echo_ops_ortho.cu -- orthogonalised updates by Newton-Schulz products.
 //
-// A step is three products P Q^T of matrices whose rows run along the sum (K-major), so that
-// both operands of the tensor core come the same way from memory:
-//   A = X X^T,  B = b A + c A A^T (A is symmetric),  X' = a X + B (X^T)^T.
-// The last needs X^T, which every product's epilogue can write beside its result at little
-// cost: a thread holds one row of the tile, so a column of it is contiguous over the warp.
-// The two symmetric products compute the tiles that reach the lower triangle and write each
-// element to both places.
+// With Y the matrix that has n rows and m <= n columns (G, or its transpose), a step is three
+// products:
+//   A = Y^T Y,  B = b A + c A A,  Y' = a Y + Y B.
+// A and B are symmetric, so each product is P Q^T with the sum along the rows of both in memory
+// (K-major), but for the first, whose sum runs down Y's columns: the tensor core takes that
+// order too (MN-major).  Y is all that a step keeps.  The symmetric products compute the tiles
+// that reach the lower triangle and write each block to both places.
 //
 // Elements are fp16 numbers times a power of two (the iterate's singular values stay near 1,
-// so its elements are at most that): one for 16-bit matrices, the sum of two for fp32 ones
-// (22 bits), multiplied as high * high + high * low + low * high with sums in fp32.
+// so its elements are at most that): one for bf16 matrices, the sum of two for fp32 and fp16
+// ones (22 bits), multiplied as high * high + high * low + low * high with sums in fp32.  One
+// fp16 number for bf16 matrices leaves the result 2.2e-3 off, of which the rounding to bf16 is
+// 1.7e-3; two take three times the products.
 #include <cuda.h>
 
 #include <algorithm>
@@ -23,9 +25,9 @@ namespace echo {
 
 namespace {
 
-// What is stored of X, A and B: the true value times this.  fp16 holds 2^-24 to 65504, so
+// What is stored of Y, A and B: the true value times this.  fp16 holds 2^-24 to 65504, so
 // elements up to 16 fit, and 22 bits remain of elements down to 2^-25.
-constexpr float kScaleX = 0x1p12f, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
+constexpr float kScaleY = 0x1p12f, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
 
 // -- Frobenius norm ------------------------------------------------------------------------------
 // Sums of squares of x, of 2^-60 x and of 2^60 x: one of them neither overflows nor underflows,
@@ -114,54 +116,50 @@ __device__ __forceinline__ void split(float v, __half (&h)[PLANES]) {
   if constexpr (PLANES == 2) h[1] = __float2half_rn(v - __half2float(h[0]));
 }
 
-// X = G / (|G| + eps), and its transpose: `same` has G's orientation, `other` the other one.
-// A block takes 64 x 64 tiles; G and both results go in runs of at least 64 bytes.
+// Y = G / (|G| + eps), or its transpose.  A block takes 64 x 64 tiles, in bands of 16 rows of
+// tiles, column by column, so that the tiles in work at a time make long runs in G and in Y.
 template <typename T, int PLANES>
-__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes same, Planes other) {
+__global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
   __shared__ Factor factor;
-  __shared__ __half tile[PLANES][64][66];
+  __shared__ float tile[64][65];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int64_t tiles_c = (cols + 63) / 64, tiles = (rows + 63) / 64 * tiles_c;
+  const int64_t tiles_r = (rows + 63) / 64, tiles_c = (cols + 63) / 64;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     if (threadIdx.x < 32) {
-      const double v = inverse_norm(part, parts, z, a.eps) * (double)kScaleX;
+      const double v = inverse_norm(part, parts, z, a.eps) * (double)kScaleY;
       if (threadIdx.x == 0) factor.set(v);
     }
     __syncthreads();
     const Factor f = factor;
     const T *g = static_cast<const T *>(a.g) + z * a.g_batch_stride;
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-      const int64_t r0 = t / tiles_c * 64, c0 = t % tiles_c * 64;
+    for (int64_t t = blockIdx.x; t < tiles_r * tiles_c; t += gridDim.x) {
+      const int64_t band = t / (16 * tiles_c), in = t % (16 * tiles_c), high = min((int64_t)16, tiles_r - band * 16);
+      const int64_t r0 = (band * 16 + in % high) * 64, c0 = in / high * 64;
       float v[8][2];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int64_t r = r0 + ty + 8 * i, c = c0 + tx + 32 * e;
-          v[i][e] = r < rows && c < cols ? f(to_f(g[r * a.g_stride + c])) : 0.f;
+          v[i][e] = r < rows && c < cols ? to_f(g[r * a.g_stride + c]) : 0.f;
         }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          __half h[PLANES];
-          split<PLANES>(v[i][e], h);
-#pragma unroll
-          for (int q = 0; q < PLANES; ++q) tile[q][ty + 8 * i][tx + 32 * e] = h[q];
-        }
+        for (int e = 0; e < 2; ++e) tile[ty + 8 * i][tx + 32 * e] = f(v[i][e]);
       __syncthreads();
+      const int64_t y0 = a.tall ? r0 : c0, x0 = a.tall ? c0 : r0, yn = a.tall ? rows : cols, xn = a.tall ? cols : rows;
 #pragma unroll
-      for (int q = 0; q < PLANES; ++q)
+      for (int i = 0; i < 8; ++i) {
+        const int at = ty + 8 * i;  // two elements of a row of Y: the padding takes an odd end
+        if (y0 + at >= yn || x0 + 2 * tx >= xn) continue;
+        __half h[2][PLANES];
+        split<PLANES>(a.tall ? tile[at][2 * tx] : tile[2 * tx][at], h[0]);
+        split<PLANES>(a.tall ? tile[at][2 * tx + 1] : tile[2 * tx + 1][at], h[1]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int at = ty + 8 * i;  // two elements of a row: in both results the padding takes an odd end
-          if (r0 + at < rows && c0 + 2 * tx < cols)
-            *reinterpret_cast<__half2 *>(same.p + q * same.plane + z * same.matrix + (r0 + at) * same.ld + c0 + 2 * tx) =
-                *reinterpret_cast<const __half2 *>(&tile[q][at][2 * tx]);
-          if (c0 + at < cols && r0 + 2 * tx < rows)
-            *reinterpret_cast<__half2 *>(other.p + q * other.plane + z * other.matrix + (c0 + at) * other.ld + r0 + 2 * tx) =
-                __halves2half2(tile[q][2 * tx][at], tile[q][2 * tx + 1][at]);
-        }
+        for (int q = 0; q < PLANES; ++q)
+          *reinterpret_cast<__half2 *>(y.p + q * y.plane + z * y.matrix + (y0 + at) * y.ld + x0 + 2 * tx) = __halves2half2(h[0][q], h[1][q]);
+      }
       __syncthreads();
     }
     __syncthreads();
@@ -195,20 +193,20 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t r
 // pair's first block issues tcgen05.mma on both blocks' stages; eight warps take the sums out
 // of tensor memory, which holds two sets of them.
 //
-// The tensor core adds to its fp32 sums with truncation: over 12288 columns of fp32 matrices
-// (2304 additions an element) the result was 8e-5 off.  So for them a set of sums covers 256
-// columns (48 additions) and the eight warps add the sets up in registers, rounding to
-// nearest; they do it while the next set is summed.
+// The tensor core adds to its fp32 sums with truncation, which is a bias: with one set of sums
+// for 12288 columns of two-number operands (2304 additions an element) the result was 8e-5 off.
+// So for them a set covers one stage, the products of the low parts first, while the sums are
+// small, and the eight warps add the sets up in registers, rounding to nearest, while the next
+// set is summed: 7e-7 off there, and 6% more clocks than with sets of eight stages.
 constexpr int kBM = 256, kBK = 64, kRows = 128;  // of a tile, of a stage; rows of P a block holds
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 // Registers of a thread of warps 0-3 and of 4-11, which hold 128 sums each; together no more
 // than the 168 a thread that the block is launched with (65536 / 384, in units of 8).
 constexpr int kFewRegs = 56, kManyRegs = 216;
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
-constexpr int kChunk = 4;                        // stages of a set of sums of fp32 matrices
 constexpr int stage_bytes(int planes, int bn) { return planes * (kRows + bn / 2) * kBK * 2; }
 constexpr int stages(int planes, int bn) { return 196608 / stage_bytes(planes, bn); }
-constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out: 32 x 32 elements of D and of D^T
+constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out: 32 x 32 elements, twice
 constexpr size_t smem_bytes(int planes, int bn) {
   return (size_t)stages(planes, bn) * stage_bytes(planes, bn) + 8 * kOutBytes + 256 + 1024;
 }
@@ -221,6 +219,7 @@ struct ProductArgs {
   int symmetric;        // D is symmetric: tiles of the lower triangle, each element written twice
   float alpha, beta;
   Planes c;             // C (p may be null)
+  float diagonal;       // added to D's diagonal (symmetric)
   void *o;              // the last product: the result instead of D
   int64_t o_stride, o_batch_stride;
   int o_transposed;
@@ -243,11 +242,11 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
                : "=r"(ok)
                : "r"(bar), "r"(parity)
                : "memory");
@@ -270,20 +269,38 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   return true;
 }
 
-// 64 columns from k (a multiple of 64) of a box of rows from `row`.
-__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap *map, int k, int row, int z, int plane, uint32_t bar) {
+// A box of a matrix from (column, row); the column is a multiple of 64.
+__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap *map, int col, int row, int z, int plane, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n" ::"r"(to),
-      "l"(map), "r"(bar), "r"(k), "r"(row), "r"(z), "r"(plane)
+      "l"(map), "r"(bar), "r"(col), "r"(row), "r"(z), "r"(plane)
       : "memory");
 }
-
-// Descriptor of an operand tile: rows of 128 bytes, swizzled in groups of 8 rows (1024 bytes).
-__device__ __forceinline__ uint64_t operand(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// R rows (of P or Q) x 64 columns of the sum from (r, k).  MN: the matrix holds the transpose, so
+// boxes of 64 of its rows (the sum) x 64 columns, one behind the other.
+template <bool MN, int R>
+__device__ __forceinline__ void copy_operand(uint32_t to, const CUtensorMap *map, int r, int k, int z, int plane, uint32_t bar) {
+  if constexpr (MN) {
+#pragma unroll
+    for (int g = 0; g < R / 64; ++g) copy_tile(to + g * 8192, map, r + g * 64, k, z, plane, bar);
+  } else {
+    copy_tile(to, map, k, r, z, plane, bar);
+  }
 }
-// fp16 operands, fp32 sums, both along K, `bn` columns, kBM rows
-constexpr uint32_t instruction(int bn) { return 1u << 4 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(kBM >> 4) << 24; }
+
+// Descriptor of an operand in shared memory, lines of 128 bytes swizzled in groups of 8 (1024
+// bytes).  Lines are rows of the operand, or (MN) of the sum, with 64 rows of the operand on a
+// line and the next 64 8192 bytes on.
+template <bool MN>
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(MN ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// 16 columns of the sum on: 32 bytes of a line, or 16 lines
+constexpr int step16(bool mn) { return (mn ? 2048 : 32) >> 4; }
+// fp16 operands, fp32 sums, `bn` columns, kBM rows
+constexpr uint32_t instruction(int bn, bool mn) {
+  return 1u << 4 | (mn ? 3u << 15 : 0u) | (uint32_t)(bn >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
+}
 
 __device__ __forceinline__ void mma(uint32_t d, uint64_t p, uint64_t q, uint32_t instr, bool add) {
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(p),
@@ -298,20 +315,27 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void load_sums(uint32_t at, float (&v)[32]) {
+// 32 columns of this warp's rows of tensor memory; sums_loaded() before the values are used.
+struct Sums {
   uint32_t r[32];
+};
+__device__ __forceinline__ void load_sums(uint32_t at, Sums &s) {
+  uint32_t (&r)[32] = s.r;
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
       "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-      "tcgen05.wait::ld.sync.aligned;\n"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
         "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
         "=r"(r[31])
       : "r"(at)
       : "memory");
+}
+__device__ __forceinline__ void sums_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
+// (the wait keeps the compiler from using a register before it: the values pass through it)
+__device__ __forceinline__ void pass(Sums &s) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(s.r[i]));
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
@@ -338,60 +362,63 @@ __device__ __forceinline__ void tile_place(const ProductArgs &a, int64_t t, int 
   c0 = (int)j * BN;
 }
 
-// 32 x 32 elements from a warp's buffer to a matrix of the iteration, by one thread; what is
-// outside the matrix is dropped.
-__device__ __forceinline__ void store_tile(const CUtensorMap *map, uint32_t from, int col, int row, int z, int plane) {
+// A warp's buffer turns 32 x 32 elements between a row a lane and four lanes to the 64 bytes of
+// a row, which is how they meet global memory.  Its halves take turns, so that a half is
+// written again only after a synchronisation behind its last reads.  Rows have their 16-byte
+// pieces exchanged (64 bytes on, they would meet in the same banks).
+__device__ __forceinline__ unsigned char *piece(unsigned char *half, int row, int i) { return half + row * 64 + (i ^ ((row >> 1) & 3)) * 16; }
+using Piece = Pack<__half, 8>;
+
+// From a half of the buffer to a matrix of the iteration, by one thread; what is outside the
+// matrix is dropped.
+__device__ __forceinline__ void store_half(const CUtensorMap *map, const unsigned char *half, int col, int row, int z, int plane) {
   asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];\ncp.async.bulk.commit_group;\n" ::"l"(map),
-               "r"(from), "r"(col), "r"(row), "r"(z), "r"(plane)
+               "r"(smem_u32(half)), "r"(col), "r"(row), "r"(z), "r"(plane)
                : "memory");
 }
-// All but the last store of this thread have read their buffer (or, at the end, all are done).
-__device__ __forceinline__ void stores_but_one_read() { asm volatile("cp.async.bulk.wait_group.read 1;\n" ::: "memory"); }
-__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
+// Before a half is written: the stores but the last have read theirs, for the whole warp.
+__device__ __forceinline__ void half_free(int lane) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;\n" ::: "memory");
+  __syncwarp();
+}
+// What the warp wrote to a half is there for the copy engine.
+__device__ __forceinline__ void half_written() {
+  asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+  __syncwarp();
+}
 
 // 32 x 32 elements of a tile out, by a warp: lane r has those of row row0 + r in v, from column
 // c.  A symmetric product writes the blocks of the lower triangle and, transposed, those of the
-// upper one.  The two halves of the buffer take turns, D's with 16-byte pieces exchanged as the
-// map's 64-byte swizzle has it (rows of 64 bytes would meet in the same banks).
+// upper one.  dmap takes rows with exchanged pieces (its 64-byte swizzle), tmap plain ones.
+//
+// By the copy engine: the tensor core's reads of the stages nearly fill shared memory's
+// bandwidth, and every pass through it that the warps do themselves waits for a gap.
 template <int PLANES>
-__device__ __forceinline__ void block_out(const CUtensorMap *dmap, const CUtensorMap *tmap, bool symmetric, int z, int row0, int c, int lane,
-                                          const float (&v)[32], unsigned char *buffer) {
-  if (symmetric && c > row0) return;
-  const bool mirror = !symmetric || c < row0;
-  const uint32_t buf = smem_u32(buffer);
-#pragma unroll
+__device__ __forceinline__ void block_out(const ProductArgs &a, const CUtensorMap *dmap, const CUtensorMap *tmap, int z, int row0, int c, int lane,
+                                          float (&v)[32], unsigned char *buffer, uint32_t &turn) {
+  if (a.symmetric && c > row0) return;
+#pragma unroll 1
   for (int q = 0; q < PLANES; ++q) {
-    __half h[32];
+    Piece h[4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      __half e[PLANES];
-      split<PLANES>(v[i], e);
-      h[i] = e[q];
+      h[i / 8].v[i % 8] = __float2half_rn(v[i]);
+      if constexpr (PLANES == 2) v[i] -= __half2float(h[i / 8].v[i % 8]);  // what the next plane holds
     }
-    if (lane == 0) stores_but_one_read();
-    __syncwarp();
+    half_free(lane);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      Pack<__half, 8> w;
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<Piece *>(piece(buffer + turn, lane, i)) = h[i];
+    half_written();
+    if (lane == 0) store_half(dmap, buffer + turn, c, row0, z, q);
+    turn ^= 2048;
+    if (!a.symmetric || c == row0) continue;
+    half_free(lane);
+    __half *t = reinterpret_cast<__half *>(buffer + turn) + lane;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w.v[e] = h[8 * i + e];
-      *reinterpret_cast<Pack<__half, 8> *>(buffer + lane * 64 + (i ^ ((lane >> 1) & 3)) * 16) = w;
-    }
-    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-    __syncwarp();
-    if (lane == 0) {
-      store_tile(dmap, buf, c, row0, z, q);
-      if (mirror) stores_but_one_read();
-      else stores_done();  // (the next block's first half is this one's)
-    }
-    if (!mirror) continue;
-    __syncwarp();
-    __half *t = reinterpret_cast<__half *>(buffer + 2048) + lane;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) t[i * 32] = h[i];
-    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-    __syncwarp();
-    if (lane == 0) store_tile(tmap, buf + 2048, row0, c, z, q);
+    for (int i = 0; i < 32; ++i) t[i * 32] = h[i / 8].v[i % 8];
+    half_written();
+    if (lane == 0) store_half(tmap, buffer + turn, row0, c, z, q);
+    turn ^= 2048;
   }
 }
 
@@ -417,13 +444,13 @@ __device__ __forceinline__ void result_out(const ProductArgs &a, int64_t z, int 
   if (c + lane < a.N) {
     o += (int64_t)row0 * a.o_stride + c + lane;
     const int rows = min(32, a.M - row0);
-#pragma unroll 8
+#pragma unroll 4
     for (int r = 0; r < rows; ++r, o += a.o_stride) *o = from_f<OUT>(f[r * 32 + (lane ^ r)]);
   }
 }
 
 // OUT: void for a product whose result goes on in planes, else the type of the result.
-template <int PLANES, int BN, typename OUT>
+template <int PLANES, int BN, bool MN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     ortho_product_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap dmap,
                          const __grid_constant__ CUtensorMap tmap, const __grid_constant__ ProductArgs a) {
@@ -453,6 +480,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
+  if (threadIdx.x == 32 * 3) {
+    asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&pmap), "l"(&qmap) : "memory");
+  }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base)), "r"(2u * BN) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
@@ -462,8 +492,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
   const uint32_t tmem = tmem_base;
+  // What is above overlaps the end of the kernel before; from here on its results are read.
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   const int64_t all = a.tiles * a.batch;
-  const int steps = (a.K + kBK - 1) / kBK, chunk = PLANES == 2 ? kChunk : steps;
+  const int steps = (a.K + kBK - 1) / kBK, chunk = PLANES == 2 ? 1 : steps;  // stages of a set of sums
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kFewRegs));
@@ -482,8 +515,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);  // both blocks' copies
 #pragma unroll
           for (int q = 0; q < PLANES; ++q) {
-            copy_tile(at + q * kP, &pmap, k * kBK, r0 + rank * kRows, z, q, bar);
-            copy_tile(at + PLANES * kP + q * kQ, &qmap, k * kBK, c0 + rank * kCols, z, q, bar);
+            copy_operand<MN, kRows>(at + q * kP, &pmap, r0 + rank * kRows, k * kBK, z, q, bar);
+            copy_operand<MN, kCols>(at + PLANES * kP + q * kQ, &qmap, c0 + rank * kCols, k * kBK, z, q, bar);
           }
         }
       }
@@ -507,15 +540,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             ok = bar_wait(full + 8 * s, (uint32_t)(it / S) & 1, abort, a);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            const uint64_t p = operand(ring + s * kStage), q = operand(ring + s * kStage + PLANES * kP);
+            const uint64_t p = operand<MN>(ring + s * kStage), q = operand<MN>(ring + s * kStage + PLANES * kP);
+            constexpr uint32_t kInstr = instruction(BN, MN);
+            if constexpr (PLANES == 2) {
 #pragma unroll
-            for (int kk = 0; kk < kBK / 16; ++kk) {  // 16 columns: 32 bytes on
-              mma(d, p + 2 * kk, q + 2 * kk, instruction(BN), k > k0 || kk > 0);
-              if constexpr (PLANES == 2) {
-                mma(d, p + 2 * kk, q + 2 * kk + (kQ >> 4), instruction(BN), true);
-                mma(d, p + 2 * kk + (kP >> 4), q + 2 * kk, instruction(BN), true);
+              for (int kk = 0; kk < kBK / 16; ++kk) {
+                mma(d, p + step16(MN) * kk, q + step16(MN) * kk + (kQ >> 4), kInstr, k > k0 || kk > 0);
+                mma(d, p + step16(MN) * kk + (kP >> 4), q + step16(MN) * kk, kInstr, true);
               }
             }
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(MN) * kk, q + step16(MN) * kk, kInstr, PLANES == 2 || k > k0 || kk > 0);
             commit_pair(empty + 8 * s);
           }
           if (ok) commit_pair(sums_full + 8 * b);
@@ -533,6 +568,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     unsigned char *buffer = buffers + (warp - 4) * kOutBytes;
     const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + side * kCols;
     int64_t n = 0;
+    uint32_t turn = 0;
     bool ok = true;
     for (int64_t t = pair; t < all && ok; t += pairs) {
       int r0, c0;
@@ -540,73 +576,106 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int z = (int)(t / a.tiles), row0 = r0 + rank * kRows + quarter * 32;
       const bool live = row0 < a.M;
       c0 += side * kCols;
-      // C's part of the tile comes to L2 during the sums, and to registers one block ahead
-      const __half *from_c = a.c.p && row0 + lane < a.M ? a.c.p + z * a.c.matrix + (int64_t)(row0 + lane) * a.c.ld : nullptr;
-      if (from_c) {
+      const bool add_c = !MN && a.c.p;
+      const __half *from_c = a.c.p + z * a.c.matrix;
+      if (add_c && row0 + lane < a.M) {  // C's part of the tile comes to L2 during the sums
 #pragma unroll
         for (int q = 0; q < PLANES; ++q)
 #pragma unroll
           for (int i = 0; i < kCols; i += 64)
-            if (c0 + i < a.N) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(from_c + q * a.c.plane + c0 + i));
+            if (c0 + i < a.N) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(from_c + q * a.c.plane + (int64_t)(row0 + lane) * a.c.ld + c0 + i));
       }
-      float acc[kCols / 32][32];
-      for (int k0 = 0; k0 < steps; k0 += chunk, ++n) {
-        const int b = (int)(n & 1);
-        ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+      // C is added to the sums a plane of a 32 x 32 block at a time, with the last sets: each piece
+      // comes one set ahead, four lanes to the 64 bytes of a row, and changes to a row a lane in
+      // the warp's buffer.
+      constexpr int kFlight = MN ? 2 : 1;
+      constexpr int kParts = kCols / 32, kPieces = MN ? 0 : PLANES * kParts;
+      const int sets = (steps + chunk - 1) / chunk, first_c = add_c ? max(0, sets - kPieces - 1) : sets;
+      Piece ahead[4] = {};
+      auto fetch = [&](int u) {
+        const int row = row0 + (lane >> 2), col = c0 + u / PLANES * 32 + (lane & 3) * 8;
+        const __half *p = from_c + (int64_t)row * a.c.ld + col + u % PLANES * a.c.plane;
 #pragma unroll
-        for (int part = 0; part < kCols / 32; ++part) {
-          __syncwarp();
-          if (k0 == 0) {
-            load_sums(from + b * BN + part * 32, acc[part]);
-          } else {
-            float v[32];
-            load_sums(from + b * BN + part * 32, v);
+        for (int i = 0; i < 4; ++i)  // (to the end of a piece: within the padding of the row)
+          if (row + 8 * i < a.M && col < a.N) ahead[i] = *reinterpret_cast<const Piece *>(p + (int64_t)(8 * i) * a.c.ld);
+      };
+      float acc[kParts][32];
+      for (int set = 0; set < max(sets, add_c ? first_c + kPieces + 1 : 0); ++set) {
+        if (set < sets) {
+          const int b = (int)(n & 1);
+          ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a);
+          if (!ok) break;
+          ++n;
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 32; ++i) acc[part][i] += v[i];
+          for (int part = 0; part < kParts; part += kFlight) {
+            Sums s[kFlight];
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < kFlight; ++e) load_sums(from + b * BN + (part + e) * 32, s[e]);
+            sums_loaded();
+#pragma unroll
+            for (int e = 0; e < kFlight; ++e) {
+              pass(s[e]);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) acc[part + e][i] = fmaf(a.alpha, __uint_as_float(s[e].r[i]), set == 0 ? 0.f : acc[part + e][i]);
+            }
           }
+          asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(in_first(sums_empty + 8 * b));
         }
-        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0) bar_arrive_cluster(in_first(sums_empty + 8 * b));
+        if (set < first_c) continue;
+        const int u = set - first_c - 1;  // this set's piece
+        if (kPieces && u >= 0 && u < kPieces) {
+          half_free(lane);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *reinterpret_cast<Piece *>(piece(buffer + turn, 8 * i + (lane >> 2), lane & 3)) = ahead[i];
+          __syncwarp();
+          auto add = [&](auto which) {
+            constexpr int part = decltype(which)::value;
+            if (part != u / PLANES) return;
+            asm volatile("" ::"n"(part));  // (keeps the blocks apart: as one, they would index the sums in memory)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float f[8];
+              unpack<__half, 8>(*reinterpret_cast<const Piece *>(piece(buffer + turn, lane, i)), f);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc[part][8 * i + e] += a.beta * f[e];
+            }
+          };
+          add(Int<0>{});
+          add(Int<1>{});
+          if constexpr (kParts == 4) {
+            add(Int<2>{});
+            add(Int<3>{});
+          }
+          __syncwarp();
+        }
+        if (u + 1 < kPieces) fetch(u + 1);
       }
       if (!ok) break;
       if (!live) continue;
-      Pack<__half, 8> ahead[PLANES][4] = {};
-      auto fetch = [&](int c) {
+      // One block after the other, in the registers of the first (unrolled, the code is 80 KB and
+      // runs once a tile).
+      float (&v)[32] = acc[0];
+#pragma unroll 1
+      for (int c = c0; c < min(a.N, c0 + kCols); c += 32) {
+        if (a.symmetric && c == row0) {
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (from_c && c + 8 * i < a.N)  // (to the end of a piece: within the padding of the row)
-              ahead[q][i] = *reinterpret_cast<const Pack<__half, 8> *>(from_c + q * a.c.plane + c + 8 * i);
-      };
-      fetch(c0);
-#pragma unroll
-      for (int part = 0; part < kCols / 32; ++part) {
-        const int c = c0 + part * 32;
-        if (c >= a.N) continue;
-        float (&v)[32] = acc[part];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= a.alpha;
-#pragma unroll
-        for (int q = 0; q < PLANES; ++q)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float f[8];
-            unpack<__half, 8>(ahead[q][i], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[8 * i + e] += a.beta * f[e];
-          }
-        if (part + 1 < kCols / 32) fetch(c + 32);
+          for (int i = 0; i < 32; ++i) v[i] += i == lane ? a.diagonal : 0.f;
+        }
         if constexpr (std::is_void_v<OUT>)
-          block_out<PLANES>(&dmap, &tmap, a.symmetric, z, row0, c, lane, v, buffer);
+          block_out<PLANES>(a, &dmap, &tmap, z, row0, c, lane, v, buffer, turn);
         else
           result_out<OUT>(a, z, row0, c, lane, v, buffer);
+#pragma unroll
+        for (int part = 1; part < kParts; ++part)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) acc[part - 1][i] = acc[part][i];
       }
     }
-    if (lane == 0) stores_done();
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
     __syncwarp();
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -634,8 +703,8 @@ EncodeTiled encoder() {
 }
 
 // Boxes of a matrix of the iteration; zeros outside it.
-cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows, int box_cols,
-                     CUtensorMapSwizzle swizzle) {
+cudaError_t box_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows, int box_cols,
+                    CUtensorMapSwizzle swizzle) {
   if (!encoder()) return cudaErrorNotSupported;
   const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)planes};
   const cuuint64_t strides[3] = {(cuuint64_t)p.ld * 2, (cuuint64_t)p.matrix * 2, (cuuint64_t)p.plane * 2};
@@ -645,6 +714,13 @@ cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t co
              ? cudaSuccess
              : cudaErrorInvalidValue;
 }
+// 64 columns, for the stages; 32 x 32 for a warp's buffer
+cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows) {
+  return box_map(map, p, rows, cols, batch, planes, box_rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+cudaError_t out_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, bool exchanged) {
+  return box_map(map, p, rows, cols, batch, planes, 32, 32, exchanged ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE);
+}
 
 int64_t padded(int64_t x) { return (x + 63) / 64 * 64; }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -653,18 +729,17 @@ Planes planes_of(char *&at, int64_t rows, int64_t cols, int64_t batch, int plane
   at += up256((size_t)planes * p.plane * sizeof(__half));
   return p;
 }
-int planes_for(int type) { return type == ECHO_F32 ? 2 : 1; }
+int planes_for(int type) { return type == ECHO_BF16 ? 1 : 2; }
 
 }  // namespace
 
 // blocks that sum a matrix for its norm
 int norm_parts(const OrthoArgs &a) { return (int)std::clamp<int64_t>(a.m * a.n / 8192, 1, 608); }
 
-// parts of the norm; X, X^T twice (a product reads one while it writes the other), A, B
+// parts of the norm; Y twice (a product reads one while it writes the other), A, B
 size_t ortho_scratch_bytes(const OrthoArgs &a) {
   char *at = nullptr;
   const int planes = planes_for(a.type);
-  planes_of(at, a.m, a.n, a.batch, planes);
   for (int i = 0; i < 2; ++i) planes_of(at, a.n, a.m, a.batch, planes);
   for (int i = 0; i < 2; ++i) planes_of(at, a.m, a.m, a.batch, planes);
   return (a.steps ? reinterpret_cast<uintptr_t>(at) : 0) + up256((size_t)a.batch * norm_parts(a) * 3 * sizeof(float));
@@ -697,70 +772,91 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
         return cudaGetLastError();
       });
     });
-  const Planes X = planes_of(at, a.m, a.n, a.batch, planes);
-  const Planes XT[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
+  const Planes Y[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
   const Planes A = planes_of(at, a.m, a.m, a.batch, planes), B = planes_of(at, a.m, a.m, a.batch, planes);
   e = timed("ortho_start", [&] {
-    const dim3 grid((unsigned)std::min<int64_t>((rows + 63) / 64 * ((cols + 63) / 64), sms * 8), gz);
-    const Planes &same = a.tall ? XT[0] : X, &other = a.tall ? X : XT[0];
+    const dim3 grid((unsigned)std::min<int64_t>((rows + 63) / 64 * ((cols + 63) / 64), std::max<int64_t>(1, sms * 6 / gz)), gz);
     return with_type(a.type, [&](auto t) {
       using T = decltype(t);
-      ortho_start_kernel<T, std::is_same_v<T, float> ? 2 : 1><<<grid, 256, 0, st>>>(a, rows, cols, part, parts, same, other);
+      ortho_start_kernel<T, std::is_same_v<T, __nv_bfloat16> ? 1 : 2><<<grid, 256, 0, st>>>(a, rows, cols, part, parts, Y[0]);
       return cudaGetLastError();
     });
   });
   if (e != cudaSuccess) return e;
 
   const int pairs = sms / 2;
-  const int64_t tm = (a.m + kBM - 1) / kBM;
-  auto tiles_of = [&](int64_t N, bool symmetric, int bn) { return symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn); };
-  struct Operand {
+  auto tiles_of = [](int64_t M, int64_t N, bool symmetric, int bn) {
+    const int64_t tm = (M + kBM - 1) / kBM;
+    return symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn);
+  };
+  struct Matrix {
     const Planes &p;
     int64_t rows, cols;
   };
-  const Operand x{X, a.m, a.n}, xt[2] = {{XT[0], a.n, a.m}, {XT[1], a.n, a.m}}, sa{A, a.m, a.m}, sb{B, a.m, a.m};
-  auto product = [&](const char *name, const Operand &p, const Operand &q, bool symmetric, float alpha, float beta, const Planes *c, const Operand *d,
-                     const Operand *dt) -> cudaError_t {
+  const Matrix y[2] = {{Y[0], a.n, a.m}, {Y[1], a.n, a.m}}, sa{A, a.m, a.m}, sb{B, a.m, a.m};
+  // D = alpha P Q^T + beta C (mn: P and Q hold the transposes); the result without a D.  D is
+  // symmetric where P is Q.
+  auto product = [&](const char *name, const Matrix &p, const Matrix &q, bool mn, float alpha, const Planes *c, float beta, float diagonal, const Matrix *d) -> cudaError_t {
     ProductArgs g{};
-    g.batch = a.batch, g.M = (int)a.m, g.N = (int)q.rows, g.K = (int)p.cols;
+    const bool symmetric = &p == &q;
+    g.batch = a.batch, g.M = (int)(mn ? p.cols : p.rows), g.N = (int)(mn ? q.cols : q.rows), g.K = (int)(mn ? p.rows : p.cols);
     g.symmetric = symmetric;
-    g.alpha = alpha, g.beta = beta;
+    g.alpha = alpha, g.beta = beta, g.diagonal = diagonal;
     if (c) g.c = *c;
-    g.o = a.o, g.o_stride = a.o_stride, g.o_batch_stride = a.o_batch_stride, g.o_transposed = a.tall;
+    g.o = a.o, g.o_stride = a.o_stride, g.o_batch_stride = a.o_batch_stride, g.o_transposed = !a.tall;
     g.status = a.status, g.wait_limit = a.wait_limit, g.skip = a.skip;
-    auto go = [&](auto planes_c, auto cols_c, auto out) -> cudaError_t {
+    auto go = [&](auto planes_c, auto cols_c, auto mn_c, auto out) -> cudaError_t {
       constexpr int P = decltype(planes_c)::value, BN = decltype(cols_c)::value;
+      constexpr bool MN = decltype(mn_c)::value;
       using O = std::remove_pointer_t<decltype(out)>;
       g.tiles_n = (int)((g.N + BN - 1) / BN);
-      g.tiles = tiles_of(g.N, symmetric, BN);
+      g.tiles = tiles_of(g.M, g.N, symmetric, BN);
       CUtensorMap pm, qm, dm{}, tm{};
-      cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, planes, kRows, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
-      if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, planes, BN / 2, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
-      if (r == cudaSuccess && d) r = tile_map(&dm, d->p, d->rows, d->cols, a.batch, planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-      if (r == cudaSuccess && d) r = tile_map(&tm, dt->p, dt->rows, dt->cols, a.batch, planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
-      auto kernel = ortho_product_kernel<P, BN, O>;
+      cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, planes, MN ? kBK : kRows);
+      if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, planes, MN ? kBK : BN / 2);
+      if (r == cudaSuccess && d) r = out_map(&dm, d->p, d->rows, d->cols, a.batch, planes, true);
+      if (r == cudaSuccess && d && symmetric) r = out_map(&tm, d->p, d->rows, d->cols, a.batch, planes, false);
+      auto kernel = ortho_product_kernel<P, BN, MN, O>;
       if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(P, BN));
       if (r != cudaSuccess) return r;
-      kernel<<<(unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2, kThreads, smem_bytes(P, BN), st>>>(pm, qm, dm, tm, g);
-      return cudaGetLastError();
+      cudaLaunchConfig_t how{};
+      how.gridDim = dim3((unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2);
+      how.blockDim = dim3(kThreads);
+      how.dynamicSmemBytes = smem_bytes(P, BN);
+      how.stream = st;
+      cudaLaunchAttribute early{};  // the blocks may start while the kernel before ends
+      early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      early.val.programmaticStreamSerializationAllowed = 1;
+      how.attrs = &early;
+      how.numAttrs = 1;
+      return cudaLaunchKernelEx(&how, kernel, pm, qm, dm, tm, g);
     };
     auto with_out = [&](auto cols_c) -> cudaError_t {
-      if (d) return planes == 2 ? go(Int<2>{}, cols_c, (void *)nullptr) : go(Int<1>{}, cols_c, (void *)nullptr);
-      return planes == 2 ? go(Int<2>{}, cols_c, (float *)nullptr)
-             : a.type == ECHO_BF16 ? go(Int<1>{}, cols_c, (__nv_bfloat16 *)nullptr)
-                                   : go(Int<1>{}, cols_c, (__half *)nullptr);
+      if (mn) return planes == 2 ? go(Int<2>{}, cols_c, Int<1>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<1>{}, (void *)nullptr);
+      if (d) return planes == 2 ? go(Int<2>{}, cols_c, Int<0>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<0>{}, (void *)nullptr);
+      return a.type == ECHO_F32 ? go(Int<2>{}, cols_c, Int<0>{}, (float *)nullptr)
+             : a.type == ECHO_BF16 ? go(Int<1>{}, cols_c, Int<0>{}, (__nv_bfloat16 *)nullptr)
+                                   : go(Int<2>{}, cols_c, Int<0>{}, (__half *)nullptr);
     };
-    // narrower tiles where the wide ones would not occupy every pair
-    const bool narrow = tiles_of(q.rows, symmetric, 256) * a.batch < pairs;
+    // The width with fewer (rounds of tiles) x (time of a stage): 1536 clocks of products, or
+    // 1020 where L2 bounds, for two-number operands; 690 and 565 for the others, both bound by L2.
+    auto cost = [&](int bn, int clocks) { return (tiles_of(g.M, g.N, symmetric, bn) * a.batch + pairs - 1) / pairs * clocks; };
+    const bool narrow = cost(128, planes == 2 ? 1020 : 565) < cost(256, planes == 2 ? 1536 : 690);
     return timed(name, [&] { return narrow ? with_out(Int<128>{}) : with_out(Int<256>{}); });
   };
   for (int s = 0; s < a.steps; ++s) {
+    const Matrix &now = y[s & 1], &next = y[(s + 1) & 1];
     const bool last = s == a.steps - 1;
-    if ((e = product("ortho_xxt", x, x, true, kScaleA / (kScaleX * kScaleX), 0.f, nullptr, &sa, &sa)) != cudaSuccess) return e;
-    if ((e = product("ortho_aa", sa, sa, true, a.c * (kScaleB / (kScaleA * kScaleA)), a.b * (kScaleB / kScaleA), &A, &sb, &sb)) != cudaSuccess) return e;
-    const float out = last ? a.scale / kScaleX : 1.f;
-    if ((e = product("ortho_bx", sb, xt[s & 1], false, out / kScaleB, out * a.a, &X, last ? nullptr : &x, &xt[(s + 1) & 1])) != cudaSuccess)
+    const float out = last ? a.scale / kScaleY : 1.f;
+    if ((e = product("ortho_yty", now, now, true, kScaleA / (kScaleY * kScaleY), nullptr, 0.f, 0.f, &sa)) != cudaSuccess) return e;
+    // a Y comes from B + a I for matrices of one number an element: the last product then reads
+    // and adds nothing.  With two numbers the larger sums would lose more to truncation than the
+    // sum of a Y and Y B in fp32 does (2.7e-6 instead of 1.0e-6 at 300 x 300).
+    const bool fold = planes == 1;
+    if ((e = product("ortho_aa", sa, sa, false, a.c * (kScaleB / (kScaleA * kScaleA)), &A, a.b * (kScaleB / kScaleA), fold ? a.a * kScaleB : 0.f, &sb)) !=
+        cudaSuccess)
       return e;
+    if ((e = product("ortho_yb", now, sb, false, out / kScaleB, fold ? nullptr : &now.p, out * a.a, 0.f, last ? nullptr : &next)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
