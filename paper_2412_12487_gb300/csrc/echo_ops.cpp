@@ -66,6 +66,10 @@ int entry(echo_ctx *c, const void *d, F &&body) {
     if (_e != cudaSuccess) return echo::op_cuda_error(c, _e, name);                           \
   } while (0)
 
+echo::OpTimer timer(echo_ctx *c) {
+  return [c](const char *name, const std::function<cudaError_t()> &f) { return echo::op_launch(c, name, f); };
+}
+
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -188,11 +192,9 @@ int echo_layer_norm_grad(echo_ctx *c, const echo_layer_norm_grad_desc *d) {
       void *scratch = nullptr;
       if (const int rc = echo::op_scratch(c, (size_t)a.parts * 2 * a.H * sizeof(float), &scratch)) return rc;
       a.part = static_cast<float *>(scratch);
-      // (before dx: it may overwrite dy or x)
-      if (a.parts) RUN(echo::launch_layer_norm_grad_columns(a, o.stream), "layer_norm_grad_columns");
-      RUN(echo::launch_layer_norm_grad_join(a, o.stream), "layer_norm_grad_join");
     }
-    if (a.dx && a.rows) RUN(echo::launch_layer_norm_grad_rows(a, o.sms, o.stream), "layer_norm_grad_rows");
+    const cudaError_t e = echo::launch_layer_norm_grad(a, o.sms, timer(c), o.stream);
+    if (e != cudaSuccess) return echo::op_cuda_error(c, e, "layer_norm_grad");
     return (int)ECHO_OK;
   });
 }
@@ -220,8 +222,7 @@ int echo_orthogonalize(echo_ctx *c, const echo_orthogonalize_desc *d) {
                       d->a, d->b, d->c, d->eps, d->scale, nullptr, nullptr, o.wait_limit, o.skip};
     if (const int rc = echo::op_status(c, &a.status)) return rc;
     if (const int rc = echo::op_scratch(c, echo::ortho_scratch_bytes(a), &a.scratch)) return rc;
-    const cudaError_t e = echo::launch_orthogonalize(
-        a, o.sms, [&](const char *name, const std::function<cudaError_t()> &f) { return echo::op_launch(c, name, f); }, o.stream);
+    const cudaError_t e = echo::launch_orthogonalize(a, o.sms, timer(c), o.stream);
     if (e != cudaSuccess) return echo::op_cuda_error(c, e, "orthogonalize");
     return (int)ECHO_OK;
   });

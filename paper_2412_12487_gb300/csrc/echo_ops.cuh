@@ -73,6 +73,37 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// Pairs of fp32 numbers: one instruction for both.
+struct Pair {
+  float a, b;
+};
+__device__ __forceinline__ uint64_t bits(Pair p) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(p.a), "f"(p.b));
+  return r;
+}
+__device__ __forceinline__ Pair pair(uint64_t r) {
+  Pair p;
+  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(p.a), "=f"(p.b) : "l"(r));
+  return p;
+}
+__device__ __forceinline__ Pair both(float x) { return {x, x}; }
+__device__ __forceinline__ Pair fma2(Pair x, Pair y, Pair z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(bits(x)), "l"(bits(y)), "l"(bits(z)));
+  return pair(r);
+}
+__device__ __forceinline__ Pair add2(Pair x, Pair y) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(bits(x)), "l"(bits(y)));
+  return pair(r);
+}
+__device__ __forceinline__ Pair mul2(Pair x, Pair y) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(bits(x)), "l"(bits(y)));
+  return pair(r);
+}
+
 constexpr int type_bytes(int type) { return type == ECHO_F32 ? 4 : 2; }
 
 // Whether rows `stride` elements apart can be read in pieces of W elements.

@@ -34,6 +34,9 @@ int op_status(echo_ctx *c, int32_t **p);
 cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch);
 
 // -- launches ------------------------------------------------------------------------------
+// Runs a launch under a name: op_launch with its context (for calls of several kernels).
+using OpTimer = std::function<cudaError_t(const char *, const std::function<cudaError_t()> &)>;
+
 struct EmbedArgs {
   int64_t n, H, V, v0;      // tokens, row length, rows of the shard, its first id
   const void *ids;
@@ -88,13 +91,12 @@ struct NormGradArgs {
   void *dx, *dw, *db;
   int64_t dy_stride, x_stride, dx_stride;
   int x_type, p_type, accumulate;
-  float *part;              // scratch: [parts][2][H] partial sums of dw and db
+  float *part;              // scratch: [parts][2][H] partial sums of dw and db, or null without them
   int parts;
 };
+// Partial sums that the call below writes (rows > 0).
 int layer_norm_grad_parts(int64_t rows, int64_t H, int x_type, int sms);
-cudaError_t launch_layer_norm_grad_rows(const NormGradArgs &a, int sms, cudaStream_t st);
-cudaError_t launch_layer_norm_grad_columns(const NormGradArgs &a, cudaStream_t st);
-cudaError_t launch_layer_norm_grad_join(const NormGradArgs &a, cudaStream_t st);
+cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
 
 // Orthogonalised update: m <= n are the smaller and the larger side, `tall` whether the
 // matrices have n rows (the others are taken transposed).
@@ -112,7 +114,6 @@ struct OrthoArgs {
   int skip;                 // failure injection for tests (ProductArgs)
 };
 size_t ortho_scratch_bytes(const OrthoArgs &a);
-using OpTimer = std::function<cudaError_t(const char *, const std::function<cudaError_t()> &)>;
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
 
 }  // namespace echo

@@ -23,60 +23,121 @@ __device__ __forceinline__ float row_sum(float v, float *sh) {
   return s;
 }
 
-// -- forward -----------------------------------------------------------------------------------
-// A row stays in the registers of blockDim.x threads, E elements each, between its mean, the
-// sum of its squared distances from it, and its output: x is read once.  Bound by the bytes.
+// A thread's E elements of a row lie in K = E / W pieces blockDim.x apart; in registers they
+// are pairs, one piece after the other.
 template <typename X, int W, int E>
-__global__ void __launch_bounds__(1024) layer_norm_kernel(NormArgs a) {
-  constexpr int K = E / W;
-  __shared__ float sh[2][32];
-  const float over_h = 1.f / (float)a.H;
-  for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += (int64_t)gridDim.x * blockDim.y) {
-    const int64_t row = row0 + threadIdx.y;
-    const bool live = row < a.rows;
-    const X *x = static_cast<const X *>(a.x) + row * a.x_stride;
-    float v[K][W];
-    float s = 0.f;
+struct Slice {
+  Pack<X, W> piece[E / W];
+  __device__ __forceinline__ static int column(int k) { return (k * (int)blockDim.x + (int)threadIdx.x) * W; }
+  // (nothing is read outside the row; those pieces hold what they held)
+  __device__ __forceinline__ void load(const X *row, int H, bool live) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int64_t j = ((int64_t)k * blockDim.x + threadIdx.x) * W;
+    for (int k = 0; k < E / W; ++k)
+      if (live && column(k) < H) piece[k] = *reinterpret_cast<const Pack<X, W> *>(row + column(k));
+  }
+  __device__ __forceinline__ void get(Pair (&v)[E / 2], int H) const {
+    float f[E];
 #pragma unroll
-      for (int i = 0; i < W; ++i) v[k][i] = 0.f;
-      if (live && j < a.H) load_piece<W>(x + j, v[k]);
-    }
+    for (int k = 0; k < E / W; ++k) {
+      unpack<X, W>(piece[k], f + k * W);
+      if (column(k) >= H) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int i = 0; i < W; ++i) s += v[k][i];
-    const float mean = row_sum(s, sh[0]) * over_h;
-    s = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const bool in = ((int64_t)k * blockDim.x + threadIdx.x) * W < a.H;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        v[k][i] -= mean;
-        s += in ? v[k][i] * v[k][i] : 0.f;
+        for (int i = 0; i < W; ++i) f[k * W + i] = 0.f;
       }
     }
-    const float rstd = 1.f / sqrtf(row_sum(s, sh[1]) * over_h + a.eps);
-    if (!live) continue;
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
+  }
+  __device__ __forceinline__ static void store(X *row, const Pair (&v)[E / 2], int H) {
+    float f[E];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) f[2 * e] = v[e].a, f[2 * e + 1] = v[e].b;
+#pragma unroll
+    for (int k = 0; k < E / W; ++k)
+      if (column(k) < H) store_piece<W>(row + column(k), f + k * W);
+  }
+  // the thread's parameters
+  __device__ __forceinline__ static void param(const void *p, int type, float none, Pair (&v)[E / 2], int H) {
+    float f[E];
+#pragma unroll
+    for (int k = 0; k < E / W; ++k) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) f[k * W + i] = none;
+      if (column(k) < H) load_param<W>(p, type, column(k), none, f + k * W);
+    }
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
+  }
+};
+
+// -- forward -----------------------------------------------------------------------------------
+// A row stays in the registers of blockDim.x threads from its load to its output, with their
+// parameters, and the next row of the block is on its way meanwhile.  The variance needs one
+// exchange between warps: each warp takes the squared distances from its own mean, and
+//   sum (x - mean)^2 = sum over warps of (their sum + n_w (mean_w - mean)^2),
+// in which nothing cancels.  Bound by the bytes of x and y as long as a row takes few
+// instructions: they are counted in pairs, parameters are not read again, and one warp-wide
+// sum joins the warps.
+template <typename X, int W, int E>
+__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a) {
+  using S = Slice<X, W, E>;
+  __shared__ float2 sh[2][32];
+  __shared__ float size[32];
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
+  const float over_h = 1.f / (float)H;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  S next;
+  next.load(static_cast<const X *>(a.x) + row * a.x_stride, H, row < a.rows);
+  Pair w[E / 2], b[E / 2];
+  S::param(a.w, a.p_type, 1.f, w, H);
+  S::param(a.b, a.p_type, 0.f, b, H);
+  // elements of each warp of a row
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < E / W; ++k) mine += max(0, min(32 * W, H - (k * (int)blockDim.x + warp * 32) * W));
+  if (threadIdx.y == 0 && lane == 0) size[warp] = (float)mine;
+  const float over_mine = mine ? 1.f / (float)mine : 0.f;
+  __syncthreads();
+  const float n_of = lane < warps ? size[lane] : 0.f;  // of warp `lane`
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+    Pair v[E / 2];
+    next.get(v, H);
+    next.load(static_cast<const X *>(a.x) + (row + step) * a.x_stride, H, row + step < a.rows);
+    Pair s = v[0];
+#pragma unroll
+    for (int e = 1; e < E / 2; ++e) s = add2(s, v[e]);
+    float mean = warp_sum(s.a + s.b) * over_mine;
+    Pair m = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+      const Pair d = add2(v[e], both(-mean));
+      if (W >= 2) {
+        if (S::column(2 * e / W) < H) m = fma2(d, d, m);
+      } else {  // (the two lie in pieces of their own)
+        if (S::column(2 * e) < H) m.a += d.a * d.a;
+        if (S::column(2 * e + 1) < H) m.b += d.b * d.b;
+      }
+    }
+    float m2 = warp_sum(m.a + m.b);
+    if (warps > 1) {
+      float2 *slots = sh[turn] + threadIdx.y * warps;
+      if (lane == 0) slots[warp] = make_float2(mean, m2);
+      __syncthreads();
+      const float2 o = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
+      mean = warp_sum(o.x * n_of) * over_h;
+      m2 = warp_sum(o.y + n_of * ((o.x - mean) * (o.x - mean)));
+    }
+    const float rstd = 1.f / sqrtf(m2 * over_h + a.eps);
+    if (row >= a.rows) continue;
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
-    X *y = static_cast<X *>(a.y) + row * a.y_stride;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int64_t j = ((int64_t)k * blockDim.x + threadIdx.x) * W;
-      if (j >= a.H) continue;
-      float w[W], b[W];
-      load_param<W>(a.w, a.p_type, j, 1.f, w);
-      load_param<W>(a.b, a.p_type, j, 0.f, b);
-#pragma unroll
-      for (int i = 0; i < W; ++i) v[k][i] = v[k][i] * rstd * w[i] + b[i];
-      store_piece<W>(y + j, v[k]);
-    }
+    for (int e = 0; e < E / 2; ++e) v[e] = fma2(mul2(add2(v[e], both(-mean)), both(rstd)), w[e], b[e]);
+    S::store(static_cast<X *>(a.y) + row * a.y_stride, v, H);
   }
 }
 
@@ -122,7 +183,131 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
 }
 
 // -- backward ----------------------------------------------------------------------------------
-// dx, a block a row: the row's two sums, then its elements.
+// One pass over dy and x: a block goes through its rows, a row among blockDim.x threads that
+// keep the weight and the sums of dweight and dbias of their columns in registers.  Each thread
+// copies its own elements of the rows ahead to shared memory (cp.async, `depth` rows in
+// flight), so no barrier stands between a copy and its use; the row's two sums need one.
+// Bound by the bytes of dy, x and dx while a row's instructions are few (in pairs, as above);
+// the blocks' partial sums come on top ([blocks][2][H] fp32, written and read once).
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(void *to, const void *from) {
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+  else if constexpr (BYTES >= 4)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(BYTES) : "memory");
+  else
+    *static_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
+}
+
+template <typename X, int W, int E>
+__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(NormGradArgs a, int depth) {
+  constexpr int K = E / W;
+  using S = Slice<X, W, E>;
+  using P = Pack<X, W>;
+  extern __shared__ __align__(16) unsigned char staging[];
+  __shared__ float2 sh[2][32];
+  const int T = blockDim.x * blockDim.y, t = threadIdx.y * blockDim.x + threadIdx.x, warps = blockDim.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
+  const float over_h = 1.f / (float)H;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  P *ring = reinterpret_cast<P *>(staging) + t;  // [depth][x, dy][K][T] pieces
+  auto copy_row = [&](int64_t row, int slot) {
+    if (row < a.rows) {
+      const X *x = static_cast<const X *>(a.x) + row * a.x_stride, *dy = static_cast<const X *>(a.dy) + row * a.dy_stride;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (S::column(k) >= H) continue;
+        copy_ahead<sizeof(P)>(ring + ((slot * 2) * K + k) * T, x + S::column(k));
+        copy_ahead<sizeof(P)>(ring + ((slot * 2 + 1) * K + k) * T, dy + S::column(k));
+      }
+    }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+  };
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  for (int d = 0; d < depth - 1; ++d) copy_row(row + d * step, d);
+  Pair w[E / 2], dw[E / 2], db[E / 2];
+  S::param(a.w, a.p_type, 1.f, w, H);
+#pragma unroll
+  for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = {0.f, 0.f};
+  int turn = 0, slot = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+    const bool live = row < a.rows;
+    const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
+    copy_row(row + (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
+    if (depth == 2) asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+    else asm volatile("cp.async.wait_group 2;\n" ::: "memory");
+    S x, g;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x.piece[k] = ring[((slot * 2) * K + k) * T];
+      g.piece[k] = ring[((slot * 2 + 1) * K + k) * T];
+    }
+    slot = slot + 1 == depth ? 0 : slot + 1;
+    Pair xh[E / 2], gw[E / 2];
+    x.get(xh, live ? H : 0);
+    g.get(gw, live ? H : 0);
+    Pair s1 = {0.f, 0.f}, s2 = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+      xh[e] = mul2(add2(xh[e], both(-mean)), both(rstd));
+      dw[e] = fma2(gw[e], xh[e], dw[e]);
+      db[e] = add2(db[e], gw[e]);
+      gw[e] = mul2(gw[e], w[e]);
+      s1 = add2(s1, gw[e]);
+      s2 = fma2(gw[e], xh[e], s2);
+    }
+    if (!a.dx) continue;
+    float m1 = warp_sum(s1.a + s1.b), m2 = warp_sum(s2.a + s2.b);
+    if (warps > 1) {
+      float2 *slots = sh[turn] + threadIdx.y * warps;
+      if (lane == 0) slots[threadIdx.x >> 5] = make_float2(m1, m2);
+      __syncthreads();
+      const float2 o = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
+      m1 = warp_sum(o.x);
+      m2 = warp_sum(o.y);
+    }
+    if (!live) continue;
+    m1 *= over_h;
+    m2 *= over_h;
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) xh[e] = mul2(fma2(xh[e], both(-m2), add2(gw[e], both(-m1))), both(rstd));
+    S::store(static_cast<X *>(a.dx) + row * a.dx_stride, xh, H);
+  }
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (!a.part) return;
+  // the block's rows together, in their order, then out
+  asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+  if (blockDim.y > 1) {
+    Pair *sums = reinterpret_cast<Pair *>(staging);  // [blockDim.y - 1][2][E / 2][blockDim.x]
+    __syncthreads();
+    if (threadIdx.y) {
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+        sums[(((threadIdx.y - 1) * 2) * (E / 2) + e) * blockDim.x + threadIdx.x] = dw[e];
+        sums[(((threadIdx.y - 1) * 2 + 1) * (E / 2) + e) * blockDim.x + threadIdx.x] = db[e];
+      }
+    }
+    __syncthreads();
+    if (threadIdx.y) return;
+    for (int y = 0; y < (int)blockDim.y - 1; ++y)
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+        dw[e] = add2(dw[e], sums[((y * 2) * (E / 2) + e) * blockDim.x + threadIdx.x]);
+        db[e] = add2(db[e], sums[((y * 2 + 1) * (E / 2) + e) * blockDim.x + threadIdx.x]);
+      }
+  }
+  float *part = a.part + (int64_t)blockIdx.x * 2 * a.H;
+  float f[2][E];
+#pragma unroll
+  for (int e = 0; e < E / 2; ++e) f[0][2 * e] = dw[e].a, f[0][2 * e + 1] = dw[e].b, f[1][2 * e] = db[e].a, f[1][2 * e + 1] = db[e].b;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (S::column(k) >= H) continue;
+    store_piece<W>(part + S::column(k), f[0] + k * W);
+    store_piece<W>(part + a.H + S::column(k), f[1] + k * W);
+  }
+}
+
+// Rows too long for that: dx, a block a row, in two passes over it (the second from L2) ...
 template <typename X, int W>
 __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs a) {
   __shared__ float sh[4][32];
@@ -159,7 +344,7 @@ __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs
   }
 }
 
-// Partial sums of dweight and dbias: a block takes blockDim.x * W columns of one part of the rows.
+// ... and partial sums of dweight and dbias, blockDim.x * W columns of one part of the rows a block.
 template <typename X, int W>
 __global__ void __launch_bounds__(128) layer_norm_grad_columns_kernel(NormGradArgs a) {
   const int64_t j = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * W;
@@ -206,6 +391,7 @@ constexpr int kJoinWarps = 16;
 
 __global__ void __launch_bounds__(kJoinWarps * 32) layer_norm_grad_join_kernel(NormGradArgs a) {
   __shared__ float sh[kJoinWarps][33];
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int64_t j = (int64_t)blockIdx.x * 32 + threadIdx.x;  // of [dweight, dbias]: 2 H columns
   float s = 0.f;
   if (j < 2 * a.H) {
@@ -241,6 +427,27 @@ cudaError_t with_pieces(int64_t H, std::initializer_list<std::pair<const void *,
 
 int row_threads(int64_t H, int E) { return (int)std::min<int64_t>(1024, (H + 32 * E - 1) / (32 * E) * 32); }
 
+constexpr int64_t kCached = 768 * 16;  // longest rows of the one-pass kernels
+// Elements of a row that a thread takes: 8 where 256 threads hold the row, else 16.
+int row_elements(int64_t H) { return H <= 2048 ? 8 : 16; }
+
+// Shape of the backward kernel for rows of H elements: threads of a row, rows at a time, rows
+// in flight (three unless they take more than the shared memory that two blocks share).
+struct GradShape {
+  int E, x, y, depth;
+  size_t smem;
+};
+GradShape grad_shape(int64_t H, int x_type) {
+  GradShape s{};
+  s.E = row_elements(H);
+  s.x = row_threads(H, s.E);
+  s.y = std::max(1, 256 / s.x);
+  const size_t row = (size_t)s.x * s.y * s.E * 2 * type_bytes(x_type);
+  s.depth = row * 3 <= (200 << 10) ? 3 : 2;
+  s.smem = std::max(row * s.depth, (size_t)(s.y - 1) * 2 * s.E * s.x * sizeof(float));
+  return s;
+}
+
 }  // namespace
 
 cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
@@ -248,53 +455,80 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
     using X = decltype(t);
     return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.y, a.y_stride}}, a.x_type, {a.w, a.b}, a.p_type, [&](auto wide) {
       constexpr int W = decltype(wide)::value;
-      if (a.H > 1024 * 32) {
+      if (a.H > kCached) {
         layer_norm_long_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, sms * 2), 1024, 0, st>>>(a);
         return cudaGetLastError();
       }
       auto go = [&](auto each) {
         constexpr int E = decltype(each)::value;
         const int x = row_threads(a.H, E);
-        const dim3 block(x, std::max(1, 128 / x));
-        const int64_t grid = std::min<int64_t>((a.rows + block.y - 1) / block.y, INT32_MAX);
-        layer_norm_kernel<X, W, E><<<(unsigned)grid, block, 0, st>>>(a);
+        const dim3 block(x, std::max(1, 256 / x));
+        const int64_t room = (int64_t)sms * std::max(1, (E > 8 ? 768 : 1024) / (int)(block.x * block.y));
+        layer_norm_kernel<X, W, E><<<(unsigned)std::min((a.rows + block.y - 1) / block.y, room), block, 0, st>>>(a);
         return cudaGetLastError();
       };
-      return a.H <= 2048 ? go(Int<8>{}) : a.H <= 8192 ? go(Int<16>{}) : go(Int<32>{});
+      return row_elements(a.H) == 8 ? go(Int<8>{}) : go(Int<16>{});
     });
   });
 }
 
 int layer_norm_grad_parts(int64_t rows, int64_t H, int x_type, int sms) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({rows / 8, (int64_t)sms, 65535}));
+  if (H > kCached) return (int)std::max<int64_t>(1, std::min<int64_t>({rows / 8, (int64_t)sms, 65535}));
+  const GradShape s = grad_shape(H, x_type);
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({(int64_t)768 / (s.x * s.y), (int64_t)((220 << 10) / (s.smem + 1024)), 2}));
+  return (int)std::min<int64_t>((rows + s.y - 1) / s.y, blocks * sms);
 }
 
-cudaError_t launch_layer_norm_grad_rows(const NormGradArgs &a, int sms, cudaStream_t st) {
-  return with_type(a.x_type, [&](auto t) {
-    using X = decltype(t);
-    return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dx, a.dx_stride}}, a.x_type, {a.w}, a.p_type, [&](auto wide) {
-      constexpr int W = decltype(wide)::value;
-      layer_norm_grad_rows_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, INT32_MAX), row_threads(a.H, 8), 0, st>>>(a);
-      return cudaGetLastError();
+cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
+  const bool params = a.dw || a.db;
+  cudaError_t e = cudaSuccess;
+  if (a.rows && (a.dx || params))
+    e = with_type(a.x_type, [&](auto t) {
+      using X = decltype(t);
+      return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dx, a.dx_stride}}, a.x_type, {a.w}, a.p_type, [&](auto wide) {
+        constexpr int W = decltype(wide)::value;
+        if (a.H > kCached) {
+          cudaError_t r = cudaSuccess;
+          const int64_t cols = 128 * W;
+          if (params)  // (before dx: it may overwrite dy or x)
+            r = timed("layer_norm_grad_columns", [&] {
+              layer_norm_grad_columns_kernel<X, W><<<dim3((unsigned)((a.H + cols - 1) / cols), a.parts), 128, 0, st>>>(a);
+              return cudaGetLastError();
+            });
+          if (r == cudaSuccess && a.dx)
+            r = timed("layer_norm_grad_rows", [&] {
+              layer_norm_grad_rows_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, INT32_MAX), row_threads(a.H, 8), 0, st>>>(a);
+              return cudaGetLastError();
+            });
+          return r;
+        }
+        const GradShape s = grad_shape(a.H, a.x_type);
+        auto go = [&](auto each) {
+          constexpr int E = decltype(each)::value;
+          auto kernel = layer_norm_grad_kernel<X, W, E>;
+          cudaError_t r = s.smem > 40 << 10 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem) : cudaSuccess;
+          if (r != cudaSuccess) return r;
+          return timed("layer_norm_grad", [&] {
+            kernel<<<(unsigned)layer_norm_grad_parts(a.rows, a.H, a.x_type, sms), dim3(s.x, s.y), s.smem, st>>>(a, s.depth);
+            return cudaGetLastError();
+          });
+        };
+        return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
+      });
     });
+  if (e != cudaSuccess || !params) return e;
+  return timed("layer_norm_grad_join", [&] {
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3((unsigned)((2 * a.H + 31) / 32));
+    how.blockDim = dim3(32, kJoinWarps);
+    how.stream = st;
+    cudaLaunchAttribute early{};  // the blocks may start while the kernel before ends
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    how.attrs = &early;
+    how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, layer_norm_grad_join_kernel, a);
   });
-}
-
-cudaError_t launch_layer_norm_grad_columns(const NormGradArgs &a, cudaStream_t st) {
-  return with_type(a.x_type, [&](auto t) {
-    using X = decltype(t);
-    return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.dy, a.dy_stride}}, a.x_type, {}, a.p_type, [&](auto wide) {
-      constexpr int W = decltype(wide)::value;
-      const int64_t cols = 128 * W;
-      layer_norm_grad_columns_kernel<X, W><<<dim3((unsigned)((a.H + cols - 1) / cols), a.parts), 128, 0, st>>>(a);
-      return cudaGetLastError();
-    });
-  });
-}
-
-cudaError_t launch_layer_norm_grad_join(const NormGradArgs &a, cudaStream_t st) {
-  layer_norm_grad_join_kernel<<<(unsigned)((2 * a.H + 31) / 32), dim3(32, kJoinWarps), 0, st>>>(a);
-  return cudaGetLastError();
 }
 
 }  // namespace echo

@@ -537,9 +537,10 @@ class Echo:
         import torch
         h = x.shape[-1]
         y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
-        _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than x")
+        _need(out is None or (y.shape == x.shape and y.dtype == x.dtype), "out has another shape or type than x")
         ptype = self._params(h, weight, bias)
-        mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
         xm, n, xs = _matrix(x)
         ym, _, ys = _matrix(y, out=True)
         self._op(self.lib.echo_layer_norm, LayerNormDesc(n, h, xm.data_ptr(), ym.data_ptr(), _dptr(weight), _dptr(bias), mean.data_ptr(),
@@ -574,13 +575,13 @@ class Echo:
     @staticmethod
     def _params(h: int, *params) -> int:
         """Common type of the parameter vectors given."""
-        types = set()
+        kind = None
         for p in params:
             if p is not None:
-                _need(p.dim() == 1 and p.shape[0] == h and (h == 1 or p.stride(0) == 1), "a parameter is not a contiguous vector of a row's length")
-                types.add(_type(p.dtype))
-        _need(len(types) <= 1, "the parameters and their gradients have different types")
-        return types.pop() if types else 0
+                _need(p.dim() == 1 and p.shape[0] == h and p.is_contiguous(), "a parameter is not a contiguous vector of a row's length")
+                _need(kind is None or p.dtype == kind, "the parameters and their gradients have different types")
+                kind = p.dtype
+        return 0 if kind is None else _type(kind)
 
     def orthogonalize(self, g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0, out=None):
         """Newton-Schulz orthogonalisation of the matrices ``g`` [..., rows, cols], times
