@@ -188,7 +188,7 @@ int echo_layer_norm_grad(echo_ctx *c, const echo_layer_norm_grad_desc *d) {
     echo::NormGradArgs a{d->rows, d->hidden, d->dy, d->x, d->weight, d->mean, d->rstd, d->dx, d->dweight, d->dbias,
                          d->dy_stride, d->x_stride, d->dx_stride, d->x_type, d->param_type, d->accumulate != 0, nullptr, 0};
     if (params) {
-      a.parts = d->rows ? echo::layer_norm_grad_parts(a.rows, a.H, a.x_type, o.sms) : 0;
+      a.parts = d->rows ? echo::layer_norm_grad_parts(a, o.sms) : 0;
       void *scratch = nullptr;
       if (const int rc = echo::op_scratch(c, (size_t)a.parts * 2 * a.H * sizeof(float), &scratch)) return rc;
       a.part = static_cast<float *>(scratch);

@@ -6,6 +6,8 @@
 #include <cuda_fp16.h>
 
 #include <cstdint>
+#include <cstring>
+#include <type_traits>
 
 #include "echo.h"
 
@@ -33,14 +35,32 @@ struct alignas(sizeof(T) * W <= 16 ? sizeof(T) * W : 16) Pack {
 };
 template <typename T, int W>
 __device__ __forceinline__ void unpack(const Pack<T, W> &p, float *f) {
+  if constexpr (W % 2 == 0 && std::is_same_v<T, __nv_bfloat16>) {  // a bf16 is the upper half of its fp32
+    uint32_t r[W / 2];
+    memcpy(r, &p, sizeof r);
 #pragma unroll
-  for (int i = 0; i < W; ++i) f[i] = to_f(p.v[i]);
+    for (int i = 0; i < W / 2; ++i) {
+      f[2 * i] = __uint_as_float(r[i] << 16);
+      f[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[i] = to_f(p.v[i]);
+  }
 }
 template <typename T, int W>
 __device__ __forceinline__ Pack<T, W> pack(const float *f) {
   Pack<T, W> p;
+  if constexpr (W % 2 == 0 && std::is_same_v<T, __nv_bfloat16>) {
 #pragma unroll
-  for (int i = 0; i < W; ++i) p.v[i] = from_f<T>(f[i]);
+    for (int i = 0; i < W / 2; ++i) reinterpret_cast<__nv_bfloat162 *>(p.v)[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+  } else if constexpr (W % 2 == 0 && std::is_same_v<T, __half>) {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) reinterpret_cast<__half2 *>(p.v)[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) p.v[i] = from_f<T>(f[i]);
+  }
   return p;
 }
 template <int W, typename T>

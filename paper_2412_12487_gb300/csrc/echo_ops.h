@@ -95,7 +95,7 @@ struct NormGradArgs {
   int parts;
 };
 // Partial sums that the call below writes (rows > 0).
-int layer_norm_grad_parts(int64_t rows, int64_t H, int x_type, int sms);
+int layer_norm_grad_parts(const NormGradArgs &a, int sms);
 cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
 
 // Orthogonalised update: m <= n are the smaller and the larger side, `tall` whether the

@@ -29,22 +29,15 @@ template <typename X, int W, int E>
 struct Slice {
   Pack<X, W> piece[E / W];
   __device__ __forceinline__ static int column(int k) { return (k * (int)blockDim.x + (int)threadIdx.x) * W; }
-  // (nothing is read outside the row; those pieces hold what they held)
-  __device__ __forceinline__ void load(const X *row, int H, bool live) {
+  // (pieces outside the row are never read: cleared once, they stay zeros)
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int k = 0; k < E / W; ++k)
-      if (live && column(k) < H) piece[k] = *reinterpret_cast<const Pack<X, W> *>(row + column(k));
+    for (int k = 0; k < E / W; ++k) piece[k] = Pack<X, W>{};
   }
-  __device__ __forceinline__ void get(Pair (&v)[E / 2], int H) const {
+  __device__ __forceinline__ void get(Pair (&v)[E / 2]) const {
     float f[E];
 #pragma unroll
-    for (int k = 0; k < E / W; ++k) {
-      unpack<X, W>(piece[k], f + k * W);
-      if (column(k) >= H) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[k * W + i] = 0.f;
-      }
-    }
+    for (int k = 0; k < E / W; ++k) unpack<X, W>(piece[k], f + k * W);
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
   }
@@ -70,25 +63,99 @@ struct Slice {
   }
 };
 
+// Rows come through shared memory, copied by the threads of a row while they work on the rows
+// before (cp.async, `depth` slots).  In pieces of 16 bytes each thread copies its own; rows in
+// narrower pieces (an odd length, stride or address) come in the 16-byte pieces of memory that
+// hold them, for which the threads wait for one another.
+template <typename X, int W, int E>
+struct Rows {
+  static constexpr bool kOwn = W * sizeof(X) == 16;
+  static size_t slot_bytes(int x, int64_t H) { return kOwn ? (size_t)x * E * sizeof(X) : ((size_t)H * sizeof(X) + 30) / 16 * 16; }
+
+  // `base`: the matrix's first row, before which nothing is read.
+  static __device__ __forceinline__ void copy(unsigned char *slot, const X *base, const X *row, int H) {
+    if constexpr (kOwn) {
+#pragma unroll
+      for (int k = 0; k < E / W; ++k) {
+        const int j = Slice<X, W, E>::column(k);
+        if (j < H) copy16(slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16, row + j, 16);
+      }
+    } else {
+      const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + (size_t)H * sizeof(X), from = begin / 16 * 16;
+      const int pieces = (int)((end - from + 15) / 16);
+      for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
+        const uintptr_t at = from + (uintptr_t)i * 16;
+        if (at >= reinterpret_cast<uintptr_t>(base)) {
+          copy16(slot + i * 16, reinterpret_cast<const void *>(at), (int)min((uintptr_t)16, end - at));
+        } else {  // (a first row inside such a piece)
+          for (uintptr_t b = begin; b < min(end, at + 16); b += sizeof(X)) *reinterpret_cast<X *>(slot + (b - from)) = *reinterpret_cast<const X *>(b);
+        }
+      }
+    }
+  }
+  // After arrived(): the thread's elements (cleared where the row has none).
+  static __device__ __forceinline__ void read(const unsigned char *slot, const X *row, int H, Slice<X, W, E> &s) {
+    if constexpr (!kOwn) slot += reinterpret_cast<uintptr_t>(row) % 16;
+#pragma unroll
+    for (int k = 0; k < E / W; ++k) {
+      const int j = Slice<X, W, E>::column(k);
+      if (j < H) s.piece[k] = *reinterpret_cast<const Pack<X, W> *>(kOwn ? slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16 : slot + j * (int)sizeof(X));
+    }
+  }
+  // Elements C c .. C c + C - 1 of the thread's (C a multiple of W), zeros where the row has none.
+  template <int C>
+  static __device__ __forceinline__ void read(const unsigned char *slot, const X *row, int H, int c, Pair (&v)[C / 2]) {
+    if constexpr (!kOwn) slot += reinterpret_cast<uintptr_t>(row) % 16;
+    float f[C];
+#pragma unroll
+    for (int i = 0; i < C / W; ++i) {
+      const int k = c * (C / W) + i, j = Slice<X, W, E>::column(k);
+      Pack<X, W> p{};
+      if (j < H) p = *reinterpret_cast<const Pack<X, W> *>(kOwn ? slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16 : slot + j * (int)sizeof(X));
+      unpack<X, W>(p, f + i * W);
+    }
+#pragma unroll
+    for (int e = 0; e < C / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
+  }
+  static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+  // All copies but those of the depth - 2 commits since are there; the slot used last is free.
+  static __device__ __forceinline__ void arrived(int depth) {
+    if (depth == 2) asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+    else if (depth == 3) asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+    else asm volatile("cp.async.wait_group 2;\n" ::: "memory");
+    if constexpr (!kOwn) __syncthreads();
+  }
+
+ private:
+  static __device__ __forceinline__ void copy16(void *to, const void *from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+  }
+};
+
 // -- forward -----------------------------------------------------------------------------------
-// A row stays in the registers of blockDim.x threads from its load to its output, with their
-// parameters, and the next row of the block is on its way meanwhile.  The variance needs one
-// exchange between warps: each warp takes the squared distances from its own mean, and
+// A row stays in the registers of blockDim.x threads, with their parameters, until its output,
+// and the block's next rows are on their way meanwhile.  The variance needs one exchange between warps: each warp takes the squared distances from its own mean, and
 //   sum (x - mean)^2 = sum over warps of (their sum + n_w (mean_w - mean)^2),
 // in which nothing cancels.  Bound by the bytes of x and y as long as a row takes few
 // instructions: they are counted in pairs, parameters are not read again, and one warp-wide
 // sum joins the warps.
 template <typename X, int W, int E>
-__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a, int depth, int slot_bytes) {
   using S = Slice<X, W, E>;
+  using R = Rows<X, W, E>;
+  extern __shared__ __align__(16) unsigned char ring[];  // [depth][rows of the block]
   __shared__ float2 sh[2][32];
   __shared__ float size[32];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
   const float over_h = 1.f / (float)H;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  S next;
-  next.load(static_cast<const X *>(a.x) + row * a.x_stride, H, row < a.rows);
+  const X *x = static_cast<const X *>(a.x);
+  auto slot_at = [&](int slot) { return ring + (size_t)(slot * (int)blockDim.y + (int)threadIdx.y) * slot_bytes; };
+  for (int d = 0; d < depth - 1; ++d) {
+    if (row + d * step < a.rows) R::copy(slot_at(d), x, x + (row + d * step) * a.x_stride, H);
+    R::commit();
+  }
   Pair w[E / 2], b[E / 2];
   S::param(a.w, a.p_type, 1.f, w, H);
   S::param(a.b, a.p_type, 0.f, b, H);
@@ -100,11 +167,18 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs
   const float over_mine = mine ? 1.f / (float)mine : 0.f;
   __syncthreads();
   const float n_of = lane < warps ? size[lane] : 0.f;  // of warp `lane`
-  int turn = 0;
+  int turn = 0, slot = 0;
+  S in;
+  in.clear();
   for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+    R::arrived(depth);
+    if (row < a.rows) R::read(slot_at(slot), x + row * a.x_stride, H, in);
+    const int64_t ahead = row + (depth - 1) * step;
+    if (ahead < a.rows) R::copy(slot_at(slot == 0 ? depth - 1 : slot - 1), x, x + ahead * a.x_stride, H);
+    R::commit();
+    slot = slot + 1 == depth ? 0 : slot + 1;
     Pair v[E / 2];
-    next.get(v, H);
-    next.load(static_cast<const X *>(a.x) + (row + step) * a.x_stride, H, row + step < a.rows);
+    in.get(v);
     Pair s = v[0];
 #pragma unroll
     for (int e = 1; e < E / 2; ++e) s = add2(s, v[e]);
@@ -184,93 +258,128 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
 
 // -- backward ----------------------------------------------------------------------------------
 // One pass over dy and x: a block goes through its rows, a row among blockDim.x threads that
-// keep the weight and the sums of dweight and dbias of their columns in registers.  Each thread
-// copies its own elements of the rows ahead to shared memory (cp.async, `depth` rows in
-// flight), so no barrier stands between a copy and its use; the row's two sums need one.
-// Bound by the bytes of dy, x and dx while a row's instructions are few (in pairs, as above);
+// keep the sums of dweight and dbias of their columns in registers.
+// Only those sums stay in registers with 16 elements a thread (the weight and the row as well
+// would spill): the row is read twice from its slot, and the weight from shared memory
+// (`staged`) or from L2 where the rows in flight leave no room.  Bound by the bytes of dy, x and dx while a row's instructions are few (in pairs, as above);
 // the blocks' partial sums come on top ([blocks][2][H] fp32, written and read once).
-template <int BYTES>
-__device__ __forceinline__ void copy_ahead(void *to, const void *from) {
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-  else if constexpr (BYTES >= 4)
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(BYTES) : "memory");
-  else
-    *static_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
-}
-
 template <typename X, int W, int E>
-__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(NormGradArgs a, int depth) {
+__global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(NormGradArgs a, int depth, int slot_bytes, int staged) {
   constexpr int K = E / W;
   using S = Slice<X, W, E>;
-  using P = Pack<X, W>;
-  extern __shared__ __align__(16) unsigned char staging[];
+  using R = Rows<X, W, E>;
+  extern __shared__ __align__(16) unsigned char staging[];  // [depth][x, dy][rows of the block]; the weight
   __shared__ float2 sh[2][32];
   const int T = blockDim.x * blockDim.y, t = threadIdx.y * blockDim.x + threadIdx.x, warps = blockDim.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
   const float over_h = 1.f / (float)H;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  P *ring = reinterpret_cast<P *>(staging) + t;  // [depth][x, dy][K][T] pieces
+  const X *xs = static_cast<const X *>(a.x), *gs = static_cast<const X *>(a.dy);
+  auto slot_at = [&](int slot, int which) { return staging + (size_t)((slot * 2 + which) * (int)blockDim.y + (int)threadIdx.y) * slot_bytes; };
   auto copy_row = [&](int64_t row, int slot) {
     if (row < a.rows) {
-      const X *x = static_cast<const X *>(a.x) + row * a.x_stride, *dy = static_cast<const X *>(a.dy) + row * a.dy_stride;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (S::column(k) >= H) continue;
-        copy_ahead<sizeof(P)>(ring + ((slot * 2) * K + k) * T, x + S::column(k));
-        copy_ahead<sizeof(P)>(ring + ((slot * 2 + 1) * K + k) * T, dy + S::column(k));
-      }
+      R::copy(slot_at(slot, 0), xs, xs + row * a.x_stride, H);
+      R::copy(slot_at(slot, 1), gs, gs + row * a.dy_stride, H);
     }
-    asm volatile("cp.async.commit_group;\n" ::: "memory");
+    R::commit();
   };
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   for (int d = 0; d < depth - 1; ++d) copy_row(row + d * step, d);
-  Pair w[E / 2], dw[E / 2], db[E / 2];
-  S::param(a.w, a.p_type, 1.f, w, H);
+  float mean = row < a.rows ? a.mean[row] : 0.f, rstd = row < a.rows ? a.rstd[row] : 0.f;
+  Pair dw[E / 2], db[E / 2], kept[E > 8 ? 1 : E / 2];  // (8 elements: the weight's values stay in registers)
+  Pair *weights = reinterpret_cast<Pair *>(staging + (size_t)depth * 2 * blockDim.y * slot_bytes) + t;  // [E / 2][T], each its own
+  if constexpr (E == 8) {
+    S::param(a.w, a.p_type, 1.f, kept, H);
+  } else if (staged) {
+    Pair w[E / 2];
+    S::param(a.w, a.p_type, 1.f, w, H);
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) weights[e * T] = w[e];
+  }
 #pragma unroll
   for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = {0.f, 0.f};
+  // x, dy and the weight of a thread's elements C c .. C c + C - 1 of a row
+  constexpr int C = W < 2 ? 2 : W;
+  auto read = [&](int slot, int64_t row, int c, Pair (&x)[C / 2], Pair (&g)[C / 2], Pair (&w)[C / 2]) {
+    R::template read<C>(slot_at(slot, 0), xs + row * a.x_stride, H, c, x);
+    R::template read<C>(slot_at(slot, 1), gs + row * a.dy_stride, H, c, g);
+    if constexpr (E == 8) {
+#pragma unroll
+      for (int e = 0; e < C / 2; ++e) w[e] = kept[c * (C / 2) + e];
+    } else if (staged) {
+#pragma unroll
+      for (int e = 0; e < C / 2; ++e) w[e] = weights[(c * (C / 2) + e) * T];
+    } else {
+      float f[C];
+#pragma unroll
+      for (int i = 0; i < C / W; ++i) {
+        const int j = S::column(c * (C / W) + i);
+#pragma unroll
+        for (int u = 0; u < W; ++u) f[i * W + u] = 1.f;
+        if (j < H) load_param<W>(a.w, a.p_type, j, 1.f, f + i * W);
+      }
+#pragma unroll
+      for (int e = 0; e < C / 2; ++e) w[e] = {f[2 * e], f[2 * e + 1]};
+    }
+  };
   int turn = 0, slot = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
-    const bool live = row < a.rows;
-    const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
+    const bool live = row < a.rows, more = row + step < a.rows;
+    const float next_mean = more ? a.mean[row + step] : 0.f, next_rstd = more ? a.rstd[row + step] : 0.f;
+    R::arrived(depth);
     copy_row(row + (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
-    if (depth == 2) asm volatile("cp.async.wait_group 1;\n" ::: "memory");
-    else asm volatile("cp.async.wait_group 2;\n" ::: "memory");
-    S x, g;
+    const Pair shift = both(-mean), scale = both(rstd);
+    Pair s1 = {0.f, 0.f}, s2 = {0.f, 0.f};
+    if (live) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      x.piece[k] = ring[((slot * 2) * K + k) * T];
-      g.piece[k] = ring[((slot * 2 + 1) * K + k) * T];
+      for (int c = 0; c < E / C; ++c) {
+        Pair x[C / 2], g[C / 2], w[C / 2];
+        read(slot, row, c, x, g, w);
+#pragma unroll
+        for (int e = 0; e < C / 2; ++e) {
+          const int at = c * (C / 2) + e;
+          const Pair xh = mul2(add2(x[e], shift), scale), gw = mul2(g[e], w[e]);
+          dw[at] = fma2(g[e], xh, dw[at]);
+          db[at] = add2(db[at], g[e]);
+          s1 = add2(s1, gw);
+          s2 = fma2(gw, xh, s2);
+        }
+      }
+    }
+    if (a.dx) {
+      float m1 = warp_sum(s1.a + s1.b), m2 = warp_sum(s2.a + s2.b);
+      if (warps > 1) {
+        float2 *slots = sh[turn] + threadIdx.y * warps;
+        if (lane == 0) slots[threadIdx.x >> 5] = make_float2(m1, m2);
+        __syncthreads();
+        const float2 o = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
+        m1 = warp_sum(o.x);
+        m2 = warp_sum(o.y);
+      }
+      if (live) {
+        const Pair n1 = both(-m1 * over_h), n2 = both(-m2 * over_h);
+        X *dx = static_cast<X *>(a.dx) + row * a.dx_stride;
+#pragma unroll
+        for (int c = 0; c < E / C; ++c) {
+          Pair x[C / 2], g[C / 2], w[C / 2];
+          read(slot, row, c, x, g, w);
+          float f[C];
+#pragma unroll
+          for (int e = 0; e < C / 2; ++e) {
+            const Pair xh = mul2(add2(x[e], shift), scale), d = mul2(fma2(xh, n2, fma2(g[e], w[e], n1)), scale);
+            f[2 * e] = d.a;
+            f[2 * e + 1] = d.b;
+          }
+#pragma unroll
+          for (int i = 0; i < C / W; ++i) {
+            const int j = S::column(c * (C / W) + i);
+            if (j < H) store_piece<W>(dx + j, f + i * W);
+          }
+        }
+      }
     }
     slot = slot + 1 == depth ? 0 : slot + 1;
-    Pair xh[E / 2], gw[E / 2];
-    x.get(xh, live ? H : 0);
-    g.get(gw, live ? H : 0);
-    Pair s1 = {0.f, 0.f}, s2 = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) {
-      xh[e] = mul2(add2(xh[e], both(-mean)), both(rstd));
-      dw[e] = fma2(gw[e], xh[e], dw[e]);
-      db[e] = add2(db[e], gw[e]);
-      gw[e] = mul2(gw[e], w[e]);
-      s1 = add2(s1, gw[e]);
-      s2 = fma2(gw[e], xh[e], s2);
-    }
-    if (!a.dx) continue;
-    float m1 = warp_sum(s1.a + s1.b), m2 = warp_sum(s2.a + s2.b);
-    if (warps > 1) {
-      float2 *slots = sh[turn] + threadIdx.y * warps;
-      if (lane == 0) slots[threadIdx.x >> 5] = make_float2(m1, m2);
-      __syncthreads();
-      const float2 o = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
-      m1 = warp_sum(o.x);
-      m2 = warp_sum(o.y);
-    }
-    if (!live) continue;
-    m1 *= over_h;
-    m2 *= over_h;
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) xh[e] = mul2(fma2(xh[e], both(-m2), add2(gw[e], both(-m1))), both(rstd));
-    S::store(static_cast<X *>(a.dx) + row * a.dx_stride, xh, H);
+    mean = next_mean;
+    rstd = next_rstd;
   }
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   if (!a.part) return;
@@ -431,21 +540,30 @@ constexpr int64_t kCached = 768 * 16;  // longest rows of the one-pass kernels
 // Elements of a row that a thread takes: 8 where 256 threads hold the row, else 16.
 int row_elements(int64_t H) { return H <= 2048 ? 8 : 16; }
 
-// Shape of the backward kernel for rows of H elements: threads of a row, rows at a time, rows
-// in flight (three unless they take more than the shared memory that two blocks share).
-struct GradShape {
-  int E, x, y, depth;
+// Shape of a one-pass kernel for rows of H elements, `arrays` of them read: threads of a row,
+// rows at a time, slots (up to 4, as two blocks' shared memory allows), bytes of a slot.
+struct Shape {
+  int E, x, y, depth, slot, staged;
   size_t smem;
 };
-GradShape grad_shape(int64_t H, int x_type) {
-  GradShape s{};
+template <typename X, int W>
+Shape row_shape(int64_t H, int arrays) {
+  Shape s{};
   s.E = row_elements(H);
   s.x = row_threads(H, s.E);
   s.y = std::max(1, 256 / s.x);
-  const size_t row = (size_t)s.x * s.y * s.E * 2 * type_bytes(x_type);
-  s.depth = row * 3 <= (200 << 10) ? 3 : 2;
-  s.smem = std::max(row * s.depth, (size_t)(s.y - 1) * 2 * s.E * s.x * sizeof(float));
+  s.slot = (int)(s.E == 8 ? Rows<X, W, 8>::slot_bytes(s.x, H) : Rows<X, W, 16>::slot_bytes(s.x, H));
+  const size_t row = (size_t)s.y * arrays * s.slot, room = s.E > 8 ? 200 << 10 : 100 << 10;
+  const size_t weights = arrays == 2 && s.E > 8 ? (size_t)s.x * s.y * s.E * sizeof(float) : 0;
+  s.staged = weights && row * 3 + weights <= room;
+  s.depth = (int)std::clamp<size_t>((room - (s.staged ? weights : 0)) / row, 2, 4);
+  s.smem = row * s.depth + (s.staged ? weights : 0);
+  if (arrays == 2) s.smem = std::max(s.smem, (size_t)(s.y - 1) * 2 * s.E * s.x * sizeof(float));
   return s;
+}
+// Blocks of it that an SM takes: 80 registers a thread with 16 elements, 64 with 8.
+int blocks_of(const Shape &s) {
+  return (int)std::max<size_t>(1, std::min<size_t>((s.E > 8 ? 768 : 1024) / (s.x * s.y), (220 << 10) / (s.smem + 2048)));
 }
 
 }  // namespace
@@ -459,12 +577,15 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
         layer_norm_long_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, sms * 2), 1024, 0, st>>>(a);
         return cudaGetLastError();
       }
+      const Shape s = row_shape<X, W>(a.H, 1);
       auto go = [&](auto each) {
         constexpr int E = decltype(each)::value;
-        const int x = row_threads(a.H, E);
-        const dim3 block(x, std::max(1, 256 / x));
-        const int64_t room = (int64_t)sms * std::max(1, (E > 8 ? 768 : 1024) / (int)(block.x * block.y));
-        layer_norm_kernel<X, W, E><<<(unsigned)std::min((a.rows + block.y - 1) / block.y, room), block, 0, st>>>(a);
+        auto kernel = layer_norm_kernel<X, W, E>;
+        const cudaError_t e =
+            s.smem > 40 << 10 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem) : cudaSuccess;
+        if (e != cudaSuccess) return e;
+        const int64_t grid = std::min<int64_t>((a.rows + s.y - 1) / s.y, (int64_t)sms * blocks_of(s));
+        kernel<<<(unsigned)grid, dim3(s.x, s.y), s.smem, st>>>(a, s.depth, s.slot);
         return cudaGetLastError();
       };
       return row_elements(a.H) == 8 ? go(Int<8>{}) : go(Int<16>{});
@@ -472,11 +593,22 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
   });
 }
 
-int layer_norm_grad_parts(int64_t rows, int64_t H, int x_type, int sms) {
-  if (H > kCached) return (int)std::max<int64_t>(1, std::min<int64_t>({rows / 8, (int64_t)sms, 65535}));
-  const GradShape s = grad_shape(H, x_type);
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({(int64_t)768 / (s.x * s.y), (int64_t)((220 << 10) / (s.smem + 1024)), 2}));
-  return (int)std::min<int64_t>((rows + s.y - 1) / s.y, blocks * sms);
+namespace {
+// Blocks of the backward kernel, each with a partial sum of the parameters' gradients.
+int grad_blocks(const Shape &s, int64_t rows, int sms) { return (int)std::min<int64_t>((rows + s.y - 1) / s.y, (int64_t)std::min(2, blocks_of(s)) * sms); }
+}  // namespace
+
+int layer_norm_grad_parts(const NormGradArgs &a, int sms) {
+  if (a.H > kCached) return (int)std::max<int64_t>(1, std::min<int64_t>({a.rows / 8, (int64_t)sms, 65535}));
+  int parts = 0;
+  (void)with_type(a.x_type, [&](auto t) {
+    using X = decltype(t);
+    return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dx, a.dx_stride}}, a.x_type, {a.w}, a.p_type, [&](auto wide) {
+      parts = grad_blocks(row_shape<X, decltype(wide)::value>(a.H, 2), a.rows, sms);
+      return cudaSuccess;
+    });
+  });
+  return parts;
 }
 
 cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
@@ -502,14 +634,14 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer
             });
           return r;
         }
-        const GradShape s = grad_shape(a.H, a.x_type);
+        const Shape s = row_shape<X, W>(a.H, 2);
         auto go = [&](auto each) {
           constexpr int E = decltype(each)::value;
           auto kernel = layer_norm_grad_kernel<X, W, E>;
           cudaError_t r = s.smem > 40 << 10 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem) : cudaSuccess;
           if (r != cudaSuccess) return r;
           return timed("layer_norm_grad", [&] {
-            kernel<<<(unsigned)layer_norm_grad_parts(a.rows, a.H, a.x_type, sms), dim3(s.x, s.y), s.smem, st>>>(a, s.depth);
+            kernel<<<(unsigned)grad_blocks(s, a.rows, sms), dim3(s.x, s.y), s.smem, st>>>(a, s.depth, s.slot, s.staged);
             return cudaGetLastError();
           });
         };
