@@ -23,31 +23,23 @@ __device__ __forceinline__ float row_sum(float v, float *sh) {
   return s;
 }
 
-// A thread's E elements of a row lie in K = E / W pieces blockDim.x apart; in registers they
-// are pairs, one piece after the other.
+// A thread's E elements of a row lie in E / W pieces blockDim.x apart; in registers they are
+// pairs, one piece after the other.
 template <typename X, int W, int E>
 struct Slice {
-  Pack<X, W> piece[E / W];
   __device__ __forceinline__ static int column(int k) { return (k * (int)blockDim.x + (int)threadIdx.x) * W; }
-  // (pieces outside the row are never read: cleared once, they stay zeros)
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int k = 0; k < E / W; ++k) piece[k] = Pack<X, W>{};
+  // Pieces of the thread that the row has: the first ones.
+  __device__ __forceinline__ static int pieces(int H) {
+    const int p = H / W - (int)threadIdx.x;
+    return p <= 0 ? 0 : min(E / W, (p + (int)blockDim.x - 1) / (int)blockDim.x);
   }
-  __device__ __forceinline__ void get(Pair (&v)[E / 2]) const {
-    float f[E];
-#pragma unroll
-    for (int k = 0; k < E / W; ++k) unpack<X, W>(piece[k], f + k * W);
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
-  }
-  __device__ __forceinline__ static void store(X *row, const Pair (&v)[E / 2], int H) {
+  __device__ __forceinline__ static void store(X *row, const Pair (&v)[E / 2], int pieces) {
     float f[E];
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) f[2 * e] = v[e].a, f[2 * e + 1] = v[e].b;
 #pragma unroll
     for (int k = 0; k < E / W; ++k)
-      if (column(k) < H) store_piece<W>(row + column(k), f + k * W);
+      if (k < pieces) store_piece<W>(row + column(k), f + k * W);
   }
   // the thread's parameters
   __device__ __forceinline__ static void param(const void *p, int type, float none, Pair (&v)[E / 2], int H) {
@@ -72,14 +64,12 @@ struct Rows {
   static constexpr bool kOwn = W * sizeof(X) == 16;
   static size_t slot_bytes(int x, int64_t H) { return kOwn ? (size_t)x * E * sizeof(X) : ((size_t)H * sizeof(X) + 30) / 16 * 16; }
 
-  // `base`: the matrix's first row, before which nothing is read.
-  static __device__ __forceinline__ void copy(unsigned char *slot, const X *base, const X *row, int H) {
+  // `base`: the matrix's first row, before which nothing is read; `mine`: the thread's pieces.
+  static __device__ __forceinline__ void copy(unsigned char *slot, const X *base, const X *row, int H, int mine) {
     if constexpr (kOwn) {
 #pragma unroll
-      for (int k = 0; k < E / W; ++k) {
-        const int j = Slice<X, W, E>::column(k);
-        if (j < H) copy16(slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16, row + j, 16);
-      }
+      for (int k = 0; k < E / W; ++k)
+        if (k < mine) copy16(slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16, row + Slice<X, W, E>::column(k), 16);
     } else {
       const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + (size_t)H * sizeof(X), from = begin / 16 * 16;
       const int pieces = (int)((end - from + 15) / 16);
@@ -93,26 +83,25 @@ struct Rows {
       }
     }
   }
-  // After arrived(): the thread's elements (cleared where the row has none).
-  static __device__ __forceinline__ void read(const unsigned char *slot, const X *row, int H, Slice<X, W, E> &s) {
-    if constexpr (!kOwn) slot += reinterpret_cast<uintptr_t>(row) % 16;
-#pragma unroll
-    for (int k = 0; k < E / W; ++k) {
-      const int j = Slice<X, W, E>::column(k);
-      if (j < H) s.piece[k] = *reinterpret_cast<const Pack<X, W> *>(kOwn ? slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16 : slot + j * (int)sizeof(X));
-    }
-  }
   // Elements C c .. C c + C - 1 of the thread's (C a multiple of W), zeros where the row has none.
+  // (Called apart for threads that have all their pieces, with E / W: the checks fall away.)
   template <int C>
-  static __device__ __forceinline__ void read(const unsigned char *slot, const X *row, int H, int c, Pair (&v)[C / 2]) {
+  static __device__ __forceinline__ void read(const unsigned char *slot, const X *row, int mine, int c, Pair (&v)[C / 2]) {
     if constexpr (!kOwn) slot += reinterpret_cast<uintptr_t>(row) % 16;
     float f[C];
 #pragma unroll
     for (int i = 0; i < C / W; ++i) {
-      const int k = c * (C / W) + i, j = Slice<X, W, E>::column(k);
-      Pack<X, W> p{};
-      if (j < H) p = *reinterpret_cast<const Pack<X, W> *>(kOwn ? slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16 : slot + j * (int)sizeof(X));
-      unpack<X, W>(p, f + i * W);
+      const int k = c * (C / W) + i;
+      if constexpr (kOwn) {
+        Pack<X, W> p{};
+        if (k < mine) p = *reinterpret_cast<const Pack<X, W> *>(slot + (k * (int)blockDim.x + (int)threadIdx.x) * 16);
+        unpack<X, W>(p, f + i * W);
+      } else {
+        const int j = k < mine ? Slice<X, W, E>::column(k) : 0;
+        unpack<X, W>(*reinterpret_cast<const Pack<X, W> *>(slot + j * (int)sizeof(X)), f + i * W);
+#pragma unroll
+        for (int u = 0; u < W; ++u) f[i * W + u] = k < mine ? f[i * W + u] : 0.f;
+      }
     }
 #pragma unroll
     for (int e = 0; e < C / 2; ++e) v[e] = {f[2 * e], f[2 * e + 1]};
@@ -134,11 +123,12 @@ struct Rows {
 
 // -- forward -----------------------------------------------------------------------------------
 // A row stays in the registers of blockDim.x threads, with their parameters, until its output,
-// and the block's next rows are on their way meanwhile.  The variance needs one exchange between warps: each warp takes the squared distances from its own mean, and
+// and the block's next rows are on their way meanwhile.  The variance needs one exchange between
+// warps: each takes the squared distances from its own mean, and
 //   sum (x - mean)^2 = sum over warps of (their sum + n_w (mean_w - mean)^2),
-// in which nothing cancels.  Bound by the bytes of x and y as long as a row takes few
-// instructions: they are counted in pairs, parameters are not read again, and one warp-wide
-// sum joins the warps.
+// in which nothing cancels.  The output starts from those distances.  The bytes of x and y would
+// bound it; what does is the instructions of a row, so they are in pairs, and addresses and
+// bounds are kept from row to row.
 template <typename X, int W, int E>
 __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a, int depth, int slot_bytes) {
   using S = Slice<X, W, E>;
@@ -151,11 +141,18 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const X *x = static_cast<const X *>(a.x);
-  auto slot_at = [&](int slot) { return ring + (size_t)(slot * (int)blockDim.y + (int)threadIdx.y) * slot_bytes; };
-  for (int d = 0; d < depth - 1; ++d) {
-    if (row + d * step < a.rows) R::copy(slot_at(d), x, x + (row + d * step) * a.x_stride, H);
+  const int own = S::pieces(H), pitch = (int)blockDim.y * slot_bytes, last = (depth - 1) * pitch;
+  unsigned char *slot0 = ring + (int)threadIdx.y * slot_bytes;
+  const X *ahead = x + row * a.x_stride;  // next row to copy
+  int64_t left = (a.rows - row + step - 1) / step;  // rows from there (of this thread)
+  const int64_t jump = step * a.x_stride;
+  auto copy_next = [&](int at) {
+    if (left > 0) R::copy(slot0 + at, x, ahead, H, own);
     R::commit();
-  }
+    ahead += jump;
+    --left;
+  };
+  for (int at = 0; at < last; at += pitch) copy_next(at);
   Pair w[E / 2], b[E / 2];
   S::param(a.w, a.p_type, 1.f, w, H);
   S::param(a.b, a.p_type, 0.f, b, H);
@@ -168,50 +165,60 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs
   __syncthreads();
   const float n_of = lane < warps ? size[lane] : 0.f;  // of warp `lane`
   int turn = 0, slot = 0;
-  S in;
-  in.clear();
-  for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
+  const X *from = x + row * a.x_stride;
+  X *y = static_cast<X *>(a.y) + row * a.y_stride;
+  const int64_t y_jump = step * a.y_stride;
+  constexpr int C = W < 2 ? 2 : W;
+  for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1, from += jump, y += y_jump) {
     R::arrived(depth);
-    if (row < a.rows) R::read(slot_at(slot), x + row * a.x_stride, H, in);
-    const int64_t ahead = row + (depth - 1) * step;
-    if (ahead < a.rows) R::copy(slot_at(slot == 0 ? depth - 1 : slot - 1), x, x + ahead * a.x_stride, H);
-    R::commit();
-    slot = slot + 1 == depth ? 0 : slot + 1;
     Pair v[E / 2];
-    in.get(v);
+    auto get = [&](int mine) {
+#pragma unroll
+      for (int c = 0; c < E / C; ++c) {
+        Pair p[C / 2];
+        R::template read<C>(slot0 + slot, from, mine, c, p);
+#pragma unroll
+        for (int e = 0; e < C / 2; ++e) v[c * (C / 2) + e] = p[e];
+      }
+    };
+    if (own == E / W) get(E / W);
+    else get(own);
+    copy_next(slot == 0 ? last : slot - pitch);
+    slot = slot == last ? 0 : slot + pitch;
     Pair s = v[0];
 #pragma unroll
     for (int e = 1; e < E / 2; ++e) s = add2(s, v[e]);
-    float mean = warp_sum(s.a + s.b) * over_mine;
+    const float mean_w = warp_sum(s.a + s.b) * over_mine;
     Pair m = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) {
-      const Pair d = add2(v[e], both(-mean));
+      v[e] = add2(v[e], both(-mean_w));
       if (W >= 2) {
-        if (S::column(2 * e / W) < H) m = fma2(d, d, m);
+        if (2 * e / W < own) m = fma2(v[e], v[e], m);
       } else {  // (the two lie in pieces of their own)
-        if (S::column(2 * e) < H) m.a += d.a * d.a;
-        if (S::column(2 * e + 1) < H) m.b += d.b * d.b;
+        if (2 * e < own) m.a += v[e].a * v[e].a;
+        if (2 * e + 1 < own) m.b += v[e].b * v[e].b;
       }
     }
-    float m2 = warp_sum(m.a + m.b);
+    float m2 = warp_sum(m.a + m.b), mean = mean_w;
     if (warps > 1) {
       float2 *slots = sh[turn] + threadIdx.y * warps;
-      if (lane == 0) slots[warp] = make_float2(mean, m2);
+      if (lane == 0) slots[warp] = make_float2(mean_w, m2);
       __syncthreads();
       const float2 o = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
       mean = warp_sum(o.x * n_of) * over_h;
       m2 = warp_sum(o.y + n_of * ((o.x - mean) * (o.x - mean)));
     }
-    const float rstd = 1.f / sqrtf(m2 * over_h + a.eps);
+    const float rstd = rsqrtf(m2 * over_h + a.eps);
     if (row >= a.rows) continue;
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
+    const Pair scale = both(rstd), shift = both((mean_w - mean) * rstd);
 #pragma unroll
-    for (int e = 0; e < E / 2; ++e) v[e] = fma2(mul2(add2(v[e], both(-mean)), both(rstd)), w[e], b[e]);
-    S::store(static_cast<X *>(a.y) + row * a.y_stride, v, H);
+    for (int e = 0; e < E / 2; ++e) v[e] = fma2(fma2(v[e], scale, shift), w[e], b[e]);
+    S::store(y, v, own);
   }
 }
 
@@ -274,19 +281,26 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   const float over_h = 1.f / (float)H;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   const X *xs = static_cast<const X *>(a.x), *gs = static_cast<const X *>(a.dy);
-  auto slot_at = [&](int slot, int which) { return staging + (size_t)((slot * 2 + which) * (int)blockDim.y + (int)threadIdx.y) * slot_bytes; };
-  auto copy_row = [&](int64_t row, int slot) {
-    if (row < a.rows) {
-      R::copy(slot_at(slot, 0), xs, xs + row * a.x_stride, H);
-      R::copy(slot_at(slot, 1), gs, gs + row * a.dy_stride, H);
+  const int own = S::pieces(H), pitch = 2 * (int)blockDim.y * slot_bytes, last = (depth - 1) * pitch, g_at = (int)blockDim.y * slot_bytes;
+  unsigned char *slot0 = staging + (int)threadIdx.y * slot_bytes;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const X *x_ahead = xs + row * a.x_stride, *g_ahead = gs + row * a.dy_stride;  // next row to copy
+  int64_t left = (a.rows - row + step - 1) / step;                               // rows from there (of this thread)
+  const int64_t x_jump = step * a.x_stride, g_jump = step * a.dy_stride, d_jump = step * a.dx_stride;
+  auto copy_next = [&](int at) {
+    if (left > 0) {
+      R::copy(slot0 + at, xs, x_ahead, H, own);
+      R::copy(slot0 + at + g_at, gs, g_ahead, H, own);
     }
     R::commit();
+    x_ahead += x_jump;
+    g_ahead += g_jump;
+    --left;
   };
-  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  for (int d = 0; d < depth - 1; ++d) copy_row(row + d * step, d);
+  for (int at = 0; at < last; at += pitch) copy_next(at);
   float mean = row < a.rows ? a.mean[row] : 0.f, rstd = row < a.rows ? a.rstd[row] : 0.f;
   Pair dw[E / 2], db[E / 2], kept[E > 8 ? 1 : E / 2];  // (8 elements: the weight's values stay in registers)
-  Pair *weights = reinterpret_cast<Pair *>(staging + (size_t)depth * 2 * blockDim.y * slot_bytes) + t;  // [E / 2][T], each its own
+  Pair *weights = reinterpret_cast<Pair *>(staging + depth * pitch) + t;  // [E / 2][T], each its own
   if constexpr (E == 8) {
     S::param(a.w, a.p_type, 1.f, kept, H);
   } else if (staged) {
@@ -299,9 +313,11 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = {0.f, 0.f};
   // x, dy and the weight of a thread's elements C c .. C c + C - 1 of a row
   constexpr int C = W < 2 ? 2 : W;
-  auto read = [&](int slot, int64_t row, int c, Pair (&x)[C / 2], Pair (&g)[C / 2], Pair (&w)[C / 2]) {
-    R::template read<C>(slot_at(slot, 0), xs + row * a.x_stride, H, c, x);
-    R::template read<C>(slot_at(slot, 1), gs + row * a.dy_stride, H, c, g);
+  const X *x_row = xs + row * a.x_stride, *g_row = gs + row * a.dy_stride;
+  X *dx = static_cast<X *>(a.dx) + row * a.dx_stride;
+  auto read = [&](int mine, int slot, int c, Pair (&x)[C / 2], Pair (&g)[C / 2], Pair (&w)[C / 2]) {
+    R::template read<C>(slot0 + slot, x_row, mine, c, x);
+    R::template read<C>(slot0 + slot + g_at, g_row, mine, c, g);
     if constexpr (E == 8) {
 #pragma unroll
       for (int e = 0; e < C / 2; ++e) w[e] = kept[c * (C / 2) + e];
@@ -312,10 +328,10 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
       float f[C];
 #pragma unroll
       for (int i = 0; i < C / W; ++i) {
-        const int j = S::column(c * (C / W) + i);
+        const int k = c * (C / W) + i, j = S::column(k);
 #pragma unroll
         for (int u = 0; u < W; ++u) f[i * W + u] = 1.f;
-        if (j < H) load_param<W>(a.w, a.p_type, j, 1.f, f + i * W);
+        if (k < own) load_param<W>(a.w, a.p_type, j, 1.f, f + i * W);
       }
 #pragma unroll
       for (int e = 0; e < C / 2; ++e) w[e] = {f[2 * e], f[2 * e + 1]};
@@ -326,25 +342,27 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
     const bool live = row < a.rows, more = row + step < a.rows;
     const float next_mean = more ? a.mean[row + step] : 0.f, next_rstd = more ? a.rstd[row + step] : 0.f;
     R::arrived(depth);
-    copy_row(row + (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
-    const Pair shift = both(-mean), scale = both(rstd);
+    copy_next(slot == 0 ? last : slot - pitch);
+    const Pair scale = both(rstd), shift = both(-mean * rstd);
     Pair s1 = {0.f, 0.f}, s2 = {0.f, 0.f};
-    if (live) {
+    auto add_up = [&](int mine) {
 #pragma unroll
       for (int c = 0; c < E / C; ++c) {
         Pair x[C / 2], g[C / 2], w[C / 2];
-        read(slot, row, c, x, g, w);
+        read(mine, slot, c, x, g, w);
 #pragma unroll
         for (int e = 0; e < C / 2; ++e) {
           const int at = c * (C / 2) + e;
-          const Pair xh = mul2(add2(x[e], shift), scale), gw = mul2(g[e], w[e]);
+          const Pair xh = fma2(x[e], scale, shift), gw = mul2(g[e], w[e]);
           dw[at] = fma2(g[e], xh, dw[at]);
           db[at] = add2(db[at], g[e]);
           s1 = add2(s1, gw);
           s2 = fma2(gw, xh, s2);
         }
       }
-    }
+    };
+    if (W > 1 && live && own == E / W) add_up(E / W);
+    else if (live) add_up(own);
     if (a.dx) {
       float m1 = warp_sum(s1.a + s1.b), m2 = warp_sum(s2.a + s2.b);
       if (warps > 1) {
@@ -355,29 +373,33 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
         m1 = warp_sum(o.x);
         m2 = warp_sum(o.y);
       }
-      if (live) {
-        const Pair n1 = both(-m1 * over_h), n2 = both(-m2 * over_h);
-        X *dx = static_cast<X *>(a.dx) + row * a.dx_stride;
+      const Pair n1 = both(-m1 * over_h), n2 = both(-m2 * over_h);
+      auto put = [&](int mine) {
 #pragma unroll
         for (int c = 0; c < E / C; ++c) {
           Pair x[C / 2], g[C / 2], w[C / 2];
-          read(slot, row, c, x, g, w);
+          read(mine, slot, c, x, g, w);
           float f[C];
 #pragma unroll
           for (int e = 0; e < C / 2; ++e) {
-            const Pair xh = mul2(add2(x[e], shift), scale), d = mul2(fma2(xh, n2, fma2(g[e], w[e], n1)), scale);
+            const Pair d = mul2(fma2(fma2(x[e], scale, shift), n2, fma2(g[e], w[e], n1)), scale);
             f[2 * e] = d.a;
             f[2 * e + 1] = d.b;
           }
 #pragma unroll
           for (int i = 0; i < C / W; ++i) {
-            const int j = S::column(c * (C / W) + i);
-            if (j < H) store_piece<W>(dx + j, f + i * W);
+            const int k = c * (C / W) + i;
+            if (k < mine) store_piece<W>(dx + S::column(k), f + i * W);
           }
         }
-      }
+      };
+      if (W > 1 && live && own == E / W) put(E / W);
+      else if (live) put(own);
+      dx += d_jump;
     }
-    slot = slot + 1 == depth ? 0 : slot + 1;
+    x_row += x_jump;
+    g_row += g_jump;
+    slot = slot == last ? 0 : slot + pitch;
     mean = next_mean;
     rstd = next_rstd;
   }
@@ -410,7 +432,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   for (int e = 0; e < E / 2; ++e) f[0][2 * e] = dw[e].a, f[0][2 * e + 1] = dw[e].b, f[1][2 * e] = db[e].a, f[1][2 * e + 1] = db[e].b;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    if (S::column(k) >= H) continue;
+    if (k >= own) continue;
     store_piece<W>(part + S::column(k), f[0] + k * W);
     store_piece<W>(part + a.H + S::column(k), f[1] + k * W);
   }
