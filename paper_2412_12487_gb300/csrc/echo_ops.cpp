@@ -122,11 +122,9 @@ int echo_embed_grad(echo_ctx *c, const echo_embed_grad_desc *d) {
     a.ids = d->ids, a.id64 = d->id_bits == 64, a.dy = d->dy, a.dtable = d->dtable;
     a.dy_stride = d->dy_stride, a.dtable_stride = d->dtable_stride, a.dy_type = d->dy_type, a.dtable_type = d->dtable_type;
     a.accumulate = d->accumulate != 0, a.scale = d->scale;
-    if (!a.accumulate) RUN(echo::launch_embed_clear(a, o.sms, o.stream), "embed_clear");
-    if (a.n == 0) return (int)ECHO_OK;
     a.window = echo::embed_grad_window(a.n, a.H, o.sms);
     const int64_t windows = (a.n + a.window - 1) / a.window;
-    if (windows * ((a.H + 31) / 32) / 8 >= INT32_MAX) return echo::op_error(c, ECHO_E_UNSUPPORTED, "too many sums for one launch");
+    if (windows * ((a.H + 31) / 32) / 8 + a.V / 128 >= INT32_MAX) return echo::op_error(c, ECHO_E_UNSUPPORTED, "too many sums for one launch");
     const size_t list = up256((size_t)a.n * 4);
     void *scratch = nullptr;
     if (const int rc = echo::op_scratch(c, 4 * list + 256 + (size_t)windows * 2 * a.H * sizeof(float), &scratch)) return rc;
@@ -139,6 +137,7 @@ int echo_embed_grad(echo_ctx *c, const echo_embed_grad_desc *d) {
     a.part = reinterpret_cast<float *>(at + 4 * list + 256);
     RUN(echo::launch_embed_sort(a, o.stream), "embed_sort");
     RUN(echo::launch_embed_sum(a, o.stream), "embed_sum");
+    if (a.n == 0) return (int)ECHO_OK;
     RUN(echo::launch_embed_join(a, o.stream), "embed_join");
     return (int)ECHO_OK;
   });

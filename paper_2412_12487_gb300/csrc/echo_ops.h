@@ -68,7 +68,7 @@ struct EmbedGradArgs {
 };
 int embed_grad_window(int64_t n, int64_t H, int sms);
 cudaError_t launch_embed_sort(const EmbedGradArgs &a, cudaStream_t st);
-cudaError_t launch_embed_clear(const EmbedGradArgs &a, int sms, cudaStream_t st);
+// (and, unless it accumulates, zeros to the rows without tokens)
 cudaError_t launch_embed_sum(const EmbedGradArgs &a, cudaStream_t st);
 cudaError_t launch_embed_join(const EmbedGradArgs &a, cudaStream_t st);
 

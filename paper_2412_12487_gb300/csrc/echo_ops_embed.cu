@@ -21,53 +21,69 @@ __device__ __forceinline__ int64_t shard_row(const void *ids, int id64, int64_t 
 }
 
 // -- lookup ----------------------------------------------------------------------------------
-// out[t] = scale * table[row of t], zeros without one.  Bound by the bytes read and written.
-// A thread takes kLookup pieces of one row; their loads are in flight together.
+// out[t] = scale * table[row of t], zeros without one.  Bound by the bytes read and written.  A
+// warp takes 32 * kLookup pieces of one token, then those of another: the next token's id is
+// read while this one's row is on its way, so that a token costs one latency and not two.
 constexpr int kLookup = 4;
 
 template <typename T, typename O, int W>
-__global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, int64_t pieces, int64_t steps) {
+__global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, int64_t pieces, int64_t chunks, int64_t units) {
   const T *table = static_cast<const T *>(a.table);
   O *out = static_cast<O *>(a.out);
-  for (int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; t < a.n; t += (int64_t)gridDim.x * blockDim.y) {
-    const int64_t row = shard_row(a.ids, a.id64, t, a.v0, a.V);
-    for (int64_t s = blockIdx.y; s < steps; s += gridDim.y) {
-      const int64_t p0 = s * kLookup * blockDim.x + threadIdx.x;
-      float f[kLookup][W];
+  const int lane = threadIdx.x & 31;
+  const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  int64_t unit = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  if (unit >= units) return;
+  // units go token by token; a step of `warps` units is this many tokens and chunks
+  const int64_t t_step = warps / chunks, c_step = warps % chunks;
+  int64_t t = unit / chunks, c = unit % chunks;
+  int64_t row = shard_row(a.ids, a.id64, t, a.v0, a.V);
+  for (;;) {
+    const int64_t p0 = c * (32 * kLookup) + lane;
+    Pack<T, W> in[kLookup];
+    if (row >= 0) {
+      const T *from = table + row * a.table_stride;
 #pragma unroll
-      for (int k = 0; k < kLookup; ++k) {
-        const int64_t p = p0 + k * (int)blockDim.x;
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[k][i] = 0.f;
-        if (row >= 0 && p < pieces) load_piece<W>(table + row * a.table_stride + p * W, f[k]);
-      }
-#pragma unroll
-      for (int k = 0; k < kLookup; ++k) {
-        const int64_t p = p0 + k * (int)blockDim.x;
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[k][i] = row >= 0 ? f[k][i] * a.scale : 0.f;
-        if (p < pieces) store_piece<W>(out + t * a.out_stride + p * W, f[k]);
-      }
+      for (int k = 0; k < kLookup; ++k)
+        if (p0 + k * 32 < pieces) in[k] = *reinterpret_cast<const Pack<T, W> *>(from + (p0 + k * 32) * W);
     }
+    O *to = out + t * a.out_stride;
+    const bool mine = row >= 0;
+    unit += warps;
+    t += t_step;
+    c += c_step;
+    if (c >= chunks) c -= chunks, ++t;
+    if (unit < units) row = shard_row(a.ids, a.id64, t, a.v0, a.V);
+#pragma unroll
+    for (int k = 0; k < kLookup; ++k) {
+      float f[W];
+      if (mine) unpack<T, W>(in[k], f);
+#pragma unroll
+      for (int i = 0; i < W; ++i) f[i] = mine ? f[i] * a.scale : 0.f;
+      if (p0 + k * 32 < pieces) store_piece<W>(to + (p0 + k * 32) * W, f);
+    }
+    if (unit >= units) break;
   }
 }
 
 // -- gradient: tokens sorted by row ------------------------------------------------------------
 // A stable radix sort, 8 bits a pass, by one cluster of 8 blocks: 256 warps each own a
-// contiguous range of the tokens.  A pass counts each warp's digits, takes the running sum
-// over (digit, block, warp) with the blocks' totals exchanged through distributed shared
-// memory, and places each token behind those before it.  The order of equal rows is the
-// tokens', so the sums' order is fixed.  Bound by the latency of its steps: one token a
-// thread up to 8192 tokens.
-constexpr int kSortBlocks = 8, kSortWarps = 32;
+// contiguous range of the tokens.  A pass counts each warp's digits, takes the running sum over
+// (digit, block, warp) with the blocks' totals exchanged through distributed shared memory, and
+// places each token behind those before it.  The order of equal rows is the tokens', so the
+// sums' order is fixed.  Bound by the latency of its steps, not by the tokens, so the first
+// kHeld tokens of each thread (all of them up to 32768 tokens) stay in registers from their
+// count to their place.
+constexpr int kSortBlocks = 8, kSortWarps = 32, kHeld = 4;
 
 __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32) embed_sort_kernel(EmbedGradArgs a, int passes) {
   __shared__ int32_t cnt[kSortWarps][256];
-  __shared__ int32_t tot[256];
+  __shared__ int32_t tot[256], start[256];
   __shared__ int32_t sums[8];
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const unsigned below = (1u << lane) - 1;
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");  // (they wait for all of this one)
   int64_t n = a.n;
   for (int pass = 0; pass < passes; ++pass) {
     const uint32_t *key_in = a.key[(pass + 1) & 1], *tok_in = a.tok[(pass + 1) & 1];
@@ -78,28 +94,59 @@ __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32)
       if (i >= end) return -1;
       return pass == 0 ? shard_row(a.ids, a.id64, i, a.v0, a.V) : (int64_t)__ldcg(key_in + i);
     };
-    for (int i = tid; i < kSortWarps * 256; i += blockDim.x) cnt[0][i] = 0;
-    __syncthreads();
-    for (int64_t i = begin; i < end; i += 32) {
-      const int64_t key = key_at(i + lane);
-      const int digit = key < 0 ? 256 : (int)(key >> (8 * pass)) & 255;
+    auto token_at = [&](int64_t i) { return pass == 0 || i >= end ? (uint32_t)i : __ldcg(tok_in + i); };
+    auto digit_of = [&](int64_t key) { return key < 0 ? 256 : (int)(key >> (8 * pass)) & 255; };
+    // place of a token among its warp's with the same digit, which is counted on the way
+    auto count = [&](int64_t key) {
+      const int digit = digit_of(key);
       const unsigned same = __match_any_sync(0xFFFFFFFFu, digit);
-      if (key >= 0 && !(same & below)) cnt[warp][digit] += __popc(same);
+      const int32_t before = key < 0 ? 0 : cnt[warp][digit];
       __syncwarp();
+      if (key >= 0 && !(same & below)) cnt[warp][digit] = before + __popc(same);
+      __syncwarp();
+      return before + __popc(same & below);
+    };
+    int64_t key[kHeld];
+    uint32_t tok[kHeld];
+    int32_t place[kHeld];
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+      key[h] = key_at(begin + h * 32 + lane);
+      tok[h] = token_at(begin + h * 32 + lane);
     }
+    for (int i = tid; i < kSortWarps * 64; i += blockDim.x) reinterpret_cast<int4 *>(cnt)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    if (tid < 256) {
-      int32_t run = 0;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const int32_t c = cnt[w][tid];
-        cnt[w][tid] = run;
-        run += c;
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+      if (begin + h * 32 < end) place[h] = count(key[h]);
+    for (int64_t i = begin + kHeld * 32; i < end; i += 32) (void)count(key_at(i + lane));
+    __syncthreads();
+    {  // running sums over the warps: four threads a digit, eight warps each
+      const int digit = tid >> 2, w0 = (tid & 3) * 8;
+      int32_t c[8], run = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        c[w] = cnt[w0 + w][digit];
+        run += c[w];
       }
-      tot[tid] = run;
+      int32_t upto = run;
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) {
+        const int32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d, 4);
+        if ((tid & 3) >= d) upto += v;
+      }
+      int32_t base = upto - run;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        cnt[w0 + w][digit] = base;
+        base += c[w];
+      }
+      if ((tid & 3) == 3) tot[digit] = upto;
     }
     cluster.sync();
     int32_t all = 0, before = 0, upto = 0;
     if (tid < 256) {
+#pragma unroll
       for (int b = 0; b < kSortBlocks; ++b) {
         const int32_t c = cluster.map_shared_rank(tot, b)[tid];
         before += b < rank ? c : 0;
@@ -114,25 +161,30 @@ __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32)
       if (lane == 31) sums[warp] = upto;
     }
     __syncthreads();
-    if (tid < 256) {
-      for (int w = 0; w < warp; ++w) upto += sums[w];
-      for (int w = 0; w < kSortWarps; ++w) cnt[w][tid] += upto - all + before;
-    }
     int64_t total = 0;
-    for (int w = 0; w < 8; ++w) total += sums[w];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      upto += w < warp ? sums[w] : 0;
+      total += sums[w];
+    }
+    if (tid < 256) start[tid] = upto - all + before;  // where the block's tokens of a digit begin
     __syncthreads();
-    for (int64_t i = begin; i < end; i += 32) {
-      const int64_t key = key_at(i + lane);
-      const int digit = key < 0 ? 256 : (int)(key >> (8 * pass)) & 255;
-      const unsigned same = __match_any_sync(0xFFFFFFFFu, digit);
-      if (key >= 0) {
-        const int64_t at = cnt[warp][digit] + __popc(same & below);
-        key_out[at] = (uint32_t)key;
-        tok_out[at] = pass == 0 ? (uint32_t)(i + lane) : __ldcg(tok_in + i + lane);
+    auto put = [&](int64_t k, uint32_t t, int64_t at) {
+      key_out[at] = (uint32_t)k;
+      tok_out[at] = t;
+    };
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+      if (key[h] >= 0) put(key[h], tok[h], (int64_t)start[digit_of(key[h])] + cnt[warp][digit_of(key[h])] + place[h]);
+    if (begin + kHeld * 32 < end) {  // the others are counted again, behind those
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h) (void)count(key[h]);
+      for (int64_t i = begin + kHeld * 32; i < end; i += 32) {
+        const int64_t k = key_at(i + lane);
+        const int32_t at = count(k);  // (from the warp's base on)
+        if (k >= 0) put(k, token_at(i + lane), (int64_t)start[digit_of(k)] + at);
       }
-      __syncwarp();
-      if (key >= 0 && !(same & below)) cnt[warp][digit] += __popc(same);
-      __syncwarp();
     }
     __threadfence();
     cluster.sync();  // (the other blocks' tokens, and their reads of `tot`)
@@ -147,15 +199,62 @@ __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32)
 // that lies inside a window is written at once; the part of a row that a window's edge cuts
 // goes to `part` ([window][0: began before it, 1: began in it][H]) and embed_join_kernel adds
 // the parts in order.  Bound by the bytes of dy and of the rows.
-constexpr int kBatch = 8;  // rows of dy in flight
+//
+// Unless the call accumulates, other blocks of the grid, between those of the sums, write zeros
+// to the rows that no token has: each marks its kClear rows' tokens among the sorted ones.
+constexpr int kClear = 128;
 
+template <typename T>
+__device__ void clear_rows(const EmbedGradArgs &a, const uint32_t *key, int64_t count, int64_t v0) {
+  __shared__ uint32_t has[kClear / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t v1 = min(a.V, v0 + kClear);
+  if (threadIdx.x < kClear / 32) has[threadIdx.x] = 0;
+  __syncthreads();
+  int64_t lo = 0, hi = count;  // the first token of these rows: a 33-fold search by each warp
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 32) / 33, at = lo + (lane + 1) * step - 1;
+    const unsigned less = __ballot_sync(0xFFFFFFFFu, at < hi && key[at] < v0);
+    const int below = __popc(less);
+    const int64_t next = lo + below * step;
+    hi = min(hi, below < 32 ? next + step - 1 : hi);
+    lo = next;
+  }
+  for (int64_t i = lo + threadIdx.x; i < count; i += blockDim.x) {
+    const uint32_t k = key[i];
+    if (k >= v1) break;
+    atomicOr(&has[(k - v0) / 32], 1u << ((k - v0) % 32));
+  }
+  __syncthreads();
+  const int64_t bytes = a.H * (int64_t)sizeof(T), pitch = a.dtable_stride * (int64_t)sizeof(T);
+  unsigned char *table = static_cast<unsigned char *>(a.dtable);
+  const bool wide = bytes % 16 == 0 && pitch % 16 == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0;
+  for (int64_t v = v0 + warp; v < v1; v += blockDim.x >> 5) {
+    if (has[(v - v0) / 32] >> ((v - v0) % 32) & 1) continue;
+    unsigned char *at = table + v * pitch;
+    if (wide) {
+      for (int64_t i = lane; i < bytes / 16; i += 32) reinterpret_cast<uint4 *>(at)[i] = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int64_t i = lane; i < a.H; i += 32) reinterpret_cast<T *>(at)[i] = T{};
+    }
+  }
+}
 template <typename D, typename T, int W>
-__global__ void __launch_bounds__(256) embed_sum_kernel(EmbedGradArgs a, const uint32_t *key, const uint32_t *tok, int64_t chunks) {
-  constexpr int N = 16 / sizeof(D), K = N / W;  // columns of a lane, in K pieces
+__global__ void __launch_bounds__(256, 3) embed_sum_kernel(EmbedGradArgs a, const uint32_t *key, const uint32_t *tok, int64_t chunks, int64_t clears) {
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  constexpr int N = 16 / sizeof(D), K = N / W;              // columns of a lane, in K pieces
+  constexpr int kBatch = W * sizeof(D) >= 4 ? 8 : 4;        // rows of dy in flight (a 16-bit piece takes a register)
   const int lane = threadIdx.x & 31;
-  const int64_t unit = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int64_t w0 = unit / chunks * a.window, col0 = unit % chunks * (32 * N) + lane * W;
   const int64_t count = *a.count;
+  // `clears` of the blocks clear rows, spread evenly over the grid
+  const int64_t cleared = (int64_t)blockIdx.x * clears / gridDim.x;
+  if (((int64_t)blockIdx.x + 1) * clears / gridDim.x != cleared) {
+    clear_rows<T>(a, key, count, cleared * kClear);
+    return;
+  }
+  const int64_t unit = ((blockIdx.x - cleared) * blockDim.x + threadIdx.x) >> 5;
+  const int64_t w0 = unit / chunks * a.window, col0 = unit % chunks * (32 * N) + lane * W;
   if (w0 >= count) return;
   const int m = (int)min((int64_t)a.window, count - w0);
   const uint32_t my_key = lane < m ? key[w0 + lane] : 0, my_tok = lane < m ? tok[w0 + lane] : 0;
@@ -224,44 +323,40 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedGradArgs a, const u
 // Rows that windows cut: the warp of the window in which the row begins adds its parts.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) embed_join_kernel(EmbedGradArgs a, const uint32_t *key, int64_t chunks) {
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31;
   const int64_t unit = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
   const int64_t w = unit / chunks, j = unit % chunks * (32 * W) + lane * W;
-  const int64_t count = *a.count, P = a.window;
-  if ((w + 1) * P >= count) return;
-  const uint32_t row = key[(w + 1) * P - 1];
-  if (key[(w + 1) * P] != row || (w > 0 && key[w * P - 1] == row)) return;  // no row begins here and is cut
-  int64_t lo = w + 1, hi = (count - 1) / P;  // the last window that begins with this row
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (key[mid * P] == row) lo = mid;
-    else hi = mid - 1;
+  const int64_t count = *a.count, P = a.window, end = (w + 1) * P;
+  if (end >= count) return;
+  // three keys at once, and the first keys of the windows behind, 32 at a time
+  const int64_t at = lane == 0 ? end - 1 : lane == 1 ? max((int64_t)0, w * P - 1) : end;
+  const uint32_t k = lane < 3 ? key[at] : 0, row = __shfl_sync(0xFFFFFFFFu, k, 0);
+  if (__shfl_sync(0xFFFFFFFFu, k, 2) != row || (w > 0 && __shfl_sync(0xFFFFFFFFu, k, 1) == row)) return;  // no row begins here and is cut
+  const int64_t windows = (count + P - 1) / P;
+  int64_t last = w + 1;  // the last window that begins with this row
+  for (;;) {
+    const int64_t u = last + 1 + lane;
+    const unsigned differs = __ballot_sync(0xFFFFFFFFu, u >= windows || key[u * P] != row);
+    last += differs ? __ffs(differs) - 1 : 32;
+    if (differs) break;
   }
   if (j >= a.H) return;
   float acc[W];
   load_piece<W>(a.part + (w * 2 + 1) * a.H + j, acc);
-#pragma unroll 4
-  for (int64_t u = w + 1; u <= lo; ++u) {
+#pragma unroll 16
+  for (int64_t u = w + 1; u <= last; ++u) {
     float f[W];
     load_piece<W>(a.part + u * 2 * a.H + j, f);
 #pragma unroll
     for (int i = 0; i < W; ++i) acc[i] += f[i];
   }
-  T *at = static_cast<T *>(a.dtable) + row * a.dtable_stride + j;
+  T *to = static_cast<T *>(a.dtable) + row * a.dtable_stride + j;
   float old[W];
-  if (a.accumulate) load_piece<W>(at, old);
+  if (a.accumulate) load_piece<W>(to, old);
 #pragma unroll
   for (int i = 0; i < W; ++i) acc[i] = acc[i] * a.scale + (a.accumulate ? old[i] : 0.f);
-  store_piece<W>(at, acc);
-}
-
-// Zeros to every row, before the rows of tokens are written.
-template <typename T, int W>
-__global__ void __launch_bounds__(256) embed_clear_kernel(EmbedGradArgs a, int64_t pieces) {
-  const float zero[W] = {};
-  T *dtable = static_cast<T *>(a.dtable);
-  for (int64_t v = blockIdx.x; v < a.V; v += gridDim.x)
-    for (int64_t p = threadIdx.x; p < pieces; p += blockDim.x) store_piece<W>(dtable + v * a.dtable_stride + p * W, zero);
+  store_piece<W>(to, acc);
 }
 
 int sort_passes(int64_t V) {
@@ -280,13 +375,10 @@ cudaError_t launch_embed(const EmbedArgs &a, int sms, cudaStream_t st) {
       constexpr int N = 16 / sizeof(O);
       auto go = [&](auto w) {
         constexpr int W = decltype(w)::value;
-        const int64_t pieces = a.H / W;
-        int x = 32;
-        while (x < 256 && x * kLookup < pieces) x *= 2;
-        const int64_t steps = (pieces + (int64_t)x * kLookup - 1) / ((int64_t)x * kLookup);
-        const dim3 block(x, 256 / x);
-        const int64_t gx = std::min<int64_t>((a.n + block.y - 1) / block.y, INT32_MAX);
-        embed_kernel<T, O, W><<<dim3((unsigned)gx, (unsigned)std::min<int64_t>(steps, 65535)), block, 0, st>>>(a, pieces, steps);
+        const int64_t pieces = a.H / W, chunks = (pieces + 32 * kLookup - 1) / (32 * kLookup);
+        if (a.n > INT64_MAX / chunks) return cudaErrorInvalidValue;
+        const int64_t units = a.n * chunks;
+        embed_kernel<T, O, W><<<(unsigned)std::min<int64_t>((units + 7) / 8, (int64_t)sms * 6), 256, 0, st>>>(a, pieces, chunks, units);
         return cudaGetLastError();
       };
       auto fits = [&](int W) {
@@ -297,28 +389,32 @@ cudaError_t launch_embed(const EmbedArgs &a, int sms, cudaStream_t st) {
   });
 }
 
+// Windows small enough that the sums occupy the SMs twice over, 24 warps each.
 int embed_grad_window(int64_t n, int64_t H, int sms) {
   int P = 8;
-  while (P < 32 && n / P * ((H + 255) / 256) > (int64_t)sms * 32) P *= 2;
+  while (P < 32 && n / (2 * P) * ((H + 255) / 256) >= (int64_t)sms * 48) P *= 2;
   return P;
 }
+
+namespace {
+// A launch whose blocks may start while the kernel before ends.
+cudaError_t launch_early(int64_t grid, cudaStream_t st, const void *kernel, void **args) {
+  cudaLaunchConfig_t how{};
+  how.gridDim = dim3((unsigned)grid);
+  how.blockDim = dim3(256);
+  how.stream = st;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  how.attrs = &early;
+  how.numAttrs = 1;
+  return cudaLaunchKernelExC(&how, kernel, args);
+}
+}  // namespace
 
 cudaError_t launch_embed_sort(const EmbedGradArgs &a, cudaStream_t st) {
   embed_sort_kernel<<<kSortBlocks, kSortWarps * 32, 0, st>>>(a, sort_passes(a.V));
   return cudaGetLastError();
-}
-
-cudaError_t launch_embed_clear(const EmbedGradArgs &a, int sms, cudaStream_t st) {
-  return with_type(a.dtable_type, [&](auto t) {
-    using T = decltype(t);
-    constexpr int N = 16 / sizeof(T);
-    auto go = [&](auto w) {
-      constexpr int W = decltype(w)::value;
-      embed_clear_kernel<T, W><<<(unsigned)std::min<int64_t>(a.V, sms * 8), 256, 0, st>>>(a, a.H / W);
-      return cudaGetLastError();
-    };
-    return a.H % N == 0 && fits_pieces(a.dtable, a.dtable_stride, a.dtable_type, N) ? go(Int<N>{}) : go(Int<1>{});
-  });
 }
 
 cudaError_t launch_embed_sum(const EmbedGradArgs &a, cudaStream_t st) {
@@ -331,8 +427,11 @@ cudaError_t launch_embed_sum(const EmbedGradArgs &a, cudaStream_t st) {
       auto go = [&](auto w) {
         constexpr int W = decltype(w)::value;
         const int64_t chunks = (a.H + 32 * N - 1) / (32 * N), units = (a.n + a.window - 1) / a.window * chunks;
-        embed_sum_kernel<D, T, W><<<(unsigned)((units + 7) / 8), 256, 0, st>>>(a, a.key[last], a.tok[last], chunks);
-        return cudaGetLastError();
+        EmbedGradArgs args = a;
+        const uint32_t *key = a.key[last], *tok = a.tok[last];
+        int64_t n_chunks = chunks, clears = a.accumulate ? 0 : (a.V + kClear - 1) / kClear;
+        void *list[] = {&args, &key, &tok, &n_chunks, &clears};
+        return launch_early((units + 7) / 8 + clears, st, (const void *)embed_sum_kernel<D, T, W>, list);
       };
       auto fits = [&](int W) {
         return a.H % W == 0 && fits_pieces(a.dy, a.dy_stride, a.dy_type, W) && fits_pieces(a.dtable, a.dtable_stride, a.dtable_type, W);
@@ -349,8 +448,11 @@ cudaError_t launch_embed_join(const EmbedGradArgs &a, cudaStream_t st) {
     auto go = [&](auto w) {
       constexpr int W = decltype(w)::value;
       const int64_t chunks = (a.H + 32 * W - 1) / (32 * W), units = (a.n + a.window - 1) / a.window * chunks;
-      embed_join_kernel<T, W><<<(unsigned)((units + 7) / 8), 256, 0, st>>>(a, a.key[last], chunks);
-      return cudaGetLastError();
+      EmbedGradArgs args = a;
+      const uint32_t *key = a.key[last];
+      int64_t n_chunks = chunks;
+      void *list[] = {&args, &key, &n_chunks};
+      return launch_early((units + 7) / 8, st, (const void *)embed_join_kernel<T, W>, list);
     };
     return a.H % 4 == 0 && fits_pieces(a.dtable, a.dtable_stride, a.dtable_type, 4) ? go(Int<4>{}) : go(Int<1>{});
   });

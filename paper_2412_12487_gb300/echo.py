@@ -490,9 +490,11 @@ class Echo:
 
     @staticmethod
     def _ids(ids) -> int:
-        bits = {"torch.int64": 64, "torch.int32": 32}.get(str(ids.dtype), 0)
-        _need(bits > 0, "ids are neither int32 nor int64")
-        return bits
+        import torch
+        if ids.dtype == torch.int64:
+            return 64
+        _need(ids.dtype == torch.int32, "ids are neither int32 nor int64")
+        return 32
 
     def embed(self, ids, table, scale: float = 1.0, vocab_start: int = 0, dtype=None, out=None):
         """``scale * table[ids - vocab_start]`` ([..., hidden] for ids [...]), zeros for ids
@@ -500,11 +502,13 @@ class Echo:
         table's by default) is the result's, unless ``out`` takes it."""
         bits = self._ids(ids)
         _need(table.dim() == 2, "the table is not a matrix")
+        import torch
         ids = ids.contiguous()
         v, h = table.shape
         if out is None:
-            out = table.new_empty((*ids.shape, h), dtype=dtype or table.dtype)
-        _need(tuple(out.shape) == (*ids.shape, h), "out has another shape than ids and the table's rows")
+            out = torch.empty((*ids.shape, h), dtype=dtype or table.dtype, device=table.device)
+        else:
+            _need(tuple(out.shape) == (*ids.shape, h), "out has another shape than ids and the table's rows")
         table, _, ts = _matrix(table)
         o, n, os_ = _matrix(out, out=True)
         self._op(self.lib.echo_embed, EmbedDesc(n, h, v, vocab_start, ids.data_ptr(), table.data_ptr(), o.data_ptr(), ts, os_, bits,
@@ -518,12 +522,13 @@ class Echo:
         import torch
         bits = self._ids(ids)
         h = dy.shape[-1]
-        _need(tuple(dy.shape[:-1]) == tuple(ids.shape), "dy has another shape than ids and a row")
+        _need(dy.shape[:-1] == ids.shape, "dy has another shape than ids and a row")
         _need(vocab_rows >= 0, "negative sizes")
         _need(out is not None or not accumulate, "accumulate needs out")
         if out is None:
-            out = dy.new_empty((vocab_rows, h), dtype=dtype or torch.float32)
-        _need(tuple(out.shape) == (vocab_rows, h), "out has another shape than vocab_rows and a row")
+            out = torch.empty((vocab_rows, h), dtype=dtype or torch.float32, device=dy.device)
+        else:
+            _need(tuple(out.shape) == (vocab_rows, h), "out has another shape than vocab_rows and a row")
         ids = ids.contiguous()
         g, n, gs = _matrix(dy)
         o, _, os_ = _matrix(out, out=True)
@@ -536,8 +541,11 @@ class Echo:
         ``layer_norm_grad`` needs (float32 [...]).  ``out`` may be ``x``."""
         import torch
         h = x.shape[-1]
-        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
-        _need(out is None or (y.shape == x.shape and y.dtype == x.dtype), "out has another shape or type than x")
+        if out is None:
+            y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            y = out
+            _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than x")
         ptype = self._params(h, weight, bias)
         mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
