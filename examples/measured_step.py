@@ -1,0 +1,93 @@
+"""Durations of a training step's kernels, measured on this GPU and composed into the step's timeline.
+
+A tracer runs each rank's kernels on one device and measures them (Sec. 4.1 of the paper).  This example does so for the
+kernel classes that the library runs itself, at the shapes of one rank of a workload: the embedding lookup and its gradient
+(first pipeline stage), the layer norms forward and backward, and the optimizer step as an orthogonalised update of every
+weight.  Their times replace the generator's for those ops; the step is composed with both.
+
+    python examples/measured_step.py [tiny | gpt1.3b | gpt175b]
+"""
+import os
+import sys
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2412_12487_gb300 import Echo  # noqa: E402
+from paper_2412_12487_gb300 import workloads as W  # noqa: E402
+
+
+def measure(e: Echo, c: W.GPTConfig, reps: int = 5):
+    """Nanoseconds of each operator on one rank: {"embed", "embed_grad", "norm", "norm_grad", "optimizer"}."""
+    tokens, hidden, rows = c.seq, c.hidden, W.VOCAB // c.tp
+    bf16, dev = torch.bfloat16, torch.device("cuda", e.device)
+    gen = torch.Generator(device=dev).manual_seed(0)
+    ids = torch.randint(0, W.VOCAB, (tokens,), generator=gen, device=dev)
+    table = torch.randn((rows, hidden), generator=gen, device=dev).to(bf16)
+    weight, bias = torch.ones(hidden, device=dev), torch.zeros(hidden, device=dev)
+    main = {k: torch.zeros_like(v, dtype=torch.float32) for k, v in (("table", table), ("weight", weight), ("bias", bias))}
+    layers, h, t = c.layers // c.pp, c.hidden, c.tp
+    grads = [torch.randn((layers, *s), generator=gen, device=dev).to(bf16) for s in ((3 * h // t, h), (h, h // t), (4 * h // t, h), (h, 4 * h // t))]
+
+    def step():
+        x = e.embed(ids, table)
+        yield "embed"
+        y, mean, rstd = e.layer_norm(x, weight, bias)
+        yield "norm"
+        dx, _, _ = e.layer_norm_grad(y, x, mean, rstd, weight, dweight=main["weight"], dbias=main["bias"], accumulate=True)
+        yield "norm_grad"
+        e.embed_grad(ids, dx, rows, out=main["table"], accumulate=True)
+        yield "embed_grad"
+        for g in grads:
+            e.orthogonalize(g, scale=max(1.0, g.shape[-2] / g.shape[-1]) ** 0.5)
+        yield "optimizer"
+
+    for _ in step():  # scratch memory is allocated
+        pass
+    times = {}
+    e.set_profiling(True)
+    e.read_profile()
+    for _ in range(reps):
+        for name in step():
+            times[name] = times.get(name, 0.0) + sum(ms for _, ms in e.read_profile().values())
+    e.set_profiling(False)
+    return {k: ms * 1e6 / reps for k, ms in times.items()}
+
+
+def put(g: W.Graph, c: W.GPTConfig, dur: np.ndarray, ns) -> np.ndarray:
+    """``dur`` [ops][scenarios] with the measured times in the place of the ops of their classes."""
+    dur = dur.copy()
+    comp = g.kind == W.KIND_COMPUTE
+    norm = comp & (g.kclass == W.KC_NORM)
+    forward = g.work < 5 * c.seq * c.hidden * W.MEM_FLOP_PER_BYTE  # (4 bytes an element; the backward norms have 6)
+    dur[norm & forward] = round(ns["norm"])
+    dur[norm & ~forward] = round(ns["norm_grad"])
+    # a lookup waits for the copy of its tokens; a gradient does not
+    first = np.minimum(g.pred_off[:-1], max(len(g.pred_idx) - 1, 0))
+    after_copy = (np.diff(g.pred_off) > 0) & (g.kind[g.pred_idx[first]] == W.KIND_MEMCPY)
+    emb = comp & (g.kclass == W.KC_EMB)
+    dur[emb & after_copy] = round(ns["embed"])
+    dur[emb & ~after_copy] = round(ns["embed_grad"])
+    dur[comp & (g.kclass == W.KC_OPT)] = round(ns["optimizer"] / 3)  # (three ops of a third of the parameters each)
+    return dur
+
+
+def main(name: str = "gpt1.3b"):
+    c = W.config(name)
+    g = W.build_gpt_graph(c)
+    sc = W.make_scenarios(g, c, n_scen=4)
+    with Echo(0) as e:
+        ns = measure(e, c)
+        for k, v in ns.items():
+            print(f"{k:12s} {v * 1e-3:10.1f} us")
+        e.load_graph(g)
+        for label, dur in (("generated", sc.dur), ("measured", put(g, c, sc.dur, ns))):
+            e.load_scenarios(sc, dur=dur)
+            e.estimate_collectives()
+            e.compose()
+            print(f"step with {label} durations: " + ", ".join(f"{m * 1e-6:.2f}" for m in e.read_makespan()) + " ms")
+
+
+if __name__ == "__main__":
+    main(*sys.argv[1:2])

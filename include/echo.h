@@ -365,7 +365,8 @@ int echo_measure_fp64(int device, double *rates);
  *     type of the output.  Every call gives the same bits for the same inputs.
  *   - NULL or misplaced pointers, unknown types, bad sizes or strides:
  *     ECHO_E_INVALID_ARG, with nothing enqueued; sizes beyond what a call states:
- *     ECHO_E_UNSUPPORTED.
+ *     ECHO_E_UNSUPPORTED.  A device-side wait that gives up (2 s) leaves that result
+ *     incomplete; the context's next operator returns ECHO_E_TIMEOUT, once.
  */
 enum { ECHO_F32 = 0, ECHO_BF16 = 1, ECHO_F16 = 2 };
 

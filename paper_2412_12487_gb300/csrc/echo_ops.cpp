@@ -124,7 +124,7 @@ int echo_embed_grad(echo_ctx *c, const echo_embed_grad_desc *d) {
     a.accumulate = d->accumulate != 0, a.scale = d->scale;
     a.window = echo::embed_grad_window(a.n, a.H, o.sms);
     const int64_t windows = (a.n + a.window - 1) / a.window;
-    if (windows * ((a.H + 31) / 32) / 8 + a.V / 128 >= INT32_MAX) return echo::op_error(c, ECHO_E_UNSUPPORTED, "too many sums for one launch");
+    if (windows * ((a.H + 31) / 32) / 8 + a.V / 32 >= INT32_MAX) return echo::op_error(c, ECHO_E_UNSUPPORTED, "too many sums for one launch");
     const size_t list = up256((size_t)a.n * 4);
     void *scratch = nullptr;
     if (const int rc = echo::op_scratch(c, 4 * list + 256 + (size_t)windows * 2 * a.H * sizeof(float), &scratch)) return rc;

@@ -201,15 +201,15 @@ __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32)
 // the parts in order.  Bound by the bytes of dy and of the rows.
 //
 // Unless the call accumulates, other blocks of the grid, between those of the sums, write zeros
-// to the rows that no token has: each marks its kClear rows' tokens among the sorted ones.
-constexpr int kClear = 128;
+// to the rows that no token has: each marks which of kClear rows have any among the sorted ones.
+constexpr int kClear = 32;
 
 template <typename T>
 __device__ void clear_rows(const EmbedGradArgs &a, const uint32_t *key, int64_t count, int64_t v0) {
-  __shared__ uint32_t has[kClear / 32];
+  __shared__ uint32_t has;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t v1 = min(a.V, v0 + kClear);
-  if (threadIdx.x < kClear / 32) has[threadIdx.x] = 0;
+  if (threadIdx.x == 0) has = 0;
   __syncthreads();
   int64_t lo = 0, hi = count;  // the first token of these rows: a 33-fold search by each warp
   while (lo < hi) {
@@ -223,14 +223,14 @@ __device__ void clear_rows(const EmbedGradArgs &a, const uint32_t *key, int64_t 
   for (int64_t i = lo + threadIdx.x; i < count; i += blockDim.x) {
     const uint32_t k = key[i];
     if (k >= v1) break;
-    atomicOr(&has[(k - v0) / 32], 1u << ((k - v0) % 32));
+    atomicOr(&has, 1u << (k - v0));
   }
   __syncthreads();
   const int64_t bytes = a.H * (int64_t)sizeof(T), pitch = a.dtable_stride * (int64_t)sizeof(T);
   unsigned char *table = static_cast<unsigned char *>(a.dtable);
   const bool wide = bytes % 16 == 0 && pitch % 16 == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0;
   for (int64_t v = v0 + warp; v < v1; v += blockDim.x >> 5) {
-    if (has[(v - v0) / 32] >> ((v - v0) % 32) & 1) continue;
+    if (has >> (v - v0) & 1) continue;
     unsigned char *at = table + v * pitch;
     if (wide) {
       for (int64_t i = lane; i < bytes / 16; i += 32) reinterpret_cast<uint4 *>(at)[i] = make_uint4(0, 0, 0, 0);

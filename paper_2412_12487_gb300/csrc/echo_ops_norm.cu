@@ -559,8 +559,10 @@ cudaError_t with_pieces(int64_t H, std::initializer_list<std::pair<const void *,
 int row_threads(int64_t H, int E) { return (int)std::min<int64_t>(1024, (H + 32 * E - 1) / (32 * E) * 32); }
 
 constexpr int64_t kCached = 768 * 16;  // longest rows of the one-pass kernels
-// Elements of a row that a thread takes: 8 where 256 threads hold the row, else 16.
-int row_elements(int64_t H) { return H <= 2048 ? 8 : 16; }
+// Elements of a row that a thread takes.  With 16 a row's sums and addresses take fewer
+// instructions (forward, 16384 x 2048 in bf16: 34 us, 38 with 8); backward, more warps are worth
+// more up to 256 threads a row (8192 x 1024 in fp32: 25 us with 8, 32 with 16).
+int row_elements(int64_t H, int arrays) { return H <= (arrays == 2 ? 2048 : 256) ? 8 : 16; }
 
 // Shape of a one-pass kernel for rows of H elements, `arrays` of them read: threads of a row,
 // rows at a time, slots (up to 4, as two blocks' shared memory allows), bytes of a slot.
@@ -571,13 +573,13 @@ struct Shape {
 template <typename X, int W>
 Shape row_shape(int64_t H, int arrays) {
   Shape s{};
-  s.E = row_elements(H);
+  s.E = row_elements(H, arrays);
   s.x = row_threads(H, s.E);
   s.y = std::max(1, 256 / s.x);
   s.slot = (int)(s.E == 8 ? Rows<X, W, 8>::slot_bytes(s.x, H) : Rows<X, W, 16>::slot_bytes(s.x, H));
   const size_t row = (size_t)s.y * arrays * s.slot, room = s.E > 8 ? 200 << 10 : 100 << 10;
   const size_t weights = arrays == 2 && s.E > 8 ? (size_t)s.x * s.y * s.E * sizeof(float) : 0;
-  s.staged = weights && row * 3 + weights <= room;
+  s.staged = weights && row * 2 + weights <= room;
   s.depth = (int)std::clamp<size_t>((room - (s.staged ? weights : 0)) / row, 2, 4);
   s.smem = row * s.depth + (s.staged ? weights : 0);
   if (arrays == 2) s.smem = std::max(s.smem, (size_t)(s.y - 1) * 2 * s.E * s.x * sizeof(float));
@@ -610,7 +612,7 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
         kernel<<<(unsigned)grid, dim3(s.x, s.y), s.smem, st>>>(a, s.depth, s.slot);
         return cudaGetLastError();
       };
-      return row_elements(a.H) == 8 ? go(Int<8>{}) : go(Int<16>{});
+      return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
     });
   });
 }

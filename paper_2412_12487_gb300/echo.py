@@ -260,6 +260,19 @@ def measure_fp64(device: int = 0) -> Dict[str, float]:
     return {"dadd": float(r[0]), "dmul": float(r[1]), "ddiv": float(r[2])}
 
 
+_raw_stream = None
+
+
+def _current_stream(device: int) -> int:
+    """Handle of torch's current stream (1.7 us less through torch's own accessor than by way
+    of a stream object, where torch has it)."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(device)
+
+
 _types: Dict[object, int] = {}  # torch dtype -> element type of the C ABI (F32, BF16, F16)
 
 
@@ -477,11 +490,13 @@ class Echo:
     def _op(self, call, desc):
         """Enqueues an operator in the order of torch's current stream: where that is not
         the context's, the context's stream waits for it and it for the operator."""
+        if (_current_stream(self.device) or CUDA_STREAM_LEGACY) == self._stream:
+            rc = call(self.h, C.byref(desc))
+            if rc:
+                self._check(rc)
+            return
         import torch
         cur = torch.cuda.current_stream(self.device)
-        if (cur.cuda_stream or CUDA_STREAM_LEGACY) == self._stream:
-            self._check(call(self.h, C.byref(desc)))
-            return
         own = (torch.cuda.default_stream(self.device) if self._stream == CUDA_STREAM_LEGACY
                else torch.cuda.ExternalStream(self._stream, device=self.device))
         own.wait_stream(cur)
