@@ -193,6 +193,46 @@ __global__ void __cluster_dims__(kSortBlocks) __launch_bounds__(kSortWarps * 32)
   if (rank == 0 && tid == 0) *a.count = (int32_t)n;
 }
 
+// The same order for few tokens, on all SMs at once: a token's place is the number of tokens
+// before it, counted against every other token (a warp takes four, 32 others at a time).  The
+// counts grow with the square of the tokens, but nothing waits for another block: with the
+// events around them, 2048 tokens take 10 us (16 by the passes above), 4096 13 us (22), 8192
+// 27 us (22).
+constexpr int kRankTokens = 5120, kRankWarps = 8, kRankEach = 4;
+
+__global__ void __launch_bounds__(kRankWarps * 32) embed_rank_kernel(EmbedGradArgs a, uint32_t *key_out, uint32_t *tok_out) {
+  extern __shared__ __align__(16) uint32_t rows[];  // of every token, padded to 128; ~0: none of the shard
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");  // (they wait for all of this one)
+  const int n = (int)a.n, padded = (n + 127) / 128 * 128, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < padded; i += blockDim.x) rows[i] = i < n ? (uint32_t)shard_row(a.ids, a.id64, i, a.v0, a.V) : ~0u;
+  __syncthreads();
+  const int t0 = (blockIdx.x * kRankWarps + (threadIdx.x >> 5)) * kRankEach;
+  uint32_t mine[kRankEach];
+  int before[kRankEach] = {}, all = 0;
+#pragma unroll
+  for (int k = 0; k < kRankEach; ++k) mine[k] = t0 + k < n ? rows[t0 + k] : ~0u;
+  for (int i = lane * 4; i < padded; i += 128) {
+    const uint4 o = *reinterpret_cast<const uint4 *>(rows + i);
+    const uint32_t other[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      all += other[e] != ~0u;
+#pragma unroll
+      for (int k = 0; k < kRankEach; ++k) before[k] += other[e] < mine[k] || (other[e] == mine[k] && i + e < t0 + k);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kRankEach; ++k) {
+    const int at = __reduce_add_sync(0xFFFFFFFFu, before[k]);
+    if (lane == k && mine[k] != ~0u) {
+      key_out[at] = mine[k];
+      tok_out[at] = (uint32_t)(t0 + k);
+    }
+  }
+  all = __reduce_add_sync(0xFFFFFFFFu, all);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = all;
+}
+
 // -- gradient: sums ----------------------------------------------------------------------------
 // The sorted tokens are cut into windows of a.window; a warp sums one window over 32 * kWide
 // columns, so that every warp has the same work however the tokens fall on the rows.  A row
@@ -389,10 +429,10 @@ cudaError_t launch_embed(const EmbedArgs &a, int sms, cudaStream_t st) {
   });
 }
 
-// Windows small enough that the sums occupy the SMs twice over, 24 warps each.
+// Windows small enough that the sums occupy the SMs, 24 warps each.
 int embed_grad_window(int64_t n, int64_t H, int sms) {
   int P = 8;
-  while (P < 32 && n / (2 * P) * ((H + 255) / 256) >= (int64_t)sms * 48) P *= 2;
+  while (P < 32 && n / (2 * P) * ((H + 255) / 256) >= (int64_t)sms * 24) P *= 2;
   return P;
 }
 
@@ -413,6 +453,12 @@ cudaError_t launch_early(int64_t grid, cudaStream_t st, const void *kernel, void
 }  // namespace
 
 cudaError_t launch_embed_sort(const EmbedGradArgs &a, cudaStream_t st) {
+  if (a.n <= kRankTokens) {
+    const int last = (sort_passes(a.V) + 1) & 1, each = kRankWarps * kRankEach;
+    embed_rank_kernel<<<(unsigned)std::max<int64_t>(1, (a.n + each - 1) / each), kRankWarps * 32, (size_t)((a.n + 127) / 128 * 128) * 4, st>>>(
+        a, a.key[last], a.tok[last]);
+    return cudaGetLastError();
+  }
   embed_sort_kernel<<<kSortBlocks, kSortWarps * 32, 0, st>>>(a, sort_passes(a.V));
   return cudaGetLastError();
 }

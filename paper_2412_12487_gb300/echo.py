@@ -277,13 +277,13 @@ _types: Dict[object, int] = {}  # torch dtype -> element type of the C ABI (F32,
 
 
 def _type(dtype) -> int:
-    if not _types:
+    kind = _types.get(dtype)
+    if kind is None:
         import torch
         _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    try:
-        return _types[dtype]
-    except KeyError:
-        raise EchoError(1, f"elements of {dtype} are not float32, bfloat16 or float16") from None
+        kind = _types.get(dtype)
+        _need(kind is not None, f"elements of {dtype} are not float32, bfloat16 or float16")
+    return kind
 
 
 def _dptr(t) -> Optional[int]:
@@ -555,19 +555,19 @@ class Echo:
         """(y, mean, rstd) of the rows of ``x`` [..., hidden]; mean and rstd are what
         ``layer_norm_grad`` needs (float32 [...]).  ``out`` may be ``x``."""
         import torch
-        h = x.shape[-1]
+        shape = x.shape
+        h = shape[-1]
         if out is None:
             y = torch.empty_like(x, memory_format=torch.contiguous_format)
         else:
             y = out
-            _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than x")
-        ptype = self._params(h, weight, bias)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+            _need(y.shape == shape and y.dtype == x.dtype, "out has another shape or type than x")
+        mean = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
         xm, n, xs = _matrix(x)
         ym, _, ys = _matrix(y, out=True)
         self._op(self.lib.echo_layer_norm, LayerNormDesc(n, h, xm.data_ptr(), ym.data_ptr(), _dptr(weight), _dptr(bias), mean.data_ptr(),
-                                                         rstd.data_ptr(), xs, ys, _type(x.dtype), ptype, eps))
+                                                         rstd.data_ptr(), xs, ys, _type(x.dtype), self._params(h, weight, bias), eps))
         return y, mean, rstd
 
     def layer_norm_grad(self, dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, accumulate: bool = False):
@@ -580,13 +580,18 @@ class Echo:
         _need(not accumulate or (dweight is not None and dbias is not None), "accumulate needs dweight and dbias")
         if dx is None:
             dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-        _need(dx.shape == x.shape and dx.dtype == x.dtype, "dx has another shape or type than x")
+        else:
+            _need(dx.shape == x.shape and dx.dtype == x.dtype, "dx has another shape or type than x")
         ptype = weight.dtype if weight is not None else dweight.dtype if dweight is not None else dbias.dtype if dbias is not None else torch.float32
-        dweight = torch.empty(h, dtype=ptype, device=x.device) if dweight is None else dweight
-        dbias = torch.empty(h, dtype=ptype, device=x.device) if dbias is None else dbias
+        if dweight is None:
+            dweight = torch.empty(h, dtype=ptype, device=x.device)
+        if dbias is None:
+            dbias = torch.empty_like(dweight)
         ptype = self._params(h, weight, dweight, dbias)
+        shape = x.shape[:-1]
         for s in (mean, rstd):
-            _need(s.shape == x.shape[:-1] and s.dtype == torch.float32 and s.is_contiguous(), "mean and rstd are float32, one of each a row")
+            if s.shape != shape or s.dtype != torch.float32 or not s.is_contiguous():
+                raise EchoError(1, "mean and rstd are float32, one of each a row")
         xm, n, xs = _matrix(x)
         gm, _, gs = _matrix(dy)
         om, _, os_ = _matrix(dx, out=True)
@@ -600,10 +605,14 @@ class Echo:
         """Common type of the parameter vectors given."""
         kind = None
         for p in params:
-            if p is not None:
-                _need(p.dim() == 1 and p.shape[0] == h and p.is_contiguous(), "a parameter is not a contiguous vector of a row's length")
-                _need(kind is None or p.dtype == kind, "the parameters and their gradients have different types")
+            if p is None:
+                continue
+            if p.numel() != h or p.dim() != 1 or not p.is_contiguous():
+                raise EchoError(1, "a parameter is not a contiguous vector of a row's length")
+            if kind is None:
                 kind = p.dtype
+            elif p.dtype != kind:
+                raise EchoError(1, "the parameters and their gradients have different types")
         return 0 if kind is None else _type(kind)
 
     def orthogonalize(self, g, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0, out=None):
