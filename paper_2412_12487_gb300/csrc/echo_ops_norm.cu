@@ -339,7 +339,8 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   };
   int turn = 0, slot = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * blockDim.y; row0 < a.rows; row0 += step, row += step, turn ^= 1) {
-    const bool live = row < a.rows, more = row + step < a.rows;
+    // (16 elements a thread: more than 2048 of a row, which a block then has to itself)
+    const bool live = E > 8 || row < a.rows, more = row + step < a.rows;
     const float next_mean = more ? a.mean[row + step] : 0.f, next_rstd = more ? a.rstd[row + step] : 0.f;
     R::arrived(depth);
     copy_next(slot == 0 ? last : slot - pitch);
