@@ -34,7 +34,7 @@ struct alignas(sizeof(T) * W <= 16 ? sizeof(T) * W : 16) Pack {
   T v[W];
 };
 template <typename T, int W>
-__device__ __forceinline__ void unpack(const Pack<T, W> &p, float *f) {
+__device__ __forceinline__ void unpack(const Pack<T, W> p, float *f) {
   if constexpr (W % 2 == 0 && std::is_same_v<T, __nv_bfloat16>) {  // a bf16 is the upper half of its fp32
     uint32_t r[W / 2];
     memcpy(r, &p, sizeof r);
@@ -65,7 +65,8 @@ __device__ __forceinline__ Pack<T, W> pack(const float *f) {
 }
 template <int W, typename T>
 __device__ __forceinline__ void load_piece(const T *at, float *f) {
-  unpack<T, W>(*reinterpret_cast<const Pack<T, W> *>(at), f);
+  const Pack<T, W> p = *reinterpret_cast<const Pack<T, W> *>(at);  // (as one piece)
+  unpack<T, W>(p, f);
 }
 template <int W, typename T>
 __device__ __forceinline__ void store_piece(T *at, const float *f) {

@@ -27,15 +27,18 @@ namespace {
 
 // What is stored of Y, A and B: the true value times this.  fp16 holds 2^-24 to 65504, so
 // elements up to 16 fit, and 22 bits remain of elements down to 2^-25.
-constexpr float kScaleY = 0x1p12f, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
+constexpr int kScaleYLog2 = 12;
+constexpr float kScaleY = 1 << kScaleYLog2, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
 
 // -- Frobenius norm ------------------------------------------------------------------------------
 // Sums of squares of x, of 2^-60 x and of 2^60 x: one of them neither overflows nor underflows,
-// whatever the size of the elements.  A block sums a part of the rows of one matrix.
+// whatever the size of the elements.  A block sums a part of one matrix (one without gaps comes
+// as a single row).
 template <typename T, int W>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t rows, int64_t cols, float *part) {
   __shared__ float sh[3][8];
   const float up = 0x1p60f, down = 0x1p-60f;
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");  // (they wait for all of this one)
   const int64_t pieces = cols / W, all = rows * pieces;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     float s[3] = {0.f, 0.f, 0.f};
@@ -48,7 +51,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t ro
         const int64_t i = i0 + k * 256;
 #pragma unroll
         for (int e = 0; e < W; ++e) v[k][e] = 0.f;
-        if (i < all) load_piece<W>(g + i / pieces * a.g_stride + i % pieces * W, v[k]);
+        if (i < all) load_piece<W>(rows == 1 ? g + i * W : g + i / pieces * a.g_stride + i % pieces * W, v[k]);
       }
 #pragma unroll
       for (int k = 0; k < kFlight; ++k)
@@ -74,34 +77,36 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t ro
   }
 }
 
-// 1 / (|G| + eps) of matrix z, by a warp, from the parts of its sums of squares.
-__device__ __forceinline__ double inverse_norm(const float *part, int parts, int64_t z, float eps) {
-  double s[3] = {0., 0., 0.};
-  for (int p = threadIdx.x & 31; p < parts; p += 32)
-#pragma unroll
-    for (int q = 0; q < 3; ++q) s[q] += part[(z * parts + p) * 3 + q];
-#pragma unroll
-  for (int q = 0; q < 3; ++q)
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s[q] += __shfl_xor_sync(0xFFFFFFFFu, s[q], d);
-  // (the plain sum unless it is near the ends of the fp32 range; a NaN stays one)
-  const double norm = s[0] > 1e30 ? sqrt(s[1]) * 0x1p60 : s[0] < 1e-24 ? sqrt(s[2]) * 0x1p-60 : sqrt(s[0]);
-  return 1. / (norm + (double)eps);
-}
-
 // x times a factor that may be outside fp32's range while the product is not: two powers of
 // two, each exact, and a number between 1/2 and 1.
 struct Factor {
   float p1, p2, f;
-  __device__ __forceinline__ void set(double v) {
-    int e = 0;
-    f = (float)frexp(v, &e);
-    const int half = e / 2;
-    p1 = ldexpf(1.f, half);
-    p2 = ldexpf(1.f, e - half);
-  }
   __device__ __forceinline__ float operator()(float x) const { return x * p1 * p2 * f; }
 };
+
+// 2^e / (|G| + eps) of matrix z, by a warp, from the parts of its sums of squares.  In fp32: a
+// common factor of all elements, and fp64 here took 6 us of every block.
+__device__ __forceinline__ Factor inverse_norm(const float *part, int parts, int64_t z, float eps, int e) {
+  float s[3] = {0.f, 0.f, 0.f};
+  for (int p = threadIdx.x & 31; p < parts; p += 32)
+#pragma unroll
+    for (int q = 0; q < 3; ++q) s[q] += part[(z * parts + p) * 3 + q];
+#pragma unroll
+  for (int q = 0; q < 3; ++q) s[q] = warp_sum(s[q]);
+  // the plain sum unless it is near the ends of the range; |G| = root * 2^size (a NaN stays one)
+  const int size = s[0] > 1e30f ? 60 : s[0] < 1e-24f ? -60 : 0;
+  const float root = sqrtf(size > 0 ? s[1] : size < 0 ? s[2] : s[0]);
+  const float inverse = 1.f / (root + ldexpf(eps, -size));
+  Factor f{1.f, 1.f, inverse};
+  if (inverse > 0.f && isfinite(inverse)) {
+    int own = 0;
+    f.f = frexpf(inverse, &own);
+    const int all = own + e - size, half = all / 2;
+    f.p1 = ldexpf(1.f, half);
+    f.p2 = ldexpf(1.f, all - half);
+  }
+  return f;
+}
 
 // -- matrices of the iteration --------------------------------------------------------------------
 // [plane][batch][rows][ld] fp16; plane 1 (fp32 matrices) is what plane 0 leaves of an element.
@@ -116,18 +121,75 @@ __device__ __forceinline__ void split(float v, __half (&h)[PLANES]) {
   if constexpr (PLANES == 2) h[1] = __float2half_rn(v - __half2float(h[0]));
 }
 
-// Y = G / (|G| + eps), or its transpose.  A block takes 64 x 64 tiles, in bands of 16 rows of
-// tiles, column by column, so that the tiles in work at a time make long runs in G and in Y.
-template <typename T, int PLANES>
+// Y = G / (|G| + eps), in pieces of W elements, four of them in flight a thread.
+template <typename T, int PLANES, int W>
 __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
   __shared__ Factor factor;
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  const uint32_t pieces = (uint32_t)(cols / W);
+  const int64_t all = rows * pieces, step = (int64_t)gridDim.x * 256 * 4;
+  for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
+    const T *g = static_cast<const T *>(a.g) + z * a.g_batch_stride;
+    __half *to = y.p + z * y.matrix;
+    float v[4][W];
+    int64_t at[4];
+    auto load = [&](int64_t i0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t i = i0 + k * 256;
+        if (i >= all) continue;
+        // (matrices of up to 2^32 elements: 32 bits hold i where pieces are wide or rows few)
+        const uint32_t r = all >> 32 ? (uint32_t)(i / pieces) : (uint32_t)i / pieces, c = (uint32_t)(i - (int64_t)r * pieces);
+        load_piece<W>(g + r * a.g_stride + (int64_t)c * W, v[k]);
+        at[k] = r * y.ld + (int64_t)c * W;
+      }
+    };
+    int64_t i0 = (int64_t)blockIdx.x * 256 * 4 + threadIdx.x;
+    load(i0);
+    if (threadIdx.x < 32) {
+      const Factor f = inverse_norm(part, parts, z, a.eps, kScaleYLog2);
+      if (threadIdx.x == 0) factor = f;
+    }
+    __syncthreads();
+    const Factor f = factor;
+    for (; i0 < all; i0 += step) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k * 256 >= all) continue;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[k][i] = f(v[k][i]);
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q) {
+          Pack<__half, W> h;
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            h.v[i] = __float2half_rn(v[k][i]);
+            if constexpr (PLANES == 2) v[k][i] -= __half2float(h.v[i]);  // what the next plane holds
+          }
+          *reinterpret_cast<Pack<__half, W> *>(to + q * y.plane + at[k]) = h;
+        }
+      }
+      load(i0 + step);
+    }
+    __syncthreads();
+  }
+}
+
+// Y = G^T / (|G| + eps).  A block takes 64 x 64 tiles, in bands of 16 rows of tiles, column by
+// column, so that the tiles in work at a time make long runs in G and in Y.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256) ortho_start_turned_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
+  __shared__ Factor factor;
   __shared__ float tile[64][65];
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int64_t tiles_r = (rows + 63) / 64, tiles_c = (cols + 63) / 64;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     if (threadIdx.x < 32) {
-      const double v = inverse_norm(part, parts, z, a.eps) * (double)kScaleY;
-      if (threadIdx.x == 0) factor.set(v);
+      const Factor f = inverse_norm(part, parts, z, a.eps, kScaleYLog2);
+      if (threadIdx.x == 0) factor = f;
     }
     __syncthreads();
     const Factor f = factor;
@@ -148,17 +210,16 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t r
 #pragma unroll
         for (int e = 0; e < 2; ++e) tile[ty + 8 * i][tx + 32 * e] = f(v[i][e]);
       __syncthreads();
-      const int64_t y0 = a.tall ? r0 : c0, x0 = a.tall ? c0 : r0, yn = a.tall ? rows : cols, xn = a.tall ? cols : rows;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int at = ty + 8 * i;  // two elements of a row of Y: the padding takes an odd end
-        if (y0 + at >= yn || x0 + 2 * tx >= xn) continue;
+        const int64_t c = c0 + ty + 8 * i, r = r0 + 2 * tx;  // two elements of a row of Y: the padding takes an odd end
+        if (c >= cols || r >= rows) continue;
         __half h[2][PLANES];
-        split<PLANES>(a.tall ? tile[at][2 * tx] : tile[2 * tx][at], h[0]);
-        split<PLANES>(a.tall ? tile[at][2 * tx + 1] : tile[2 * tx + 1][at], h[1]);
+        split<PLANES>(tile[2 * tx][ty + 8 * i], h[0]);
+        split<PLANES>(tile[2 * tx + 1][ty + 8 * i], h[1]);
 #pragma unroll
         for (int q = 0; q < PLANES; ++q)
-          *reinterpret_cast<__half2 *>(y.p + q * y.plane + z * y.matrix + (y0 + at) * y.ld + x0 + 2 * tx) = __halves2half2(h[0][q], h[1][q]);
+          *reinterpret_cast<__half2 *>(y.p + q * y.plane + z * y.matrix + c * y.ld + r) = __halves2half2(h[0][q], h[1][q]);
       }
       __syncthreads();
     }
@@ -172,8 +233,8 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t r
   __shared__ Factor factor;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     if (threadIdx.x < 32) {
-      const double v = inverse_norm(part, parts, z, a.eps);
-      if (threadIdx.x == 0) factor.set(v);
+      const Factor f = inverse_norm(part, parts, z, a.eps, 0);
+      if (threadIdx.x == 0) factor = f;
     }
     __syncthreads();
     const Factor f = factor;
@@ -733,6 +794,22 @@ int planes_for(int type) { return type == ECHO_BF16 ? 1 : 2; }
 
 }  // namespace
 
+// A launch whose blocks may start while the kernel before ends.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int block, size_t smem, cudaStream_t st, const A &...args) {
+  cudaLaunchConfig_t how{};
+  how.gridDim = grid;
+  how.blockDim = dim3(block);
+  how.dynamicSmemBytes = smem;
+  how.stream = st;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  how.attrs = &early;
+  how.numAttrs = 1;
+  return cudaLaunchKernelEx(&how, kernel, P(args)...);
+}
+
 // blocks that sum a matrix for its norm
 int norm_parts(const OrthoArgs &a) { return (int)std::clamp<int64_t>(a.m * a.n / 8192, 1, 608); }
 
@@ -756,10 +833,12 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
     return with_type(a.type, [&](auto t) {
       using T = decltype(t);
       constexpr int N = 16 / sizeof(T);
+      const bool one = a.g_stride == cols || rows == 1;  // without gaps
+      const int64_t sum_rows = one ? 1 : rows, sum_cols = one ? rows * cols : cols;
       if (cols % N == 0 && fits_pieces(a.g, a.g_stride, a.type, N) && fits_pieces(a.g, a.g_batch_stride, a.type, N))
-        ortho_norm_kernel<T, N><<<dim3(parts, gz), 256, 0, st>>>(a, rows, cols, part);
+        ortho_norm_kernel<T, N><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part);
       else
-        ortho_norm_kernel<T, 1><<<dim3(parts, gz), 256, 0, st>>>(a, rows, cols, part);
+        ortho_norm_kernel<T, 1><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part);
       return cudaGetLastError();
     });
   });
@@ -775,11 +854,16 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   const Planes Y[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
   const Planes A = planes_of(at, a.m, a.m, a.batch, planes), B = planes_of(at, a.m, a.m, a.batch, planes);
   e = timed("ortho_start", [&] {
-    const dim3 grid((unsigned)std::min<int64_t>((rows + 63) / 64 * ((cols + 63) / 64), std::max<int64_t>(1, sms * 6 / gz)), gz);
     return with_type(a.type, [&](auto t) {
       using T = decltype(t);
-      ortho_start_kernel<T, std::is_same_v<T, __nv_bfloat16> ? 1 : 2><<<grid, 256, 0, st>>>(a, rows, cols, part, parts, Y[0]);
-      return cudaGetLastError();
+      constexpr int P = std::is_same_v<T, __nv_bfloat16> ? 1 : 2, N = 16 / sizeof(T);
+      const int64_t room = std::max<int64_t>(1, sms * 6 / gz);
+      auto grid = [&](int64_t want) { return dim3((unsigned)std::min(want, room), gz); };
+      if (!a.tall)
+        return launch_early(ortho_start_turned_kernel<T, P>, grid((rows + 63) / 64 * ((cols + 63) / 64)), 256, 0, st, a, rows, cols, part, parts, Y[0]);
+      if (cols % N == 0 && fits_pieces(a.g, a.g_stride, a.type, N) && fits_pieces(a.g, a.g_batch_stride, a.type, N))
+        return launch_early(ortho_start_kernel<T, P, N>, grid((rows * cols / N + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
+      return launch_early(ortho_start_kernel<T, P, 1>, grid((rows * cols + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
     });
   });
   if (e != cudaSuccess) return e;
@@ -819,17 +903,7 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
       auto kernel = ortho_product_kernel<P, BN, MN, O>;
       if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(P, BN));
       if (r != cudaSuccess) return r;
-      cudaLaunchConfig_t how{};
-      how.gridDim = dim3((unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2);
-      how.blockDim = dim3(kThreads);
-      how.dynamicSmemBytes = smem_bytes(P, BN);
-      how.stream = st;
-      cudaLaunchAttribute early{};  // the blocks may start while the kernel before ends
-      early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      early.val.programmaticStreamSerializationAllowed = 1;
-      how.attrs = &early;
-      how.numAttrs = 1;
-      return cudaLaunchKernelEx(&how, kernel, pm, qm, dm, tm, g);
+      return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2), kThreads, smem_bytes(P, BN), st, pm, qm, dm, tm, g);
     };
     auto with_out = [&](auto cols_c) -> cudaError_t {
       if (mn) return planes == 2 ? go(Int<2>{}, cols_c, Int<1>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<1>{}, (void *)nullptr);
