@@ -220,7 +220,7 @@ int echo_orthogonalize(echo_ctx *c, const echo_orthogonalize_desc *d) {
                       d->g_stride, d->g_batch_stride, d->o_stride, d->o_batch_stride, d->type, d->steps,
                       d->a, d->b, d->c, d->eps, d->scale, nullptr, nullptr, o.wait_limit, o.skip};
     if (const int rc = echo::op_status(c, &a.status)) return rc;
-    if (const int rc = echo::op_scratch(c, echo::ortho_scratch_bytes(a), &a.scratch)) return rc;
+    if (const int rc = echo::op_scratch(c, echo::ortho_scratch_bytes(a, o.sms), &a.scratch)) return rc;
     const cudaError_t e = echo::launch_orthogonalize(a, o.sms, timer(c), o.stream);
     if (e != cudaSuccess) return echo::op_cuda_error(c, e, "orthogonalize");
     return (int)ECHO_OK;

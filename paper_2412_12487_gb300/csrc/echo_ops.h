@@ -113,7 +113,7 @@ struct OrthoArgs {
   long long wait_limit;     // bound of every wait of the kernels, in SM clock cycles
   int skip;                 // failure injection for tests (ProductArgs)
 };
-size_t ortho_scratch_bytes(const OrthoArgs &a);
+size_t ortho_scratch_bytes(const OrthoArgs &a, int sms);
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
 
 }  // namespace echo

@@ -35,10 +35,12 @@ constexpr float kScaleY = 1 << kScaleYLog2, kScaleA = 0x1p12f, kScaleB = 0x1p10f
 // whatever the size of the elements.  A block sums a part of one matrix (one without gaps comes
 // as a single row).
 template <typename T, int W>
-__global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t rows, int64_t cols, float *part) {
+__global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t rows, int64_t cols, float *part, int32_t *arrived, int n_arrived) {
   __shared__ float sh[3][8];
   const float up = 0x1p60f, down = 0x1p-60f;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");  // (they wait for all of this one)
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < n_arrived; i += blockDim.x) arrived[i] = 0;
   const int64_t pieces = cols / W, all = rows * pieces;
   for (int64_t z = blockIdx.y; z < a.batch; z += gridDim.y) {
     float s[3] = {0.f, 0.f, 0.f};
@@ -254,6 +256,10 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t r
 // pair's first block issues tcgen05.mma on both blocks' stages; eight warps take the sums out
 // of tensor memory, which holds two sets of them.
 //
+// Tiles that do not fill a round of the pairs are split along the sum, so that the round's other
+// pairs have parts of them: each warp writes its part of the sums, and the one that comes last
+// adds the parts, in their order, and finishes the tile.  Nobody waits for another block.
+//
 // The tensor core adds to its fp32 sums with truncation, which is a bias: with one set of sums
 // for 12288 columns of two-number operands (2304 additions an element) the result was 8e-5 off.
 // So for them a set covers one stage, the products of the low parts first, while the sums are
@@ -277,6 +283,10 @@ struct ProductArgs {
   int M, N, K;
   int tiles_n;          // tiles of a row of tiles (not symmetric)
   int64_t tiles;        // of a matrix
+  int64_t whole;        // tiles of the batch that are not split; the others, `split` parts each
+  int split;
+  float4 *parts;        // sums of the parts: [split tile][part][block of the pair][warp][columns / 4][lane]
+  int32_t *arrived;     // [split tile][block of the pair][warp] parts that are there: zeros between launches
   int symmetric;        // D is symmetric: tiles of the lower triangle, each element written twice
   float alpha, beta;
   Planes c;             // C (p may be null)
@@ -556,19 +566,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   // What is above overlaps the end of the kernel before; from here on its results are read.
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  const int64_t all = a.tiles * a.batch;
+  const int64_t all = a.whole + (a.tiles * a.batch - a.whole) * a.split;
   const int steps = (a.K + kBK - 1) / kBK, chunk = PLANES == 2 ? 1 : steps;  // stages of a set of sums
+
+  // Piece of work i: tile t (of the batch), stages k0 to k1 of its sum.
+  auto work_at = [&](int64_t i, int64_t &t, int &part, int &k0, int &k1) {
+    const int64_t j = i - a.whole;
+    const bool whole = j < 0;
+    t = whole ? i : a.whole + j / a.split;
+    part = whole ? 0 : (int)(j % a.split);
+    k0 = whole ? 0 : (int)((int64_t)steps * part / a.split);
+    k1 = whole ? steps : (int)((int64_t)steps * (part + 1) / a.split);
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kFewRegs));
     if (warp == 0 && lane == 0) {
       int64_t it = 0;
       bool ok = true;
-      for (int64_t t = pair; t < all && ok; t += pairs) {
-        int r0, c0;
+      for (int64_t i = pair; i < all && ok; i += pairs) {
+        int64_t t;
+        int r0, c0, part, k0, k1;
+        work_at(i, t, part, k0, k1);
         tile_place<BN>(a, t % a.tiles, r0, c0);
         const int z = (int)(t / a.tiles);
-        for (int k = 0; k < steps; ++k, ++it) {
+        for (int k = k0; k < k1; ++k, ++it) {
           const int s = (int)(it % S);
           ok = k != a.skip && bar_wait(empty + 8 * s, (uint32_t)(it / S + 1) & 1, abort, a);
           if (!ok) break;
@@ -589,14 +611,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     } else if (warp == 1 && lane == 0 && rank == 0) {
       int64_t it = 0, n = 0;
       bool ok = true;
-      for (int64_t t = pair; t < all && ok; t += pairs) {
-        for (int k0 = 0; k0 < steps && ok; k0 += chunk, ++n) {
+      for (int64_t i = pair; i < all && ok; i += pairs) {
+        int64_t t;
+        int part, begin, end;
+        work_at(i, t, part, begin, end);
+        for (int k0 = begin; k0 < end && ok; k0 += chunk, ++n) {
           const int b = (int)(n & 1);
           ok = bar_wait(sums_empty + 8 * b, (uint32_t)(n / 2 + 1) & 1, abort, a);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           const uint32_t d = tmem + b * BN;
-          for (int k = k0; k < min(steps, k0 + chunk); ++k, ++it) {
+          for (int k = k0; k < min(end, k0 + chunk); ++k, ++it) {
             const int s = (int)(it % S);
             ok = bar_wait(full + 8 * s, (uint32_t)(it / S) & 1, abort, a);
             if (!ok) break;
@@ -631,13 +656,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     int64_t n = 0;
     uint32_t turn = 0;
     bool ok = true;
-    for (int64_t t = pair; t < all && ok; t += pairs) {
-      int r0, c0;
+    for (int64_t i = pair; i < all && ok; i += pairs) {
+      int64_t t;
+      int r0, c0, part_of, begin, end;
+      work_at(i, t, part_of, begin, end);
       tile_place<BN>(a, t % a.tiles, r0, c0);
       const int z = (int)(t / a.tiles), row0 = r0 + rank * kRows + quarter * 32;
       const bool live = row0 < a.M;
       c0 += side * kCols;
-      const bool add_c = !MN && a.c.p;
+      const bool add_c = !MN && a.c.p && part_of == 0;
       const __half *from_c = a.c.p + z * a.c.matrix;
       if (add_c && row0 + lane < a.M) {  // C's part of the tile comes to L2 during the sums
 #pragma unroll
@@ -646,12 +673,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int i = 0; i < kCols; i += 64)
             if (c0 + i < a.N) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(from_c + q * a.c.plane + (int64_t)(row0 + lane) * a.c.ld + c0 + i));
       }
-      // C is added to the sums a plane of a 32 x 32 block at a time, with the last sets: each piece
-      // comes one set ahead, four lanes to the 64 bytes of a row, and changes to a row a lane in
-      // the warp's buffer.
+      // C is added to the sums a plane of a 32 x 32 block at a time, between the last sets, or
+      // before the first one where they are few: then it comes while the first stages do.  Each
+      // piece comes one turn ahead, four lanes to the 64 bytes of a row, and changes to a row a lane
+      // in the warp's buffer.
       constexpr int kFlight = MN ? 2 : 1;
       constexpr int kParts = kCols / 32, kPieces = MN ? 0 : PLANES * kParts;
-      const int sets = (steps + chunk - 1) / chunk, first_c = add_c ? max(0, sets - kPieces - 1) : sets;
+      const int sets = (end - begin + chunk - 1) / chunk;
+      const bool c_before = add_c && sets <= 2 * kPieces;
+      const int set0 = c_before ? kPieces + 1 : 0, first_c = c_before ? 0 : add_c ? sets - kPieces - 1 : sets;  // turns
       Piece ahead[4] = {};
       auto fetch = [&](int u) {
         const int row = row0 + (lane >> 2), col = c0 + u / PLANES * 32 + (lane & 3) * 8;
@@ -660,9 +690,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i)  // (to the end of a piece: within the padding of the row)
           if (row + 8 * i < a.M && col < a.N) ahead[i] = *reinterpret_cast<const Piece *>(p + (int64_t)(8 * i) * a.c.ld);
       };
-      float acc[kParts][32];
-      for (int set = 0; set < max(sets, add_c ? first_c + kPieces + 1 : 0); ++set) {
-        if (set < sets) {
+      float acc[kParts][32] = {};
+      for (int turn_c = 0; turn_c < set0 + sets; ++turn_c) {
+        if (turn_c >= set0) {
           const int b = (int)(n & 1);
           ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a);
           if (!ok) break;
@@ -679,15 +709,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             for (int e = 0; e < kFlight; ++e) {
               pass(s[e]);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) acc[part + e][i] = fmaf(a.alpha, __uint_as_float(s[e].r[i]), set == 0 ? 0.f : acc[part + e][i]);
+              for (int i = 0; i < 32; ++i) acc[part + e][i] = fmaf(a.alpha, __uint_as_float(s[e].r[i]), acc[part + e][i]);
             }
           }
           asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(in_first(sums_empty + 8 * b));
         }
-        if (set < first_c) continue;
-        const int u = set - first_c - 1;  // this set's piece
+        if (turn_c < first_c) continue;
+        const int u = turn_c - first_c - 1;  // this turn's piece
         if (kPieces && u >= 0 && u < kPieces) {
           half_free(lane);
 #pragma unroll
@@ -717,6 +747,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (!live) continue;
+      if (i >= a.whole && a.split > 1) {
+        const int64_t tile = t - a.whole;
+        const int64_t place = (int64_t)(rank * 8 + warp - 4) * (kCols / 4 * 32) + lane;
+        constexpr int64_t kPart = 16 * (kCols / 4 * 32);
+        float4 *mine = a.parts + (tile * a.split + part_of) * kPart + place;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            mine[(part * 8 + e) * 32] = make_float4(acc[part][4 * e], acc[part][4 * e + 1], acc[part][4 * e + 2], acc[part][4 * e + 3]);
+        __threadfence();
+        __syncwarp();
+        int32_t *count = a.arrived + tile * 16 + rank * 8 + warp - 4, before = 0;
+        if (lane == 0) before = atomicAdd(count, 1);
+        if (__shfl_sync(0xFFFFFFFFu, before, 0) != a.split - 1) continue;  // another part comes later
+        if (lane == 0) *count = 0;
+        __threadfence();
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[part][e] = 0.f;
+#pragma unroll 1
+        for (int other = 0; other < a.split; ++other) {
+          const float4 *from_part = a.parts + (tile * a.split + other) * kPart + place;
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 f = __ldcg(from_part + (part * 8 + e) * 32);
+              acc[part][4 * e] += f.x;
+              acc[part][4 * e + 1] += f.y;
+              acc[part][4 * e + 2] += f.z;
+              acc[part][4 * e + 3] += f.w;
+            }
+        }
+      }
       // One block after the other, in the registers of the first (unrolled, the code is 80 KB and
       // runs once a tile).
       float (&v)[32] = acc[0];
@@ -813,13 +879,55 @@ cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int block, size_t smem
 // blocks that sum a matrix for its norm
 int norm_parts(const OrthoArgs &a) { return (int)std::clamp<int64_t>(a.m * a.n / 8192, 1, 608); }
 
-// parts of the norm; Y twice (a product reads one while it writes the other), A, B
-size_t ortho_scratch_bytes(const OrthoArgs &a) {
+// How a product goes: the width of its tiles and the tiles that are split, with the smallest
+// estimate of its clocks.  A stage takes 1536 clocks of products at 256 columns, 1080 at 128 (the
+// operands' reads from shared memory bound it), 690 and 565 where the operands are one number an
+// element (L2 bounds both); joining parts takes about 6000 and, for each part, what 256 or 128 KB
+// of a pair's sums take to L2 and back.
+struct Plan {
+  int bn;
+  int64_t tiles, whole;
+  int split;
+};
+Plan plan_product(int64_t M, int64_t N, int64_t K, bool symmetric, int64_t batch, int planes, int pairs) {
+  Plan best{};
+  double least = 0;
+  for (const int bn : {256, 128}) {
+    const int64_t tm = (M + kBM - 1) / kBM, tiles = symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn);
+    const int64_t all = tiles * batch, rest = all % pairs, steps = (K + kBK - 1) / kBK;
+    const double stage = planes == 2 ? (bn == 256 ? 1536 : 1080) : (bn == 256 ? 690 : 565), join = bn == 256 ? 3000 : 1500;
+    int split = 1;
+    double round = rest ? stage * steps : 0;
+    for (int64_t p = 2; rest && p <= std::min(pairs / rest, steps); ++p) {
+      const double c = stage * ((steps + p - 1) / p) + 6000 + join * p;
+      if (c < round) round = c, split = (int)p;
+    }
+    const double clocks = stage * steps * (all / pairs) + round;
+    if (!best.bn || clocks < least) least = clocks, best = {bn, tiles, split > 1 ? all - rest : all, split};
+  }
+  return best;
+}
+Plan plan_of(const OrthoArgs &a, int product, int sms) {  // A, B, Y
+  return plan_product(product < 2 ? a.m : a.n, a.m, product == 0 ? a.n : a.m, product < 2, a.batch, planes_for(a.type), sms / 2);
+}
+
+// parts of the norm; counts and sums of split tiles; Y twice (a product reads one while it
+// writes the other), A, B
+size_t parts_bytes(const OrthoArgs &a, int sms) {
+  size_t most = 0;
+  for (int product = 0; product < 3; ++product) {
+    const Plan p = plan_of(a, product, sms);
+    most = std::max(most, (size_t)(p.tiles * a.batch - p.whole) * p.split * kBM * p.bn * sizeof(float));
+  }
+  return most;
+}
+size_t ortho_scratch_bytes(const OrthoArgs &a, int sms) {
   char *at = nullptr;
   const int planes = planes_for(a.type);
   for (int i = 0; i < 2; ++i) planes_of(at, a.n, a.m, a.batch, planes);
   for (int i = 0; i < 2; ++i) planes_of(at, a.m, a.m, a.batch, planes);
-  return (a.steps ? reinterpret_cast<uintptr_t>(at) : 0) + up256((size_t)a.batch * norm_parts(a) * 3 * sizeof(float));
+  return (a.steps ? reinterpret_cast<uintptr_t>(at) + up256((size_t)sms * 8 * sizeof(int32_t)) + parts_bytes(a, sms) : 0) +
+         up256((size_t)a.batch * norm_parts(a) * 3 * sizeof(float));
 }
 
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
@@ -827,6 +935,8 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   char *at = static_cast<char *>(a.scratch);
   float *part = reinterpret_cast<float *>(at);
   at += up256((size_t)a.batch * parts * 3 * sizeof(float));
+  const int pairs = sms / 2;
+  int32_t *arrived = reinterpret_cast<int32_t *>(at);
   const unsigned gz = (unsigned)std::min<int64_t>(a.batch, 65535);
   const int64_t rows = a.tall ? a.n : a.m, cols = a.tall ? a.m : a.n;
   cudaError_t e = timed("ortho_norm", [&] {
@@ -836,9 +946,9 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
       const bool one = a.g_stride == cols || rows == 1;  // without gaps
       const int64_t sum_rows = one ? 1 : rows, sum_cols = one ? rows * cols : cols;
       if (cols % N == 0 && fits_pieces(a.g, a.g_stride, a.type, N) && fits_pieces(a.g, a.g_batch_stride, a.type, N))
-        ortho_norm_kernel<T, N><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part);
+        ortho_norm_kernel<T, N><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part, arrived, a.steps ? pairs * 16 : 0);
       else
-        ortho_norm_kernel<T, 1><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part);
+        ortho_norm_kernel<T, 1><<<dim3(parts, gz), 256, 0, st>>>(a, sum_rows, sum_cols, part, arrived, a.steps ? pairs * 16 : 0);
       return cudaGetLastError();
     });
   });
@@ -851,6 +961,9 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
         return cudaGetLastError();
       });
     });
+  at += up256((size_t)sms * 8 * sizeof(int32_t));
+  float4 *split_parts = reinterpret_cast<float4 *>(at);
+  at += parts_bytes(a, sms);
   const Planes Y[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
   const Planes A = planes_of(at, a.m, a.m, a.batch, planes), B = planes_of(at, a.m, a.m, a.batch, planes);
   e = timed("ortho_start", [&] {
@@ -868,11 +981,6 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   });
   if (e != cudaSuccess) return e;
 
-  const int pairs = sms / 2;
-  auto tiles_of = [](int64_t M, int64_t N, bool symmetric, int bn) {
-    const int64_t tm = (M + kBM - 1) / kBM;
-    return symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn);
-  };
   struct Matrix {
     const Planes &p;
     int64_t rows, cols;
@@ -880,9 +988,10 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   const Matrix y[2] = {{Y[0], a.n, a.m}, {Y[1], a.n, a.m}}, sa{A, a.m, a.m}, sb{B, a.m, a.m};
   // D = alpha P Q^T + beta C (mn: P and Q hold the transposes); the result without a D.  D is
   // symmetric where P is Q.
-  auto product = [&](const char *name, const Matrix &p, const Matrix &q, bool mn, float alpha, const Planes *c, float beta, float diagonal, const Matrix *d) -> cudaError_t {
+  auto product = [&](int which, const char *name, const Matrix &p, const Matrix &q, bool mn, float alpha, const Planes *c, float beta, float diagonal, const Matrix *d) -> cudaError_t {
     ProductArgs g{};
     const bool symmetric = &p == &q;
+    const Plan plan = plan_of(a, which, sms);
     g.batch = a.batch, g.M = (int)(mn ? p.cols : p.rows), g.N = (int)(mn ? q.cols : q.rows), g.K = (int)(mn ? p.rows : p.cols);
     g.symmetric = symmetric;
     g.alpha = alpha, g.beta = beta, g.diagonal = diagonal;
@@ -894,7 +1003,7 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
       constexpr bool MN = decltype(mn_c)::value;
       using O = std::remove_pointer_t<decltype(out)>;
       g.tiles_n = (int)((g.N + BN - 1) / BN);
-      g.tiles = tiles_of(g.M, g.N, symmetric, BN);
+      g.tiles = plan.tiles, g.whole = plan.whole, g.split = plan.split, g.parts = split_parts, g.arrived = arrived;
       CUtensorMap pm, qm, dm{}, tm{};
       cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, planes, MN ? kBK : kRows);
       if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, planes, MN ? kBK : BN / 2);
@@ -903,7 +1012,7 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
       auto kernel = ortho_product_kernel<P, BN, MN, O>;
       if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(P, BN));
       if (r != cudaSuccess) return r;
-      return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles * g.batch, pairs) * 2), kThreads, smem_bytes(P, BN), st, pm, qm, dm, tm, g);
+      return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.whole + (g.tiles * g.batch - g.whole) * g.split, pairs) * 2), kThreads, smem_bytes(P, BN), st, pm, qm, dm, tm, g);
     };
     auto with_out = [&](auto cols_c) -> cudaError_t {
       if (mn) return planes == 2 ? go(Int<2>{}, cols_c, Int<1>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<1>{}, (void *)nullptr);
@@ -912,25 +1021,21 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
              : a.type == ECHO_BF16 ? go(Int<1>{}, cols_c, Int<0>{}, (__nv_bfloat16 *)nullptr)
                                    : go(Int<2>{}, cols_c, Int<0>{}, (__half *)nullptr);
     };
-    // The width with fewer (rounds of tiles) x (time of a stage): 1536 clocks of products, or
-    // 1020 where L2 bounds, for two-number operands; 690 and 565 for the others, both bound by L2.
-    auto cost = [&](int bn, int clocks) { return (tiles_of(g.M, g.N, symmetric, bn) * a.batch + pairs - 1) / pairs * clocks; };
-    const bool narrow = cost(128, planes == 2 ? 1020 : 565) < cost(256, planes == 2 ? 1536 : 690);
-    return timed(name, [&] { return narrow ? with_out(Int<128>{}) : with_out(Int<256>{}); });
+    return timed(name, [&] { return plan.bn == 128 ? with_out(Int<128>{}) : with_out(Int<256>{}); });
   };
   for (int s = 0; s < a.steps; ++s) {
     const Matrix &now = y[s & 1], &next = y[(s + 1) & 1];
     const bool last = s == a.steps - 1;
     const float out = last ? a.scale / kScaleY : 1.f;
-    if ((e = product("ortho_yty", now, now, true, kScaleA / (kScaleY * kScaleY), nullptr, 0.f, 0.f, &sa)) != cudaSuccess) return e;
+    if ((e = product(0, "ortho_yty", now, now, true, kScaleA / (kScaleY * kScaleY), nullptr, 0.f, 0.f, &sa)) != cudaSuccess) return e;
     // a Y comes from B + a I for matrices of one number an element: the last product then reads
     // and adds nothing.  With two numbers the larger sums would lose more to truncation than the
     // sum of a Y and Y B in fp32 does (2.7e-6 instead of 1.0e-6 at 300 x 300).
     const bool fold = planes == 1;
-    if ((e = product("ortho_aa", sa, sa, false, a.c * (kScaleB / (kScaleA * kScaleA)), &A, a.b * (kScaleB / kScaleA), fold ? a.a * kScaleB : 0.f, &sb)) !=
+    if ((e = product(1, "ortho_aa", sa, sa, false, a.c * (kScaleB / (kScaleA * kScaleA)), &A, a.b * (kScaleB / kScaleA), fold ? a.a * kScaleB : 0.f, &sb)) !=
         cudaSuccess)
       return e;
-    if ((e = product("ortho_yb", now, sb, false, out / kScaleB, fold ? nullptr : &now.p, out * a.a, 0.f, last ? nullptr : &next)) != cudaSuccess) return e;
+    if ((e = product(2, "ortho_yb", now, sb, false, out / kScaleB, fold ? nullptr : &now.p, out * a.a, 0.f, last ? nullptr : &next)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
