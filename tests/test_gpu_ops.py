@@ -631,3 +631,73 @@ def test_refusals_at_the_c_boundary(echo):
     buf = C.create_string_buffer(256)
     assert lib.echo_last_error(h, buf, 256) == 0 and buf.value
     assert embed() == 0
+
+
+# -- sizes at which the kernels change their ways ----------------------------------------------
+@pytest.mark.parametrize("n,v", [(5120, 51200), (5121, 51200), (32768, 300), (33000, 70000), (70001, 17), (40000, 1)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_grad_many_tokens(echo, n, v, accumulate):
+    """Around the number of tokens that are sorted by counting, and that a sort's threads hold."""
+    ids = _ids(n, -1, v + 2, 100)
+    dy = _randn((n, 24), 101, BF16)
+    old = _randn((v, 24), 102)
+    got = echo.embed_grad(ids, dy, v, out=old.clone(), accumulate=accumulate)
+    want, tol = _embed_grad_ref(ids, dy, v, 1.0, 0, old if accumulate else None)
+    _close(got, want, tol, F32)
+    assert torch.equal(got, echo.embed_grad(ids, dy, v, out=old.clone(), accumulate=accumulate))
+
+
+@pytest.mark.parametrize("h", [8, 256, 257, 2048, 2049, 4096, 4097, 12288, 12289, 12296])
+@pytest.mark.parametrize("x_t", [F32, BF16])
+def test_layer_norm_row_lengths(echo, h, x_t):
+    """Around the lengths at which a row's threads, or the kernel, change."""
+    rows = 700 if h < 5000 else 170
+    x, dy = _randn((rows, h), 110, x_t, 2.0, 0.5), _randn((rows, h), 111, x_t)
+    w, b = _randn((h,), 112, F32, 0.2, 1.0), _randn((h,), 113)
+    y, mean, rstd = echo.layer_norm(x, w, b)
+    wy, wm, wr = _ln_ref(x, w, b, 1e-5)
+    _close(y, wy, _ln_tol(x, w, b, wm, wr), x_t)
+    want, tol = _ln_grad_ref(dy, x, mean, rstd, w)
+    for g, v, t, d in zip(echo.layer_norm_grad(dy, x, mean, rstd, w), want, tol, (x_t, F32, F32)):
+        _close(g, v, t, d)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("shape", [(40, 3000), (3000, 40), (300, 5000), (2, 130, 4001), (1100, 1300), (7, 256, 512), (2500, 2600)])
+def test_orthogonalize_split_sums(echo, dtype, shape):
+    """Few tiles with long sums, which go in parts, and more tiles than one round takes."""
+    g = _randn(shape, 120, dtype, 1e-2)
+    got = echo.orthogonalize(g)
+    _ortho_close(got, _ortho_ref(g, 5, QUINTIC, 1e-7, 1.0), dtype)
+    assert torch.equal(got, echo.orthogonalize(g))
+
+
+def test_orthogonalize_one_context_many_shapes(echo):
+    """Calls of different sizes share scratch memory: none sees what another left there."""
+    for k, (shape, dtype) in enumerate([((700, 900), F32), ((33, 2000), BF16), ((64, 64), F16), ((2000, 33), F32), ((3, 128, 300), BF16), ((700, 900), F32)]):
+        g = _randn(shape, 130 + k, dtype)
+        _ortho_close(echo.orthogonalize(g), _ortho_ref(g, 5, QUINTIC, 1e-7, 1.0), dtype)
+
+
+def test_capture_in_a_graph():
+    """After a first call of each size the operators can be captured and replayed."""
+    side = torch.cuda.Stream()
+    x, g, ids = _randn((64, 512), 140), _randn((96, 200), 141), _ids(64, 0, 50, 142)
+    with Echo(0, stream=side) as e, torch.cuda.stream(side):
+        def step():
+            y, mean, rstd = e.layer_norm(x)
+            dx, dw, db = e.layer_norm_grad(y, x, mean, rstd)
+            return y, dx, dw, e.embed_grad(ids, dx, 50), e.orthogonalize(g)
+
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step()
+        x.mul_(1.5)
+        g.add_(0.25)
+        graph.replay()
+        want = step()
+        side.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
