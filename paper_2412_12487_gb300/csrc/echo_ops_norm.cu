@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
     const float next_mean = more ? a.mean[row + step] : 0.f, next_rstd = more ? a.rstd[row + step] : 0.f;
     R::arrived(depth);
     copy_next(slot == 0 ? last : slot - pitch);
-    const Pair scale = both(rstd), shift = both(-mean * rstd);
+    const Pair scale = both(rstd), shift = both(-mean);  // (x - mean first: far from zero, x * rstd would lose what they differ by)
     Pair s1 = {0.f, 0.f}, s2 = {0.f, 0.f};
     auto add_up = [&](int mine) {
 #pragma unroll
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
 #pragma unroll
         for (int e = 0; e < C / 2; ++e) {
           const int at = c * (C / 2) + e;
-          const Pair xh = fma2(x[e], scale, shift), gw = mul2(g[e], w[e]);
+          const Pair xh = mul2(add2(x[e], shift), scale), gw = mul2(g[e], w[e]);
           dw[at] = fma2(g[e], xh, dw[at]);
           db[at] = add2(db[at], g[e]);
           s1 = add2(s1, gw);
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
         m1 = warp_sum(o.x);
         m2 = warp_sum(o.y);
       }
-      const Pair n1 = both(-m1 * over_h), n2 = both(-m2 * over_h);
+      const Pair n1 = both(-m1 * over_h), n2 = both(-m2 * over_h * rstd);
       auto put = [&](int mine) {
 #pragma unroll
         for (int c = 0; c < E / C; ++c) {
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
           float f[C];
 #pragma unroll
           for (int e = 0; e < C / 2; ++e) {
-            const Pair d = mul2(fma2(fma2(x[e], scale, shift), n2, fma2(g[e], w[e], n1)), scale);
+            const Pair d = mul2(fma2(add2(x[e], shift), n2, fma2(g[e], w[e], n1)), scale);
             f[2 * e] = d.a;
             f[2 * e + 1] = d.b;
           }

@@ -701,3 +701,19 @@ def test_capture_in_a_graph():
         side.synchronize()
         for a, b in zip(out, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("h", [200, 201, 2500, 13000])
+def test_layer_norm_grad_far_from_zero(echo, h):
+    """Rows that differ by 1 around 3000: x - mean comes before the product with rstd, so that
+    (x - mean) rstd is within 3 u of itself, and not of |mean| rstd."""
+    rows = 300
+    x, dy, w = _randn((rows, h), 120, F32, 1.0, 3000.0), _randn((rows, h), 121), _randn((h,), 122, F32, 0.2, 1.0)
+    _, mean, rstd = echo.layer_norm(x, w)
+    g, xh, r = dy.double() * w.double(), (x.double() - mean.double()[:, None]) * rstd.double()[:, None], rstd.double()[:, None]
+    m1, m2 = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+    e1, e2 = (132 * U * t.abs().mean(1, keepdim=True) for t in (g, g * xh))
+    dx, dw, db = echo.layer_norm_grad(dy, x, mean, rstd, w)
+    _close(dx, r * (g - m1 - xh * m2), r * (12 * U * (g.abs() + m1.abs() + (xh * m2).abs()) + e1 + xh.abs() * e2), F32)
+    _close(dw, (dy * xh).sum(0), (rows + 8) * U * (dy * xh).abs().sum(0), F32)
+    _close(db, dy.double().sum(0), (rows + 4) * U * dy.double().abs().sum(0), F32)
