@@ -127,13 +127,17 @@ struct Rows {
 // warps: each takes the squared distances from its own mean, and
 //   sum (x - mean)^2 = sum over warps of (their sum + n_w (mean_w - mean)^2),
 // in which nothing cancels.  The output starts from those distances.  The bytes of x and y would
-// bound it; what does is the instructions of a row, so they are in pairs, and addresses and
-// bounds are kept from row to row.
+// bound it; what does is the instructions of a row and its two barriers (issue slots 59% taken at
+// 2048 x 12288 in bf16), so they are in pairs, and addresses and bounds are kept from row to row.
+// There a call takes 22 to 25 us in a row of them, 1.0e8 bytes: up to 4.6 TB/s.  Two rows a block
+// with 32 elements a thread took 16% longer.
 template <typename X, int W, int E>
 __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a, int depth, int slot_bytes) {
   using S = Slice<X, W, E>;
   using R = Rows<X, W, E>;
   extern __shared__ __align__(16) unsigned char ring[];  // [depth][rows of the block]
+  kernel_begin();
+  next_may_start();
   __shared__ float2 sh[2][32];
   __shared__ float size[32];
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
@@ -222,10 +226,13 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs
   }
 }
 
-// Rows too long for registers: three passes over the row, a block each.
+// Rows too long for registers: three passes over the row, a block each; the second and third come
+// from L2, whose bytes bound it.
 template <typename X, int W>
 __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
   __shared__ float sh[2][32];
+  kernel_begin();
+  next_may_start();
   const float over_h = 1.f / (float)a.H;
   const int64_t step = (int64_t)blockDim.x * W;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -264,18 +271,23 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
 }
 
 // -- backward ----------------------------------------------------------------------------------
+// With xh = (x - mean) rstd and g = dy w:
+//   dx = rstd (g - mean(g) - xh mean(g xh)),  dweight = sum over rows of dy xh,  dbias = of dy.
 // One pass over dy and x: a block goes through its rows, a row among blockDim.x threads that
-// keep the sums of dweight and dbias of their columns in registers.
-// Only those sums stay in registers with 16 elements a thread (the weight and the row as well
-// would spill): the row is read twice from its slot, and the weight from shared memory
-// (`staged`) or from L2 where the rows in flight leave no room.  Bound by the bytes of dy, x and dx while a row's instructions are few (in pairs, as above);
-// the blocks' partial sums come on top ([blocks][2][H] fp32, written and read once).
+// keep the sums of dweight and dbias of their columns in registers.  Only those sums stay in
+// registers with 16 elements a thread (the weight and the row as well would spill): the row is
+// read twice from its slot, and the weight from shared memory (`staged`) or from L2 where the rows
+// in flight leave no room.  The bytes of dy, x and dx would bound it; what does is shared memory
+// and the instructions of a row (50% and 53% of their slots at 2048 x 12288 in bf16, where a call
+// takes 47.6 us with the join, 3.2 TB/s).  The blocks' partial sums come on top ([blocks][2][H]
+// fp32, written and read once).
 template <typename X, int W, int E>
 __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(NormGradArgs a, int depth, int slot_bytes, int staged) {
   constexpr int K = E / W;
   using S = Slice<X, W, E>;
   using R = Rows<X, W, E>;
   extern __shared__ __align__(16) unsigned char staging[];  // [depth][x, dy][rows of the block]; the weight
+  kernel_begin();
   __shared__ float2 sh[2][32];
   const int T = blockDim.x * blockDim.y, t = threadIdx.y * blockDim.x + threadIdx.x, warps = blockDim.x >> 5, lane = threadIdx.x & 31, H = (int)a.H;
   const float over_h = 1.f / (float)H;
@@ -404,7 +416,7 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
     mean = next_mean;
     rstd = next_rstd;
   }
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  next_may_start();
   if (!a.part) return;
   // the block's rows together, in their order, then out
   asm volatile("cp.async.wait_group 0;\n" ::: "memory");
@@ -439,10 +451,13 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   }
 }
 
-// Rows too long for that: dx, a block a row, in two passes over it (the second from L2) ...
+// Rows too long for that: dx, a block a row, in two passes over it (the second from L2, whose bytes
+// bound it) ...
 template <typename X, int W>
 __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs a) {
   __shared__ float sh[4][32];
+  kernel_begin();
+  next_may_start();
   const float over_h = 1.f / (float)a.H;
   const int64_t step = (int64_t)blockDim.x * W;
   int turn = 0;
@@ -476,9 +491,12 @@ __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs
   }
 }
 
-// ... and partial sums of dweight and dbias, blockDim.x * W columns of one part of the rows a block.
+// ... and partial sums of dweight and dbias, blockDim.x * W columns of one part of the rows a block:
+// dy and x once more, whose bytes bound it.
 template <typename X, int W>
 __global__ void __launch_bounds__(128) layer_norm_grad_columns_kernel(NormGradArgs a) {
+  kernel_begin();
+  next_may_start();
   const int64_t j = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * W;
   if (j >= a.H) return;
   const int64_t per = (a.rows + a.parts - 1) / a.parts;
@@ -518,12 +536,14 @@ __device__ __forceinline__ void put_param(void *p, int type, int64_t j, float v,
 }
 
 // dweight and dbias from their parts: 32 columns of one of the two a block, its warps taking
-// the parts in turn, then the warps' sums in order.
+// the parts in turn, then the warps' sums in order, so that calls repeat to the bit.  152 parts of
+// 12288 columns, 1.5e7 bytes, take 8.7 us by themselves.
 constexpr int kJoinWarps = 16;
 
 __global__ void __launch_bounds__(kJoinWarps * 32) layer_norm_grad_join_kernel(NormGradArgs a) {
   __shared__ float sh[kJoinWarps][33];
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  kernel_begin();
+  next_may_start();
   const int64_t j = (int64_t)blockIdx.x * 32 + threadIdx.x;  // of [dweight, dbias]: 2 H columns
   float s = 0.f;
   if (j < 2 * a.H) {
@@ -590,6 +610,23 @@ Shape row_shape(int64_t H, int arrays) {
 int blocks_of(const Shape &s) {
   return (int)std::max<size_t>(1, std::min<size_t>((s.E > 8 ? 768 : 1024) / (s.x * s.y), (220 << 10) / (s.smem + 2048)));
 }
+// A grid that goes through its rows in turns has to lie evenly on the SMs, which blocks that come
+// while another kernel ends do not by themselves: where it fills them, a block asks for so much
+// shared memory that no more than its share fit an SM (4999 x 1537 in fp32, backward: 40 us a
+// call in a row of them, 63 without).
+size_t even_smem(const Shape &s, int64_t grid, int sms) {
+  return grid > sms && grid % sms == 0 ? std::max<size_t>(s.smem, (228 << 10) / (grid / sms + 1)) : s.smem;
+}
+
+template <typename K, typename... A>
+cudaError_t launch_rows(K kernel, const Shape &s, int64_t grid, int sms, cudaStream_t st, const A &...args) {
+  const size_t smem = even_smem(s, grid, sms);
+  if (smem > 40 << 10) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_early(kernel, dim3((unsigned)grid), dim3(s.x, s.y), smem, st, args...);
+}
 
 }  // namespace
 
@@ -599,19 +636,13 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
     return with_pieces<X>(a.H, {{a.x, a.x_stride}, {a.y, a.y_stride}}, a.x_type, {a.w, a.b}, a.p_type, [&](auto wide) {
       constexpr int W = decltype(wide)::value;
       if (a.H > kCached) {
-        layer_norm_long_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, sms * 2), 1024, 0, st>>>(a);
-        return cudaGetLastError();
+        return launch_early(layer_norm_long_kernel<X, W>, dim3((unsigned)std::min<int64_t>(a.rows, sms * 2)), 1024, 0, st, a);
       }
       const Shape s = row_shape<X, W>(a.H, 1);
       auto go = [&](auto each) {
         constexpr int E = decltype(each)::value;
-        auto kernel = layer_norm_kernel<X, W, E>;
-        const cudaError_t e =
-            s.smem > 40 << 10 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem) : cudaSuccess;
-        if (e != cudaSuccess) return e;
         const int64_t grid = std::min<int64_t>((a.rows + s.y - 1) / s.y, (int64_t)sms * blocks_of(s));
-        kernel<<<(unsigned)grid, dim3(s.x, s.y), s.smem, st>>>(a, s.depth, s.slot);
-        return cudaGetLastError();
+        return launch_rows(layer_norm_kernel<X, W, E>, s, grid, sms, st, a, s.depth, s.slot);
       };
       return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
     });
@@ -649,25 +680,19 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer
           const int64_t cols = 128 * W;
           if (params)  // (before dx: it may overwrite dy or x)
             r = timed("layer_norm_grad_columns", [&] {
-              layer_norm_grad_columns_kernel<X, W><<<dim3((unsigned)((a.H + cols - 1) / cols), a.parts), 128, 0, st>>>(a);
-              return cudaGetLastError();
+              return launch_early(layer_norm_grad_columns_kernel<X, W>, dim3((unsigned)((a.H + cols - 1) / cols), a.parts), 128, 0, st, a);
             });
           if (r == cudaSuccess && a.dx)
             r = timed("layer_norm_grad_rows", [&] {
-              layer_norm_grad_rows_kernel<X, W><<<(unsigned)std::min<int64_t>(a.rows, INT32_MAX), row_threads(a.H, 8), 0, st>>>(a);
-              return cudaGetLastError();
+              return launch_early(layer_norm_grad_rows_kernel<X, W>, dim3((unsigned)std::min<int64_t>(a.rows, INT32_MAX)), row_threads(a.H, 8), 0, st, a);
             });
           return r;
         }
         const Shape s = row_shape<X, W>(a.H, 2);
         auto go = [&](auto each) {
           constexpr int E = decltype(each)::value;
-          auto kernel = layer_norm_grad_kernel<X, W, E>;
-          cudaError_t r = s.smem > 40 << 10 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem) : cudaSuccess;
-          if (r != cudaSuccess) return r;
           return timed("layer_norm_grad", [&] {
-            kernel<<<(unsigned)grad_blocks(s, a.rows, sms), dim3(s.x, s.y), s.smem, st>>>(a, s.depth, s.slot, s.staged);
-            return cudaGetLastError();
+            return launch_rows(layer_norm_grad_kernel<X, W, E>, s, grad_blocks(s, a.rows, sms), sms, st, a, s.depth, s.slot, s.staged);
           });
         };
         return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
@@ -675,16 +700,7 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer
     });
   if (e != cudaSuccess || !params) return e;
   return timed("layer_norm_grad_join", [&] {
-    cudaLaunchConfig_t how{};
-    how.gridDim = dim3((unsigned)((2 * a.H + 31) / 32));
-    how.blockDim = dim3(32, kJoinWarps);
-    how.stream = st;
-    cudaLaunchAttribute early{};  // the blocks may start while the kernel before ends
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    how.attrs = &early;
-    how.numAttrs = 1;
-    return cudaLaunchKernelEx(&how, layer_norm_grad_join_kernel, a);
+    return launch_early(layer_norm_grad_join_kernel, dim3((unsigned)((2 * a.H + 31) / 32)), dim3(32, kJoinWarps), 0, st, a);
   });
 }
 
