@@ -24,8 +24,8 @@ __device__ __forceinline__ int64_t shard_row(const void *ids, int id64, int64_t 
 // out[t] = scale * table[row of t], zeros without one.  Bound by the bytes read and written.  A
 // warp takes 32 * kLookup pieces of one token, then those of another: the next token's id is
 // read while this one's row is on its way, so that a token costs one latency and not two.  2048
-// tokens of 12288, fp32 to bf16, 8.4e7 bytes: 15.6 us in a row of calls, 5.35 TB/s; with half the
-// pieces and twice the blocks 6.5 us more.
+// tokens of 12288, fp32 to bf16, 8.4e7 bytes: 15.6 us in a row of calls, 5.35 TB/s; half the
+// pieces, in registers for six blocks an SM, took 6.5 us more.
 constexpr int kLookup = 4;
 
 template <typename T, typename O, int W>
