@@ -618,11 +618,13 @@ size_t even_smem(const Shape &s, int64_t grid, int sms) {
   return grid > sms && grid % sms == 0 ? std::max<size_t>(s.smem, (228 << 10) / (grid / sms + 1)) : s.smem;
 }
 
+constexpr int kMostSmem = 224 << 10;  // a block's, beside what the kernels hold for their sums
+
 template <typename K, typename... A>
 cudaError_t launch_rows(K kernel, const Shape &s, int64_t grid, int sms, cudaStream_t st, const A &...args) {
   const size_t smem = even_smem(s, grid, sms);
-  if (smem > 40 << 10) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 40 << 10) {  // (one limit for all lengths: calls of other threads, or a graph's, may lie between)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
     if (e != cudaSuccess) return e;
   }
   return launch_early(kernel, dim3((unsigned)grid), dim3(s.x, s.y), smem, st, args...);

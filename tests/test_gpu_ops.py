@@ -717,3 +717,24 @@ def test_layer_norm_grad_far_from_zero(echo, h):
     _close(dx, r * (g - m1 - xh * m2), r * (12 * U * (g.abs() + m1.abs() + (xh * m2).abs()) + e1 + xh.abs() * e2), F32)
     _close(dw, (dy * xh).sum(0), (rows + 8) * U * (dy * xh).abs().sum(0), F32)
     _close(db, dy.double().sum(0), (rows + 4) * U * dy.double().abs().sum(0), F32)
+
+
+def test_captured_lengths_stay_launchable():
+    """A shorter row's call between a longer one's capture and the graph's start takes none of
+    the shared memory that the longer one asked for."""
+    side = torch.cuda.Stream()
+    xs = [_randn((400, h), 150 + h) for h in (12288, 5000)]  # slots of 48 KB and of 20 KB
+    with Echo(0, stream=side) as e, torch.cuda.stream(side):
+        def step():
+            outs = [e.layer_norm(x) for x in xs]
+            return [o[0] for o in outs] + [e.layer_norm_grad(o[0], x, o[1], o[2])[0] for o, x in zip(outs, xs)]
+
+        want = step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step()
+        graph.replay()
+        side.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
