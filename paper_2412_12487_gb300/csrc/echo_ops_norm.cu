@@ -581,8 +581,8 @@ int row_threads(int64_t H, int E) { return (int)std::min<int64_t>(1024, (H + 32 
 
 constexpr int64_t kCached = 768 * 16;  // longest rows of the one-pass kernels
 // Elements of a row that a thread takes.  With 16 a row's sums and addresses take fewer
-// instructions (forward, 16384 x 2048 in bf16: 34 us, 38 with 8); backward, more warps are worth
-// more up to 256 threads a row (8192 x 1024 in fp32: 25 us with 8, 32 with 16).
+// instructions (forward, 16384 x 2048 in bf16: 27 us, 31 with 8); backward, more warps are worth
+// more up to 256 threads a row (8192 x 1024 in fp32: 22 us with 8, 28 with 16).
 int row_elements(int64_t H, int arrays) { return H <= (arrays == 2 ? 2048 : 256) ? 8 : 16; }
 
 // Shape of a one-pass kernel for rows of H elements, `arrays` of them read: threads of a row,
