@@ -8,11 +8,10 @@
 // order too (MN-major).  Y is all that a step keeps.  The symmetric products compute the tiles
 // that reach the lower triangle and write each block to both places.
 //
-// Elements are fp16 numbers times a power of two (the iterate's singular values stay near 1,
-// so its elements are at most that): one for bf16 matrices, the sum of two for fp32 and fp16
-// ones (22 bits), multiplied as high * high + high * low + low * high with sums in fp32.  One
-// fp16 number for bf16 matrices leaves the result 2.2e-3 off, of which the rounding to bf16 is
-// 1.7e-3; two take three times the products.
+// Elements are sums of two fp16 numbers times a power of two (the iterate's singular values stay
+// near 1, so its elements are at most that): 22 bits, whatever the matrices' type, multiplied as
+// high * high + high * low + low * high with sums in fp32.  One number an element takes a third
+// of the products, but leaves a bf16 result 2.1e-3 off, 1.7e-3 of which is its own rounding.
 #include <cuda.h>
 
 #include <algorithm>
@@ -112,21 +111,21 @@ __device__ __forceinline__ Factor inverse_norm(const float *part, int parts, int
 }
 
 // -- matrices of the iteration --------------------------------------------------------------------
-// [plane][batch][rows][ld] fp16; plane 1 (fp32 matrices) is what plane 0 leaves of an element.
+// [plane][batch][rows][ld] fp16; plane 1 is what plane 0 leaves of an element.
+constexpr int kPlanes = 2;
 struct Planes {
   __half *p;
   int64_t ld, matrix, plane;  // elements of a row, of a matrix, of a plane
 };
 
-template <int PLANES>
-__device__ __forceinline__ void split(float v, __half (&h)[PLANES]) {
+__device__ __forceinline__ void split(float v, __half (&h)[kPlanes]) {
   h[0] = __float2half_rn(v);
-  if constexpr (PLANES == 2) h[1] = __float2half_rn(v - __half2float(h[0]));
+  h[1] = __float2half_rn(v - __half2float(h[0]));
 }
 
 // Y = G / (|G| + eps), in pieces of W elements, four of them in flight a thread.  Bound by latency
 // while G and Y fit L2, behind the norm: 6 x 2048 x 1024 in bf16, 5.0e7 bytes, 20 us by itself.
-template <typename T, int PLANES, int W>
+template <typename T, int W>
 __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
   __shared__ Factor factor;
   kernel_begin();
@@ -164,12 +163,12 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t r
 #pragma unroll
         for (int i = 0; i < W; ++i) v[k][i] = f(v[k][i]);
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q) {
+        for (int q = 0; q < kPlanes; ++q) {
           Pack<__half, W> h;
 #pragma unroll
           for (int i = 0; i < W; ++i) {
             h.v[i] = __float2half_rn(v[k][i]);
-            if constexpr (PLANES == 2) v[k][i] -= __half2float(h.v[i]);  // what the next plane holds
+            v[k][i] -= __half2float(h.v[i]);  // what the next plane holds
           }
           *reinterpret_cast<Pack<__half, W> *>(to + q * y.plane + at[k]) = h;
         }
@@ -183,7 +182,7 @@ __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t r
 // Y = G^T / (|G| + eps).  A block takes 64 x 64 tiles, in bands of 16 rows of tiles, column by
 // column, so that the tiles in work at a time make long runs in G and in Y.  Bound by the bytes:
 // 2048 x 8192 in fp32, 1.3e8 bytes, 27 us, 4.9 TB/s.
-template <typename T, int PLANES>
+template <typename T>
 __global__ void __launch_bounds__(256) ortho_start_turned_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
   __shared__ Factor factor;
   __shared__ float tile[64][65];
@@ -219,11 +218,11 @@ __global__ void __launch_bounds__(256) ortho_start_turned_kernel(OrthoArgs a, in
       for (int i = 0; i < 8; ++i) {
         const int64_t c = c0 + ty + 8 * i, r = r0 + 2 * tx;  // two elements of a row of Y: the padding takes an odd end
         if (c >= cols || r >= rows) continue;
-        __half h[2][PLANES];
-        split<PLANES>(tile[2 * tx][ty + 8 * i], h[0]);
-        split<PLANES>(tile[2 * tx + 1][ty + 8 * i], h[1]);
+        __half h[2][kPlanes];
+        split(tile[2 * tx][ty + 8 * i], h[0]);
+        split(tile[2 * tx + 1][ty + 8 * i], h[1]);
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q)
+        for (int q = 0; q < kPlanes; ++q)
           *reinterpret_cast<__half2 *>(y.p + q * y.plane + z * y.matrix + c * y.ld + r) = __halves2half2(h[0][q], h[1][q]);
       }
       __syncthreads();
@@ -266,27 +265,25 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t r
 // adds the parts, in their order, and finishes the tile.  Nobody waits for another block.
 //
 // The tensor core adds to its fp32 sums with truncation, which is a bias: with one set of sums
-// for 12288 columns of two-number operands (2304 additions an element) the result was 8e-5 off.
-// So for them a set covers one stage, the products of the low parts first, while the sums are
-// small, and the eight warps add the sets up in registers, rounding to nearest, while the next
-// set is summed: 7e-7 off there, and 6% more clocks than with sets of eight stages.
+// for 12288 columns (2304 additions an element) the result was 8e-5 off.  So a set covers one
+// stage, the products of the low parts first, while the sums are small, and the eight warps add
+// the sets up in registers, rounding to nearest, while the next set is summed: 7e-7 off there,
+// and 6% more clocks than with sets of eight stages.
 //
 // Large matrices are bound by the tensor cores: 4608 x 12288 in fp32, five steps, 1.3e13
 // operations on fp16 numbers, 8.7 to 9.0 ms, 1.5 PFLOP/s.  Small ones are bound by the operands'
 // way from L2 and by what a launch waits for (fill, drain, a round that is not full): 6 matrices
-// of 2048 x 1024 in bf16, 2.3e11 operations, 325 us, 0.7 PFLOP/s; 1003 x 517 in fp32 15 us a product.
+// of 2048 x 1024, 6.9e11 operations, 785 us, 0.9 PFLOP/s; 1003 x 517 14 to 15 us a product.
 constexpr int kBM = 256, kBK = 64, kRows = 128;  // of a tile, of a stage; rows of P a block holds
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 // Registers of a thread of warps 0-3 and of 4-11, which hold 128 sums each; together no more
 // than the 168 a thread that the block is launched with (65536 / 384, in units of 8).
 constexpr int kFewRegs = 56, kManyRegs = 216;
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
-constexpr int stage_bytes(int planes, int bn) { return planes * (kRows + bn / 2) * kBK * 2; }
-constexpr int stages(int planes, int bn) { return 196608 / stage_bytes(planes, bn); }
+constexpr int stage_bytes(int bn) { return kPlanes * (kRows + bn / 2) * kBK * 2; }
+constexpr int stages(int bn) { return 196608 / stage_bytes(bn); }
 constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out: 32 x 32 elements, twice
-constexpr size_t smem_bytes(int planes, int bn) {
-  return (size_t)stages(planes, bn) * stage_bytes(planes, bn) + 8 * kOutBytes + 256 + 1024;
-}
+constexpr size_t smem_bytes(int bn) { return (size_t)stages(bn) * stage_bytes(bn) + 8 * kOutBytes + 256 + 1024; }
 
 struct ProductArgs {
   int64_t batch;
@@ -300,7 +297,6 @@ struct ProductArgs {
   int symmetric;        // D is symmetric: tiles of the lower triangle, each element written twice
   float alpha, beta;
   Planes c;             // C (p may be null)
-  float diagonal;       // added to D's diagonal (symmetric)
   void *o;              // the last product: the result instead of D
   int64_t o_stride, o_batch_stride;
   int o_transposed;
@@ -474,17 +470,16 @@ __device__ __forceinline__ void half_written() {
 //
 // By the copy engine: the tensor core's reads of the stages nearly fill shared memory's
 // bandwidth, and every pass through it that the warps do themselves waits for a gap.
-template <int PLANES>
 __device__ __forceinline__ void block_out(const ProductArgs &a, const CUtensorMap *dmap, const CUtensorMap *tmap, int z, int row0, int c, int lane,
                                           float (&v)[32], unsigned char *buffer, uint32_t &turn) {
   if (a.symmetric && c > row0) return;
 #pragma unroll 1
-  for (int q = 0; q < PLANES; ++q) {
+  for (int q = 0; q < kPlanes; ++q) {
     Piece h[4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       h[i / 8].v[i % 8] = __float2half_rn(v[i]);
-      if constexpr (PLANES == 2) v[i] -= __half2float(h[i / 8].v[i % 8]);  // what the next plane holds
+      v[i] -= __half2float(h[i / 8].v[i % 8]);  // what the next plane holds
     }
     half_free(lane);
 #pragma unroll
@@ -531,11 +526,11 @@ __device__ __forceinline__ void result_out(const ProductArgs &a, int64_t z, int 
 }
 
 // OUT: void for a product whose result goes on in planes, else the type of the result.
-template <int PLANES, int BN, bool MN, typename OUT>
+template <int BN, bool MN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     ortho_product_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap dmap,
                          const __grid_constant__ CUtensorMap tmap, const __grid_constant__ ProductArgs a) {
-  constexpr int S = stages(PLANES, BN), kStage = stage_bytes(PLANES, BN), kP = kRows * kBK * 2, kQ = BN / 2 * kBK * 2, kCols = BN / 2;
+  constexpr int S = stages(BN), kStage = stage_bytes(BN), kP = kRows * kBK * 2, kQ = BN / 2 * kBK * 2, kCols = BN / 2;
   extern __shared__ unsigned char raw[];
   unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
   unsigned char *buffers = base + S * kStage;
@@ -577,7 +572,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   kernel_begin();
   next_may_start();
   const int64_t all = a.whole + (a.tiles * a.batch - a.whole) * a.split;
-  const int steps = (a.K + kBK - 1) / kBK, chunk = PLANES == 2 ? 1 : steps;  // stages of a set of sums
+  const int steps = (a.K + kBK - 1) / kBK;  // stages: each has a set of sums
 
   // Piece of work i: tile t (of the batch), stages k0 to k1 of its sum.
   auto work_at = [&](int64_t i, int64_t &t, int &part, int &k0, int &k1) {
@@ -607,9 +602,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const uint32_t at = ring + s * kStage, bar = in_first(full + 8 * s);
           if (rank == 0) bar_expect(full + 8 * s, 2 * kStage);  // both blocks' copies
 #pragma unroll
-          for (int q = 0; q < PLANES; ++q) {
+          for (int q = 0; q < kPlanes; ++q) {
             copy_operand<MN, kRows>(at + q * kP, &pmap, r0 + rank * kRows, k * kBK, z, q, bar);
-            copy_operand<MN, kCols>(at + PLANES * kP + q * kQ, &qmap, c0 + rank * kCols, k * kBK, z, q, bar);
+            copy_operand<MN, kCols>(at + kPlanes * kP + q * kQ, &qmap, c0 + rank * kCols, k * kBK, z, q, bar);
           }
         }
       }
@@ -619,37 +614,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
     } else if (warp == 1 && lane == 0 && rank == 0) {
-      int64_t it = 0, n = 0;
+      int64_t it = 0;
       bool ok = true;
       for (int64_t i = pair; i < all && ok; i += pairs) {
         int64_t t;
         int part, begin, end;
         work_at(i, t, part, begin, end);
-        for (int k0 = begin; k0 < end && ok; k0 += chunk, ++n) {
-          const int b = (int)(n & 1);
-          ok = bar_wait(sums_empty + 8 * b, (uint32_t)(n / 2 + 1) & 1, abort, a);
+        for (int k = begin; k < end; ++k, ++it) {
+          const int b = (int)(it & 1), s = (int)(it % S);
+          ok = bar_wait(sums_empty + 8 * b, (uint32_t)(it / 2 + 1) & 1, abort, a) && bar_wait(full + 8 * s, (uint32_t)(it / S) & 1, abort, a);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           const uint32_t d = tmem + b * BN;
-          for (int k = k0; k < min(end, k0 + chunk); ++k, ++it) {
-            const int s = (int)(it % S);
-            ok = bar_wait(full + 8 * s, (uint32_t)(it / S) & 1, abort, a);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            const uint64_t p = operand<MN>(ring + s * kStage), q = operand<MN>(ring + s * kStage + PLANES * kP);
-            constexpr uint32_t kInstr = instruction(BN, MN);
-            if constexpr (PLANES == 2) {
+          const uint64_t p = operand<MN>(ring + s * kStage), q = operand<MN>(ring + s * kStage + kPlanes * kP);
+          constexpr uint32_t kInstr = instruction(BN, MN);
 #pragma unroll
-              for (int kk = 0; kk < kBK / 16; ++kk) {
-                mma(d, p + step16(MN) * kk, q + step16(MN) * kk + (kQ >> 4), kInstr, k > k0 || kk > 0);
-                mma(d, p + step16(MN) * kk + (kP >> 4), q + step16(MN) * kk, kInstr, true);
-              }
-            }
-#pragma unroll
-            for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(MN) * kk, q + step16(MN) * kk, kInstr, PLANES == 2 || k > k0 || kk > 0);
-            commit_pair(empty + 8 * s);
+          for (int kk = 0; kk < kBK / 16; ++kk) {
+            mma(d, p + step16(MN) * kk, q + step16(MN) * kk + (kQ >> 4), kInstr, kk > 0);
+            mma(d, p + step16(MN) * kk + (kP >> 4), q + step16(MN) * kk, kInstr, true);
           }
-          if (ok) commit_pair(sums_full + 8 * b);
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(MN) * kk, q + step16(MN) * kk, kInstr, true);
+          commit_pair(empty + 8 * s);
+          commit_pair(sums_full + 8 * b);
         }
       }
       commit(done);  // nothing is in flight when the block ends
@@ -678,7 +665,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const __half *from_c = a.c.p + z * a.c.matrix;
       if (add_c && row0 + lane < a.M) {  // C's part of the tile comes to L2 during the sums
 #pragma unroll
-        for (int q = 0; q < PLANES; ++q)
+        for (int q = 0; q < kPlanes; ++q)
 #pragma unroll
           for (int i = 0; i < kCols; i += 64)
             if (c0 + i < a.N) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(from_c + q * a.c.plane + (int64_t)(row0 + lane) * a.c.ld + c0 + i));
@@ -688,14 +675,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // piece comes one turn ahead, four lanes to the 64 bytes of a row, and changes to a row a lane
       // in the warp's buffer.
       constexpr int kFlight = MN ? 2 : 1;
-      constexpr int kParts = kCols / 32, kPieces = MN ? 0 : PLANES * kParts;
-      const int sets = (end - begin + chunk - 1) / chunk;
+      constexpr int kParts = kCols / 32, kPieces = MN ? 0 : kPlanes * kParts;
+      const int sets = end - begin;
       const bool c_before = add_c && sets <= 2 * kPieces;
       const int set0 = c_before ? kPieces + 1 : 0, first_c = c_before ? 0 : add_c ? sets - kPieces - 1 : sets;  // turns
       Piece ahead[4] = {};
       auto fetch = [&](int u) {
-        const int row = row0 + (lane >> 2), col = c0 + u / PLANES * 32 + (lane & 3) * 8;
-        const __half *p = from_c + (int64_t)row * a.c.ld + col + u % PLANES * a.c.plane;
+        const int row = row0 + (lane >> 2), col = c0 + u / kPlanes * 32 + (lane & 3) * 8;
+        const __half *p = from_c + (int64_t)row * a.c.ld + col + u % kPlanes * a.c.plane;
 #pragma unroll
         for (int i = 0; i < 4; ++i)  // (to the end of a piece: within the padding of the row)
           if (row + 8 * i < a.M && col < a.N) ahead[i] = *reinterpret_cast<const Piece *>(p + (int64_t)(8 * i) * a.c.ld);
@@ -735,7 +722,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           __syncwarp();
           auto add = [&](auto which) {
             constexpr int part = decltype(which)::value;
-            if (part != u / PLANES) return;
+            if (part != u / kPlanes) return;
             asm volatile("" ::"n"(part));  // (keeps the blocks apart: as one, they would index the sums in memory)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -798,12 +785,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       float (&v)[32] = acc[0];
 #pragma unroll 1
       for (int c = c0; c < min(a.N, c0 + kCols); c += 32) {
-        if (a.symmetric && c == row0) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] += i == lane ? a.diagonal : 0.f;
-        }
         if constexpr (std::is_void_v<OUT>)
-          block_out<PLANES>(a, &dmap, &tmap, z, row0, c, lane, v, buffer, turn);
+          block_out(a, &dmap, &tmap, z, row0, c, lane, v, buffer, turn);
         else
           result_out<OUT>(a, z, row0, c, lane, v, buffer);
 #pragma unroll
@@ -840,10 +823,10 @@ EncodeTiled encoder() {
 }
 
 // Boxes of a matrix of the iteration; zeros outside it.
-cudaError_t box_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows, int box_cols,
+cudaError_t box_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int box_rows, int box_cols,
                     CUtensorMapSwizzle swizzle) {
   if (!encoder()) return cudaErrorNotSupported;
-  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)planes};
+  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)kPlanes};
   const cuuint64_t strides[3] = {(cuuint64_t)p.ld * 2, (cuuint64_t)p.matrix * 2, (cuuint64_t)p.plane * 2};
   const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
   return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p.p, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
@@ -852,21 +835,20 @@ cudaError_t box_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t col
              : cudaErrorInvalidValue;
 }
 // 64 columns, for the stages; 32 x 32 for a warp's buffer
-cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, int box_rows) {
-  return box_map(map, p, rows, cols, batch, planes, box_rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+cudaError_t tile_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int box_rows) {
+  return box_map(map, p, rows, cols, batch, box_rows, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-cudaError_t out_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, int planes, bool exchanged) {
-  return box_map(map, p, rows, cols, batch, planes, 32, 32, exchanged ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE);
+cudaError_t out_map(CUtensorMap *map, const Planes &p, int64_t rows, int64_t cols, int64_t batch, bool exchanged) {
+  return box_map(map, p, rows, cols, batch, 32, 32, exchanged ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 int64_t padded(int64_t x) { return (x + 63) / 64 * 64; }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-Planes planes_of(char *&at, int64_t rows, int64_t cols, int64_t batch, int planes) {
+Planes planes_of(char *&at, int64_t rows, int64_t cols, int64_t batch) {
   Planes p{reinterpret_cast<__half *>(at), padded(cols), rows * padded(cols), batch * rows * padded(cols)};
-  at += up256((size_t)planes * p.plane * sizeof(__half));
+  at += up256((size_t)kPlanes * p.plane * sizeof(__half));
   return p;
 }
-int planes_for(int type) { return type == ECHO_BF16 ? 1 : 2; }
 
 }  // namespace
 
@@ -875,21 +857,20 @@ int norm_parts(const OrthoArgs &a) { return (int)std::clamp<int64_t>(a.m * a.n /
 
 // How a product goes: the width of its tiles and the tiles that are split, with the smallest
 // estimate of its clocks.  A stage takes 1536 clocks of products at 256 columns, 1080 at 128 (the
-// operands' reads from shared memory bound it), 690 and 565 where the operands are one number an
-// element (L2 bounds both); joining parts takes about 6000 and, for each part, what 256 or 128 KB
-// of a pair's sums take to L2 and back.
+// operands' reads from shared memory bound it); joining parts takes about 6000 and, for each part,
+// what 256 or 128 KB of a pair's sums take to L2 and back.
 struct Plan {
   int bn;
   int64_t tiles, whole;
   int split;
 };
-Plan plan_product(int64_t M, int64_t N, int64_t K, bool symmetric, int64_t batch, int planes, int pairs) {
+Plan plan_product(int64_t M, int64_t N, int64_t K, bool symmetric, int64_t batch, int pairs) {
   Plan best{};
   double least = 0;
   for (const int bn : {256, 128}) {
     const int64_t tm = (M + kBM - 1) / kBM, tiles = symmetric ? kBM / bn * tm * (tm + 1) / 2 : tm * ((N + bn - 1) / bn);
     const int64_t all = tiles * batch, rest = all % pairs, steps = (K + kBK - 1) / kBK;
-    const double stage = planes == 2 ? (bn == 256 ? 1536 : 1080) : (bn == 256 ? 690 : 565), join = bn == 256 ? 3000 : 1500;
+    const double stage = bn == 256 ? 1536 : 1080, join = bn == 256 ? 3000 : 1500;
     int split = 1;
     double round = rest ? stage * steps : 0;
     for (int64_t p = 2; rest && p <= std::min(pairs / rest, steps); ++p) {
@@ -902,7 +883,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, bool symmetric, int64_t batch
   return best;
 }
 Plan plan_of(const OrthoArgs &a, int product, int sms) {  // A, B, Y
-  return plan_product(product < 2 ? a.m : a.n, a.m, product == 0 ? a.n : a.m, product < 2, a.batch, planes_for(a.type), sms / 2);
+  return plan_product(product < 2 ? a.m : a.n, a.m, product == 0 ? a.n : a.m, product < 2, a.batch, sms / 2);
 }
 
 // parts of the norm; counts and sums of split tiles; Y twice (a product reads one while it
@@ -917,15 +898,14 @@ size_t parts_bytes(const OrthoArgs &a, int sms) {
 }
 size_t ortho_scratch_bytes(const OrthoArgs &a, int sms) {
   char *at = nullptr;
-  const int planes = planes_for(a.type);
-  for (int i = 0; i < 2; ++i) planes_of(at, a.n, a.m, a.batch, planes);
-  for (int i = 0; i < 2; ++i) planes_of(at, a.m, a.m, a.batch, planes);
+  for (int i = 0; i < 2; ++i) planes_of(at, a.n, a.m, a.batch);
+  for (int i = 0; i < 2; ++i) planes_of(at, a.m, a.m, a.batch);
   return (a.steps ? reinterpret_cast<uintptr_t>(at) + up256((size_t)sms * 8 * sizeof(int32_t)) + parts_bytes(a, sms) : 0) +
          up256((size_t)a.batch * norm_parts(a) * 3 * sizeof(float));
 }
 
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
-  const int planes = planes_for(a.type), parts = norm_parts(a);
+  const int parts = norm_parts(a);
   char *at = static_cast<char *>(a.scratch);
   float *part = reinterpret_cast<float *>(at);
   at += up256((size_t)a.batch * parts * 3 * sizeof(float));
@@ -955,19 +935,19 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   at += up256((size_t)sms * 8 * sizeof(int32_t));
   float4 *split_parts = reinterpret_cast<float4 *>(at);
   at += parts_bytes(a, sms);
-  const Planes Y[2] = {planes_of(at, a.n, a.m, a.batch, planes), planes_of(at, a.n, a.m, a.batch, planes)};
-  const Planes A = planes_of(at, a.m, a.m, a.batch, planes), B = planes_of(at, a.m, a.m, a.batch, planes);
+  const Planes Y[2] = {planes_of(at, a.n, a.m, a.batch), planes_of(at, a.n, a.m, a.batch)};
+  const Planes A = planes_of(at, a.m, a.m, a.batch), B = planes_of(at, a.m, a.m, a.batch);
   e = timed("ortho_start", [&] {
     return with_type(a.type, [&](auto t) {
       using T = decltype(t);
-      constexpr int P = std::is_same_v<T, __nv_bfloat16> ? 1 : 2, N = 16 / sizeof(T);
+      constexpr int N = 16 / sizeof(T);
       const int64_t room = std::max<int64_t>(1, sms * 6 / gz);
       auto grid = [&](int64_t want) { return dim3((unsigned)std::min(want, room), gz); };
       if (!a.tall)
-        return launch_early(ortho_start_turned_kernel<T, P>, grid((rows + 63) / 64 * ((cols + 63) / 64)), 256, 0, st, a, rows, cols, part, parts, Y[0]);
+        return launch_early(ortho_start_turned_kernel<T>, grid((rows + 63) / 64 * ((cols + 63) / 64)), 256, 0, st, a, rows, cols, part, parts, Y[0]);
       if (cols % N == 0 && fits_pieces(a.g, a.g_stride, a.type, N) && fits_pieces(a.g, a.g_batch_stride, a.type, N))
-        return launch_early(ortho_start_kernel<T, P, N>, grid((rows * cols / N + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
-      return launch_early(ortho_start_kernel<T, P, 1>, grid((rows * cols + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
+        return launch_early(ortho_start_kernel<T, N>, grid((rows * cols / N + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
+      return launch_early(ortho_start_kernel<T, 1>, grid((rows * cols + 1023) / 1024), 256, 0, st, a, rows, cols, part, parts, Y[0]);
     });
   });
   if (e != cudaSuccess) return e;
@@ -979,38 +959,38 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
   const Matrix y[2] = {{Y[0], a.n, a.m}, {Y[1], a.n, a.m}}, sa{A, a.m, a.m}, sb{B, a.m, a.m};
   // D = alpha P Q^T + beta C (mn: P and Q hold the transposes); the result without a D.  D is
   // symmetric where P is Q.
-  auto product = [&](int which, const char *name, const Matrix &p, const Matrix &q, bool mn, float alpha, const Planes *c, float beta, float diagonal, const Matrix *d) -> cudaError_t {
+  auto product = [&](int which, const char *name, const Matrix &p, const Matrix &q, bool mn, float alpha, const Planes *c, float beta, const Matrix *d) -> cudaError_t {
     ProductArgs g{};
     const bool symmetric = &p == &q;
     const Plan plan = plan_of(a, which, sms);
     g.batch = a.batch, g.M = (int)(mn ? p.cols : p.rows), g.N = (int)(mn ? q.cols : q.rows), g.K = (int)(mn ? p.rows : p.cols);
     g.symmetric = symmetric;
-    g.alpha = alpha, g.beta = beta, g.diagonal = diagonal;
+    g.alpha = alpha, g.beta = beta;
     if (c) g.c = *c;
     g.o = a.o, g.o_stride = a.o_stride, g.o_batch_stride = a.o_batch_stride, g.o_transposed = !a.tall;
     g.status = a.status, g.wait_limit = a.wait_limit, g.skip = a.skip;
-    auto go = [&](auto planes_c, auto cols_c, auto mn_c, auto out) -> cudaError_t {
-      constexpr int P = decltype(planes_c)::value, BN = decltype(cols_c)::value;
+    auto go = [&](auto cols_c, auto mn_c, auto out) -> cudaError_t {
+      constexpr int BN = decltype(cols_c)::value;
       constexpr bool MN = decltype(mn_c)::value;
       using O = std::remove_pointer_t<decltype(out)>;
       g.tiles_n = (int)((g.N + BN - 1) / BN);
       g.tiles = plan.tiles, g.whole = plan.whole, g.split = plan.split, g.parts = split_parts, g.arrived = arrived;
       CUtensorMap pm, qm, dm{}, tm{};
-      cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, planes, MN ? kBK : kRows);
-      if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, planes, MN ? kBK : BN / 2);
-      if (r == cudaSuccess && d) r = out_map(&dm, d->p, d->rows, d->cols, a.batch, planes, true);
-      if (r == cudaSuccess && d && symmetric) r = out_map(&tm, d->p, d->rows, d->cols, a.batch, planes, false);
-      auto kernel = ortho_product_kernel<P, BN, MN, O>;
-      if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(P, BN));
+      cudaError_t r = tile_map(&pm, p.p, p.rows, p.cols, a.batch, MN ? kBK : kRows);
+      if (r == cudaSuccess) r = tile_map(&qm, q.p, q.rows, q.cols, a.batch, MN ? kBK : BN / 2);
+      if (r == cudaSuccess && d) r = out_map(&dm, d->p, d->rows, d->cols, a.batch, true);
+      if (r == cudaSuccess && d && symmetric) r = out_map(&tm, d->p, d->rows, d->cols, a.batch, false);
+      auto kernel = ortho_product_kernel<BN, MN, O>;
+      if (r == cudaSuccess) r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(BN));
       if (r != cudaSuccess) return r;
-      return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.whole + (g.tiles * g.batch - g.whole) * g.split, pairs) * 2), kThreads, smem_bytes(P, BN), st, pm, qm, dm, tm, g);
+      return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.whole + (g.tiles * g.batch - g.whole) * g.split, pairs) * 2), kThreads, smem_bytes(BN), st, pm, qm, dm, tm, g);
     };
     auto with_out = [&](auto cols_c) -> cudaError_t {
-      if (mn) return planes == 2 ? go(Int<2>{}, cols_c, Int<1>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<1>{}, (void *)nullptr);
-      if (d) return planes == 2 ? go(Int<2>{}, cols_c, Int<0>{}, (void *)nullptr) : go(Int<1>{}, cols_c, Int<0>{}, (void *)nullptr);
-      return a.type == ECHO_F32 ? go(Int<2>{}, cols_c, Int<0>{}, (float *)nullptr)
-             : a.type == ECHO_BF16 ? go(Int<1>{}, cols_c, Int<0>{}, (__nv_bfloat16 *)nullptr)
-                                   : go(Int<2>{}, cols_c, Int<0>{}, (__half *)nullptr);
+      if (mn) return go(cols_c, Int<1>{}, (void *)nullptr);
+      if (d) return go(cols_c, Int<0>{}, (void *)nullptr);
+      return a.type == ECHO_F32 ? go(cols_c, Int<0>{}, (float *)nullptr)
+             : a.type == ECHO_BF16 ? go(cols_c, Int<0>{}, (__nv_bfloat16 *)nullptr)
+                                   : go(cols_c, Int<0>{}, (__half *)nullptr);
     };
     return timed(name, [&] { return plan.bn == 128 ? with_out(Int<128>{}) : with_out(Int<256>{}); });
   };
@@ -1018,15 +998,11 @@ cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &tim
     const Matrix &now = y[s & 1], &next = y[(s + 1) & 1];
     const bool last = s == a.steps - 1;
     const float out = last ? a.scale / kScaleY : 1.f;
-    if ((e = product(0, "ortho_yty", now, now, true, kScaleA / (kScaleY * kScaleY), nullptr, 0.f, 0.f, &sa)) != cudaSuccess) return e;
-    // a Y comes from B + a I for matrices of one number an element: the last product then reads
-    // and adds nothing.  With two numbers the larger sums would lose more to truncation than the
-    // sum of a Y and Y B in fp32 does (2.7e-6 instead of 1.0e-6 at 300 x 300).
-    const bool fold = planes == 1;
-    if ((e = product(1, "ortho_aa", sa, sa, false, a.c * (kScaleB / (kScaleA * kScaleA)), &A, a.b * (kScaleB / kScaleA), fold ? a.a * kScaleB : 0.f, &sb)) !=
-        cudaSuccess)
-      return e;
-    if ((e = product(2, "ortho_yb", now, sb, false, out / kScaleB, fold ? nullptr : &now.p, out * a.a, 0.f, last ? nullptr : &next)) != cudaSuccess) return e;
+    if ((e = product(0, "ortho_yty", now, now, true, kScaleA / (kScaleY * kScaleY), nullptr, 0.f, &sa)) != cudaSuccess) return e;
+    if ((e = product(1, "ortho_aa", sa, sa, false, a.c * (kScaleB / (kScaleA * kScaleA)), &A, a.b * (kScaleB / kScaleA), &sb)) != cudaSuccess) return e;
+    // (a Y is added to the sums in fp32: as a on B's diagonal it would cost nothing to add, but the
+    // larger sums lose more to truncation, 2.7e-6 instead of 1.0e-6 at 300 x 300)
+    if ((e = product(2, "ortho_yb", now, sb, false, out / kScaleB, &now.p, out * a.a, last ? nullptr : &next)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }

@@ -1,0 +1,80 @@
+"""Operators of a training step at the ends of what their interface promises.
+
+Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roundoff, uo the output type's.
+
+* Newton-Schulz: an iterate's elements are sums of two fp16 numbers whatever the matrix's type, so e = 2^-22; a step
+  multiplies an error by at most 3.9 while the iterate grows by up to 3.44, and five steps stay within 100 e of the result's
+  norm (1210 e for an iterate of rank one, which starts at its final norm: the sum of 3.9^k).  A row's or a column's error is
+  part of the matrix's.  Rounding the output adds uo of each element.
+* A 16-bit result is the rounded exact one but where an error d moves an element across a boundary between two roundings.
+  Boundaries lie at least uo |w| apart, so that happens to a share min(1, d / (uo |w|)) of elements w; for d = 100 e times their
+  root mean square and normally distributed w the mean of it is 0.8 r (1 - log r), r = 100 e / uo: 3% for bf16 and 16% for fp16.
+"""
+
+import pytest
+
+from paper_2412_12487_gb300 import Echo
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+UO = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(scope="module")
+def echo():
+    with Echo(0) as e:
+        yield e
+
+
+def _randn(shape, seed, dtype=F32):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(dtype)
+
+
+def _ortho_ref(g, steps=5, coef=QUINTIC, eps=0.0):
+    a, b, c = (torch.tensor(v, dtype=F32).double().item() for v in coef)
+    x = g.double()
+    x = x / (x.flatten(-2).norm(dim=-1)[..., None, None] + torch.tensor(eps, dtype=F32).double().item())
+    tall = x.shape[-2] > x.shape[-1]
+    x = x.mT if tall else x
+    for _ in range(steps):
+        q = x @ x.mT
+        x = a * x + (b * q + c * q @ q) @ x
+    return x.mT if tall else x
+
+
+def _ortho_close(got, want, gain=100.0):
+    """Every row and column of every matrix, by norm."""
+    uo = UO[got.dtype]
+    got, want = (t.double().reshape(-1, *t.shape[-2:]) for t in (got, want))
+    assert torch.isfinite(got).all()
+    tol = gain * 2.0 ** -22 * want.flatten(1).norm(dim=1)[:, None]
+    for dim in (1, 2):
+        off = (got - want).norm(dim=dim) - (uo * want.norm(dim=dim) + tol * (1 + uo))
+        assert float(off.max()) <= 0, float(off.max())
+    assert ((got - want).flatten(1).norm(dim=1) <= uo * want.flatten(1).norm(dim=1) + tol[:, 0] * (1 + uo)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shape", [(513, 512), (300, 1000), (1000, 300), (5, 384, 256), (129, 127), (2, 2048, 1024), (40, 3000), (1003, 517)])
+def test_orthogonalize_16_bit_results_are_the_rounded_ones(echo, dtype, shape):
+    g = _randn(shape, 1, dtype)
+    got, want = echo.orthogonalize(g, eps=0.0), _ortho_ref(g)
+    _ortho_close(got, want)
+    moved = float((got != want.to(dtype)).double().mean())
+    assert moved <= {BF16: 0.05, F16: 0.25}[dtype], moved
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_orthogonalize_rows_and_columns(echo, dtype):
+    """Matrices at the edges of tiles, split sums, one row or column: nothing missing at an edge."""
+    for k, shape in enumerate([(1, 7), (2, 33), (33, 2000), (255, 257), (256, 256), (257, 255), (3, 128, 300), (300, 5000), (2500, 2600), (700, 64)]):
+        g = _randn(shape, 10 + k, dtype)
+        _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), 1210 if shape[0] <= 2 else 100)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_orthogonalize_low_rank(echo, dtype):
+    g = torch.outer(_randn((70,), 30), _randn((300,), 31)).to(dtype)
+    _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), gain=1210)
