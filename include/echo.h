@@ -357,8 +357,12 @@ int echo_measure_fp64(int device, double *rates);
  *     multiple of its element size.  Matrices are rows of contiguous elements, `stride`
  *     elements apart: at least the row's length for outputs, any value >= 0 for inputs.
  *   - Work is enqueued on the context's stream and is not waited for.  Scratch memory
- *     belongs to the context and grows on the first call of a size (that call allocates,
- *     so make it before a stream capture); calls on one context share it in stream order.
+ *     belongs to the context and grows on the first call of a size; calls on one context
+ *     share it in stream order.
+ *   - Calls can be captured into a graph, each size after a first call outside the capture
+ *     (ECHO_E_STATE where one would have to allocate).  The graph uses the scratch that the
+ *     context had then, which is kept until echo_destroy whatever larger calls follow: its
+ *     launches have to be ordered with the context's stream, and end before echo_destroy.
  *   - They need no graph or scenarios and leave those of the context as they are.
  *   - Outputs overlap no other array, except where a call says so.
  *   - Sums, statistics and products accumulate in fp32; results are rounded once, to the

@@ -1584,6 +1584,8 @@ struct echo_ctx {
   // scratch of the operators (echo_ops.cpp)
   void *ops = nullptr;
   size_t ops_bytes = 0;
+  bool ops_captured = false;      // a captured graph may hold its address
+  std::vector<void *> ops_kept;   // outgrown, but captured: freed with the context
   int32_t *ops_status = nullptr;  // host memory: set by a kernel whose wait gave up
   // profiling
   bool prof = false;
@@ -1892,8 +1894,21 @@ int op_begin(echo_ctx *c, OpContext *o) {
   *o = {c->device, c->sms, c->stream, c->wait_limit_cycles, c->skip_level};
   return ECHO_OK;
 }
+// Whether the context's stream is being captured into a graph.
+int op_capturing(echo_ctx *c, bool *yes) {
+  cudaStreamCaptureStatus how = cudaStreamCaptureStatusNone;
+  CK(cudaStreamIsCapturing(c->stream, &how), "asking whether the stream is captured");
+  *yes = how != cudaStreamCaptureStatusNone;
+  return ECHO_OK;
+}
+int op_not_in_capture(echo_ctx *c) {
+  return set_err(c, ECHO_E_STATE, "an operator's first call of a size allocates: it has to come before the capture of a graph");
+}
 int op_status(echo_ctx *c, int32_t **p) {
   if (!c->ops_status) {
+    bool capturing = false;
+    if (const int rc = op_capturing(c, &capturing)) return rc;
+    if (capturing) return op_not_in_capture(c);
     void *q = nullptr;
     CK(cudaHostAlloc(&q, sizeof(int32_t), cudaHostAllocMapped), "allocating the operators' status");
     c->ops_status = static_cast<int32_t *>(q);
@@ -1905,21 +1920,35 @@ int op_status(echo_ctx *c, int32_t **p) {
 int op_error(echo_ctx *c, int code, const std::string &msg) { return set_err(c, code, msg); }
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what) { return cuda_fail(c, e, what); }
 
+// A captured graph holds the address that its calls were given, so what a capture has used stays
+// until the context goes; the rest is freed when it is outgrown.  Each block is twice the one before,
+// or 1 GB larger, if there is memory for that: calls of slowly growing sizes allocate seldom.
 int op_scratch(echo_ctx *c, size_t bytes, void **p) {
+  bool capturing = false;
+  if (const int rc = op_capturing(c, &capturing)) return rc;
   if (c->ops_bytes < bytes) {
-    if (c->ops) {
+    if (capturing) return op_not_in_capture(c);
+    const size_t more = c->ops_bytes + std::min<size_t>(c->ops_bytes, (size_t)1 << 30);
+    if (c->ops_captured) {
+      c->ops_kept.push_back(c->ops);
+    } else if (c->ops) {
       CK(cudaStreamSynchronize(c->stream), "waiting for the work that uses the scratch");
       cudaFree(c->ops);
     }
     c->ops = nullptr;
     c->ops_bytes = 0;
-    if (cudaMalloc(&c->ops, bytes) != cudaSuccess) {
+    c->ops_captured = false;
+    for (const size_t want : {std::max(bytes, more), bytes}) {
+      if (cudaMalloc(&c->ops, want) == cudaSuccess) {
+        c->ops_bytes = want;
+        break;
+      }
       (void)cudaGetLastError();
       c->ops = nullptr;
-      return set_err(c, ECHO_E_OOM, "cudaMalloc of " + std::to_string(bytes) + " bytes of scratch failed");
     }
-    c->ops_bytes = bytes;
+    if (!c->ops) return set_err(c, ECHO_E_OOM, "cudaMalloc of " + std::to_string(bytes) + " bytes of scratch failed");
   }
+  c->ops_captured |= capturing;
   *p = c->ops;
   return ECHO_OK;
 }
@@ -2023,6 +2052,7 @@ int echo_destroy(echo_ctx *c) {
   free_all(c->raw_allocs);
   if (c->stage) cudaFree(c->stage);
   if (c->ops) cudaFree(c->ops);
+  free_all(c->ops_kept);
   if (c->ops_status) cudaFreeHost(c->ops_status);
   for (auto &r : c->recs) {
     cudaEventDestroy(r.second.first);

@@ -24,7 +24,8 @@ struct OpContext {
 int op_begin(echo_ctx *c, OpContext *o);
 int op_error(echo_ctx *c, int code, const std::string &msg);
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what);
-// Memory of the context that lasts until a later call's: at least `bytes`, 256-byte aligned.
+// Memory of the context that lasts until a later call's, or as long as the context where a graph
+// is captured: at least `bytes`, 256-byte aligned.
 int op_scratch(echo_ctx *c, size_t bytes, void **p);
 // Whether p is memory of the context's device.
 bool op_device_memory(echo_ctx *c, const void *p);

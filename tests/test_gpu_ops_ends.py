@@ -13,7 +13,7 @@ Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roun
 
 import pytest
 
-from paper_2412_12487_gb300 import Echo
+from paper_2412_12487_gb300 import Echo, EchoError
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -78,3 +78,60 @@ def test_orthogonalize_rows_and_columns(echo, dtype):
 def test_orthogonalize_low_rank(echo, dtype):
     g = torch.outer(_randn((70,), 30), _randn((300,), 31)).to(dtype)
     _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), gain=1210)
+
+
+def _code(call):
+    with pytest.raises(EchoError) as err:
+        call()
+    return err.value.code
+
+
+def test_a_larger_call_leaves_a_captured_graph_its_scratch():
+    """A graph keeps the address of the scratch that it was captured with.  Larger calls come after the capture, then
+    arrays that would take the place of memory given back: the graph's results stay right, and the arrays as they were."""
+    side = torch.cuda.Stream()
+    x, g, ids = _randn((64, 512), 60), _randn((96, 200), 61), torch.arange(64, device="cuda") % 50
+    with Echo(0, stream=side) as e, torch.cuda.stream(side):
+        def step(x, g, ids):
+            y, mean, rstd = e.layer_norm(x)
+            return *e.layer_norm_grad(y, x, mean, rstd), e.embed_grad(ids, y, 50), e.orthogonalize(g)
+
+        want = step(x, g, ids)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step(x, g, ids)
+        large = [step(_randn((r, 2048), 62), _randn((m, 2 * m), 63), torch.arange(r, device="cuda") % 50) for r, m in ((3000, 400), (9000, 1200))]
+        side.synchronize()
+        arrays = [torch.full((n,), 7.0, device="cuda") for n in (1 << 10, 1 << 16, 1 << 20, 1 << 21, 1 << 22, 1 << 24) for _ in range(4)]
+        for _ in range(3):
+            for o in out:
+                o.zero_()
+            graph.replay()
+            for a, b in zip(out, want):
+                assert torch.equal(a, b)
+        assert all((a == 7).all() for a in arrays)
+        for k, (r, m) in enumerate(((3000, 400), (9000, 1200))):
+            again = step(_randn((r, 2048), 62), _randn((m, 2 * m), 63), torch.arange(r, device="cuda") % 50)
+            assert all(torch.equal(a, b) for a, b in zip(large[k], again))
+        side.synchronize()
+
+
+def test_a_call_that_would_allocate_in_a_capture_is_refused():
+    """... and the capture goes on without it."""
+    side = torch.cuda.Stream()
+    x, g = _randn((64, 512), 64), _randn((96, 200), 65)
+    with Echo(0, stream=side) as e, torch.cuda.stream(side):
+        y, mean, rstd = e.layer_norm(x)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            assert _code(lambda: e.orthogonalize(g)) == 4  # ECHO_E_STATE
+            assert _code(lambda: e.layer_norm_grad(x, x, mean, rstd)) == 4
+            z = e.layer_norm(x)[0]
+        graph.replay()
+        side.synchronize()
+        assert torch.equal(z, y)
+        e.orthogonalize(g)
+        e.layer_norm_grad(x, x, mean, rstd)
+        side.synchronize()
