@@ -30,13 +30,14 @@ constexpr int kScaleYLog2 = 12;
 constexpr float kScaleY = 1 << kScaleYLog2, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
 
 // -- Frobenius norm ------------------------------------------------------------------------------
-// Sums of squares of x, of 2^-60 x and of 2^60 x: one of them neither overflows nor underflows,
-// whatever the size of the elements.  A block sums a part of one matrix (one without gaps comes
-// as a single row).  Bound by the bytes of G: 2048 x 8192 in fp32, 6.7e7 bytes, 15 us, 4.5 TB/s.
+// Sums of squares of x, of 2^-90 x and of 2^90 x.  Of up to 2^32 elements between 2^-149 and 2^128
+// the second sum stays below 2^108, and the third has no term below 2^-118; the plain one keeps
+// its digits for norms from 2^-40 to 2^50.  A block sums a part of one matrix (one without gaps
+// comes as a single row).  Bound by the bytes of G: 2048 x 8192 in fp32, 6.7e7 bytes, 15 us, 4.5 TB/s.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(OrthoArgs a, int64_t rows, int64_t cols, float *part, int32_t *arrived, int n_arrived) {
   __shared__ float sh[3][8];
-  const float up = 0x1p60f, down = 0x1p-60f;
+  const float up = 0x1p90f, down = 0x1p-90f;
   kernel_begin();
   next_may_start();
   if (blockIdx.x == 0 && blockIdx.y == 0)
@@ -96,7 +97,7 @@ __device__ __forceinline__ Factor inverse_norm(const float *part, int parts, int
 #pragma unroll
   for (int q = 0; q < 3; ++q) s[q] = warp_sum(s[q]);
   // the plain sum unless it is near the ends of the range; |G| = root * 2^size (a NaN stays one)
-  const int size = s[0] > 1e30f ? 60 : s[0] < 1e-24f ? -60 : 0;
+  const int size = s[0] > 0x1p100f ? 90 : s[0] < 0x1p-80f ? -90 : 0;
   const float root = sqrtf(size > 0 ? s[1] : size < 0 ? s[2] : s[0]);
   const float inverse = 1.f / (root + ldexpf(eps, -size));
   Factor f{1.f, 1.f, inverse};

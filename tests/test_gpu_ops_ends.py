@@ -80,6 +80,18 @@ def test_orthogonalize_low_rank(echo, dtype):
     _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), gain=1210)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_orthogonalize_ends_of_the_range(echo, dtype):
+    """Norms beyond fp32's largest number, and elements below its smallest normal one."""
+    g = _randn((6, 48, 80), 34).double()
+    g = g / g.abs().amax(dim=(1, 2), keepdim=True)
+    sized = torch.stack([g[i] * 2.0 ** k for i, k in enumerate((127, 126, 100, -110, -124, -126))]).to(dtype)
+    assert torch.isfinite(sized).all()
+    _ortho_close(echo.orthogonalize(sized, eps=0.0), _ortho_ref(sized))
+    tiny = (g * 2.0 ** -130).to(dtype)  # a few bits of each are left: the result is that matrix's own
+    _ortho_close(echo.orthogonalize(tiny, eps=0.0), _ortho_ref(tiny))
+
+
 def _code(call):
     with pytest.raises(EchoError) as err:
         call()
