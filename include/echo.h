@@ -370,7 +370,8 @@ int echo_measure_fp64(int device, double *rates);
  *   - NULL or misplaced pointers, unknown types, bad sizes or strides:
  *     ECHO_E_INVALID_ARG, with nothing enqueued; sizes beyond what a call states:
  *     ECHO_E_UNSUPPORTED.  A device-side wait that gives up (2 s) leaves that result
- *     incomplete; the context's next operator returns ECHO_E_TIMEOUT, once.
+ *     incomplete; the context's next operator returns ECHO_E_TIMEOUT, once (and
+ *     enqueues nothing).
  */
 enum { ECHO_F32 = 0, ECHO_BF16 = 1, ECHO_F16 = 2 };
 

@@ -1884,13 +1884,9 @@ int activate_fold(echo_ctx *c, bool want) {
 // -- what the operators use of a context (echo_ops.h) ----------------------------------------
 namespace echo {
 
-int op_begin(echo_ctx *c, OpContext *o) {
+int op_context(echo_ctx *c, OpContext *o) {
   const int rc = check_ctx(c);
   if (rc) return rc;
-  if (c->ops_status && *(volatile int32_t *)c->ops_status) {
-    *(volatile int32_t *)c->ops_status = 0;
-    return set_err(c, ECHO_E_TIMEOUT, "a device-side wait of an earlier operator gave up: its result is incomplete");
-  }
   *o = {c->device, c->sms, c->stream, c->wait_limit_cycles, c->skip_level};
   return ECHO_OK;
 }
@@ -1900,6 +1896,15 @@ int op_capturing(echo_ctx *c, bool *yes) {
   CK(cudaStreamIsCapturing(c->stream, &how), "asking whether the stream is captured");
   *yes = how != cudaStreamCaptureStatusNone;
   return ECHO_OK;
+}
+int op_report(echo_ctx *c) {
+  if (!c->ops_status || !*(volatile int32_t *)c->ops_status) return ECHO_OK;
+  *(volatile int32_t *)c->ops_status = 0;
+  return set_err(c, ECHO_E_TIMEOUT, "a device-side wait of an earlier operator gave up: its result is incomplete");
+}
+int op_begin(echo_ctx *c, OpContext *o) {
+  const int rc = op_context(c, o);
+  return rc ? rc : op_report(c);
 }
 int op_not_in_capture(echo_ctx *c) {
   return set_err(c, ECHO_E_STATE, "an operator's first call of a size allocates: it has to come before the capture of a graph");

@@ -49,15 +49,22 @@ struct Checks {
 
 // Runs an entry point: no C++ exception leaves it.
 template <typename F>
-int entry(echo_ctx *c, const void *d, F &&body) {
+int guarded(F &&body) {
   try {
+    return body();
+  } catch (const std::exception &) {
+    return ECHO_E_OOM;
+  }
+}
+// The entry point of an operator.
+template <typename F>
+int entry(echo_ctx *c, const void *d, F &&body) {
+  return guarded([&]() -> int {
     OpContext o;
     if (const int rc = echo::op_begin(c, &o)) return rc;
     if (!d) return echo::op_error(c, ECHO_E_INVALID_ARG, "an argument is NULL");
     return body(o);
-  } catch (const std::exception &) {
-    return ECHO_E_OOM;
-  }
+  });
 }
 
 #define RUN(call, name)                                                                       \
@@ -77,9 +84,12 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 extern "C" {
 
 int echo_stream_get(echo_ctx *c, void **cuda_stream) {
-  return entry(c, cuda_stream, [&](const OpContext &o) {
+  return guarded([&]() -> int {
+    OpContext o;
+    if (const int rc = echo::op_context(c, &o)) return rc;
+    if (!cuda_stream) return echo::op_error(c, ECHO_E_INVALID_ARG, "an argument is NULL");
     *cuda_stream = o.stream;
-    return (int)ECHO_OK;
+    return ECHO_OK;
   });
 }
 

@@ -19,8 +19,9 @@ struct OpContext {
   long long wait_limit;  // bound of every device-side wait, in SM clock cycles
   int skip;              // failure injection for tests (-1: none)
 };
-// Makes the context's device current; an echo_status: ECHO_E_TIMEOUT where a kernel of an
-// earlier call gave up.
+// Makes the context's device current; an echo_status.
+int op_context(echo_ctx *c, OpContext *o);
+// The same for an operator: ECHO_E_TIMEOUT where a kernel of an earlier call gave up.
 int op_begin(echo_ctx *c, OpContext *o);
 int op_error(echo_ctx *c, int code, const std::string &msg);
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what);

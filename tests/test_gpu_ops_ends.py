@@ -11,6 +11,8 @@ Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roun
   root mean square and normally distributed w the mean of it is 0.8 r (1 - log r), r = 100 e / uo: 3% for bf16 and 16% for fp16.
 """
 
+import ctypes as C
+
 import pytest
 
 from paper_2412_12487_gb300 import Echo, EchoError
@@ -20,6 +22,7 @@ pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 UO = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
 QUINTIC = (3.4445, -4.7750, 2.0315)
+TIMEOUT = 7  # ECHO_E_TIMEOUT
 
 
 @pytest.fixture(scope="module")
@@ -92,10 +95,28 @@ def test_orthogonalize_ends_of_the_range(echo, dtype):
     _ortho_close(echo.orthogonalize(tiny, eps=0.0), _ortho_ref(tiny))
 
 
+def _gives_up(monkeypatch, limit_ms="20"):
+    monkeypatch.setenv("ECHO_TEST_SKIP_LEVEL", "1")
+    monkeypatch.setenv("ECHO_TEST_WAIT_LIMIT_MS", limit_ms)
+
+
 def _code(call):
     with pytest.raises(EchoError) as err:
         call()
     return err.value.code
+
+
+def test_the_stream_is_no_operator(monkeypatch):
+    """Asking for the stream leaves the report of a wait that ran out to the next operator."""
+    g = _randn((300, 280), 40)
+    _gives_up(monkeypatch)
+    with Echo(0) as e:
+        e.orthogonalize(g, steps=1)
+        torch.cuda.synchronize()
+        s = C.c_void_p()
+        assert e.lib.echo_stream_get(e.h, C.byref(s)) == 0 and s.value == e._stream
+        assert _code(lambda: e.layer_norm(g)) == TIMEOUT
+        e.layer_norm(g)
 
 
 def test_a_larger_call_leaves_a_captured_graph_its_scratch():
