@@ -1897,8 +1897,13 @@ int op_capturing(echo_ctx *c, bool *yes) {
   *yes = how != cudaStreamCaptureStatusNone;
   return ECHO_OK;
 }
+// What kernels have reported so far, once.  Kernels of the same call may still be running, and
+// give up in their turn: they end first (each wait has its limit), so that they are part of it.
 int op_report(echo_ctx *c) {
   if (!c->ops_status || !*(volatile int32_t *)c->ops_status) return ECHO_OK;
+  bool capturing = false;
+  if (const int rc = op_capturing(c, &capturing)) return rc;
+  if (!capturing) CK(cudaStreamSynchronize(c->stream), "waiting for an operator that gave up");
   *(volatile int32_t *)c->ops_status = 0;
   return set_err(c, ECHO_E_TIMEOUT, "a device-side wait of an earlier operator gave up: its result is incomplete");
 }

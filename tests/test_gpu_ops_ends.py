@@ -12,6 +12,7 @@ Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roun
 """
 
 import ctypes as C
+import time
 
 import pytest
 
@@ -117,6 +118,18 @@ def test_the_stream_is_no_operator(monkeypatch):
         assert e.lib.echo_stream_get(e.h, C.byref(s)) == 0 and s.value == e._stream
         assert _code(lambda: e.layer_norm(g)) == TIMEOUT
         e.layer_norm(g)
+
+
+def test_a_wait_is_reported_once_while_the_rest_still_runs(monkeypatch):
+    """The first products have given up, the others of the same call will: one report for all of them."""
+    g = _randn((300, 280), 41)
+    _gives_up(monkeypatch, "40")
+    with Echo(0) as e:
+        e.orthogonalize(g, steps=5)
+        time.sleep(0.15)
+        assert _code(lambda: e.layer_norm(g)) == TIMEOUT
+        torch.cuda.synchronize()
+        assert torch.isfinite(e.layer_norm(g)[0]).all()
 
 
 def test_a_larger_call_leaves_a_captured_graph_its_scratch():
