@@ -370,14 +370,18 @@ int echo_measure_fp64(int device, double *rates);
  *   - NULL or misplaced pointers, unknown types, bad sizes or strides:
  *     ECHO_E_INVALID_ARG, with nothing enqueued; sizes beyond what a call states:
  *     ECHO_E_UNSUPPORTED.  A device-side wait that gives up (2 s) leaves that result
- *     incomplete; the context's next operator returns ECHO_E_TIMEOUT, once (and
- *     enqueues nothing).
+ *     incomplete; the context's next operator, or echo_wait, returns ECHO_E_TIMEOUT, once
+ *     (and enqueues nothing).  After a last operator, only echo_wait can tell.
  */
 enum { ECHO_F32 = 0, ECHO_BF16 = 1, ECHO_F16 = 2 };
 
 /* The stream the context enqueues on (its own, or the one given to echo_create), for
  * ordering other work with the operators'. */
 int echo_stream_get(echo_ctx *ctx, void **cuda_stream);
+
+/* Waits for all work enqueued on the context's stream.  ECHO_E_TIMEOUT where an operator's
+ * wait gave up since the last such report; ECHO_E_STATE while the stream is captured. */
+int echo_wait(echo_ctx *ctx);
 
 /* Embedding lookup (kernel class of the first pipeline stage) in a vocabulary shard:
  *   out[t][:] = scale * table[ids[t] - vocab_start][:]

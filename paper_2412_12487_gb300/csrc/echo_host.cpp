@@ -1911,6 +1911,15 @@ int op_begin(echo_ctx *c, OpContext *o) {
   const int rc = op_context(c, o);
   return rc ? rc : op_report(c);
 }
+int op_wait(echo_ctx *c) {
+  const int rc = check_ctx(c);
+  if (rc) return rc;
+  bool capturing = false;
+  if (const int r = op_capturing(c, &capturing)) return r;
+  if (capturing) return set_err(c, ECHO_E_STATE, "the context's stream is being captured: there is nothing to wait for");
+  CK(cudaStreamSynchronize(c->stream), "waiting for the context's stream");
+  return op_report(c);
+}
 int op_not_in_capture(echo_ctx *c) {
   return set_err(c, ECHO_E_STATE, "an operator's first call of a size allocates: it has to come before the capture of a graph");
 }

@@ -93,6 +93,10 @@ int echo_stream_get(echo_ctx *c, void **cuda_stream) {
   });
 }
 
+int echo_wait(echo_ctx *c) {
+  return guarded([&] { return echo::op_wait(c); });
+}
+
 int echo_embed(echo_ctx *c, const echo_embed_desc *d) {
   return entry(c, d, [&](const OpContext &o) {
     Checks k{c};

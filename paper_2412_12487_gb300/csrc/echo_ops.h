@@ -23,6 +23,8 @@ struct OpContext {
 int op_context(echo_ctx *c, OpContext *o);
 // The same for an operator: ECHO_E_TIMEOUT where a kernel of an earlier call gave up.
 int op_begin(echo_ctx *c, OpContext *o);
+// Waits for the context's stream; ECHO_E_TIMEOUT as above.
+int op_wait(echo_ctx *c);
 int op_error(echo_ctx *c, int code, const std::string &msg);
 int op_cuda_error(echo_ctx *c, cudaError_t e, const char *what);
 // Memory of the context that lasts until a later call's, or as long as the context where a graph

@@ -25,7 +25,7 @@ EXPORTS = ["echo_create", "echo_destroy", "echo_check_graph", "echo_check_replic
            "echo_read_cc", "echo_read_overlap", "echo_cc_query", "echo_cc_query_noalloc",
            "echo_graph_info_get", "echo_set_cc_model",
            "echo_set_profiling", "echo_read_profile", "echo_measure_fp64", "echo_strerror", "echo_last_error",
-           "echo_stream_get", "echo_embed", "echo_embed_grad", "echo_layer_norm", "echo_layer_norm_grad", "echo_orthogonalize"]
+           "echo_stream_get", "echo_wait", "echo_embed", "echo_embed_grad", "echo_layer_norm", "echo_layer_norm_grad", "echo_orthogonalize"]
 
 
 class EchoError(RuntimeError):
@@ -166,6 +166,7 @@ def load_library(path: Optional[str] = None):
         "echo_strerror": ([C.c_int], C.c_char_p),
         "echo_last_error": ([vp, C.c_char_p, C.c_size_t], C.c_int),
         "echo_stream_get": ([vp, C.POINTER(vp)], C.c_int),
+        "echo_wait": ([vp], C.c_int),
         "echo_embed": ([vp, C.POINTER(EmbedDesc)], C.c_int),
         "echo_embed_grad": ([vp, C.POINTER(EmbedGradDesc)], C.c_int),
         "echo_layer_norm": ([vp, C.POINTER(LayerNormDesc)], C.c_int),
@@ -502,6 +503,11 @@ class Echo:
         own.wait_stream(cur)
         self._check(call(self.h, C.byref(desc)))
         cur.wait_stream(own)
+
+    def wait(self):
+        """Waits for the work on the context's stream; raises (ECHO_E_TIMEOUT) where an operator's
+        device-side wait gave up and no later call has reported it."""
+        self._check(self.lib.echo_wait(self.h))
 
     @staticmethod
     def _ids(ids) -> int:

@@ -132,6 +132,20 @@ def test_a_wait_is_reported_once_while_the_rest_still_runs(monkeypatch):
         assert torch.isfinite(e.layer_norm(g)[0]).all()
 
 
+def test_a_last_operator_is_waited_for(monkeypatch):
+    g = _randn((300, 280), 42)
+    with Echo(0) as e:
+        e.wait()
+        e.orthogonalize(g)
+        e.wait()
+    _gives_up(monkeypatch)
+    with Echo(0) as e:
+        e.orthogonalize(g, steps=1)
+        assert _code(e.wait) == TIMEOUT
+        e.wait()
+        e.layer_norm(g)
+
+
 def test_a_larger_call_leaves_a_captured_graph_its_scratch():
     """A graph keeps the address of the scratch that it was captured with.  Larger calls come after the capture, then
     arrays that would take the place of memory given back: the graph's results stay right, and the arrays as they were."""
