@@ -462,9 +462,10 @@ int echo_layer_norm_grad(echo_ctx *ctx, const echo_layer_norm_grad_desc *d);
  *   X = G / (|G| + eps), |G| the Frobenius norm;
  *   `steps` times: A = X X^T, X = a X + (b A + c A A) X;
  *   O = scale * X (transposed back).
- * Matrices of every type are multiplied as sums of two fp16 numbers (22 bits); sums are in
- * fp32.  (a, b, c) has to keep singular values in [0, 1] within [0, 2] over the steps, as the
- * usual quintics do; a matrix with an infinite or NaN element gives NaN.
+ * Matrices of every type are multiplied as sums of two fp16 numbers, with sums in fp32: 22 bits
+ * of X's elements from 2^-14 on, an error of 2^-37 in smaller ones.  (a, b, c) has to keep
+ * singular values in [0, 1] within [0, 2] over the steps, as the usual quintics do; a matrix
+ * with an infinite or NaN element gives NaN.
  * rows and cols are 1 to 65536, steps 0 to 64. */
 typedef struct {
   int64_t batch, rows, cols;

@@ -9,9 +9,10 @@
 // that reach the lower triangle and write each block to both places.
 //
 // Elements are sums of two fp16 numbers times a power of two (the iterate's singular values stay
-// near 1, so its elements are at most that): 22 bits, whatever the matrices' type, multiplied as
-// high * high + high * low + low * high with sums in fp32.  One number an element takes a third
-// of the products, but leaves a bf16 result 2.1e-3 off, 1.7e-3 of which is its own rounding.
+// near 1, so its elements are at most that): 22 bits of all but small ones (kScaleY), whatever the
+// matrices' type, multiplied as high * high + high * low + low * high with sums in fp32.  One
+// number an element takes a third of the products, but leaves a bf16 result 2.1e-3 off, 1.7e-3 of
+// which is its own rounding.
 #include <cuda.h>
 
 #include <algorithm>
@@ -25,7 +26,9 @@ namespace echo {
 namespace {
 
 // What is stored of Y, A and B: the true value times this.  fp16 holds 2^-24 to 65504, so
-// elements up to 16 fit, and 22 bits remain of elements down to 2^-25.
+// elements up to 16 fit (64 of B), and 22 bits remain of elements down to 2^-14 (2^-12 of B);
+// smaller ones keep an error of 2^-37 (2^-35), which the norm of a matrix does not see: 2^32 such
+// elements add up to 2^-21.
 constexpr int kScaleYLog2 = 12;
 constexpr float kScaleY = 1 << kScaleYLog2, kScaleA = 0x1p12f, kScaleB = 0x1p10f;
 

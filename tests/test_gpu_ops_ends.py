@@ -84,6 +84,13 @@ def test_orthogonalize_low_rank(echo, dtype):
     _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), gain=1210)
 
 
+def test_orthogonalize_elements_far_below_the_largest(echo):
+    """Elements over thirty powers of two: those below 2^-14 of the norm have fewer bits, at no cost to the result's norm
+    (their absolute error stays at 2^-37: 450 * 2^-37 of the norm for 200 x 1000)."""
+    g = _randn((200, 1000), 32) * torch.exp2(-30 * torch.rand((200, 1000), generator=torch.Generator(device="cuda").manual_seed(33), device="cuda"))
+    _ortho_close(echo.orthogonalize(g, eps=0.0), _ortho_ref(g), gain=101)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_orthogonalize_ends_of_the_range(echo, dtype):
     """Norms beyond fp32's largest number, and elements below its smallest normal one."""
