@@ -103,6 +103,16 @@ def test_orthogonalize_ends_of_the_range(echo, dtype):
     _ortho_close(echo.orthogonalize(tiny, eps=0.0), _ortho_ref(tiny))
 
 
+@pytest.mark.parametrize("h", [64, 256, 1024])
+def test_layer_norm_rstd_is_the_rounded_one(echo, h):
+    """Rows of +a and -a: every sum is exact, so nothing but the last rounding is left of 1 / sqrt(a^2)."""
+    a = torch.arange(1, 1024, device="cuda", dtype=F32)
+    sign = torch.tensor([1.0, -1.0], device="cuda").repeat(h // 2)
+    _, mean, rstd = echo.layer_norm(a[:, None] * sign, eps=0.0)
+    assert not mean.any()
+    assert torch.equal(rstd, (1 / a.double()).float())
+
+
 def _gives_up(monkeypatch, limit_ms="20"):
     monkeypatch.setenv("ECHO_TEST_SKIP_LEVEL", "1")
     monkeypatch.setenv("ECHO_TEST_WAIT_LIMIT_MS", limit_ms)
