@@ -352,7 +352,8 @@ int echo_measure_fp64(int device, double *rates);
  * Operators of a rank's training step.  An execution graph's compute ops stand for
  * kernels whose durations a tracer measures on one device (Sec. 4.1); these calls run
  * the memory-bound and optimizer ones among them on this device, so that their times
- * (echo_set_profiling, echo_read_profile) can go into echo_load_scenarios.
+ * (of a captured row of calls: echo_set_profiling adds events to each) can go into
+ * echo_load_scenarios.
  *   - Arrays are DEVICE memory of the context's device, owned by the caller, each at a
  *     multiple of its element size.  Matrices are rows of contiguous elements, `stride`
  *     elements apart: at least the row's length for outputs, any value >= 0 for inputs.

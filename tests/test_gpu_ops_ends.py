@@ -12,11 +12,14 @@ Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roun
 """
 
 import ctypes as C
+import importlib.util
+import os
 import time
 
 import pytest
 
 from paper_2412_12487_gb300 import Echo, EchoError
+from paper_2412_12487_gb300 import workloads as W
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -161,6 +164,27 @@ def test_a_last_operator_is_waited_for(monkeypatch):
         assert _code(e.wait) == TIMEOUT
         e.wait()
         e.layer_norm(g)
+
+
+def test_measured_times_are_the_kernels_own():
+    """A layer norm that is measured for a timeline takes what it takes in a row of kernels, not what it takes between events."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "measured_step.py")
+    spec = importlib.util.spec_from_file_location("measured_step", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    c = W.config("tiny")
+    with Echo(0) as e:
+        ns = m.measure(e, c)
+        x, w, b = _randn((c.seq, c.hidden), 50, BF16), _randn((c.hidden,), 51), _randn((c.hidden,), 52)
+        for _ in range(5):
+            e.layer_norm(x, w, b)
+        e.read_profile()
+        e.set_profiling(True)
+        for _ in range(20):
+            e.layer_norm(x, w, b)
+        between_events = min(1e6 * ms / n for n, ms in e.read_profile().values())
+        e.set_profiling(False)
+    assert ns["norm"] <= 0.75 * between_events, (ns, between_events)
 
 
 def test_a_larger_call_leaves_a_captured_graph_its_scratch():
