@@ -2,8 +2,11 @@
 
 A tracer runs each rank's kernels on one device and measures them (Sec. 4.1 of the paper).  This example does so for the
 kernel classes that the library runs itself, at the shapes of one rank of a workload: the embedding lookup and its gradient
-(first pipeline stage), the layer norms forward and backward, and the optimizer step as an orthogonalised update of every
-weight.  Their times replace the generator's for those ops; the step is composed with both.
+(first pipeline stage), the layer norms forward and backward, and the step of a matrix optimizer, whose updates the library
+makes orthogonal.  Their times replace the generator's for those ops; the step is composed with both.  The optimizer is
+another one than the generator's, which reads and writes 16 bytes a parameter in three ops: the measured step is the same
+workload with a matrix optimizer, and the whole time of its step, momentum and weights included, is spread over the three.
+Matrix products and attention keep the generator's durations.
 
     python examples/measured_step.py [tiny | gpt1.3b | gpt175b]
 """
@@ -16,6 +19,13 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2412_12487_gb300 import Echo  # noqa: E402
 from paper_2412_12487_gb300 import workloads as W  # noqa: E402
+
+
+def update(e: Echo, weight, momentum, grad, rate: float = 0.02, decay: float = 0.95):
+    """A matrix optimizer's step for weights [..., rows, cols]: the momentum's orthogonalised update, scaled for tall ones."""
+    momentum.mul_(decay).add_(grad)
+    rows, cols = weight.shape[-2:]
+    weight.add_(e.orthogonalize(momentum, scale=max(1.0, rows / cols) ** 0.5), alpha=-rate)
 
 
 def measure(e: Echo, c: W.GPTConfig, reps: int = 5):
@@ -35,7 +45,8 @@ def measure(e: Echo, c: W.GPTConfig, reps: int = 5):
         weight, bias = torch.ones(hidden, device=dev), torch.zeros(hidden, device=dev)
         main = {k: torch.zeros_like(v, dtype=torch.float32) for k, v in (("table", table), ("weight", weight), ("bias", bias))}
         layers, h, t = c.layers // c.pp, c.hidden, c.tp
-        grads = [torch.randn((layers, *s), generator=gen, device=dev).to(bf16) for s in ((3 * h // t, h), (h, h // t), (4 * h // t, h), (h, 4 * h // t))]
+        shapes = [(layers, *s) for s in ((3 * h // t, h), (h, h // t), (4 * h // t, h), (h, 4 * h // t))]  # of a stage's layers
+        weights, momenta, grads = ([torch.randn(s, generator=gen, device=dev, dtype=bf16) for s in shapes] for _ in range(3))
 
         def time(call, n):
             result = call()  # scratch memory is allocated
@@ -53,8 +64,8 @@ def measure(e: Echo, c: W.GPTConfig, reps: int = 5):
             return result, begin.elapsed_time(end) * 1e6 / n
 
         def optimizer():
-            for g in grads:
-                own.orthogonalize(g, scale=max(1.0, g.shape[-2] / g.shape[-1]) ** 0.5)
+            for w, m, g in zip(weights, momenta, grads):
+                update(own, w, m, g)
 
         ns, many = {}, 20 * reps
         x, ns["embed"] = time(lambda: own.embed(ids, table), many)
@@ -80,7 +91,7 @@ def put(g: W.Graph, c: W.GPTConfig, dur: np.ndarray, ns) -> np.ndarray:
     emb = comp & (g.kclass == W.KC_EMB)
     dur[emb & after_copy] = round(ns["embed"])
     dur[emb & ~after_copy] = round(ns["embed_grad"])
-    dur[comp & (g.kclass == W.KC_OPT)] = round(ns["optimizer"] / 3)  # (three ops of a third of the parameters each)
+    dur[comp & (g.kclass == W.KC_OPT)] = round(ns["optimizer"] / 3)  # (the step's three ops; every stage has as many layers)
     return dur
 
 

@@ -13,6 +13,7 @@ Tolerances are written down before the first run.  u = 2^-24 is fp32's unit roun
 
 import ctypes as C
 import importlib.util
+import math
 import os
 import time
 
@@ -166,6 +167,14 @@ def test_a_last_operator_is_waited_for(monkeypatch):
         e.layer_norm(g)
 
 
+def _example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "measured_step.py")
+    spec = importlib.util.spec_from_file_location("measured_step", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
 def test_measured_times_are_the_kernels_own():
     """A layer norm that is measured for a timeline takes what it takes in a row of kernels, not what it takes between events."""
     path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "measured_step.py")
@@ -236,3 +245,16 @@ def test_a_call_that_would_allocate_in_a_capture_is_refused():
         e.orthogonalize(g)
         e.layer_norm_grad(x, x, mean, rstd)
         side.synchronize()
+
+
+def test_the_measured_optimizer_step_is_a_whole_one(echo):
+    """Momentum, orthogonalised update and weights: what the workload's optimizer ops stand for."""
+    m = _example()
+    w, v, g = (_randn((2, 96, 40), 70 + k) for k in range(3))
+    w2, v2 = w.clone(), v.clone()
+    m.update(echo, w2, v2, g, rate=0.125, decay=0.5)
+    assert torch.equal(v2, v * 0.5 + g)
+    want = math.sqrt(96 / 40) * _ortho_ref(v2, eps=1e-7)
+    got = (w.double() - w2.double()) / 0.125
+    # the update's own error, and a rounding of the weights in fp32, eight times as large in it
+    assert float((got - want).norm()) <= 102 * 2.0 ** -22 * float(want.norm()) + 8 * 2.0 ** -24 * float(w2.double().norm())
