@@ -622,16 +622,20 @@ int blocks_of(const Shape &s) {
 // A grid that goes through its rows in turns has to lie evenly on the SMs, which blocks that come
 // while another kernel ends do not by themselves: where it fills them, a block asks for so much
 // shared memory that no more than its share fit an SM (4999 x 1537 in fp32, backward: 40 us a
-// call in a row of them, 63 without).
-size_t even_smem(const Shape &s, int64_t grid, int sms) {
+// call in a row of them, 63 without).  Backward, up to as many blocks as SMs get an SM each in the
+// same way (64 x 2048 in bf16, in a graph: 4.8 us, 5.2 to 6.2 where they come several to an SM; 100 x
+// 1537 in fp32 6.0 and 6.6).  Forward, and for less than a quarter of the SMs, it changes nothing but
+// the call, which sets the kernel's limit (0.6 us).
+size_t even_smem(const Shape &s, int64_t grid, int sms, int arrays) {
+  if (arrays == 2 && grid <= sms && grid > sms / 4) return std::max<size_t>(s.smem, (228 << 10) / 2);
   return grid > sms && grid % sms == 0 ? std::max<size_t>(s.smem, (228 << 10) / (grid / sms + 1)) : s.smem;
 }
 
 constexpr int kMostSmem = 224 << 10;  // a block's, beside what the kernels hold for their sums
 
 template <typename K, typename... A>
-cudaError_t launch_rows(K kernel, const Shape &s, int64_t grid, int sms, cudaStream_t st, const A &...args) {
-  const size_t smem = even_smem(s, grid, sms);
+cudaError_t launch_rows(K kernel, const Shape &s, int arrays, int64_t grid, int sms, cudaStream_t st, const A &...args) {
+  const size_t smem = even_smem(s, grid, sms, arrays);
   if (smem > 40 << 10) {  // (one limit for all lengths: calls of other threads, or a graph's, may lie between)
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
     if (e != cudaSuccess) return e;
@@ -653,7 +657,7 @@ cudaError_t launch_layer_norm(const NormArgs &a, int sms, cudaStream_t st) {
       auto go = [&](auto each) {
         constexpr int E = decltype(each)::value;
         const int64_t grid = std::min<int64_t>((a.rows + s.y - 1) / s.y, (int64_t)sms * blocks_of(s));
-        return launch_rows(layer_norm_kernel<X, W, E>, s, grid, sms, st, a, s.depth, s.slot);
+        return launch_rows(layer_norm_kernel<X, W, E>, s, 1, grid, sms, st, a, s.depth, s.slot);
       };
       return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
     });
@@ -703,7 +707,7 @@ cudaError_t launch_layer_norm_grad(const NormGradArgs &a, int sms, const OpTimer
         auto go = [&](auto each) {
           constexpr int E = decltype(each)::value;
           return timed("layer_norm_grad", [&] {
-            return launch_rows(layer_norm_grad_kernel<X, W, E>, s, grad_blocks(s, a.rows, sms), sms, st, a, s.depth, s.slot, s.staged);
+            return launch_rows(layer_norm_grad_kernel<X, W, E>, s, 2, grad_blocks(s, a.rows, sms), sms, st, a, s.depth, s.slot, s.staged);
           });
         };
         return s.E == 8 ? go(Int<8>{}) : go(Int<16>{});
