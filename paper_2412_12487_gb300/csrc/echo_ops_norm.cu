@@ -136,10 +136,12 @@ struct Rows {
 // warps: each takes the squared distances from its own mean, and
 //   sum (x - mean)^2 = sum over warps of (their sum + n_w (mean_w - mean)^2),
 // in which nothing cancels.  The output starts from those distances.  The bytes of x and y would
-// bound it; what does is the instructions of a row and its two barriers (issue slots 59% taken at
-// 2048 x 12288 in bf16), so they are in pairs, and addresses and bounds are kept from row to row.
-// There a call takes 22 to 25 us in a row of them, 1.0e8 bytes: up to 4.6 TB/s.  Two rows a block
-// with 32 elements a thread took 16% longer.
+// bound it; what does is latency.  At 2048 x 12288 in bf16 an SM holds one row's 24 warps (37% of its
+// places), which wait for shuffles, shared memory and one another's results; no unit is full (issue
+// slots 64%, L1 41%, DRAM 29%).  So arithmetic is in pairs, addresses and bounds are kept from row to
+// row, and a row has one barrier (two in pieces of less than 16 bytes).  A call takes 22 to 25 us in
+// a row of them, 1.0e8 bytes: up to 4.6 TB/s.  Two rows a block with 32 elements a thread took 16%
+// longer.
 template <typename X, int W, int E>
 __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs a, int depth, int slot_bytes) {
   using S = Slice<X, W, E>;
@@ -235,8 +237,9 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_kernel(NormArgs
   }
 }
 
-// Rows too long for registers: three passes over the row, a block each; the second and third come
-// from L2, whose bytes bound it.
+// Rows too long for registers: three passes over the row, a block each, the second and third from
+// L2.  The loads' latency bounds it, a pass behind the other: 2048 x 16384 in bf16, 1.3e8 bytes, takes
+// 73 us, 2048 x 32768 100 us (1.8 and 2.7 TB/s).
 template <typename X, int W>
 __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
   __shared__ float sh[2][32];
@@ -286,10 +289,10 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(NormArgs a) {
 // keep the sums of dweight and dbias of their columns in registers.  Only those sums stay in
 // registers with 16 elements a thread (the weight and the row as well would spill): the row is
 // read twice from its slot, and the weight from shared memory (`staged`) or from L2 where the rows
-// in flight leave no room.  The bytes of dy, x and dx would bound it; what does is shared memory
-// and the instructions of a row (50% and 53% of their slots at 2048 x 12288 in bf16, where a call
-// takes 47.6 us with the join, 3.2 TB/s).  The blocks' partial sums come on top ([blocks][2][H]
-// fp32, written and read once).
+// in flight leave no room.  The bytes of dy, x and dx would bound it; what does is latency, as in the
+// forward pass, at twice the reads: at 2048 x 12288 in bf16 L1 is 68% busy (shared memory 51%), the
+// issue slots 55%, DRAM 35%, and a call takes 47 to 48 us with the join, 3.2 TB/s.  The blocks'
+// partial sums come on top ([blocks][2][H] fp32, written and read once).
 template <typename X, int W, int E>
 __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(NormGradArgs a, int depth, int slot_bytes, int staged) {
   constexpr int K = E / W;
@@ -460,8 +463,8 @@ __global__ void __launch_bounds__(E > 8 ? 768 : 1024) layer_norm_grad_kernel(Nor
   }
 }
 
-// Rows too long for that: dx, a block a row, in two passes over it (the second from L2, whose bytes
-// bound it) ...
+// Rows too long for that: dx, a block a row, in two passes over it, the second from L2.  Bound by the
+// loads' latency: 77 us by itself at 2048 x 16384 in bf16 ...
 template <typename X, int W>
 __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs a) {
   __shared__ float sh[4][32];
@@ -501,7 +504,7 @@ __global__ void __launch_bounds__(1024) layer_norm_grad_rows_kernel(NormGradArgs
 }
 
 // ... and partial sums of dweight and dbias, blockDim.x * W columns of one part of the rows a block:
-// dy and x once more, whose bytes bound it.
+// dy and x once more, 46 us there, 2.9 TB/s.  The whole call takes 129 us, 2.0e8 bytes.
 template <typename X, int W>
 __global__ void __launch_bounds__(128) layer_norm_grad_columns_kernel(NormGradArgs a) {
   kernel_begin();

@@ -128,7 +128,7 @@ __device__ __forceinline__ void split(float v, __half (&h)[kPlanes]) {
 }
 
 // Y = G / (|G| + eps), in pieces of W elements, four of them in flight a thread.  Bound by latency
-// while G and Y fit L2, behind the norm: 6 x 2048 x 1024 in bf16, 5.0e7 bytes, 20 us by itself.
+// while G and Y fit L2, behind the norm: 6 x 2048 x 1024 in bf16, 7.5e7 bytes, 22 us by itself.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) ortho_start_kernel(OrthoArgs a, int64_t rows, int64_t cols, const float *part, int parts, Planes y) {
   __shared__ Factor factor;
@@ -275,9 +275,10 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(OrthoArgs a, int64_t r
 // and 6% more clocks than with sets of eight stages.
 //
 // Large matrices are bound by the tensor cores: 4608 x 12288 in fp32, five steps, 1.3e13
-// operations on fp16 numbers, 8.7 to 9.0 ms, 1.5 PFLOP/s.  Small ones are bound by the operands'
-// way from L2 and by what a launch waits for (fill, drain, a round that is not full): 6 matrices
-// of 2048 x 1024, 6.9e11 operations, 785 us, 0.9 PFLOP/s; 1003 x 517 14 to 15 us a product.
+// operations on fp16 numbers, 8.7 to 9.1 ms, 1.5 PFLOP/s.  Small ones are bound by rounds that are
+// not full and by what a launch waits for (fill, drain): 6 matrices of 2048 x 1024, 6.8e11 operations,
+// 785 to 810 us, 0.8 to 0.9 PFLOP/s, where the symmetric products have 60 tiles for 76 pairs and the
+// last one 192 for three rounds; 1003 x 517 14 us a product.
 constexpr int kBM = 256, kBK = 64, kRows = 128;  // of a tile, of a stage; rows of P a block holds
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 // Registers of a thread of warps 0-3 and of 4-11, which hold 128 sums each; together no more
