@@ -364,6 +364,7 @@ int echo_measure_fp64(int device, double *rates);
  *     (ECHO_E_STATE where one would have to allocate).  The graph uses the scratch that the
  *     context had then, which is kept until echo_destroy whatever larger calls follow: its
  *     launches have to be ordered with the context's stream, and end before echo_destroy.
+ *     They are not profiled.
  *   - They need no graph or scenarios and leave those of the context as they are.
  *   - Outputs overlap no other array, except where a call says so.
  *   - Sums, statistics and products accumulate in fp32; results are rounded once, to the

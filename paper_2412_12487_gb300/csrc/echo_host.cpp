@@ -1981,7 +1981,12 @@ bool op_device_memory(echo_ctx *c, const void *p) {
   return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == c->device);
 }
 
-cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch) { return timed(c, name, launch); }
+cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch) {
+  if (!c->prof) return launch();
+  bool capturing = false;  // (a capture runs nothing: events recorded in it have no times)
+  if (op_capturing(c, &capturing) == ECHO_OK && capturing) return launch();
+  return timed(c, name, launch);
+}
 
 }  // namespace echo
 

@@ -34,7 +34,7 @@ int op_scratch(echo_ctx *c, size_t bytes, void **p);
 bool op_device_memory(echo_ctx *c, const void *p);
 // Word of the context in host memory that kernels set when a wait gives up.
 int op_status(echo_ctx *c, int32_t **p);
-// Runs a launch, between two events while the context is profiled.
+// Runs a launch, between two events while the context is profiled and its stream not captured.
 cudaError_t op_launch(echo_ctx *c, const char *name, const std::function<cudaError_t()> &launch);
 
 // -- launches ------------------------------------------------------------------------------

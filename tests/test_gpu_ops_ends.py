@@ -258,3 +258,24 @@ def test_the_measured_optimizer_step_is_a_whole_one(echo):
     got = (w.double() - w2.double()) / 0.125
     # the update's own error, and a rounding of the weights in fp32, eight times as large in it
     assert float((got - want).norm()) <= 102 * 2.0 ** -22 * float(want.norm()) + 8 * 2.0 ** -24 * float(w2.double().norm())
+
+
+def test_captured_calls_are_not_profiled():
+    """A capture runs nothing, so it has no times: the profile holds what ran between its events, and no error is left behind."""
+    side = torch.cuda.Stream()
+    x = _randn((64, 512), 80)
+    with Echo(0, stream=side) as e, torch.cuda.stream(side):
+        want = e.layer_norm(x)[0]
+        e.set_profiling(True)
+        e.layer_norm(x)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            y = e.layer_norm(x)[0]
+        graph.replay()
+        (name, (launches, ms)), = e.read_profile().items()
+        assert launches == 1 and ms > 0
+        assert torch.equal(y, want)
+        e.layer_norm(x)
+        assert e.read_profile()[name][0] == 1
+        torch.cuda.current_stream().synchronize()
