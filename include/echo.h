@@ -12,8 +12,9 @@
  *   echo_compose               timeline composer (Sec. 4.2) + validator adjustment (Sec. 3, 6)
  *   echo_read_*                per-op start/finish, step makespan, CC estimates
  *
- * Beside it, echo_embed, echo_layer_norm, echo_orthogonalize and their gradients run
- * operators of a training step on the device, whose measured times are such durations.
+ * Beside it, echo_embed, echo_layer_norm, echo_rotary, echo_cross_entropy, echo_distill,
+ * their gradients and echo_orthogonalize run operators of a training step on the device,
+ * whose measured times are such durations.
  *
  * Conventions for every call:
  *   - The return value is an echo_status; ECHO_OK (0) on success.  On failure the
@@ -351,7 +352,7 @@ int echo_measure_fp64(int device, double *rates);
 /*
  * Operators of a rank's training step.  An execution graph's compute ops stand for
  * kernels whose durations a tracer measures on one device (Sec. 4.1); these calls run
- * the memory-bound and optimizer ones among them on this device, so that their times
+ * the memory-bound ones, the head's loss and the optimizer's among them on this device, so that their times
  * (of a captured row of calls: echo_set_profiling adds events to each) can go into
  * echo_load_scenarios.
  *   - Arrays are DEVICE memory of the context's device, owned by the caller, each at a
@@ -479,6 +480,126 @@ typedef struct {
   float a, b, c, eps, scale;
 } echo_orthogonalize_desc;
 int echo_orthogonalize(echo_ctx *ctx, const echo_orthogonalize_desc *d);
+
+/* Softmax cross entropy of a language model's head (kernel classes of the last pipeline
+ * stage: the product with the vocabulary and the loss), straight from hidden states and a
+ * vocabulary shard of the head's weight, without keeping the logits.  With
+ * z[t][v] = scale * <x[t], weight[v]>, for every token t:
+ *   lse = log(sum over the shard's rows of exp(z[t][v])) (-infinity without rows),
+ *   target = z[t][label - vocab_start], 0 where the shard has no such row,
+ *   loss = lse - target, 0 where label < 0 (an ignored token).
+ * Of one shard of many, the loss is not of use: the loss of the whole vocabulary is the
+ * logarithm of the sum of the shards' exp(lse) minus the sum of their targets.
+ * Each of loss, lse and target may be NULL.  n_tokens and vocab_rows may be 0; hidden is 1
+ * to 2^24, n_tokens and vocab_rows at most 2^30.  The sums of fp32 matrices are of 22 bits of
+ * elements down to 2^-14 of the matrix's largest one, with an error of 2^-37 of that in
+ * smaller ones. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start;
+  const void *x;      /* [n_tokens][hidden]                                             */
+  const void *weight; /* [vocab_rows][hidden]                                           */
+  const void *labels; /* [n_tokens] int32 or int64                                      */
+  float *loss, *lse, *target; /* [n_tokens]                                             */
+  int64_t x_stride, weight_stride;
+  int32_t type;       /* of x and weight                                                */
+  int32_t id_bits;    /* of labels: 32 or 64                                            */
+  float scale;
+} echo_cross_entropy_desc;
+int echo_cross_entropy(echo_ctx *ctx, const echo_cross_entropy_desc *d);
+
+/* Gradients of the loss above, given lse of the whole vocabulary (the shard's own where it
+ * is whole) and the gradients of loss and, if not NULL, of lse:
+ *   dz[t][v] = (dloss[t] + dlse[t]) * exp(z[t][v] - lse[t]) - dloss[t] where v is the label's row,
+ *   dx = scale * dz * weight,  dweight = scale * dz^T * x,
+ * with 0 for dloss[t] where label < 0.  dx has x's type and is this shard's part of the sum
+ * over shards.  dweight is written (accumulate = 0; zeros without tokens) or added to (1).
+ * Each of dx and dweight may be NULL.  A token whose dloss (or label) and dlse are 0 has no
+ * gradient and adds none to dweight, whatever its x holds.
+ * dz is rounded to the matrices' 16-bit type where the results have 16 bits, and taken to 22
+ * bits for fp32 ones.  fp16: elements of dz below 2^-29 of the largest are rounded to
+ * multiples of 2^-40 of it. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start;
+  const float *dloss;       /* [n_tokens]                                               */
+  const float *dlse;        /* [n_tokens] or NULL (0)                                   */
+  const void *x, *weight, *labels;
+  const float *lse;         /* [n_tokens]                                               */
+  void *dx, *dweight;       /* [n_tokens][hidden], [vocab_rows][hidden]                 */
+  int64_t x_stride, weight_stride, dx_stride, dweight_stride;
+  int32_t type;             /* of x, weight and dx                                      */
+  int32_t dweight_type, id_bits;
+  int32_t accumulate;
+  float scale;
+} echo_cross_entropy_grad_desc;
+int echo_cross_entropy_grad(echo_ctx *ctx, const echo_cross_entropy_grad_desc *d);
+
+/* Distillation of a head from a teacher's top logits.  Token t has n_top entries, each a
+ * token id and the teacher's logit; entries with id < 0 or logit -infinity are missing.
+ * With T the temperature and z as above:
+ *   q[k] = exp(logit[k] / T - L), L = log of the sum of exp(logit / T) over the entries, or
+ *          teacher_lse[t], of all of the teacher's logits over T, where that is not NULL,
+ *   lse = log(sum over the shard's rows of exp(z / T)),
+ *   cross = sum of q[k] * z[t][id[k] - vocab_start] / T over the entries of the shard's rows,
+ *   loss = T^2 * (sum of q log q + (sum of q) * lse - cross), 0 without entries.
+ * Entries with the same id add up.  Shards are put together as for the cross entropy.
+ * n_top is 1 to 256. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start, n_top;
+  const void *x, *weight;
+  const void *ids;          /* [n_tokens][n_top] int32 or int64                         */
+  const void *logits;       /* [n_tokens][n_top] of logits_type                         */
+  const float *teacher_lse; /* [n_tokens] or NULL                                       */
+  float *loss, *lse, *cross; /* [n_tokens], each may be NULL                            */
+  int64_t x_stride, weight_stride;
+  int32_t type, id_bits, logits_type;
+  float scale, temperature; /* temperature > 0                                          */
+} echo_distill_desc;
+int echo_distill(echo_ctx *ctx, const echo_distill_desc *d);
+
+/* Gradients of the distillation's loss for x and weight (the teacher has none), with lse of
+ * the whole vocabulary at that temperature:
+ *   dz[t][v] = T * dloss[t] * ((sum of q) * exp(z / T - lse) - sum of q[k] where v is id[k]'s row)
+ *              + dlse[t] / T * exp(z / T - lse),
+ * and all else as in echo_cross_entropy_grad. */
+typedef struct {
+  int64_t n_tokens, hidden, vocab_rows, vocab_start, n_top;
+  const float *dloss, *dlse;
+  const void *x, *weight, *ids, *logits;
+  const float *teacher_lse, *lse;
+  void *dx, *dweight;
+  int64_t x_stride, weight_stride, dx_stride, dweight_stride;
+  int32_t type, dweight_type, id_bits, logits_type;
+  int32_t accumulate;
+  float scale, temperature;
+} echo_distill_grad_desc;
+int echo_distill_grad(echo_ctx *ctx, const echo_distill_grad_desc *d);
+
+/* Rotary positions (the `rotary` kernels of every layer) of queries and keys, as up to two
+ * arrays of heads in one pass.  In each head the pairs i of the first `rot` of its `dim`
+ * elements, elements (i, i + rot / 2) or, interleaved, (2 i, 2 i + 1), become
+ *   a' = scale * (a * cos(w) - b * sin(w)),  b' = scale * (a * sin(w) + b * cos(w)),
+ * with w = positions[b][t] * frequencies[i] in radians, exact to fp32's last bits for every
+ * position; the other elements are copied.  out has x's type and may be x itself (same
+ * strides).  echo_rotary_grad turns back (w negative): given the gradients of out it
+ * returns those of x.
+ * Strides are those of a batch, a token and a head; elements of a head are contiguous.  An
+ * output's heads must not overlap.  dim is 1 to 65536, rot even and 2 to 512. */
+typedef struct {
+  int64_t n_batch, n_tokens;
+  int64_t heads[2];          /* of each array; 0: none                                  */
+  const void *x[2];          /* [n_batch][n_tokens][heads][dim]                         */
+  void *out[2];
+  int64_t x_batch_stride[2], x_stride[2], x_head_stride[2];
+  int64_t out_batch_stride[2], out_stride[2], out_head_stride[2];
+  const void *positions;     /* [n_batch][n_tokens] int32 or int64                      */
+  int64_t positions_stride;  /* of a batch; 0 for the same ones in each                 */
+  const double *frequencies; /* HOST memory: [rot / 2], |frequency| <= 2^32             */
+  int32_t dim, rot, type, id_bits;
+  int32_t interleaved;
+  float scale;
+} echo_rotary_desc;
+int echo_rotary(echo_ctx *ctx, const echo_rotary_desc *d);
+int echo_rotary_grad(echo_ctx *ctx, const echo_rotary_desc *d);
 
 const char *echo_strerror(int status);
 /* Copies the context's last error message (NUL-terminated) into buf. */

@@ -4,6 +4,6 @@
 hot path (CC estimation, composition, overlap adjustment) runs in ``libecho.so``.
 ``workloads`` builds seeded synthetic Megatron-shaped inputs.
 """
-from .echo import Echo, EchoError, check_graph, load_library, library_path  # noqa: F401
+from .echo import Echo, EchoError, check_graph, load_library, library_path, rotary_frequencies  # noqa: F401
 
-__all__ = ["Echo", "EchoError", "check_graph", "load_library", "library_path"]
+__all__ = ["Echo", "EchoError", "check_graph", "load_library", "library_path", "rotary_frequencies"]

@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libecho.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 # (source, extra nvcc flags, object)
 UNITS = [(f, [], f + ".o") for f in ("echo_kernels.cu", "echo_compose.cu", "echo_levels.cu", "echo_dataflow.cu", "echo_host.cpp",
-                                        "echo_ops.cpp", "echo_ops_embed.cu", "echo_ops_norm.cu", "echo_ops_ortho.cu")] + [
+                                        "echo_ops.cpp", "echo_ops_embed.cu", "echo_ops_norm.cu", "echo_ops_ortho.cu",
+                                        "echo_ops_head.cu", "echo_ops_rotary.cu")] + [
     ("echo_overlap.cu", [f"-DECHO_OV_LAUNCH={l}", f"-DECHO_OV_PROP={p}"], f"echo_overlap_l{l}_p{p}.o")
     for l in (0, 1) for p in (0, 1)]
 SOURCES = sorted({u[0] for u in UNITS})

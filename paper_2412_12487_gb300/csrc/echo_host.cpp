@@ -1577,6 +1577,7 @@ struct echo_ctx {
   int cc_model = ECHO_CC_MODEL_WHITEBOX;
   int est_policy = ECHO_AR_PER_OP;  // all-reduce policy of the current estimates
   long long wait_limit_cycles = 0;  // bound of every device-side wait
+  int64_t head_piece = echo::head_piece_bytes();  // scratch of a head's gradient for a piece of the vocabulary
   int32_t skip_level = -1;          // failure injection for tests
   // scratch for readback / queries
   void *stage = nullptr;
@@ -1887,7 +1888,7 @@ namespace echo {
 int op_context(echo_ctx *c, OpContext *o) {
   const int rc = check_ctx(c);
   if (rc) return rc;
-  *o = {c->device, c->sms, c->stream, c->wait_limit_cycles, c->skip_level};
+  *o = {c->device, c->sms, c->stream, c->wait_limit_cycles, c->skip_level, c->head_piece};
   return ECHO_OK;
 }
 // Whether the context's stream is being captured into a graph.
@@ -2061,6 +2062,7 @@ int echo_create(echo_ctx **out, int device, void *cuda_stream) {
   double limit_ms = 2000.0;
   if (const char *e = std::getenv("ECHO_TEST_WAIT_LIMIT_MS")) limit_ms = std::atof(e);
   c->wait_limit_cycles = (long long)(std::max(clock_khz, 1000) * limit_ms);
+  if (const char *e = std::getenv("ECHO_TEST_HEAD_PIECE")) c->head_piece = std::atoll(e);
   if (const char *e = std::getenv("ECHO_TEST_SKIP_LEVEL")) c->skip_level = std::atoi(e);
   *out = c;
   return ECHO_OK;

@@ -18,6 +18,7 @@ struct OpContext {
   cudaStream_t stream;
   long long wait_limit;  // bound of every device-side wait, in SM clock cycles
   int skip;              // failure injection for tests (-1: none)
+  int64_t head_piece;    // scratch of a head's gradient for a piece of the vocabulary, at most
 };
 // Makes the context's device current; an echo_status.
 int op_context(echo_ctx *c, OpContext *o);
@@ -119,5 +120,52 @@ struct OrthoArgs {
 };
 size_t ortho_scratch_bytes(const OrthoArgs &a, int sms);
 cudaError_t launch_orthogonalize(const OrthoArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
+
+// Losses of a head and their gradients (echo_ops_head.cu): a list of K targets a token, labels
+// (K = 1, no logits) or a teacher's top logits.
+struct HeadArgs {
+  bool grad;
+  int64_t n, H, V, v0;      // tokens, row length, rows of the shard, its first id
+  const void *x, *w;
+  int64_t x_stride, w_stride;
+  int type;
+  const void *ids;
+  int id64, K;
+  const void *logits;
+  int logits_type;
+  const float *teacher_lse;
+  float scale, tau;
+  float *loss, *lse, *part;                // forward; `part`: sum of q z over the shard's targets
+  const float *dloss, *dlse, *lse_in;      // backward
+  void *dx, *dw;
+  int64_t dx_stride, dw_stride;
+  int dw_type, accumulate;
+  int64_t piece_bytes;      // of scratch for a piece of the vocabulary
+  void *scratch;
+  int32_t *status;          // of op_status
+  long long wait_limit;     // bound of every wait of the kernels, in SM clock cycles
+  int skip;                 // failure injection for tests
+};
+int64_t head_piece_bytes();
+int head_most_targets();
+size_t head_scratch_bytes(const HeadArgs &a, int sms);
+cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaStream_t st);
+
+// Rotary positions of up to two arrays [batch][tokens][heads][dim] (strides in elements).
+constexpr int kRotaryPairs = 256;
+struct RotaryArgs {
+  int64_t batch, tokens, heads[2];
+  const void *x[2];
+  void *out[2];
+  int64_t x_batch[2], x_token[2], x_head[2], out_batch[2], out_token[2], out_head[2];
+  const void *positions;
+  int64_t positions_batch;
+  int id64, dim, rot, type, interleaved;
+  bool back;                // the turn back
+  float scale;
+  uint64_t turns[kRotaryPairs];  // of a position, times 2^64
+};
+uint64_t rotary_turns(double frequency);
+cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st);
 
 }  // namespace echo

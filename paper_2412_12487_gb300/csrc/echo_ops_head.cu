@@ -1,0 +1,964 @@
+// echo_ops_head.cu -- losses of a language model's head, straight from hidden states and the
+// head's weight: softmax cross entropy and distillation from a teacher's top logits, with their
+// gradients.
+//
+// With z[t][v] = <x_t, w_v> scale / tau over the rows of a vocabulary shard, both losses are
+//   tau^2 (sum q log q + Q lse - cross),  lse = log sum exp z,  cross = sum of q_k z[id_k],
+// for a list of targets (id_k, q_k) a token with Q = sum q_k: one label with q = 1, or a teacher's
+// top logits.  The gradient of the products <x_t, w_v> is
+//   P[t][v] = coef_t exp(z - lse) - (sum of weight_k where id_k = v),
+// and dx = P W, dW = P^T x.
+//
+// The logits are never kept.  Forward, each tile of the product leaves the largest element and
+// the sum of exponentials of each of its rows, and the elements that a target names; a small
+// kernel joins them.  Backward, the product is made again for a piece of the vocabulary, whose
+// part of P goes to scratch memory for the two products that follow.
+//
+// Operands are 16-bit numbers on the tensor cores, with sums in fp32:
+//   - bf16 and fp16 matrices as they are; fp32 ones as sums of two fp16 numbers times a power of
+//     two that the largest element sets (22 bits of elements down to 2^-14 of it, an error of
+//     2^-37 of it below), multiplied as high * high + high * low + low * high;
+//   - P as one number of the matrices' type where the results have 16 bits: an error of 2^-9
+//     (bf16) of each element, independent of the others, where the results are rounded to the
+//     same.  For an fp32 dW as the sum of two fp16 numbers, with x as fp16 (the same way): a
+//     gradient added up over micro-batches in fp32 would otherwise be 2e-3 off.
+// The tensor core truncates the sums that it adds to, so they are added up in registers, rounding
+// to nearest, every kSet stages.
+#include <algorithm>
+#include <cfloat>
+#include <climits>
+#include <cmath>
+
+#include "echo_ops.h"
+#include "echo_tensor.cuh"
+
+namespace echo {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kAmaxParts = 304;  // blocks that look for a largest element, at most
+
+// Where the exponent of a matrix's power of two comes from: the largest elements that blocks
+// found.  None: the matrix is as it is.
+struct Scale {
+  const float *part;
+  int parts;
+};
+// By a warp, the same in all lanes: the largest element times 2^exponent is 2^14 to 2^15, if it is
+// within 2^-96 and 2^124.
+__device__ __forceinline__ int exponent(Scale s) {
+  float m = 0.f;
+  for (int i = threadIdx.x & 31; i < s.parts; i += 32) m = fmaxf(m, s.part[i]);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  return m > 0.f ? max(-110, min(110, 14 - ilogbf(m))) : 0;
+}
+__device__ __forceinline__ float finite_size(float x) {
+  x = fabsf(x);
+  return x <= FLT_MAX ? x : 0.f;
+}
+
+// -- operands as the tensor cores take them ----------------------------------------------------
+// [plane][rows][ld] 16-bit elements; plane 1 is what plane 0 leaves of an element.
+struct Operand {
+  const void *p;
+  int64_t rows, cols, ld, plane;
+  int planes;
+  bool bf16;
+  Scale scale;
+};
+
+// The largest finite element of each block's part of a matrix (without gaps, a single row).
+// Bound by the bytes.
+template <typename T, int W>
+__global__ void __launch_bounds__(256) head_amax_kernel(const T *x, int64_t rows, int64_t cols, int64_t stride, float *part) {
+  __shared__ float sh[8];
+  kernel_begin();
+  next_may_start();
+  const int64_t pieces = cols / W, all = rows * pieces;
+  float m = 0.f;
+  constexpr int kFlight = 4;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
+    float v[kFlight][W];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const int64_t i = i0 + k * 256;
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[k][e] = 0.f;
+      if (i < all) load_piece<W>(rows == 1 ? x + i * W : x + i / pieces * stride + i % pieces * W, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+#pragma unroll
+      for (int e = 0; e < W; ++e) m = fmaxf(m, finite_size(v[k][e]));
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) m = fmaxf(m, sh[w]);
+    part[blockIdx.x] = m;
+  }
+}
+
+// A matrix as PLANES planes of type D (fp16 ones times 2^exponent); rows that are not live become
+// zeros, so that whatever they hold (padding) meets nothing in a product.  Bound by the bytes.
+template <typename T, typename D, int PLANES, int W>
+__global__ void __launch_bounds__(256) head_pack_kernel(const T *x, int64_t rows, int64_t cols, int64_t stride, Scale scale, const float *live, D *to,
+                                                        int64_t ld, int64_t plane) {
+  __shared__ int sh;
+  kernel_begin();
+  next_may_start();
+  if (threadIdx.x < 32) {
+    const int e = exponent(scale);
+    if (threadIdx.x == 0) sh = e;
+  }
+  __syncthreads();
+  const float up = ldexpf(1.f, sh);
+  const uint32_t pieces = (uint32_t)(cols / W);
+  const int64_t all = rows * pieces;
+  constexpr int kFlight = 4;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
+    float v[kFlight][W];
+    int64_t at[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const int64_t i = i0 + k * 256;
+      if (i >= all) continue;
+      const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), c = i - r * pieces;
+      at[k] = r * ld + c * W;
+      if (!live || live[r] != 0.f) {
+        load_piece<W>(x + r * stride + c * W, v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[k][e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      if (i0 + k * 256 >= all) continue;
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[k][e] *= up;
+#pragma unroll
+      for (int q = 0; q < PLANES; ++q) {
+        Pack<D, W> h;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          h.v[e] = from_f<D>(v[k][e]);
+          v[k][e] -= to_f(h.v[e]);  // what the next plane holds
+        }
+        *reinterpret_cast<Pack<D, W> *>(to + q * plane + at[k]) = h;
+      }
+    }
+  }
+}
+
+// -- targets -------------------------------------------------------------------------------------
+// A token's targets in the order of their rows: [tokens][K] rows of the shard (INT_MAX: none) and
+// weights; what the loss needs beside them.
+struct Targets {
+  int32_t *idx;
+  float *weight;
+  float *coef;            // backward: of the softmax
+  float *live;            // backward: 0 where a token has no gradient
+  float *entropy, *mass;  // forward: sum q log q, Q
+  float *size_part;       // backward: the largest |coef| + sum |weight| of a block's tokens
+};
+
+constexpr int kTargetWarps = 8;
+constexpr int kMaxTargets = 256;
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+  return v;
+}
+
+__device__ __forceinline__ int64_t id_at(const HeadArgs &a, int64_t i) {
+  return a.id64 ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
+}
+__device__ __forceinline__ int32_t row_of(const HeadArgs &a, int64_t id) {
+  return id >= a.v0 && id - a.v0 < a.V ? (int32_t)(id - a.v0) : INT_MAX;
+}
+
+// A warp per token: the teacher's distribution, sorted by row by counting the rows before each.
+__global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArgs a, Targets o) {
+  __shared__ int32_t rows[kTargetWarps][kMaxTargets];
+  __shared__ float sizes[kTargetWarps];
+  kernel_begin();
+  next_may_start();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool grad = a.grad;
+  float largest = 0.f;
+  for (int64_t t = (int64_t)blockIdx.x * kTargetWarps + warp; t < a.n; t += (int64_t)gridDim.x * kTargetWarps) {
+    float up = 0.f, lse_up = 0.f;  // of the loss (times tau) and of lse (over tau)
+    if (grad) {
+      up = a.scale * a.tau * a.dloss[t];
+      if (a.dlse) lse_up = a.scale / a.tau * a.dlse[t];
+    }
+    float coef, size;
+    if (!a.logits) {
+      const int64_t id = id_at(a, t);
+      const bool valid = id >= 0;
+      const float q = valid ? (grad ? up : 1.f) : 0.f;
+      if (lane == 0) {
+        o.idx[t] = valid ? row_of(a, id) : INT_MAX;
+        o.weight[t] = q;
+        if (!grad) o.entropy[t] = 0.f, o.mass[t] = q;
+      }
+      coef = q + lse_up;
+      size = fabsf(coef) + fabsf(q);
+    } else {
+      float v[kMaxTargets / 32];
+      int32_t row[kMaxTargets / 32];
+      float most = -INFINITY;
+      bool any = false;
+      const int own = (a.K - lane + 31) / 32;  // this lane's entries: lane, lane + 32, ...
+#pragma unroll
+      for (int i = 0; i < kMaxTargets / 32; ++i) {
+        v[i] = -INFINITY;
+        row[i] = INT_MAX;
+        if (i >= own) continue;
+        const int64_t at = t * a.K + lane + 32 * i, id = id_at(a, at);
+        if (id >= 0) {
+          float logit;
+          load_param<1>(a.logits, a.logits_type, at, 0.f, &logit);
+          v[i] = logit / a.tau;
+          row[i] = row_of(a, id);
+          any |= !(v[i] == -INFINITY);
+        }
+        most = fmaxf(most, v[i]);
+        rows[warp][lane + 32 * i] = row[i];
+      }
+      any = __any_sync(0xFFFFFFFFu, any);
+      most = warp_max(most);
+      float log_sum = a.teacher_lse ? a.teacher_lse[t] : 0.f;
+      if (!a.teacher_lse) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMaxTargets / 32; ++i)
+          if (i < own && !(v[i] == -INFINITY)) sum += expf(v[i] - most);
+        log_sum = most + logf(warp_sum(sum));
+      }
+      float mass = 0.f, entropy = 0.f;
+#pragma unroll
+      for (int i = 0; i < kMaxTargets / 32; ++i) {
+        if (i >= own) continue;
+        const bool has = !(v[i] == -INFINITY);  // (a missing entry, or one without weight)
+        const float log_q = has ? v[i] - log_sum : 0.f, q = has ? expf(log_q) : 0.f;
+        mass += q;
+        entropy += q * log_q;
+        v[i] = grad && has ? q * up : q;
+      }
+      mass = warp_sum(mass);
+      entropy = warp_sum(entropy);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kMaxTargets / 32; ++i) {
+        if (i >= own) continue;
+        const int k = lane + 32 * i;
+        int before = 0;
+        for (int j = 0; j < a.K; ++j) before += rows[warp][j] < row[i] || (rows[warp][j] == row[i] && j < k);
+        o.idx[t * a.K + before] = row[i];
+        o.weight[t * a.K + before] = v[i];
+      }
+      __syncwarp();
+      if (!grad && lane == 0) o.entropy[t] = entropy, o.mass[t] = any ? mass : 0.f;
+      coef = (any ? up * mass : 0.f) + lse_up;
+      size = fabsf(coef) + (any ? fabsf(up) * mass : 0.f);
+    }
+    if (grad && lane == 0) {
+      o.coef[t] = coef;
+      o.live[t] = size;
+    }
+    largest = fmaxf(largest, finite_size(size));
+  }
+  if (!grad) return;
+  if (lane == 0) sizes[warp] = largest;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kTargetWarps; ++w) largest = fmaxf(largest, sizes[w]);
+    o.size_part[blockIdx.x] = largest;
+  }
+}
+
+// -- products --------------------------------------------------------------------------------------
+// D = A B^T on tiles of 256 x 256 by persistent pairs of blocks (echo_tensor.cuh).  The sum may run
+// along the rows of an operand in memory (K-major) or down its columns (MN-major), and over several
+// pairs of planes.  A launch has up to two products, whose tiles follow one another.
+constexpr int kTile = 256, kHalf = 128, kBK = 64;
+constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
+constexpr int kFewRegs = 56, kManyRegs = 216;    // a thread of warps 0-3 and of 4-11
+static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
+constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
+constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out
+constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kOutBytes + 256 + 1024;
+constexpr int kSet = 4;                          // stages that the tensor core adds up by itself
+
+struct Job {
+  int M, N, steps;  // rows, columns; stages of a pair of planes
+  int pairs, plane_a[3], plane_b[3];
+  int a_mn, b_mn;
+  uint32_t instr;
+  int tiles_n;
+  int64_t tiles;
+  Scale scale_a, scale_b;
+  // D, times 2^-(both exponents), plus `from`, plus what `out` holds
+  void *out;
+  int64_t out_stride;
+  int type, add;
+  const float *from;
+  int64_t from_stride;
+};
+struct HeadProduct {
+  Job job[2];
+  int64_t tiles;     // of both
+  WaitLimit wait;
+  int skip;          // failure injection for tests: this 64-column step is never copied (-1: none)
+  // the logits' product
+  int64_t n;         // tokens
+  int K, v_begin;    // targets of a token; the piece's first row
+  float alpha;       // scale / tau
+  const int32_t *idx;
+  const float *weight, *coef, *lse;
+  float2 *part;      // [columns / 128][n] largest element (times log2 e) and sum of exponentials
+  float *picked;     // [n][K] z of the targets
+  int p_bf16, p_half;  // planes of P: one of bf16, of fp16
+  Scale p_scale;       // of the fp16 ones
+};
+enum { kStats, kGrad, kOut };  // what becomes of the sums
+
+__device__ __forceinline__ void tile_place(const Job &j, int64_t t, int &r0, int &c0) {
+  const int64_t rows = (j.M + kTile - 1) / kTile, band = t / (8 * j.tiles_n), in = t % (8 * j.tiles_n), high = min((int64_t)8, rows - band * 8);
+  r0 = (int)(band * 8 + in % high) * kTile;
+  c0 = (int)(in / high) * kTile;
+}
+
+__device__ __forceinline__ void copy_rows(uint32_t to, const CUtensorMap *map, bool mn, int r, int k, int plane, uint32_t bar) {
+  if (mn) {
+    copy_tile(to, map, r, k, 0, plane, bar);
+    copy_tile(to + 8192, map, r + 64, k, 0, plane, bar);
+  } else {
+    copy_tile(to, map, k, r, 0, plane, bar);
+  }
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// 32 x 32 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
+template <typename T>
+__device__ __forceinline__ void block_out(const Job &j, int row0, int c, int lane, float f1, float f2, const float (&v)[32], unsigned char *buffer) {
+  float *f = reinterpret_cast<float *>(buffer);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[lane * 32 + (i ^ lane)] = v[i] * f1 * f2;
+  __syncwarp();
+  if (c + lane >= j.N) return;
+  T *o = static_cast<T *>(j.out) + (int64_t)row0 * j.out_stride + c + lane;
+  const float *from = j.from + (int64_t)row0 * j.from_stride + c + lane;
+  const int rows = min(32, j.M - row0);
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 8) {
+    float x[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      x[r] = 0.f;
+      if (r0 + r >= rows) continue;
+      if (j.from) x[r] = from[(int64_t)(r0 + r) * j.from_stride];
+      if (j.add) x[r] += to_f(o[(int64_t)(r0 + r) * j.out_stride]);
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (r0 + r < rows) o[(int64_t)(r0 + r) * j.out_stride] = from_f<T>(f[(r0 + r) * 32 + (lane ^ (r0 + r))] + x[r]);
+  }
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    head_product_kernel(const __grid_constant__ CUtensorMap amap0, const __grid_constant__ CUtensorMap bmap0, const __grid_constant__ CUtensorMap amap1,
+                        const __grid_constant__ CUtensorMap bmap1, const __grid_constant__ CUtensorMap pmap, const __grid_constant__ HeadProduct a) {
+  extern __shared__ unsigned char raw[];
+  unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
+  unsigned char *buffers = base + kStages * kStageBytes;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(buffers + 8 * kOutBytes);
+  __shared__ uint32_t tmem_base;
+  __shared__ int give_up;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;  // (clusters of two along x)
+  // `full` and `sums_empty` are used in the first block alone, the others in both
+  const uint32_t ring = smem_u32(base), full = smem_u32(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages, sums_empty = sums_full + 16,
+                 done = sums_empty + 16;
+  volatile int *abort = &give_up;
+  if (threadIdx.x == 0) {
+    give_up = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(sums_full + 8 * b, 1);
+      bar_init(sums_empty + 8 * b, 16);
+    }
+    bar_init(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (threadIdx.x == 32 * 3) asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&amap0), "l"(&bmap0) : "memory");
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base)), "r"(2u * kTile) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  cluster_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+  const uint32_t tmem = tmem_base;
+  // What is above overlaps the end of the kernel before; from here on its results are read.
+  kernel_begin();
+  next_may_start();
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kFewRegs));
+    if (warp == 0 && lane == 0) {
+      int64_t it = 0;
+      bool ok = true;
+      for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
+        const int which = MODE == kOut && i >= a.job[0].tiles;
+        const Job &j = a.job[which];
+        const CUtensorMap *amap = which ? &amap1 : &amap0, *bmap = which ? &bmap1 : &bmap0;
+        int r0, c0;
+        tile_place(j, which ? i - a.job[0].tiles : i, r0, c0);
+        for (int p = 0; p < j.pairs && ok; ++p)
+          for (int k = 0; k < j.steps; ++k, ++it) {
+            const int s = (int)(it % kStages);
+            ok = k != a.skip && bar_wait(empty + 8 * s, (uint32_t)(it / kStages + 1) & 1, abort, a.wait);
+            if (!ok) break;
+            const uint32_t at = ring + s * kStageBytes, bar = in_first(full + 8 * s);
+            if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);  // both blocks' copies
+            copy_rows(at, amap, j.a_mn, r0 + rank * kHalf, k * kBK, j.plane_a[p], bar);
+            copy_rows(at + kOperandBytes, bmap, j.b_mn, c0 + rank * kHalf, k * kBK, j.plane_b[p], bar);
+          }
+      }
+      if (!ok) {  // what is still being copied lands long before this
+        const long long t0 = clock64();
+        while (clock64() - t0 < 1000000) {
+        }
+      }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+      int64_t it = 0, set = 0;
+      bool ok = true;
+      for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
+        const Job &j = a.job[MODE == kOut && i >= a.job[0].tiles];
+        const int steps = j.steps * j.pairs, step_a = step16(j.a_mn), step_b = step16(j.b_mn);
+        for (int k = 0; k < steps; ++k, ++it) {
+          const int b = (int)(set & 1), s = (int)(it % kStages);
+          ok = (k % kSet || bar_wait(sums_empty + 8 * b, (uint32_t)(set / 2 + 1) & 1, abort, a.wait)) &&
+               bar_wait(full + 8 * s, (uint32_t)(it / kStages) & 1, abort, a.wait);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+          const uint32_t d = tmem + b * kTile;
+          const uint64_t p = operand(ring + s * kStageBytes, j.a_mn), q = operand(ring + s * kStageBytes + kOperandBytes, j.b_mn);
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step_a * kk, q + step_b * kk, j.instr, kk > 0 || k % kSet);
+          commit_pair(empty + 8 * s);
+          if (k % kSet == kSet - 1 || k == steps - 1) {
+            commit_pair(sums_full + 8 * b);
+            ++set;
+          }
+        }
+      }
+      commit(done);  // nothing is in flight when the block ends
+      const long long t0 = clock64();
+      while (!bar_try(done, 0) && clock64() - t0 <= a.wait.clocks) {
+      }
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kManyRegs));
+    const int quarter = warp & 3, side = (warp - 4) >> 2;  // (a warp reaches the 32 rows of tensor memory of its number modulo 4)
+    unsigned char *buffer = buffers + (warp - 4) * kOutBytes;
+    const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + side * kHalf;
+    constexpr int kParts = kHalf / 32;
+    int down[2] = {0, 0};
+    for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
+    const float alpha = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]), alpha2 = alpha * kLog2e;
+    const float p_up = MODE == kGrad ? ldexpf(1.f, exponent(a.p_scale)) : 1.f;
+    int64_t n = 0;
+    uint32_t turn = 0;
+    bool ok = true;
+    for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
+      const int which = MODE == kOut && i >= a.job[0].tiles;
+      const Job &j = a.job[which];
+      int r0, c0;
+      tile_place(j, which ? i - a.job[0].tiles : i, r0, c0);
+      const int row0 = r0 + rank * kHalf + quarter * 32;
+      c0 += side * kHalf;
+      // what the tile's end needs comes during the sums
+      const int64_t row = row0 + lane;
+      const bool in = row < j.M;
+      int k_at = 0, next = INT_MAX;
+      float coef = 0.f, shift = 0.f;
+      if (MODE != kOut && in) {
+        const int32_t *idx = a.idx + row * a.K;
+        for (int hi = a.K; k_at < hi;) {
+          const int mid = (k_at + hi) / 2;
+          if (idx[mid] < a.v_begin + c0) k_at = mid + 1;
+          else hi = mid;
+        }
+        if (k_at < a.K && idx[k_at] != INT_MAX) next = idx[k_at] - a.v_begin;
+        if (MODE == kGrad) {
+          // coef exp(z - lse) = coef' exp2(z log2 e - shift): the rounding of shift goes into coef'
+          const float lse = a.lse[row];
+          coef = a.coef[row];
+          shift = lse * kLog2e;
+          const float rest = fmaf(lse, kLog2e, -shift);
+          if (coef != 0.f && fabsf(rest) < 1.f) coef *= exp2f(-rest);
+        }
+      }
+      float acc[kParts][32] = {};
+      const int sets = (j.steps * j.pairs + kSet - 1) / kSet;
+      for (int set = 0; set < sets; ++set) {
+        const int b = (int)(n & 1);
+        ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait);
+        if (!ok) break;
+        ++n;
+        asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          Sums s;
+          __syncwarp();
+          load_sums(from + b * kTile + part * 32, s);
+          sums_loaded();
+          pass(s);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[part][e] += __uint_as_float(s.r[e]);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(in_first(sums_empty + 8 * b));
+      }
+      if (!ok) break;
+      if (row0 >= j.M || c0 >= j.N) continue;
+      if constexpr (MODE == kStats) {
+        if (c0 + kHalf > j.N)
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (c0 + part * 32 + e >= j.N) acc[part][e] = alpha2 < 0.f ? INFINITY : -INFINITY;
+        float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, s[4] = {};
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], acc[part][e] * alpha2);
+        const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), zero = most == -INFINITY ? 0.f : most;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[e & 3] += exp2_fast(fmaf(acc[part][e], alpha2, -zero));
+        if (in) a.part[(int64_t)(c0 / kHalf) * a.n + row] = make_float2(most, (s[0] + s[1]) + (s[2] + s[3]));
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          const int end = c0 + part * 32 + 32;
+          while (__any_sync(0xFFFFFFFFu, next < end)) {
+            const bool hit = next < end;
+            const int at = hit ? next - (end - 32) : -1;
+            float z = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) z = at == e ? acc[part][e] : z;
+            if (hit) {
+              a.picked[row * a.K + k_at] = z * alpha;
+              next = ++k_at < a.K ? a.idx[row * a.K + k_at] : INT_MAX;
+            }
+          }
+        }
+        continue;
+      }
+      // One block after the other, in the registers of the first (unrolled, the code would be long
+      // and runs once a tile).
+      float (&v)[32] = acc[0];
+      const float f1 = ldexpf(1.f, down[which] / 2), f2 = ldexpf(1.f, down[which] - down[which] / 2);
+#pragma unroll 1
+      for (int c = c0; c < min(j.N, c0 + kHalf); c += 32) {
+        if constexpr (MODE == kGrad) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = coef == 0.f ? 0.f : coef * exp2_fast(fmaf(v[e], alpha2, -shift));
+          while (__any_sync(0xFFFFFFFFu, next < c + 32)) {
+            const bool hit = next < c + 32;
+            const int at = hit ? next - c : -1;
+            const float w = hit ? a.weight[row * a.K + k_at] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (at == e) v[e] -= w;
+            if (hit) {
+              next = INT_MAX;
+              if (++k_at < a.K && a.idx[row * a.K + k_at] != INT_MAX) next = a.idx[row * a.K + k_at] - a.v_begin;
+            }
+          }
+#pragma unroll 1
+          for (int q = 0; q < a.p_bf16 + a.p_half; ++q) {
+            Piece h[4];
+            if (q < a.p_bf16) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const Pack<__nv_bfloat16, 8> b = pack<__nv_bfloat16, 8>(v + 8 * e);
+                memcpy(&h[e], &b, sizeof b);
+              }
+            } else {
+              const float up = q == a.p_bf16 ? p_up : 1.f;
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                v[e] *= up;
+                h[e / 8].v[e % 8] = __float2half_rn(v[e]);
+                v[e] -= __half2float(h[e / 8].v[e % 8]);  // what the next plane holds
+              }
+            }
+            half_free(lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<Piece *>(piece(buffer + turn, lane, e)) = h[e];
+            half_written();
+            if (lane == 0) store_half(&pmap, buffer + turn, c, row0, 0, q);
+            turn ^= 2048;
+          }
+        } else {
+          if (j.type == ECHO_F32) block_out<float>(j, row0, c, lane, f1, f2, v, buffer);
+          else if (j.type == ECHO_BF16) block_out<__nv_bfloat16>(j, row0, c, lane, f1, f2, v, buffer);
+          else block_out<__half>(j, row0, c, lane, f1, f2, v, buffer);
+        }
+#pragma unroll
+        for (int part = 1; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[part - 1][e] = acc[part][e];
+      }
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
+    __syncwarp();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+  __syncthreads();
+  cluster_sync();  // (the other block's products read this one's stages, and signal its barriers)
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * kTile) : "memory");
+  }
+}
+
+// -- the end of the forward pass -------------------------------------------------------------------
+// A block joins the parts of 32 rows: a warp every eighth part of all rows, then a warp a row's
+// targets, in their order.
+__global__ void __launch_bounds__(256) head_join_kernel(HeadArgs a, Targets t, const float2 *part, int64_t chunks, const float *picked) {
+  __shared__ float2 sh[8][32];
+  __shared__ float lses[32];
+  kernel_begin();
+  next_may_start();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto join = [](float2 x, float2 y) {  // (an empty part has -inf and 0)
+    const float m = fmaxf(x.x, y.x);
+    if (m == -INFINITY) return make_float2(m, x.y + y.y);
+    return make_float2(m, x.y * exp2f(x.x - m) + y.y * exp2f(y.x - m));
+  };
+  for (int64_t r0 = (int64_t)blockIdx.x * 32; r0 < a.n; r0 += (int64_t)gridDim.x * 32) {
+    float2 s = make_float2(-INFINITY, 0.f);
+    if (r0 + lane < a.n)
+      for (int64_t k = warp; k < chunks; k += 8) s = join(s, part[k * a.n + r0 + lane]);
+    sh[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0) {
+      for (int w = 1; w < 8; ++w) s = join(s, sh[w][lane]);
+      lses[lane] = s.x == -INFINITY ? s.y == 0.f ? -INFINITY : NAN : fmaf(s.x, 0.693147180559945309f, logf(s.y));
+    }
+    __syncthreads();
+    for (int r = warp; r < 32 && r0 + r < a.n; r += 8) {
+      const int64_t row = r0 + r;
+      float cross = 0.f;
+      for (int k = lane; k < a.K; k += 32)
+        if (t.idx[row * a.K + k] != INT_MAX) cross += t.weight[row * a.K + k] * picked[row * a.K + k];
+      cross = warp_sum(cross);
+      if (lane == 0) {
+        const float lse = lses[r], mass = t.mass[row];
+        if (a.loss) a.loss[row] = mass == 0.f ? 0.f : a.tau * a.tau * (t.entropy[row] + fmaf(mass, lse, -cross));
+        if (a.lse) a.lse[row] = lse;
+        if (a.part) a.part[row] = cross;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// -- host -------------------------------------------------------------------------------------------
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+int64_t padded(int64_t x) { return (x + 63) / 64 * 64; }
+
+// Scratch memory, from its beginning on; without an address, its size.
+struct Carver {
+  char *base;
+  size_t at = 0;
+  template <typename T>
+  T *take(int64_t count) {
+    T *p = reinterpret_cast<T *>(base + at);
+    at += up256((size_t)count * sizeof(T));
+    return p;
+  }
+};
+
+// A matrix that the TMA engine can read where it is: 16-byte rows at 16-byte addresses.
+bool readable(const void *p, int64_t rows, int64_t cols, int64_t stride, int type) {
+  return type != ECHO_F32 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride % 8 == 0 && stride >= cols && stride < (int64_t)1 << 38));
+}
+Operand in_place(const void *p, int64_t rows, int64_t cols, int64_t stride, int type) {
+  return {p, rows, cols, rows <= 1 ? padded(cols) : stride, 0, 1, type == ECHO_BF16, {nullptr, 0}};
+}
+
+// Memory of a piece of P at most; a vocabulary whose P is larger is taken in pieces.  Pieces that
+// stay in L2 (129 MB) would save no time: the products are bound by the tensor cores, and each
+// piece of dx is added up in memory.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+
+struct Layout {
+  Targets targets;
+  float2 *part;
+  float *picked;
+  int64_t chunks;
+  float *amax_x, *amax_w;
+  Operand x, w;       // of the logits' product (w: of dx too)
+  Operand x_dw;       // of dW
+  bool pack_x, pack_w, pack_x_dw;
+  int target_blocks;
+  // P: planes of a piece
+  int p_bf16, p_half;
+  int64_t piece, ldp;
+  uint16_t *P;
+  float *dx_sum;      // fp32, where dx is added up over pieces
+  size_t bytes;
+};
+
+Layout layout_of(const HeadArgs &a, int sms) {
+  Layout l{};
+  Carver c{static_cast<char *>(a.scratch)};
+  const bool f32 = a.type == ECHO_F32;
+  l.target_blocks = (int)std::min<int64_t>((a.n + kTargetWarps - 1) / kTargetWarps, 2 * sms);
+  l.targets.idx = c.take<int32_t>(a.n * a.K);
+  l.targets.weight = c.take<float>(a.n * a.K);
+  l.amax_x = c.take<float>(kAmaxParts);
+  l.amax_w = c.take<float>(kAmaxParts);
+  auto planes = [&](int64_t rows, int64_t cols, int count, bool bf16, Scale scale) {
+    const int64_t ld = padded(cols);
+    return Operand{c.take<uint16_t>(count * rows * ld), rows, cols, ld, rows * ld, count, bf16, scale};
+  };
+  l.pack_x = !readable(a.x, a.n, a.H, a.x_stride, a.type);
+  l.pack_w = !readable(a.w, a.V, a.H, a.w_stride, a.type);
+  const Scale sx{l.amax_x, kAmaxParts}, sw{l.amax_w, kAmaxParts}, none{nullptr, 0};
+  l.x = l.pack_x ? planes(a.n, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sx : none) : in_place(a.x, a.n, a.H, a.x_stride, a.type);
+  l.w = l.pack_w ? planes(a.V, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sw : none) : in_place(a.w, a.V, a.H, a.w_stride, a.type);
+  if (!a.grad) {
+    l.chunks = (a.V + kHalf - 1) / kHalf;
+    l.targets.entropy = c.take<float>(a.n);
+    l.targets.mass = c.take<float>(a.n);
+    l.part = c.take<float2>(l.chunks * a.n);
+    l.picked = c.take<float>(a.n * a.K);
+  } else {
+    l.targets.coef = c.take<float>(a.n);
+    l.targets.live = c.take<float>(a.n);
+    l.targets.size_part = c.take<float>(l.target_blocks);
+    const bool exact_dw = a.dw && a.dw_type == ECHO_F32;  // (whose P has 22 bits)
+    l.p_bf16 = a.type == ECHO_BF16 && (a.dx || !exact_dw);
+    l.p_half = f32 || exact_dw ? 2 : a.type == ECHO_F16 ? 1 : 0;
+    // dW's x has zeros for tokens without gradients
+    l.pack_x_dw = a.dw && !f32;
+    if (l.pack_x_dw) {
+      const bool as_half = a.type == ECHO_BF16 && exact_dw;
+      l.x_dw = planes(a.n, a.H, 1, a.type == ECHO_BF16 && !as_half, as_half ? sx : none);
+    } else {
+      l.x_dw = l.x;
+    }
+    const int64_t row_bytes = std::max<int64_t>(1, a.n) * 2 * (l.p_bf16 + l.p_half);
+    const int64_t columns = std::max<int64_t>(kTile, a.piece_bytes / row_bytes / kTile * kTile);
+    const int64_t pieces = (a.V + columns - 1) / columns;  // of equal size
+    l.piece = pieces <= 1 ? a.V : ((a.V + pieces - 1) / pieces + kTile - 1) / kTile * kTile;
+    l.ldp = padded(l.piece);
+    l.P = c.take<uint16_t>((l.p_bf16 + l.p_half) * a.n * l.ldp);
+    if (a.dx && l.piece < a.V) l.dx_sum = c.take<float>(a.n * a.H);
+  }
+  l.bytes = c.at;
+  return l;
+}
+
+cudaError_t box_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t plane, int planes, int box_rows, int box_cols,
+                    CUtensorMapSwizzle swizzle) {
+  if (!encoder()) return cudaErrorNotSupported;
+  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, 1, (cuuint64_t)planes};
+  const cuuint64_t far = (cuuint64_t)(planes > 1 ? plane : ld) * 2;  // (not used with one plane)
+  const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, far, far};
+  const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+// Stages of an operand: its rows (and 64 columns of the sum), or (mn) 64 rows of the sum and 64 columns
+cudaError_t stage_map(CUtensorMap *map, const Operand &o, bool mn) {
+  return box_map(map, o.p, o.rows, o.cols, o.ld, o.plane, o.planes, mn ? kBK : kHalf, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// D = A B^T; mn: the operand is held transposed
+Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn) {
+  Job j{};
+  j.M = (int)(a_mn ? a.cols : a.rows);
+  j.N = (int)(b_mn ? b.cols : b.rows);
+  j.steps = (int)(((a_mn ? a.rows : a.cols) + kBK - 1) / kBK);
+  for (int p = 0; p < a.planes; ++p)
+    for (int q = 0; q < b.planes; ++q)
+      if (p + q < 2) j.plane_a[j.pairs] = p, j.plane_b[j.pairs++] = q;
+  j.a_mn = a_mn, j.b_mn = b_mn;
+  j.instr = instruction(kTile, a_mn, b_mn, a.bf16);
+  j.tiles_n = (j.N + kTile - 1) / kTile;
+  j.tiles = (int64_t)((j.M + kTile - 1) / kTile) * j.tiles_n;
+  j.scale_a = a.scale, j.scale_b = b.scale;
+  return j;
+}
+
+struct Maps {
+  CUtensorMap a[2], b[2], p;
+};
+template <int MODE>
+cudaError_t launch_product(const Maps &m, const HeadProduct &g, int sms, cudaStream_t st) {
+  auto kernel = head_product_kernel<MODE>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  if (e != cudaSuccess) return e;
+  return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles, sms / 2) * 2), kThreads, kSmem, st, m.a[0], m.b[0], m.a[1], m.b[1], m.p, g);
+}
+
+#define TRY(call)                                \
+  do {                                           \
+    const cudaError_t _e = (call);               \
+    if (_e != cudaSuccess) return _e;            \
+  } while (0)
+
+cudaError_t launch_amax(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, float *part, cudaStream_t st) {
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    constexpr int N = 16 / sizeof(T);
+    const bool one = stride == cols || rows == 1;
+    const int64_t r = one ? 1 : rows, c = one ? rows * cols : cols;
+    if (cols % N == 0 && fits_pieces(x, stride, type, N))
+      return launch_early(head_amax_kernel<T, N>, dim3(kAmaxParts), 256, 0, st, static_cast<const T *>(x), r, c, stride, part);
+    return launch_early(head_amax_kernel<T, 1>, dim3(kAmaxParts), 256, 0, st, static_cast<const T *>(x), r, c, stride, part);
+  });
+}
+
+cudaError_t launch_pack(const void *x, int type, int64_t stride, const Operand &o, const float *live, int sms, cudaStream_t st) {
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    auto go = [&](auto d, auto planes) {
+      using D = decltype(d);
+      auto with = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const int64_t blocks = std::min<int64_t>((o.rows * (o.cols / W) + 1023) / 1024, sms * 6);
+        return launch_early(head_pack_kernel<T, D, decltype(planes)::value, W>, dim3((unsigned)blocks), 256, 0, st, static_cast<const T *>(x), o.rows, o.cols,
+                            stride, o.scale, live, static_cast<D *>(const_cast<void *>(o.p)), o.ld, o.plane);
+      };
+      return o.cols % 8 == 0 && fits_pieces(x, stride, type, 8) ? with(Int<8>{}) : with(Int<1>{});
+    };
+    if constexpr (std::is_same_v<T, float>) return go(__half{}, Int<2>{});
+    else if constexpr (std::is_same_v<T, __half>) return go(__half{}, Int<1>{});
+    else return o.bf16 ? go(__nv_bfloat16{}, Int<1>{}) : go(__half{}, Int<1>{});
+  });
+}
+
+}  // namespace
+
+int64_t head_piece_bytes() { return kPieceBytes; }
+int head_most_targets() { return kMaxTargets; }
+size_t head_scratch_bytes(const HeadArgs &a, int sms) { return layout_of(a, sms).bytes; }
+
+cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaStream_t st) {
+  const Layout l = layout_of(a, sms);
+  const bool f32 = a.type == ECHO_F32;
+  TRY(timed("head_targets", [&] { return launch_early(head_targets_kernel, dim3(l.target_blocks), kTargetWarps * 32, 0, st, a, l.targets); }));
+  const bool exact_dw = a.grad && a.dw && a.dw_type == ECHO_F32;
+  if (f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16))
+    TRY(timed("head_amax", [&] { return launch_amax(a.x, a.type, a.n, a.H, a.x_stride, l.amax_x, st); }));
+  if (f32 && a.V) TRY(timed("head_amax", [&] { return launch_amax(a.w, a.type, a.V, a.H, a.w_stride, l.amax_w, st); }));
+  // (backward, the rows of tokens without gradients are zeros in fp32's planes, which both products read)
+  if (l.pack_x) TRY(timed("head_pack", [&] { return launch_pack(a.x, a.type, a.x_stride, l.x, a.grad ? l.targets.live : nullptr, sms, st); }));
+  if (l.pack_w && a.V) TRY(timed("head_pack", [&] { return launch_pack(a.w, a.type, a.w_stride, l.w, nullptr, sms, st); }));
+  if (l.pack_x_dw) TRY(timed("head_pack", [&] { return launch_pack(a.x, a.type, a.x_stride, l.x_dw, l.targets.live, sms, st); }));
+
+  HeadProduct g{};
+  g.wait = {a.status, a.wait_limit}, g.skip = a.skip;
+  g.n = a.n, g.K = a.K, g.alpha = a.scale / a.tau;
+  g.idx = l.targets.idx, g.weight = l.targets.weight, g.coef = l.targets.coef, g.lse = a.lse_in;
+  Maps m{};
+  if (!a.grad) {
+    g.part = l.part, g.picked = l.picked;
+    if (a.V) {
+      g.job[0] = job_of(l.x, false, l.w, false);
+      g.tiles = g.job[0].tiles;
+      TRY(stage_map(&m.a[0], l.x, false));
+      TRY(stage_map(&m.b[0], l.w, false));
+      TRY(timed("head_logits", [&] { return launch_product<kStats>(m, g, sms, st); }));
+    }
+    return timed("head_join", [&] {
+      return launch_early(head_join_kernel, dim3((unsigned)std::min<int64_t>((a.n + 31) / 32, 8 * sms)), 256, 0, st, a, l.targets, l.part, l.chunks, l.picked);
+    });
+  }
+
+  g.p_bf16 = l.p_bf16, g.p_half = l.p_half, g.p_scale = {l.targets.size_part, l.target_blocks};
+  for (int64_t v = 0; v < a.V; v += l.piece) {
+    const int64_t rows = std::min(l.piece, a.V - v);
+    Operand w = l.w;
+    w.p = static_cast<const uint16_t *>(w.p) + v * w.ld;
+    w.rows = rows;
+    // the planes of P that dx and dW read
+    const int64_t plane = a.n * l.ldp;
+    const Operand p{l.P, a.n, rows, l.ldp, plane, l.p_bf16 + l.p_half, false, {nullptr, 0}};
+    auto planes = [&](bool bf16, int count) {
+      Operand o = p;
+      o.bf16 = bf16, o.planes = count;
+      if (!bf16) o.p = l.P + l.p_bf16 * plane, o.scale = g.p_scale;
+      return o;
+    };
+    HeadProduct h = g;
+    h.v_begin = (int)v;
+    h.job[0] = job_of(l.x, false, w, false);
+    h.tiles = h.job[0].tiles;
+    TRY(stage_map(&m.a[0], l.x, false));
+    TRY(stage_map(&m.b[0], w, false));
+    TRY(box_map(&m.p, l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+    TRY(timed("head_dlogits", [&] { return launch_product<kGrad>(m, h, sms, st); }));
+
+    HeadProduct d = g;
+    int jobs = 0;
+    if (a.dx) {
+      const Operand q = planes(a.type == ECHO_BF16, f32 ? 2 : 1);
+      Job &j = d.job[jobs] = job_of(q, false, w, true);
+      TRY(stage_map(&m.a[jobs], q, false));
+      TRY(stage_map(&m.b[jobs], w, true));
+      const bool last = v + l.piece >= a.V;
+      if (last) j.out = a.dx, j.out_stride = a.dx_stride, j.type = a.type;
+      else j.out = l.dx_sum, j.out_stride = a.H, j.type = ECHO_F32;
+      if (v) j.from = l.dx_sum, j.from_stride = a.H;
+      ++jobs;
+    }
+    if (a.dw) {
+      const Operand q = planes(l.x_dw.bf16, f32 || exact_dw ? 2 : 1);
+      Job &j = d.job[jobs] = job_of(q, true, l.x_dw, true);
+      TRY(stage_map(&m.a[jobs], q, true));
+      TRY(stage_map(&m.b[jobs], l.x_dw, true));
+      j.out = static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type);
+      j.out_stride = a.dw_stride, j.type = a.dw_type, j.add = a.accumulate;
+      ++jobs;
+    }
+    d.tiles = d.job[0].tiles + d.job[1].tiles;
+    if (jobs == 1) m.a[1] = m.a[0], m.b[1] = m.b[0];
+    TRY(timed("head_grads", [&] { return launch_product<kOut>(m, d, sms, st); }));
+  }
+  return cudaSuccess;
+}
+
+}  // namespace echo

@@ -25,7 +25,8 @@ EXPORTS = ["echo_create", "echo_destroy", "echo_check_graph", "echo_check_replic
            "echo_read_cc", "echo_read_overlap", "echo_cc_query", "echo_cc_query_noalloc",
            "echo_graph_info_get", "echo_set_cc_model",
            "echo_set_profiling", "echo_read_profile", "echo_measure_fp64", "echo_strerror", "echo_last_error",
-           "echo_stream_get", "echo_wait", "echo_embed", "echo_embed_grad", "echo_layer_norm", "echo_layer_norm_grad", "echo_orthogonalize"]
+           "echo_stream_get", "echo_wait", "echo_embed", "echo_embed_grad", "echo_layer_norm", "echo_layer_norm_grad", "echo_orthogonalize",
+           "echo_cross_entropy", "echo_cross_entropy_grad", "echo_distill", "echo_distill_grad", "echo_rotary", "echo_rotary_grad"]
 
 
 class EchoError(RuntimeError):
@@ -124,6 +125,37 @@ class OrthogonalizeDesc(C.Structure):
                 ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float), ("scale", C.c_float)]
 
 
+def _fields(spec: str):
+    """ctypes fields of "type: name name; ...", in order (p: pointer, l: int64, i: int32, f: float, l2 and p2: two of them)."""
+    kinds = {"p": C.c_void_p, "l": C.c_int64, "i": C.c_int32, "f": C.c_float, "p2": C.c_void_p * 2, "l2": C.c_int64 * 2}
+    return [(name, kinds[kind.strip()]) for kind, names in (part.split(":") for part in spec.split(";")) for name in names.split()]
+
+
+class CrossEntropyDesc(C.Structure):
+    _fields_ = _fields("l: n_tokens hidden vocab_rows vocab_start; p: x weight labels loss lse target; l: x_stride weight_stride; i: type id_bits; f: scale")
+
+
+class CrossEntropyGradDesc(C.Structure):
+    _fields_ = _fields("l: n_tokens hidden vocab_rows vocab_start; p: dloss dlse x weight labels lse dx dweight; "
+                       "l: x_stride weight_stride dx_stride dweight_stride; i: type dweight_type id_bits accumulate; f: scale")
+
+
+class DistillDesc(C.Structure):
+    _fields_ = _fields("l: n_tokens hidden vocab_rows vocab_start n_top; p: x weight ids logits teacher_lse loss lse cross; "
+                       "l: x_stride weight_stride; i: type id_bits logits_type; f: scale temperature")
+
+
+class DistillGradDesc(C.Structure):
+    _fields_ = _fields("l: n_tokens hidden vocab_rows vocab_start n_top; p: dloss dlse x weight ids logits teacher_lse lse dx dweight; "
+                       "l: x_stride weight_stride dx_stride dweight_stride; i: type dweight_type id_bits logits_type accumulate; f: scale temperature")
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = _fields("l: n_batch n_tokens; l2: heads; p2: x out; "
+                       "l2: x_batch_stride x_stride x_head_stride out_batch_stride out_stride out_head_stride; "
+                       "p: positions; l: positions_stride; p: frequencies; i: dim rot type id_bits interleaved; f: scale")
+
+
 _lib = None
 
 
@@ -172,6 +204,12 @@ def load_library(path: Optional[str] = None):
         "echo_layer_norm": ([vp, C.POINTER(LayerNormDesc)], C.c_int),
         "echo_layer_norm_grad": ([vp, C.POINTER(LayerNormGradDesc)], C.c_int),
         "echo_orthogonalize": ([vp, C.POINTER(OrthogonalizeDesc)], C.c_int),
+        "echo_cross_entropy": ([vp, C.POINTER(CrossEntropyDesc)], C.c_int),
+        "echo_cross_entropy_grad": ([vp, C.POINTER(CrossEntropyGradDesc)], C.c_int),
+        "echo_distill": ([vp, C.POINTER(DistillDesc)], C.c_int),
+        "echo_distill_grad": ([vp, C.POINTER(DistillGradDesc)], C.c_int),
+        "echo_rotary": ([vp, C.POINTER(RotaryDesc)], C.c_int),
+        "echo_rotary_grad": ([vp, C.POINTER(RotaryDesc)], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -325,6 +363,39 @@ def _batch(t, out: bool = False):
         return t, t.shape[0], t.stride(1), t.stride(0)
     _need(not out, "an output's matrices have no contiguous rows")
     return _batch(t.contiguous())
+
+
+def _heads(t, out: bool = False):
+    """``t`` [..., heads, dim] as [batch, tokens, heads, dim]: (tensor, batch, tokens, strides of the three)."""
+    if t.stride(-1) == 1 or t.shape[-1] == 1:
+        d = t.dim()
+        if d == 2:
+            return t, 1, 1, (0, 0, t.stride(0))
+        if d == 3:
+            return t, 1, t.shape[0], (0, t.stride(0), t.stride(1))
+        if d == 4:
+            return t, t.shape[0], t.shape[1], t.stride()[:3]
+        try:
+            return _heads(t.view(-1, *t.shape[-2:]), out)
+        except RuntimeError:
+            pass
+    _need(not out, "an output's heads are not contiguous, or its tokens not a fixed distance apart")
+    return _heads(t.contiguous())
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, length: Optional[int] = None, low: float = 1.0,
+                       high: float = 32.0) -> np.ndarray:
+    """Frequencies of ``rotary``, in radians a position, for ``rot`` elements of a head: ``base ** (-2 i / rot)``.  For
+    contexts ``factor`` times as long as trained ones, all are divided by ``factor``; or, where ``length`` gives the trained
+    length, by parts: those that turn ``high`` times over it stay, those that turn ``low`` times or less are divided, and
+    between the two the shares change linearly with the number of turns."""
+    _need(rot >= 2 and rot % 2 == 0, "rot is odd, or not at least 2")
+    f = float(base) ** (-np.arange(0, rot, 2, dtype=np.float64) / rot)
+    if length is None:
+        return f / factor
+    _need(high > low, "high is not above low")
+    keep = np.clip((length * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+    return f * (keep + (1 - keep) / factor)
 
 
 class Echo:
@@ -635,3 +706,153 @@ class Echo:
         self._op(self.lib.echo_orthogonalize, OrthogonalizeDesc(n, r, c, gm.data_ptr(), om.data_ptr(), gs, gb, os_, ob, _type(g.dtype), steps,
                                                                 a, b, cc, eps, scale))
         return o
+
+    # -- losses of a head --------------------------------------------------------------------
+    @staticmethod
+    def _head(x, weight):
+        """(x, weight, rows of x, of weight, hidden, strides of both, type)"""
+        _need(weight.dim() == 2 and x.dim() >= 1, "weight is not a matrix")
+        _need(x.dtype == weight.dtype, "x and weight have different types")
+        h = weight.shape[1]
+        _need(x.shape[-1] == h, "x and weight have rows of different lengths")
+        xm, n, xs = _matrix(x)
+        wm, _, ws = _matrix(weight)
+        return xm, wm, n, weight.shape[0], h, xs, ws, _type(x.dtype)
+
+    @staticmethod
+    def _per_token(shape, **given):
+        """The float32 values given, one a token, contiguous; dlse and teacher_lse may be None."""
+        import torch
+        found = []
+        for name, t in given.items():
+            _need(t is not None or name in ("dlse", "teacher_lse"), f"{name} is missing")
+            if t is not None:
+                _need(t.dtype == torch.float32 and t.shape == shape, f"{name} is not float32, one of them a token")
+            found.append(None if t is None else t.contiguous())
+        return found
+
+    def cross_entropy(self, x, weight, labels, scale: float = 1.0, vocab_start: int = 0):
+        """(loss, lse, target), float32 [...], of logits ``scale * x @ weight.T`` for ``labels`` [...], without keeping the
+        logits: ``lse`` of the weight's rows, ``target`` the label's logit (0 where it is of another shard, whose rows begin
+        at another ``vocab_start``), ``loss = lse - target``, 0 for labels below 0.  Of a shard, ``lse`` and ``target`` go into
+        the loss of the whole vocabulary."""
+        import torch
+        bits = self._ids(labels)
+        xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
+        _need(labels.shape == x.shape[:-1], "labels have another shape than x without its rows")
+        labels = labels.contiguous()
+        loss, lse, target = out = tuple(torch.empty((3, *labels.shape), dtype=torch.float32, device=x.device).unbind())
+        self._op(self.lib.echo_cross_entropy, CrossEntropyDesc(n, h, v, vocab_start, xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), loss.data_ptr(),
+                                                               lse.data_ptr(), target.data_ptr(), xs, ws, kind, bits, scale))
+        return out
+
+    def _head_grads(self, x, weight, dx, dweight, dtype, accumulate):
+        import torch
+        _need(dweight is not None or not accumulate, "accumulate needs dweight")
+        if dx is None:
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            _need(dx.shape == x.shape and dx.dtype == x.dtype, "dx has another shape or type than x")
+        if dweight is None:
+            dweight = torch.empty(weight.shape, dtype=dtype or torch.float32, device=x.device)
+        else:
+            _need(dweight.shape == weight.shape, "dweight has another shape than weight")
+        xm, _, xs = _matrix(dx, out=True)
+        wm, _, ws = _matrix(dweight, out=True)
+        return dx, dweight, xm.data_ptr(), wm.data_ptr(), xs, ws, _type(dweight.dtype)
+
+    def cross_entropy_grad(self, dloss, x, weight, labels, lse, scale: float = 1.0, vocab_start: int = 0, dlse=None, dtype=None, dx=None,
+                           dweight=None, accumulate: bool = False):
+        """(dx, dweight) of ``cross_entropy``, from the gradients of its loss (and lse) and ``lse`` of the whole vocabulary, all
+        float32 [...].  dweight has ``dtype`` (float32 by default), unless given; ``accumulate`` adds to the one given.  Of a
+        shard, dx is its part of the sum over shards."""
+        bits = self._ids(labels)
+        xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
+        _need(labels.shape == x.shape[:-1], "labels have another shape than x without its rows")
+        labels = labels.contiguous()
+        dloss, lse, dlse = self._per_token(labels.shape, dloss=dloss, lse=lse, dlse=dlse)
+        dx, dweight, dxp, dwp, dxs, dws, dkind = self._head_grads(x, weight, dx, dweight, dtype, accumulate)
+        self._op(self.lib.echo_cross_entropy_grad,
+                 CrossEntropyGradDesc(n, h, v, vocab_start, dloss.data_ptr(), _dptr(dlse), xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), lse.data_ptr(),
+                                      dxp, dwp, xs, ws, dxs, dws, kind, dkind, bits, 1 if accumulate else 0, scale))
+        return dx, dweight
+
+    def _teacher(self, x, ids, logits, teacher_lse):
+        bits = self._ids(ids)
+        _need(ids.dim() == x.dim() and ids.shape[:-1] == x.shape[:-1], "ids have another shape than x without its rows, and the teacher's entries")
+        _need(logits.shape == ids.shape, "logits have another shape than ids")
+        (teacher_lse,) = self._per_token(ids.shape[:-1], teacher_lse=teacher_lse)
+        return bits, ids.contiguous(), logits.contiguous(), teacher_lse, ids.shape[-1], _type(logits.dtype)
+
+    def distill(self, x, weight, ids, logits, temperature: float = 1.0, teacher_lse=None, scale: float = 1.0, vocab_start: int = 0):
+        """(loss, lse, cross), float32 [...], of a student with logits ``scale * x @ weight.T`` against a teacher's top
+        ``logits`` [..., top] of tokens ``ids`` (below 0: no entry).  The teacher's probabilities are those among its entries,
+        or with ``teacher_lse`` [...] (of all of its logits over the temperature) their own.  ``lse`` is the student's, over the
+        temperature; ``loss`` is temperature^2 times the divergence from the teacher.  Shards as for ``cross_entropy``."""
+        import torch
+        xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
+        bits, ids, logits, teacher_lse, top, lkind = self._teacher(x, ids, logits, teacher_lse)
+        loss, lse, cross = out = tuple(torch.empty((3, *ids.shape[:-1]), dtype=torch.float32, device=x.device).unbind())
+        self._op(self.lib.echo_distill, DistillDesc(n, h, v, vocab_start, top, xm.data_ptr(), wm.data_ptr(), ids.data_ptr(), logits.data_ptr(), _dptr(teacher_lse),
+                                                    loss.data_ptr(), lse.data_ptr(), cross.data_ptr(), xs, ws, kind, bits, lkind, scale, temperature))
+        return out
+
+    def distill_grad(self, dloss, x, weight, ids, logits, lse, temperature: float = 1.0, teacher_lse=None, scale: float = 1.0, vocab_start: int = 0, dlse=None,
+                     dtype=None, dx=None, dweight=None, accumulate: bool = False):
+        """(dx, dweight) of ``distill``, as ``cross_entropy_grad`` returns them."""
+        xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
+        bits, ids, logits, teacher_lse, top, lkind = self._teacher(x, ids, logits, teacher_lse)
+        dloss, lse, dlse = self._per_token(ids.shape[:-1], dloss=dloss, lse=lse, dlse=dlse)
+        dx, dweight, dxp, dwp, dxs, dws, dkind = self._head_grads(x, weight, dx, dweight, dtype, accumulate)
+        self._op(self.lib.echo_distill_grad,
+                 DistillGradDesc(n, h, v, vocab_start, top, dloss.data_ptr(), _dptr(dlse), xm.data_ptr(), wm.data_ptr(), ids.data_ptr(), logits.data_ptr(),
+                                 _dptr(teacher_lse), lse.data_ptr(), dxp, dwp, xs, ws, dxs, dws, kind, dkind, bits, lkind, 1 if accumulate else 0, scale,
+                                 temperature))
+        return dx, dweight
+
+    # -- rotary positions ----------------------------------------------------------------------
+    def _rotary(self, call, q, k, positions, frequencies, interleaved, scale, out):
+        import torch
+        bits = self._ids(positions)
+        f = np.ascontiguousarray(frequencies, dtype=np.float64)
+        _need(f.ndim == 1, "frequencies are not one of each pair")
+        one = k is None
+        _need(out is None or one or len(out) == 2, "out is not one of each of q and k")
+        xs = [q] if one else [q, k]
+        outs = [torch.empty_like(x, memory_format=torch.contiguous_format) for x in xs] if out is None else [out] if one else list(out)
+        d = RotaryDesc(dim=q.shape[-1], rot=2 * f.shape[0], type=_type(q.dtype), id_bits=bits, interleaved=1 if interleaved else 0, scale=scale,
+                       frequencies=f.ctypes.data)
+        keep = []
+        for i, (x, y) in enumerate(zip(xs, outs)):
+            _need(x.dim() >= 2 and x.shape[-1] == q.shape[-1] and x.shape[:-2] == q.shape[:-2] and x.dtype == q.dtype,
+                  "q and k have other tokens, lengths of a head or types")
+            _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than q or k")
+            y, _, _, ys = _heads(y, out=True)
+            if x.dim() > 4 and y.dim() <= 3:
+                x = x.reshape(-1, *x.shape[-2:])
+            x, d.n_batch, d.n_tokens, strides = _heads(x)
+            keep.append(x)
+            d.heads[i], d.x[i], d.out[i] = x.shape[-2], x.data_ptr(), y.data_ptr()
+            d.x_batch_stride[i], d.x_stride[i], d.x_head_stride[i] = strides
+            d.out_batch_stride[i], d.out_stride[i], d.out_head_stride[i] = ys
+        # positions of all batches, or the same ones for each
+        lead = q.shape[:-2]
+        if q.dim() == 4 and positions.shape == lead[1:]:
+            positions = positions.contiguous()
+        else:
+            _need(positions.shape == lead, "positions have another shape than the tokens")
+            positions, d.positions_stride = positions.contiguous(), d.n_tokens
+        d.positions = positions.data_ptr()
+        self._op(call, d)
+        return outs[0] if one else tuple(outs)
+
+    def rotary(self, q, k, positions, frequencies, interleaved: bool = False, scale: float = 1.0, out=None):
+        """``q`` and ``k`` [..., heads, dim] (k may be None) with the first 2 * len(frequencies) elements of each head turned by
+        ``positions`` [...] times the ``frequencies`` (radians a position, on the host: ``rotary_frequencies``), times ``scale``.
+        Pairs are an element and the one half of the turned part further on, or neighbours (``interleaved``).  Positions
+        [tokens] serve every batch of [batch, tokens, heads, dim].  ``out`` may be (q, k), or q without k."""
+        return self._rotary(self.lib.echo_rotary, q, k, positions, frequencies, interleaved, scale, out)
+
+    def rotary_grad(self, dq, dk, positions, frequencies, interleaved: bool = False, scale: float = 1.0, out=None):
+        """Gradients of q and k from those of ``rotary``'s results: the turn back."""
+        return self._rotary(self.lib.echo_rotary_grad, dq, dk, positions, frequencies, interleaved, scale, out)
