@@ -18,7 +18,7 @@
 //   - bf16 and fp16 matrices as they are; fp32 ones as sums of two fp16 numbers times a power of
 //     two that the largest element sets (22 bits of elements down to 2^-14 of it, an error of
 //     2^-37 of it below), multiplied as high * high + high * low + low * high;
-//   - P as one number of the matrices' type where the results have 16 bits: an error of 2^-9
+//   - P, scaled so that its largest element is a power of two, as one number of the matrices' type where the results have 16 bits: an error of 2^-9
 //     (bf16) of each element, independent of the others, where the results are rounded to the
 //     same.  For an fp32 dW as the sum of two fp16 numbers, with x as fp16 (the same way): a
 //     gradient added up over micro-batches in fp32 would otherwise be 2e-3 off.
@@ -45,14 +45,23 @@ struct Scale {
   const float *part;
   int parts;
 };
-// By a warp, the same in all lanes: the largest element times 2^exponent is 2^14 to 2^15, if it is
-// within 2^-96 and 2^124.
-__device__ __forceinline__ int exponent(Scale s) {
+__device__ __forceinline__ float largest(Scale s) {
   float m = 0.f;
   for (int i = threadIdx.x & 31; i < s.parts; i += 32) m = fmaxf(m, s.part[i]);
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-  return m > 0.f ? max(-110, min(110, 14 - ilogbf(m))) : 0;
+  return m;
+}
+__device__ __forceinline__ int exponent_of(float m) { return m > 0.f ? max(-110, min(110, 14 - ilogbf(m))) : 0; }
+// By a warp, the same in all lanes: the largest element times 2^exponent is 2^14 to 2^15, if it is
+// within 2^-96 and 2^124.
+__device__ __forceinline__ int exponent(Scale s) { return exponent_of(largest(s)); }
+// The same for P, whose largest element becomes 2^15 itself: tokens have the same weight as a rule,
+// and 1 is what its targets then round to, not all of them up or down (that left dx 3.0e-3 off in bf16
+// where a token's weight is 1 / 1984, and 2.4e-3 so).  What P is multiplied by is 2^exponent times this.
+__device__ __forceinline__ float fraction(Scale s) {
+  const float m = largest(s), at = ldexpf(m, exponent_of(m));
+  return at >= 16384.f && at < 32768.f ? 32768.f / at : 1.f;
 }
 __device__ __forceinline__ float finite_size(float x) {
   x = fabsf(x);
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
   next_may_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool grad = a.grad;
-  float largest = 0.f;
+  float most_size = 0.f;
   for (int64_t t = (int64_t)blockIdx.x * kTargetWarps + warp; t < a.n; t += (int64_t)gridDim.x * kTargetWarps) {
     float up = 0.f, lse_up = 0.f;  // of the loss (times tau) and of lse (over tau)
     if (grad) {
@@ -273,14 +282,14 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
       o.coef[t] = coef;
       o.live[t] = size;
     }
-    largest = fmaxf(largest, finite_size(size));
+    most_size = fmaxf(most_size, finite_size(size));
   }
   if (!grad) return;
-  if (lane == 0) sizes[warp] = largest;
+  if (lane == 0) sizes[warp] = most_size;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kTargetWarps; ++w) largest = fmaxf(largest, sizes[w]);
-    o.size_part[blockIdx.x] = largest;
+    for (int w = 1; w < kTargetWarps; ++w) most_size = fmaxf(most_size, sizes[w]);
+    o.size_part[blockIdx.x] = most_size;
   }
 }
 
@@ -292,10 +301,10 @@ constexpr int kTile = 256, kHalf = 128, kBK = 64;
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 constexpr int kFewRegs = 56, kManyRegs = 216;    // a thread of warps 0-3 and of 4-11
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
-constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
-constexpr int kOutBytes = 4096;                  // a warp's buffer on the way out
-constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kOutBytes + 256 + 1024;
-constexpr int kSet = 4;                          // stages that the tensor core adds up by itself
+constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 4;
+constexpr int kSlots = 4, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
+constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 256 + 1024;
+constexpr int kSet = 16;                         // stages that the tensor core adds up by itself
 
 struct Job {
   int M, N, steps;  // rows, columns; stages of a pair of planes
@@ -305,12 +314,11 @@ struct Job {
   int tiles_n;
   int64_t tiles;
   Scale scale_a, scale_b;
-  // D, times 2^-(both exponents), plus `from`, plus what `out` holds
+  // D, times 2^-(both exponents), plus what `out` holds
   void *out;
   int64_t out_stride;
   int type, add;
-  const float *from;
-  int64_t from_stride;
+  int by_engine;    // the TMA engine writes (or adds, in fp32) it
 };
 struct HeadProduct {
   Job job[2];
@@ -326,7 +334,7 @@ struct HeadProduct {
   float2 *part;      // [columns / 128][n] largest element (times log2 e) and sum of exponentials
   float *picked;     // [n][K] z of the targets
   int p_bf16, p_half;  // planes of P: one of bf16, of fp16
-  Scale p_scale;       // of the fp16 ones
+  Scale p_scale;
 };
 enum { kStats, kGrad, kOut };  // what becomes of the sums
 
@@ -351,42 +359,90 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// 32 x 32 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
-template <typename T>
-__device__ __forceinline__ void block_out(const Job &j, int row0, int c, int lane, float f1, float f2, const float (&v)[32], unsigned char *buffer) {
-  float *f = reinterpret_cast<float *>(buffer);
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 32; ++i) f[lane * 32 + (i ^ lane)] = v[i] * f1 * f2;
-  __syncwarp();
-  if (c + lane >= j.N) return;
-  T *o = static_cast<T *>(j.out) + (int64_t)row0 * j.out_stride + c + lane;
-  const float *from = j.from + (int64_t)row0 * j.from_stride + c + lane;
-  const int rows = min(32, j.M - row0);
-#pragma unroll 1
-  for (int r0 = 0; r0 < rows; r0 += 8) {
-    float x[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      x[r] = 0.f;
-      if (r0 + r >= rows) continue;
-      if (j.from) x[r] = from[(int64_t)(r0 + r) * j.from_stride];
-      if (j.add) x[r] += to_f(o[(int64_t)(r0 + r) * j.out_stride]);
-    }
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-      if (r0 + r < rows) o[(int64_t)(r0 + r) * j.out_stride] = from_f<T>(f[(r0 + r) * 32 + (lane ^ (r0 + r))] + x[r]);
+// A warp's buffers on the way out take turns: one is written again once the copy engine has read it.
+struct Slots {
+  unsigned char *base;
+  uint32_t turn;
+  int lane;
+  // The next one, for the whole warp, 64 bytes a row, pieces of 16 bytes as piece() has them.
+  __device__ __forceinline__ unsigned char *next() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(kSlots - 1) : "memory");
+    __syncwarp();
+    unsigned char *p = base + turn * kSlotBytes;
+    turn = (turn + 1) % kSlots;
+    return p;
   }
+  // All of them.
+  __device__ __forceinline__ unsigned char *all() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
+    __syncwarp();
+    return base;
+  }
+};
+// 16 fp32 columns of a slot added to what a matrix holds; what is outside the matrix is dropped.
+__device__ __forceinline__ void add_half(const CUtensorMap *map, const unsigned char *slot, int col, int row) {
+  asm volatile("cp.reduce.async.bulk.tensor.4d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4, %4}], [%1];\ncp.async.bulk.commit_group;\n" ::"l"(map),
+               "r"(smem_u32(slot)), "r"(col), "r"(row), "r"(0)
+               : "memory");
+}
+
+// 32 x 32 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
+// By the copy engine: a 16-byte aligned matrix that is written, or an fp32 one that is added to
+// (each element by one addition, so that the result has one order).
+template <typename T>
+__device__ __forceinline__ void engine_out(const Job &j, const CUtensorMap *map, int row0, int c, const float (&v)[32], Slots &slots) {
+  constexpr int kCols = 64 / sizeof(T), kPiece = 16 / sizeof(T);
+#pragma unroll
+  for (int c1 = 0; c1 < 32; c1 += kCols) {
+    unsigned char *slot = slots.next();
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<Pack<T, kPiece> *>(piece(slot, slots.lane, e)) = pack<T, kPiece>(v + c1 + e * kPiece);
+    half_written();
+    if (slots.lane == 0) {
+      if (sizeof(T) == 4 && j.add) add_half(map, slot, c + c1, row0);
+      else store_half(map, slot, c + c1, row0, 0, 0);
+    }
+  }
+}
+// By the warp, a row's 32 elements at a time.
+template <typename T>
+__device__ __forceinline__ void lanes_out(const Job &j, int row0, int c, const float (&v)[32], Slots &slots) {
+  const int lane = slots.lane;
+  float *f = reinterpret_cast<float *>(slots.all());
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[lane * 32 + (i ^ lane)] = v[i];
+  __syncwarp();
+  if (c + lane < j.N) {
+    T *o = static_cast<T *>(j.out) + (int64_t)row0 * j.out_stride + c + lane;
+    const int rows = min(32, j.M - row0);
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+      float x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = j.add && r0 + r < rows ? to_f(o[(int64_t)(r0 + r) * j.out_stride]) : 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (r0 + r < rows) o[(int64_t)(r0 + r) * j.out_stride] = from_f<T>(f[(r0 + r) * 32 + (lane ^ (r0 + r))] + x[r]);
+    }
+  }
+  __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void block_out(const Job &j, const CUtensorMap *map, int row0, int c, const float (&v)[32], Slots &slots) {
+  if (j.by_engine) engine_out<T>(j, map, row0, c, v, slots);
+  else lanes_out<T>(j, row0, c, v, slots);
 }
 
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap amap0, const __grid_constant__ CUtensorMap bmap0, const __grid_constant__ CUtensorMap amap1,
-                        const __grid_constant__ CUtensorMap bmap1, const __grid_constant__ CUtensorMap pmap, const __grid_constant__ HeadProduct a) {
+                        const __grid_constant__ CUtensorMap bmap1, const __grid_constant__ CUtensorMap out0, const __grid_constant__ CUtensorMap out1,
+                        const __grid_constant__ HeadProduct a) {
   extern __shared__ unsigned char raw[];
   unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
   unsigned char *buffers = base + kStages * kStageBytes;
-  uint64_t *bars = reinterpret_cast<uint64_t *>(buffers + 8 * kOutBytes);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(buffers + 8 * kSlots * kSlotBytes);
   __shared__ uint32_t tmem_base;
   __shared__ int give_up;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -481,15 +537,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kManyRegs));
     const int quarter = warp & 3, side = (warp - 4) >> 2;  // (a warp reaches the 32 rows of tensor memory of its number modulo 4)
-    unsigned char *buffer = buffers + (warp - 4) * kOutBytes;
+    Slots slots{buffers + (warp - 4) * kSlots * kSlotBytes, 0, lane};
     const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + side * kHalf;
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
     for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
     const float alpha = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]), alpha2 = alpha * kLog2e;
-    const float p_up = MODE == kGrad ? ldexpf(1.f, exponent(a.p_scale)) : 1.f;
+    const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
-    uint32_t turn = 0;
     bool ok = true;
     for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
       const int which = MODE == kOut && i >= a.job[0].tiles;
@@ -514,7 +569,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (MODE == kGrad) {
           // coef exp(z - lse) = coef' exp2(z log2 e - shift): the rounding of shift goes into coef'
           const float lse = a.lse[row];
-          coef = a.coef[row];
+          coef = a.coef[row] * p_up;
           shift = lse * kLog2e;
           const float rest = fmaf(lse, kLog2e, -shift);
           if (coef != 0.f && fabsf(rest) < 1.f) coef *= exp2f(-rest);
@@ -582,7 +637,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // One block after the other, in the registers of the first (unrolled, the code would be long
       // and runs once a tile).
       float (&v)[32] = acc[0];
-      const float f1 = ldexpf(1.f, down[which] / 2), f2 = ldexpf(1.f, down[which] - down[which] / 2);
+      const float f1 = ldexpf(p_down, down[which] / 2), f2 = ldexpf(1.f, down[which] - down[which] / 2);
 #pragma unroll 1
       for (int c = c0; c < min(j.N, c0 + kHalf); c += 32) {
         if constexpr (MODE == kGrad) {
@@ -591,7 +646,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           while (__any_sync(0xFFFFFFFFu, next < c + 32)) {
             const bool hit = next < c + 32;
             const int at = hit ? next - c : -1;
-            const float w = hit ? a.weight[row * a.K + k_at] : 0.f;
+            const float w = hit ? a.weight[row * a.K + k_at] * p_up : 0.f;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (at == e) v[e] -= w;
@@ -610,25 +665,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 memcpy(&h[e], &b, sizeof b);
               }
             } else {
-              const float up = q == a.p_bf16 ? p_up : 1.f;
 #pragma unroll
               for (int e = 0; e < 32; ++e) {
-                v[e] *= up;
                 h[e / 8].v[e % 8] = __float2half_rn(v[e]);
                 v[e] -= __half2float(h[e / 8].v[e % 8]);  // what the next plane holds
               }
             }
-            half_free(lane);
+            unsigned char *slot = slots.next();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *reinterpret_cast<Piece *>(piece(buffer + turn, lane, e)) = h[e];
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<Piece *>(piece(slot, lane, e)) = h[e];
             half_written();
-            if (lane == 0) store_half(&pmap, buffer + turn, c, row0, 0, q);
-            turn ^= 2048;
+            if (lane == 0) store_half(&out0, slot, c, row0, 0, q);
           }
         } else {
-          if (j.type == ECHO_F32) block_out<float>(j, row0, c, lane, f1, f2, v, buffer);
-          else if (j.type == ECHO_BF16) block_out<__nv_bfloat16>(j, row0, c, lane, f1, f2, v, buffer);
-          else block_out<__half>(j, row0, c, lane, f1, f2, v, buffer);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = v[e] * f1 * f2;
+          const CUtensorMap *map = which ? &out1 : &out0;
+          if (j.type == ECHO_F32) block_out<float>(j, map, row0, c, v, slots);
+          else if (j.type == ECHO_BF16) block_out<__nv_bfloat16>(j, map, row0, c, v, slots);
+          else block_out<__half>(j, map, row0, c, v, slots);
         }
 #pragma unroll
         for (int part = 1; part < kParts; ++part)
@@ -646,6 +701,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * kTile) : "memory");
   }
+}
+
+// dx from its sum over pieces.
+template <typename T>
+__global__ void __launch_bounds__(256) head_round_kernel(const float *from, int64_t ld, int64_t rows, int64_t cols, T *to, int64_t stride) {
+  kernel_begin();
+  next_may_start();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256)
+    to[i / cols * stride + i % cols] = from_f<T>(from[i / cols * ld + i % cols]);
 }
 
 // -- the end of the forward pass -------------------------------------------------------------------
@@ -734,6 +798,7 @@ struct Layout {
   int64_t piece, ldp;
   uint16_t *P;
   float *dx_sum;      // fp32, where dx is added up over pieces
+  int64_t dx_ld;
   size_t bytes;
 };
 
@@ -782,20 +847,21 @@ Layout layout_of(const HeadArgs &a, int sms) {
     l.piece = pieces <= 1 ? a.V : ((a.V + pieces - 1) / pieces + kTile - 1) / kTile * kTile;
     l.ldp = padded(l.piece);
     l.P = c.take<uint16_t>((l.p_bf16 + l.p_half) * a.n * l.ldp);
-    if (a.dx && l.piece < a.V) l.dx_sum = c.take<float>(a.n * a.H);
+    l.dx_ld = padded(a.H);
+    if (a.dx && l.piece < a.V) l.dx_sum = c.take<float>(a.n * l.dx_ld);
   }
   l.bytes = c.at;
   return l;
 }
 
 cudaError_t box_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t plane, int planes, int box_rows, int box_cols,
-                    CUtensorMapSwizzle swizzle) {
+                    CUtensorMapSwizzle swizzle, int size = 2, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_UINT16) {
   if (!encoder()) return cudaErrorNotSupported;
   const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, 1, (cuuint64_t)planes};
-  const cuuint64_t far = (cuuint64_t)(planes > 1 ? plane : ld) * 2;  // (not used with one plane)
-  const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, far, far};
+  const cuuint64_t far = (cuuint64_t)(planes > 1 ? plane : ld) * size;  // (not used with one plane)
+  const cuuint64_t strides[3] = {(cuuint64_t)ld * size, far, far};
   const cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
-  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+  return encoder()(map, type, 4, const_cast<void *>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess
              : cudaErrorInvalidValue;
@@ -803,6 +869,18 @@ cudaError_t box_map(CUtensorMap *map, const void *p, int64_t rows, int64_t cols,
 // Stages of an operand: its rows (and 64 columns of the sum), or (mn) 64 rows of the sum and 64 columns
 cudaError_t stage_map(CUtensorMap *map, const Operand &o, bool mn) {
   return box_map(map, o.p, o.rows, o.cols, o.ld, o.plane, o.planes, mn ? kBK : kHalf, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// Where a product's result goes: by the copy engine where its rows are 16-byte ones at 16-byte
+// addresses, but for sums of 16-bit matrices, which are rounded once.
+cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type, bool add) {
+  const int size = type_bytes(type);
+  if (j.M <= 1) stride = (j.N + 7) / 8 * 8;
+  j.out = out, j.out_stride = stride, j.type = type, j.add = add;
+  j.by_engine = reinterpret_cast<uintptr_t>(out) % 16 == 0 && stride * size % 16 == 0 && stride < (int64_t)1 << 37 && !(add && type != ECHO_F32);
+  if (!j.by_engine) return cudaSuccess;
+  return box_map(map, out, j.M, j.N, stride, 0, 1, 32, 64 / size, CU_TENSOR_MAP_SWIZZLE_64B, size,
+                 type == ECHO_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16);
 }
 
 // D = A B^T; mn: the operand is held transposed
@@ -823,14 +901,14 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn) {
 }
 
 struct Maps {
-  CUtensorMap a[2], b[2], p;
+  CUtensorMap a[2], b[2], out[2];
 };
 template <int MODE>
 cudaError_t launch_product(const Maps &m, const HeadProduct &g, int sms, cudaStream_t st) {
   auto kernel = head_product_kernel<MODE>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles, sms / 2) * 2), kThreads, kSmem, st, m.a[0], m.b[0], m.a[1], m.b[1], m.p, g);
+  return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles, sms / 2) * 2), kThreads, kSmem, st, m.a[0], m.b[0], m.a[1], m.b[1], m.out[0], m.out[1], g);
 }
 
 #define TRY(call)                                \
@@ -919,8 +997,8 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     const Operand p{l.P, a.n, rows, l.ldp, plane, l.p_bf16 + l.p_half, false, {nullptr, 0}};
     auto planes = [&](bool bf16, int count) {
       Operand o = p;
-      o.bf16 = bf16, o.planes = count;
-      if (!bf16) o.p = l.P + l.p_bf16 * plane, o.scale = g.p_scale;
+      o.bf16 = bf16, o.planes = count, o.scale = g.p_scale;
+      if (!bf16) o.p = l.P + l.p_bf16 * plane;
       return o;
     };
     HeadProduct h = g;
@@ -929,7 +1007,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     h.tiles = h.job[0].tiles;
     TRY(stage_map(&m.a[0], l.x, false));
     TRY(stage_map(&m.b[0], w, false));
-    TRY(box_map(&m.p, l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+    TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     TRY(timed("head_dlogits", [&] { return launch_product<kGrad>(m, h, sms, st); }));
 
     HeadProduct d = g;
@@ -939,10 +1017,8 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
       Job &j = d.job[jobs] = job_of(q, false, w, true);
       TRY(stage_map(&m.a[jobs], q, false));
       TRY(stage_map(&m.b[jobs], w, true));
-      const bool last = v + l.piece >= a.V;
-      if (last) j.out = a.dx, j.out_stride = a.dx_stride, j.type = a.type;
-      else j.out = l.dx_sum, j.out_stride = a.H, j.type = ECHO_F32;
-      if (v) j.from = l.dx_sum, j.from_stride = a.H;
+      if (l.dx_sum) TRY(out_to(j, &m.out[jobs], l.dx_sum, l.dx_ld, ECHO_F32, v > 0));
+      else TRY(out_to(j, &m.out[jobs], a.dx, a.dx_stride, a.type, false));
       ++jobs;
     }
     if (a.dw) {
@@ -950,15 +1026,21 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
       Job &j = d.job[jobs] = job_of(q, true, l.x_dw, true);
       TRY(stage_map(&m.a[jobs], q, true));
       TRY(stage_map(&m.b[jobs], l.x_dw, true));
-      j.out = static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type);
-      j.out_stride = a.dw_stride, j.type = a.dw_type, j.add = a.accumulate;
+      TRY(out_to(j, &m.out[jobs], static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type), a.dw_stride, a.dw_type, a.accumulate));
       ++jobs;
     }
     d.tiles = d.job[0].tiles + d.job[1].tiles;
     if (jobs == 1) m.a[1] = m.a[0], m.b[1] = m.b[0];
     TRY(timed("head_grads", [&] { return launch_product<kOut>(m, d, sms, st); }));
   }
-  return cudaSuccess;
+  if (!l.dx_sum) return cudaSuccess;
+  return timed("head_round", [&] {
+    return with_type(a.type, [&](auto t) {
+      using T = decltype(t);
+      const int64_t blocks = std::min<int64_t>((a.n * a.H + 255) / 256, sms * 8);
+      return launch_early(head_round_kernel<T>, dim3((unsigned)blocks), 256, 0, st, (const float *)l.dx_sum, l.dx_ld, a.n, a.H, static_cast<T *>(a.dx), a.dx_stride);
+    });
+  });
 }
 
 }  // namespace echo
