@@ -174,6 +174,8 @@ struct Targets {
   float *live;            // backward: 0 where a token has no gradient
   float *entropy, *mass;  // forward: sum q log q, Q
   float *size_part;       // backward: the largest |coef| + sum |weight| of a block's tokens
+  int32_t *arrived;       // of the products: zeros
+  int n_arrived;
 };
 
 constexpr int kTargetWarps = 8;
@@ -199,6 +201,8 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
   kernel_begin();
   next_may_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < o.n_arrived; i += blockDim.x) o.arrived[i] = 0;
   const bool grad = a.grad;
   float most_size = 0.f;
   for (int64_t t = (int64_t)blockIdx.x * kTargetWarps + warp; t < a.n; t += (int64_t)gridDim.x * kTargetWarps) {
@@ -299,10 +303,10 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 // pairs of planes.  A launch has up to two products, whose tiles follow one another.
 constexpr int kTile = 256, kHalf = 128, kBK = 64;
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
-constexpr int kFewRegs = 56, kManyRegs = 216;    // a thread of warps 0-3 and of 4-11
+constexpr int kFewRegs = 72, kManyRegs = 208;    // a thread of warps 0-3 and of 4-11
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
-constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 4;
-constexpr int kSlots = 4, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
+constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
+constexpr int kSlots = 2, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
 constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 256 + 1024;
 constexpr int kSet = 16;                         // stages that the tensor core adds up by itself
 
@@ -320,9 +324,25 @@ struct Job {
   int type, add;
   int by_engine;    // the TMA engine writes (or adds, in fp32) it
 };
+// Who computes what, of two products whose tiles take steps0 and steps1 stages.
+//   - Of the first one `whole` tiles, each in `split` parts of (almost) equal length along its sum, a
+//     part of every tile and then the next one, go to the pairs of blocks in turn.
+//   - Of the tiles of the second one, the pairs that had one part less take `early` each, in turn; the
+//     others go to all pairs in turn.
+//   - What is left of the first one is the pool: its stages, one tile behind the other, are split evenly
+//     over `pool_pairs`, so that a tile has up to three parts as a rule.
+struct Schedule {
+  int64_t whole, tiles1, pool;
+  int split, steps0, steps1, early, pool_pairs;
+};
+
 struct HeadProduct {
+  // Of kOut dx (its first operand K-major, the second MN-major) and dW (both MN-major): either may have no
+  // tiles.  Else the logits (both K-major) and nothing.
   Job job[2];
-  int64_t tiles;     // of both
+  Schedule schedule;
+  float4 *parts;     // sums of parts of tiles: [place][block][warp][columns / 4][lane]
+  int32_t *arrived;  // [tile][block][warp] parts that are there: zeros between launches
   WaitLimit wait;
   int skip;          // failure injection for tests: this 64-column step is never copied (-1: none)
   // the logits' product
@@ -434,6 +454,63 @@ __device__ __forceinline__ void block_out(const Job &j, const CUtensorMap *map, 
   else lanes_out<T>(j, row0, c, v, slots);
 }
 
+// What a pair of blocks does, one after the other: stages k0 to k1 of a tile's sum, which is one of
+// several parts of it or all.
+struct Share {
+  int which, k0, k1;
+  int64_t tile;
+  int64_t count;      // of the tile, among the counts of parts
+  int parts;          // 1: all
+  int64_t place, first, second, step;  // of this part's sums; of the first and the second; from there on
+};
+struct Worker {
+  const Schedule &s;
+  const int pair, pairs;
+  int64_t i, j, x, end;
+  int early;
+  __device__ __forceinline__ Worker(const Schedule &s, int pair, int pairs) : s(s), pair(pair), pairs(pairs), i(pair), x(0), end(0) {
+    const int64_t n = s.whole * s.split;
+    const int extra = (int)(n % pairs);  // pairs with one part more
+    early = extra && pair >= extra ? s.early : 0;
+    j = early ? pair - extra : (extra ? (int64_t)s.early * (pairs - extra) : 0) + pair;
+    if (pair < s.pool_pairs) x = s.pool * pair / s.pool_pairs, end = s.pool * (pair + 1) / s.pool_pairs;
+  }
+  __device__ __forceinline__ bool next(Share &w) {
+    w.parts = 1;
+    if (i < s.whole * s.split) {
+      const int part = s.split > 1 ? (int)(i / s.whole) : 0;
+      w.which = 0, w.tile = i - part * s.whole;
+      w.k0 = (int)((int64_t)s.steps0 * part / s.split), w.k1 = (int)((int64_t)s.steps0 * (part + 1) / s.split);
+      w.parts = s.split, w.count = w.tile;
+      w.place = i, w.first = w.tile, w.second = w.tile + s.whole, w.step = s.whole;
+      i += pairs;
+      return true;
+    }
+    if (j < s.tiles1) {
+      w.which = 1, w.tile = j, w.k0 = 0, w.k1 = s.steps1;
+      if (early) {
+        const int extra = (int)(s.whole * s.split % pairs);
+        j = --early ? j + (pairs - extra) : (int64_t)s.early * (pairs - extra) + pair;
+      } else {
+        j += pairs;
+      }
+      return true;
+    }
+    if (x >= end) return false;
+    const int64_t t = x / s.steps0, base = t * s.steps0;
+    w.which = 0, w.tile = s.whole + t, w.count = t;
+    w.k0 = (int)(x - base);
+    w.k1 = (int)min((int64_t)s.steps0, end - base);
+    // pair p begins at floor(pool p / pool_pairs): the last one at or before a stage s is floor(((s + 1) pool_pairs - 1) / pool).
+    // A pair has two places: of a tile's beginning, and of its end or a part between.
+    const int first = (int)(((base + 1) * s.pool_pairs - 1) / s.pool);
+    w.parts = (int)(((base + s.steps0) * s.pool_pairs - 1) / s.pool) - first + 1;
+    w.place = 2 * pair + (pair == first), w.first = 2 * first + 1, w.second = 2 * first + 2, w.step = 2;
+    x = base + w.k1;
+    return true;
+  }
+};
+
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap amap0, const __grid_constant__ CUtensorMap bmap0, const __grid_constant__ CUtensorMap amap1,
@@ -481,24 +558,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kFewRegs));
     if (warp == 0 && lane == 0) {
-      int64_t it = 0;
+      // (a stage's way is short: what it takes is in registers, and nothing is divided)
+      const uint32_t full_first = in_first(full);
+      const WaitLimit wait = a.wait;
+      const int skip = a.skip;
+      int s = 0;
+      uint32_t phase = 1;
       bool ok = true;
-      for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
-        const int which = MODE == kOut && i >= a.job[0].tiles;
-        const Job &j = a.job[which];
-        const CUtensorMap *amap = which ? &amap1 : &amap0, *bmap = which ? &bmap1 : &bmap0;
-        int r0, c0;
-        tile_place(j, which ? i - a.job[0].tiles : i, r0, c0);
-        for (int p = 0; p < j.pairs && ok; ++p)
-          for (int k = 0; k < j.steps; ++k, ++it) {
-            const int s = (int)(it % kStages);
-            ok = k != a.skip && bar_wait(empty + 8 * s, (uint32_t)(it / kStages + 1) & 1, abort, a.wait);
-            if (!ok) break;
-            const uint32_t at = ring + s * kStageBytes, bar = in_first(full + 8 * s);
-            if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);  // both blocks' copies
-            copy_rows(at, amap, j.a_mn, r0 + rank * kHalf, k * kBK, j.plane_a[p], bar);
-            copy_rows(at + kOperandBytes, bmap, j.b_mn, c0 + rank * kHalf, k * kBK, j.plane_b[p], bar);
+      auto copy = [&](auto a_mn, auto b_mn, const CUtensorMap *amap, const CUtensorMap *bmap, const Job &j, const Share &w) {
+        const int steps = j.steps;
+        int r0, c0, p = w.k0 / steps, k = w.k0 - p * steps;
+        tile_place(j, w.tile, r0, c0);
+        r0 += rank * kHalf, c0 += rank * kHalf;
+        int plane_a = j.plane_a[p], plane_b = j.plane_b[p];
+        for (int left = w.k1 - w.k0; left; --left) {
+          ok = k != skip && bar_wait(empty + 8 * s, phase, abort, wait);
+          if (!ok) break;
+          const uint32_t at = ring + s * kStageBytes, bar = full_first + 8 * s;
+          if (rank == 0) bar_expect(full + 8 * s, 2 * kStageBytes);  // both blocks' copies
+          copy_rows(at, amap, decltype(a_mn)::value, r0, k * kBK, plane_a, bar);
+          copy_rows(at + kOperandBytes, bmap, decltype(b_mn)::value, c0, k * kBK, plane_b, bar);
+          if (++s == kStages) s = 0, phase ^= 1;
+          if (++k == steps && left > 1) {
+            k = 0, ++p;
+            plane_a = j.plane_a[p], plane_b = j.plane_b[p];
           }
+        }
+      };
+      Worker worker(a.schedule, pair, pairs);
+      for (Share w; ok && worker.next(w);) {
+        if (MODE != kOut) copy(Int<0>{}, Int<0>{}, &amap0, &bmap0, a.job[0], w);
+        else if (w.which == 0) copy(Int<0>{}, Int<1>{}, &amap0, &bmap0, a.job[0], w);
+        else copy(Int<1>{}, Int<1>{}, &amap1, &bmap1, a.job[1], w);
       }
       if (!ok) {  // what is still being copied lands long before this
         const long long t0 = clock64();
@@ -506,27 +597,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
     } else if (warp == 1 && lane == 0 && rank == 0) {
-      int64_t it = 0, set = 0;
+      const WaitLimit wait = a.wait;
+      int s = 0, b = 0;
+      uint32_t phase = 0, sums_phase = 1;  // (of both sets alike: they take turns)
       bool ok = true;
-      for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
-        const Job &j = a.job[MODE == kOut && i >= a.job[0].tiles];
-        const int steps = j.steps * j.pairs, step_a = step16(j.a_mn), step_b = step16(j.b_mn);
-        for (int k = 0; k < steps; ++k, ++it) {
-          const int b = (int)(set & 1), s = (int)(it % kStages);
-          ok = (k % kSet || bar_wait(sums_empty + 8 * b, (uint32_t)(set / 2 + 1) & 1, abort, a.wait)) &&
-               bar_wait(full + 8 * s, (uint32_t)(it / kStages) & 1, abort, a.wait);
+      auto multiply = [&](auto a_mn, auto b_mn, uint32_t instr, int steps) {
+        constexpr bool A = decltype(a_mn)::value, B = decltype(b_mn)::value;
+        const uint64_t p0 = operand(ring, A), q0 = operand(ring + kOperandBytes, B);
+        for (int left = steps, in_set = 0; left; --left) {
+          ok = (in_set || bar_wait(sums_empty + 8 * b, sums_phase, abort, wait)) && bar_wait(full + 8 * s, phase, abort, wait);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
           const uint32_t d = tmem + b * kTile;
-          const uint64_t p = operand(ring + s * kStageBytes, j.a_mn), q = operand(ring + s * kStageBytes + kOperandBytes, j.b_mn);
+          const uint64_t p = p0 + (uint32_t)s * (kStageBytes >> 4), q = q0 + (uint32_t)s * (kStageBytes >> 4);
 #pragma unroll
-          for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step_a * kk, q + step_b * kk, j.instr, kk > 0 || k % kSet);
+          for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(A) * kk, q + step16(B) * kk, instr, kk > 0 || in_set);
           commit_pair(empty + 8 * s);
-          if (k % kSet == kSet - 1 || k == steps - 1) {
+          if (++s == kStages) s = 0, phase ^= 1;
+          if (++in_set == kSet || left == 1) {
             commit_pair(sums_full + 8 * b);
-            ++set;
+            in_set = 0;
+            b ^= 1;
+            if (b == 0) sums_phase ^= 1;
           }
         }
+      };
+      Worker worker(a.schedule, pair, pairs);
+      for (Share w; ok && worker.next(w);) {
+        if (MODE != kOut) multiply(Int<0>{}, Int<0>{}, a.job[0].instr, w.k1 - w.k0);
+        else if (w.which == 0) multiply(Int<0>{}, Int<1>{}, a.job[0].instr, w.k1 - w.k0);
+        else multiply(Int<1>{}, Int<1>{}, a.job[1].instr, w.k1 - w.k0);
       }
       commit(done);  // nothing is in flight when the block ends
       const long long t0 = clock64();
@@ -546,11 +646,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
     bool ok = true;
-    for (int64_t i = pair; i < a.tiles && ok; i += pairs) {
-      const int which = MODE == kOut && i >= a.job[0].tiles;
+    Worker worker(a.schedule, pair, pairs);
+    for (Share w; ok && worker.next(w);) {
+      const int which = MODE == kOut ? w.which : 0;
       const Job &j = a.job[which];
       int r0, c0;
-      tile_place(j, which ? i - a.job[0].tiles : i, r0, c0);
+      tile_place(j, w.tile, r0, c0);
       const int row0 = r0 + rank * kHalf + quarter * 32;
       c0 += side * kHalf;
       // what the tile's end needs comes during the sums
@@ -576,7 +677,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
       float acc[kParts][32] = {};
-      const int sets = (j.steps * j.pairs + kSet - 1) / kSet;
+      const int sets = (w.k1 - w.k0 + kSet - 1) / kSet;
       for (int set = 0; set < sets; ++set) {
         const int b = (int)(n & 1);
         ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait);
@@ -599,6 +700,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (row0 >= j.M || c0 >= j.N) continue;
+      if (w.parts > 1) {
+        // this part's sums to memory; who comes last adds the parts, in their order, and goes on with the tile
+        constexpr int64_t kPart = 16 * (kHalf / 4 * 32);
+        const int64_t place = (int64_t)(rank * 8 + warp - 4) * (kHalf / 4 * 32) + lane;
+        float4 *mine = a.parts + w.place * kPart + place;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            mine[(part * 8 + e) * 32] = make_float4(acc[part][4 * e], acc[part][4 * e + 1], acc[part][4 * e + 2], acc[part][4 * e + 3]);
+        __threadfence();
+        __syncwarp();
+        int32_t *count = a.arrived + w.count * 16 + rank * 8 + warp - 4, before = 0;
+        if (lane == 0) before = atomicAdd(count, 1);
+        if (__shfl_sync(0xFFFFFFFFu, before, 0) != w.parts - 1) continue;  // another part comes later
+        if (lane == 0) *count = 0;
+        __threadfence();
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[part][e] = 0.f;
+#pragma unroll 1
+        for (int q = 0; q < w.parts; ++q) {
+          const float4 *from_part = a.parts + (q ? w.second + (q - 1) * w.step : w.first) * kPart + place;
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 f = __ldcg(from_part + (part * 8 + e) * 32);
+              acc[part][4 * e] += f.x;
+              acc[part][4 * e + 1] += f.y;
+              acc[part][4 * e + 2] += f.z;
+              acc[part][4 * e + 3] += f.w;
+            }
+        }
+      }
       if constexpr (MODE == kStats) {
         if (c0 + kHalf > j.N)
 #pragma unroll
@@ -646,10 +783,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           while (__any_sync(0xFFFFFFFFu, next < c + 32)) {
             const bool hit = next < c + 32;
             const int at = hit ? next - c : -1;
-            const float w = hit ? a.weight[row * a.K + k_at] * p_up : 0.f;
+            const float weight = hit ? a.weight[row * a.K + k_at] * p_up : 0.f;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (at == e) v[e] -= w;
+              if (at == e) v[e] -= weight;
             if (hit) {
               next = INT_MAX;
               if (++k_at < a.K && a.idx[row * a.K + k_at] != INT_MAX) next = a.idx[row * a.K + k_at] - a.v_begin;
@@ -789,6 +926,7 @@ struct Layout {
   float *picked;
   int64_t chunks;
   float *amax_x, *amax_w;
+  float4 *parts;
   Operand x, w;       // of the logits' product (w: of dx too)
   Operand x_dw;       // of dW
   bool pack_x, pack_w, pack_x_dw;
@@ -809,6 +947,10 @@ Layout layout_of(const HeadArgs &a, int sms) {
   l.target_blocks = (int)std::min<int64_t>((a.n + kTargetWarps - 1) / kTargetWarps, 2 * sms);
   l.targets.idx = c.take<int32_t>(a.n * a.K);
   l.targets.weight = c.take<float>(a.n * a.K);
+  // (split tiles have two parts for each pair of blocks at most, and are no more than that)
+  l.targets.n_arrived = sms * 16;
+  l.targets.arrived = c.take<int32_t>(l.targets.n_arrived);
+  l.parts = c.take<float4>((int64_t)sms / 2 * 2 * kTile * kTile / 4);
   l.amax_x = c.take<float>(kAmaxParts);
   l.amax_w = c.take<float>(kAmaxParts);
   auto planes = [&](int64_t rows, int64_t cols, int count, bool bf16, Scale scale) {
@@ -903,12 +1045,43 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn) {
 struct Maps {
   CUtensorMap a[2], b[2], out[2];
 };
+// The schedule, by an estimate of the pair of blocks that takes longest.  In stages of 560 clocks (512
+// of products at 256 columns): joining the parts of a tile takes about 6000 clocks and 3000 for each part.
+// Nothing is split where that saves nothing.  Two products have no pool: the first one's operands are
+// long, and are in L2 while its tiles are at the same place of their sums.
+double joining(int64_t parts) { return (6000. + 3000. * parts) / 560; }
+Schedule plan(const Job *j, int pairs) {
+  Schedule s{};
+  const int64_t tiles = j[0].tiles;
+  s.whole = tiles, s.tiles1 = j[1].tiles, s.split = 1;
+  s.steps0 = j[0].steps * j[0].pairs, s.steps1 = j[1].steps * j[1].pairs;
+  double least = 0;
+  for (int64_t split = 1; split <= std::max<int64_t>(1, s.steps0 / 4) && (split == 1 || tiles * split <= 2 * pairs); ++split) {
+    const int64_t n = tiles * split, extra = n % pairs;
+    const double length = (double)((s.steps0 + split - 1) / split);
+    const int early = extra && s.tiles1 ? (int)std::min<double>(length / s.steps1 + 0.5, (double)(s.tiles1 / (pairs - extra))) : 0;
+    const int64_t late = s.tiles1 - (extra ? early * (pairs - extra) : 0);
+    const int64_t most = (late + pairs - 1) / pairs;  // (of a pair; the first ones have it)
+    const double clocks = std::max((double)(n / pairs + (extra > 0)) * length, (double)(n / pairs) * length + (double)early * s.steps1) + (double)most * s.steps1 +
+                          (split > 1 ? joining(split) : 0);
+    if (split == 1 || clocks < least) least = clocks, s.split = (int)split, s.early = early;
+  }
+  const int64_t rest = tiles % pairs, pool = rest * s.steps0;
+  if (s.tiles1 || !rest) return s;
+  const int pool_pairs = (int)std::clamp<int64_t>(pool / 4, 1, pairs);  // (each has a few stages at least)
+  const double clocks = (double)(tiles / pairs * s.steps0) + (double)((pool + pool_pairs - 1) / pool_pairs) + joining(((int64_t)s.steps0 * pool_pairs + pool - 1) / pool + 1);
+  if (clocks < least) s.whole = tiles - rest, s.split = 1, s.pool = pool, s.pool_pairs = pool_pairs;
+  return s;
+}
 template <int MODE>
-cudaError_t launch_product(const Maps &m, const HeadProduct &g, int sms, cudaStream_t st) {
+cudaError_t launch_product(const Maps &m, HeadProduct &g, int sms, cudaStream_t st) {
   auto kernel = head_product_kernel<MODE>;
+  const int pairs = sms / 2;
+  g.schedule = plan(g.job, pairs);
+  const int64_t busy = std::max<int64_t>(g.schedule.pool_pairs, g.schedule.whole * g.schedule.split + g.schedule.tiles1);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (e != cudaSuccess) return e;
-  return launch_early(kernel, dim3((unsigned)std::min<int64_t>(g.tiles, sms / 2) * 2), kThreads, kSmem, st, m.a[0], m.b[0], m.a[1], m.b[1], m.out[0], m.out[1], g);
+  return launch_early(kernel, dim3((unsigned)std::min<int64_t>(busy, pairs) * 2), kThreads, kSmem, st, m.a[0], m.b[0], m.a[1], m.b[1], m.out[0], m.out[1], g);
 }
 
 #define TRY(call)                                \
@@ -969,6 +1142,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
 
   HeadProduct g{};
   g.wait = {a.status, a.wait_limit}, g.skip = a.skip;
+  g.parts = l.parts, g.arrived = l.targets.arrived;
   g.n = a.n, g.K = a.K, g.alpha = a.scale / a.tau;
   g.idx = l.targets.idx, g.weight = l.targets.weight, g.coef = l.targets.coef, g.lse = a.lse_in;
   Maps m{};
@@ -976,7 +1150,6 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     g.part = l.part, g.picked = l.picked;
     if (a.V) {
       g.job[0] = job_of(l.x, false, l.w, false);
-      g.tiles = g.job[0].tiles;
       TRY(stage_map(&m.a[0], l.x, false));
       TRY(stage_map(&m.b[0], l.w, false));
       TRY(timed("head_logits", [&] { return launch_product<kStats>(m, g, sms, st); }));
@@ -1004,33 +1177,27 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     HeadProduct h = g;
     h.v_begin = (int)v;
     h.job[0] = job_of(l.x, false, w, false);
-    h.tiles = h.job[0].tiles;
     TRY(stage_map(&m.a[0], l.x, false));
     TRY(stage_map(&m.b[0], w, false));
     TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
     TRY(timed("head_dlogits", [&] { return launch_product<kGrad>(m, h, sms, st); }));
 
     HeadProduct d = g;
-    int jobs = 0;
     if (a.dx) {
       const Operand q = planes(a.type == ECHO_BF16, f32 ? 2 : 1);
-      Job &j = d.job[jobs] = job_of(q, false, w, true);
-      TRY(stage_map(&m.a[jobs], q, false));
-      TRY(stage_map(&m.b[jobs], w, true));
-      if (l.dx_sum) TRY(out_to(j, &m.out[jobs], l.dx_sum, l.dx_ld, ECHO_F32, v > 0));
-      else TRY(out_to(j, &m.out[jobs], a.dx, a.dx_stride, a.type, false));
-      ++jobs;
+      Job &j = d.job[0] = job_of(q, false, w, true);
+      TRY(stage_map(&m.a[0], q, false));
+      TRY(stage_map(&m.b[0], w, true));
+      if (l.dx_sum) TRY(out_to(j, &m.out[0], l.dx_sum, l.dx_ld, ECHO_F32, v > 0));
+      else TRY(out_to(j, &m.out[0], a.dx, a.dx_stride, a.type, false));
     }
     if (a.dw) {
       const Operand q = planes(l.x_dw.bf16, f32 || exact_dw ? 2 : 1);
-      Job &j = d.job[jobs] = job_of(q, true, l.x_dw, true);
-      TRY(stage_map(&m.a[jobs], q, true));
-      TRY(stage_map(&m.b[jobs], l.x_dw, true));
-      TRY(out_to(j, &m.out[jobs], static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type), a.dw_stride, a.dw_type, a.accumulate));
-      ++jobs;
+      Job &j = d.job[1] = job_of(q, true, l.x_dw, true);
+      TRY(stage_map(&m.a[1], q, true));
+      TRY(stage_map(&m.b[1], l.x_dw, true));
+      TRY(out_to(j, &m.out[1], static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type), a.dw_stride, a.dw_type, a.accumulate));
     }
-    d.tiles = d.job[0].tiles + d.job[1].tiles;
-    if (jobs == 1) m.a[1] = m.a[0], m.b[1] = m.b[0];
     TRY(timed("head_grads", [&] { return launch_product<kOut>(m, d, sms, st); }));
   }
   if (!l.dx_sum) return cudaSuccess;
