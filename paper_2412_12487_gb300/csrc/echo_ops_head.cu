@@ -36,7 +36,7 @@ namespace echo {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr int kAmaxParts = 304;  // blocks that look for a largest element, at most
 
 // Where the exponent of a matrix's power of two comes from: the largest elements that blocks
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 // pairs of planes.  A launch has up to two products, whose tiles follow one another.
 constexpr int kTile = 256, kHalf = 128, kBK = 64;
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
-constexpr int kFewRegs = 72, kManyRegs = 208;    // a thread of warps 0-3 and of 4-11
+constexpr int kFewRegs = 88, kManyRegs = 208;    // a thread of warps 0-3 and of 4-11
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
 constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
 constexpr int kSlots = 2, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
@@ -330,7 +330,8 @@ struct Job {
 //   - Of the tiles of the second one, the pairs that had one part less take `early` each, in turn; the
 //     others go to all pairs in turn.
 //   - What is left of the first one is the pool: its stages, one tile behind the other, are split evenly
-//     over `pool_pairs`, so that a tile has up to three parts as a rule.
+//     over `pool_pairs`, so that a tile has up to three parts as a rule.  It comes first: parts are
+//     joined while the next tile is summed.
 struct Schedule {
   int64_t whole, tiles1, pool;
   int split, steps0, steps1, early, pool_pairs;
@@ -477,6 +478,19 @@ struct Worker {
   }
   __device__ __forceinline__ bool next(Share &w) {
     w.parts = 1;
+    if (x < end) {
+      const int64_t t = x / s.steps0, base = t * s.steps0;
+      w.which = 0, w.tile = s.whole + t, w.count = t;
+      w.k0 = (int)(x - base);
+      w.k1 = (int)min((int64_t)s.steps0, end - base);
+      // pair p begins at floor(pool p / pool_pairs): the last one at or before a stage s is floor(((s + 1) pool_pairs - 1) / pool).
+      // A pair has two places: of a tile's beginning, and of its end or a part between.
+      const int first = (int)(((base + 1) * s.pool_pairs - 1) / s.pool);
+      w.parts = (int)(((base + s.steps0) * s.pool_pairs - 1) / s.pool) - first + 1;
+      w.place = 2 * pair + (pair == first), w.first = 2 * first + 1, w.second = 2 * first + 2, w.step = 2;
+      x = base + w.k1;
+      return true;
+    }
     if (i < s.whole * s.split) {
       const int part = s.split > 1 ? (int)(i / s.whole) : 0;
       w.which = 0, w.tile = i - part * s.whole;
@@ -496,18 +510,41 @@ struct Worker {
       }
       return true;
     }
-    if (x >= end) return false;
-    const int64_t t = x / s.steps0, base = t * s.steps0;
-    w.which = 0, w.tile = s.whole + t, w.count = t;
-    w.k0 = (int)(x - base);
-    w.k1 = (int)min((int64_t)s.steps0, end - base);
-    // pair p begins at floor(pool p / pool_pairs): the last one at or before a stage s is floor(((s + 1) pool_pairs - 1) / pool).
-    // A pair has two places: of a tile's beginning, and of its end or a part between.
-    const int first = (int)(((base + 1) * s.pool_pairs - 1) / s.pool);
-    w.parts = (int)(((base + s.steps0) * s.pool_pairs - 1) / s.pool) - first + 1;
-    w.place = 2 * pair + (pair == first), w.first = 2 * first + 1, w.second = 2 * first + 2, w.step = 2;
-    x = base + w.k1;
-    return true;
+    return false;
+  }
+};
+
+// A row's targets from a column on, in their order; the one after the next is on its way.
+struct Cursor {
+  const int32_t *idx;
+  const float *weight;
+  int K, begin, k, next, after;
+  float w, w_after;
+  __device__ __forceinline__ void load(int at, int &column, float &x) {
+    column = INT_MAX;
+    if (at >= K) return;
+    const int row = idx[at];
+    if (weight) x = weight[at];
+    if (row != INT_MAX) column = row - begin;
+  }
+  // `weights` may be null: w is 0 then
+  __device__ __forceinline__ void start(const int32_t *rows, const float *weights, int count, int v_begin, int column) {
+    idx = rows, weight = weights, K = count, begin = v_begin, k = 0, w = w_after = 0.f;
+    for (int hi = K; k < hi;) {
+      const int mid = (k + hi) / 2;
+      if (idx[mid] < v_begin + column) k = mid + 1;
+      else hi = mid;
+    }
+    load(k, next, w);
+    load(k + 1, after, w_after);
+  }
+  __device__ __forceinline__ void none() {
+    idx = nullptr, weight = nullptr, K = 0, begin = 0, k = 0, next = after = INT_MAX, w = w_after = 0.f;
+  }
+  __device__ __forceinline__ void step() {
+    ++k;
+    next = after, w = w_after;
+    load(k + 1, after, w_after);
   }
 };
 
@@ -642,7 +679,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
     for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
-    const float alpha = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]), alpha2 = alpha * kLog2e;
+    const float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
     const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
     bool ok = true;
@@ -657,16 +694,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // what the tile's end needs comes during the sums
       const int64_t row = row0 + lane;
       const bool in = row < j.M;
-      int k_at = 0, next = INT_MAX;
+      Cursor at;
+      at.none();
       float coef = 0.f, shift = 0.f;
       if (MODE != kOut && in) {
-        const int32_t *idx = a.idx + row * a.K;
-        for (int hi = a.K; k_at < hi;) {
-          const int mid = (k_at + hi) / 2;
-          if (idx[mid] < a.v_begin + c0) k_at = mid + 1;
-          else hi = mid;
-        }
-        if (k_at < a.K && idx[k_at] != INT_MAX) next = idx[k_at] - a.v_begin;
+        at.start(a.idx + row * a.K, MODE == kGrad ? a.weight + row * a.K : nullptr, a.K, a.v_begin, c0);
         if (MODE == kGrad) {
           // coef exp(z - lse) = coef' exp2(z log2 e - shift): the rounding of shift goes into coef'
           const float lse = a.lse[row];
@@ -692,7 +724,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           sums_loaded();
           pass(s);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[part][e] += __uint_as_float(s.r[e]);
+          for (int e = 0; e < 32; e += 2) {
+            const Pair x{__uint_as_float(s.r[e]), __uint_as_float(s.r[e + 1])}, y{acc[part][e], acc[part][e + 1]};
+            const Pair sum = MODE == kOut ? add2(x, y) : fma2(x, both(alpha2), y);
+            acc[part][e] = sum.a, acc[part][e + 1] = sum.b;
+          }
         }
         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
         __syncwarp();
@@ -742,30 +778,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (c0 + part * 32 + e >= j.N) acc[part][e] = alpha2 < 0.f ? INFINITY : -INFINITY;
-        float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, s[4] = {};
+              if (c0 + part * 32 + e >= j.N) acc[part][e] = -INFINITY;
+        float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], acc[part][e] * alpha2);
+          for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], acc[part][e]);
         const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), zero = most == -INFINITY ? 0.f : most;
+        Pair sum[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) s[e & 3] += exp2_fast(fmaf(acc[part][e], alpha2, -zero));
-        if (in) a.part[(int64_t)(c0 / kHalf) * a.n + row] = make_float2(most, (s[0] + s[1]) + (s[2] + s[3]));
+          for (int e = 0; e < 32; e += 2) {
+            const Pair x = add2({acc[part][e], acc[part][e + 1]}, both(-zero));
+            sum[e / 2 & 1] = add2(sum[e / 2 & 1], {exp2_fast(x.a), exp2_fast(x.b)});
+          }
+        sum[0] = add2(sum[0], sum[1]);
+        if (in) a.part[(int64_t)(c0 / kHalf) * a.n + row] = make_float2(most, sum[0].a + sum[0].b);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
           const int end = c0 + part * 32 + 32;
-          while (__any_sync(0xFFFFFFFFu, next < end)) {
-            const bool hit = next < end;
-            const int at = hit ? next - (end - 32) : -1;
+          while (__any_sync(0xFFFFFFFFu, at.next < end)) {
+            const bool hit = at.next < end;
+            const int column = hit ? at.next - (end - 32) : -1;
             float z = 0.f;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) z = at == e ? acc[part][e] : z;
+            for (int e = 0; e < 32; ++e) z = column == e ? acc[part][e] : z;
             if (hit) {
-              a.picked[row * a.K + k_at] = z * alpha;
-              next = ++k_at < a.K ? a.idx[row * a.K + k_at] : INT_MAX;
+              a.picked[row * a.K + at.k] = z * kLn2;
+              at.step();
             }
           }
         }
@@ -779,18 +820,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       for (int c = c0; c < min(j.N, c0 + kHalf); c += 32) {
         if constexpr (MODE == kGrad) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = coef == 0.f ? 0.f : coef * exp2_fast(fmaf(v[e], alpha2, -shift));
-          while (__any_sync(0xFFFFFFFFu, next < c + 32)) {
-            const bool hit = next < c + 32;
-            const int at = hit ? next - c : -1;
-            const float weight = hit ? a.weight[row * a.K + k_at] * p_up : 0.f;
+          for (int e = 0; e < 32; ++e) v[e] = coef == 0.f ? 0.f : coef * exp2_fast(v[e] - shift);
+          while (__any_sync(0xFFFFFFFFu, at.next < c + 32)) {
+            const bool hit = at.next < c + 32;
+            const int column = hit ? at.next - c : -1;
+            const float weight = at.w * p_up;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (at == e) v[e] -= weight;
-            if (hit) {
-              next = INT_MAX;
-              if (++k_at < a.K && a.idx[row * a.K + k_at] != INT_MAX) next = a.idx[row * a.K + k_at] - a.v_begin;
-            }
+              if (column == e) v[e] -= weight;
+            if (hit) at.step();
           }
 #pragma unroll 1
           for (int q = 0; q < a.p_bf16 + a.p_half; ++q) {
@@ -871,7 +909,7 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadArgs a, Targets t, c
     __syncthreads();
     if (warp == 0) {
       for (int w = 1; w < 8; ++w) s = join(s, sh[w][lane]);
-      lses[lane] = s.x == -INFINITY ? s.y == 0.f ? -INFINITY : NAN : fmaf(s.x, 0.693147180559945309f, logf(s.y));
+      lses[lane] = s.x == -INFINITY ? s.y == 0.f ? -INFINITY : NAN : fmaf(s.x, kLn2, logf(s.y));
     }
     __syncthreads();
     for (int r = warp; r < 32 && r0 + r < a.n; r += 8) {
