@@ -18,6 +18,7 @@ namespace echo {
 namespace {
 
 constexpr int kThreads = 256, kItems = 4;        // items of a thread in flight
+constexpr int kBlocks = 4;                       // of an SM
 constexpr int kAngles = 1024, kTokens = 128;     // angles and tokens of a block, at most
 static_assert(kRotaryPairs <= kAngles, "a token's angles fit");
 
@@ -33,8 +34,8 @@ __device__ __forceinline__ uint32_t divide(uint32_t n, uint32_t by) { return by 
 
 // A block takes some tokens and heads: their angles once, to shared memory, while the first items
 // are on their way.  Bound by the bytes.
-template <typename T, int W>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs a, const RotaryPlan p) {
+template <typename T, int W, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_constant__ RotaryArgs a, const RotaryPlan p) {
   __shared__ float2 angles[kAngles];
   __shared__ int64_t in_at[2][kTokens], out_at[2][kTokens];
   kernel_begin();
@@ -53,62 +54,56 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
   }
   __syncthreads();
   const uint32_t per_token = (uint32_t)(heads * p.per_head), items = tokens * per_token;
+  const int apart = INTERLEAVED ? W : half;  // the second piece of an item that is turned, from the first
   struct Item {
-    float v[2][W];
+    Pack<T, W> v[2];
     T *to;
-    int pair;       // of the first element, in the block's angles; -1: copied
-    int second;     // where the second piece is, from the first; 0: none
-    bool live;
+    int pair;  // of the first element, in the block's angles; or:
   };
+  constexpr int kCopied = -1, kCopiedFirst = -2, kNothing = -3;  // both pieces as they are, the first one alone, no item
   auto load = [&](uint32_t i, Item &m) {
-    m.live = i < items;
-    if (!m.live) return;
-    uint32_t token = i;
-    if (p.tokens_block == 1) token = 0;
-    else token = heads == p.heads_block ? divide(i, p.by_token) : i / per_token;
+    m.pair = kNothing;
+    if (i >= items) return;
+    uint32_t token = 0;
+    if (p.tokens_block > 1) token = heads == p.heads_block ? divide(i, p.by_token) : i / per_token;
     const uint32_t in_token = i - token * per_token, h = divide(in_token, p.by_head), j = in_token - h * p.per_head;
     const int head = head0 + (int)h, k = head >= a.heads[0];
     const int64_t hh = head - (k ? a.heads[0] : 0);
-    int first;
+    int first, second = apart;
     if ((int)j < p.turned) {
-      first = a.interleaved ? 2 * W * (int)j : W * (int)j;
-      m.second = a.interleaved ? W : half;
+      first = INTERLEAVED ? 2 * W * (int)j : W * (int)j;
       m.pair = (int)token * half + W * (int)j;
     } else {
       first = a.rot + 2 * W * ((int)j - p.turned);
-      m.second = first + W < a.dim ? W : 0;
-      m.pair = -1;
+      second = W;
+      m.pair = first + W < a.dim ? kCopied : kCopiedFirst;
     }
     const T *from = static_cast<const T *>(a.x[k]) + in_at[k][token] + hh * a.x_head[k] + first;
     m.to = static_cast<T *>(a.out[k]) + out_at[k][token] + hh * a.out_head[k] + first;
-    load_piece<W>(from, m.v[0]);
-    if (m.second) load_piece<W>(from + m.second, m.v[1]);
+    m.v[0] = *reinterpret_cast<const Pack<T, W> *>(from);
+    if (m.pair != kCopiedFirst) m.v[1] = *reinterpret_cast<const Pack<T, W> *>(from + second);
   };
-  auto finish = [&](Item &m) {
-    if (!m.live) return;
-    if (m.pair >= 0) {
-      if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          // pairs of neighbours: elements 2e and 2e + 1 of the two pieces
-          float &x = m.v[2 * e / W][2 * e % W], &y = m.v[(2 * e + 1) / W][(2 * e + 1) % W];
-          const float2 c = angles[m.pair + e];
-          const float x0 = x;
-          x = x0 * c.x - y * c.y;
-          y = x0 * c.y + y * c.x;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float2 c = angles[m.pair + e];
-          const float x0 = m.v[0][e], y0 = m.v[1][e];
-          m.v[0][e] = x0 * c.x - y0 * c.y;
-          m.v[1][e] = x0 * c.y + y0 * c.x;
-        }
-      }
+  auto finish = [&](const Item &m) {
+    if (m.pair == kNothing) return;
+    if (m.pair < 0) {
+      *reinterpret_cast<Pack<T, W> *>(m.to) = m.v[0];
+      if (m.pair == kCopied) *reinterpret_cast<Pack<T, W> *>(m.to + W) = m.v[1];
+      return;
     }
-    store_piece<W>(m.to, m.v[0]);
-    if (m.second) store_piece<W>(m.to + m.second, m.v[1]);
+    float v[2][W];
+    unpack<T, W>(m.v[0], v[0]);
+    unpack<T, W>(m.v[1], v[1]);
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const float2 c = angles[m.pair + e];
+      // interleaved: elements 2e and 2e + 1 of the two pieces
+      float &x = INTERLEAVED ? v[2 * e / W][2 * e % W] : v[0][e], &y = INTERLEAVED ? v[(2 * e + 1) / W][(2 * e + 1) % W] : v[1][e];
+      const float x0 = x;
+      x = fmaf(x0, c.x, -__fmul_rn(y, c.y));  // (one order of roundings for every layout)
+      y = fmaf(x0, c.y, __fmul_rn(y, c.x));
+    }
+    store_piece<W>(m.to, v[0]);
+    store_piece<W>(m.to + apart, v[1]);
   };
   Item m[kItems];
 #pragma unroll
@@ -141,7 +136,7 @@ uint64_t rotary_turns(double f) {
   const double high = 0x1.45f306dc9c883p-3, low = -0x1.6b01ec5417056p-57;
   if (f < 0) return -rotary_turns(-f);
   const double p = f * high, rest = std::fma(f, high, -p) + f * low;
-  return (uint64_t)std::ldexp(p - std::floor(p), 64) + (uint64_t)std::llrint(std::ldexp(rest, 64));  // (the difference is exact)
+  return (uint64_t)((p - std::floor(p)) * 0x1p64) + (uint64_t)std::llrint(rest * 0x1p64);  // (the difference is exact)
 }
 
 cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st) {
@@ -168,7 +163,8 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st) {
       p.by_head = (uint32_t)((((uint64_t)1 << 32) + p.per_head - 1) / p.per_head);
       p.by_token = (uint32_t)((((uint64_t)1 << 32) + per_token - 1) / per_token);
       const dim3 grid((unsigned)((a.batch * a.tokens + p.tokens_block - 1) / p.tokens_block), (unsigned)((heads + p.heads_block - 1) / p.heads_block));
-      return launch_early(rotary_kernel<T, W>, grid, kThreads, 0, st, a, p);
+      if (a.interleaved) return launch_early(rotary_kernel<T, W, true>, grid, kThreads, 0, st, a, p);
+      return launch_early(rotary_kernel<T, W, false>, grid, kThreads, 0, st, a, p);
     };
     constexpr int N = 16 / sizeof(T);
     return fits(N) ? go(Int<N>{}) : fits(2) ? go(Int<2>{}) : go(Int<1>{});

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Tuple
 
 import numpy as np
@@ -156,6 +157,19 @@ class RotaryDesc(C.Structure):
                        "p: positions; l: positions_stride; p: frequencies; i: dim rot type id_bits interleaved; f: scale")
 
 
+# Descriptors as the calls pack them: RotaryDesc, CrossEntropyDesc and DistillDesc (ctypes takes several times as long)
+_ROTARY = struct.Struct("@4q4P12qPqP5if")
+_CROSS_ENTROPY = struct.Struct("@4q6P2q2if0q")
+_DISTILL = struct.Struct("@5q8P2q3iff0q")
+
+
+def _packed(form: struct.Struct, *values) -> bytes:
+    try:
+        return form.pack(*values)
+    except (struct.error, OverflowError) as err:
+        raise EchoError(1, f"a size or a number does not fit its type: {err}") from None
+
+
 _lib = None
 
 
@@ -204,12 +218,12 @@ def load_library(path: Optional[str] = None):
         "echo_layer_norm": ([vp, C.POINTER(LayerNormDesc)], C.c_int),
         "echo_layer_norm_grad": ([vp, C.POINTER(LayerNormGradDesc)], C.c_int),
         "echo_orthogonalize": ([vp, C.POINTER(OrthogonalizeDesc)], C.c_int),
-        "echo_cross_entropy": ([vp, C.POINTER(CrossEntropyDesc)], C.c_int),
+        "echo_cross_entropy": ([vp, vp], C.c_int),  # (packed descriptors)
         "echo_cross_entropy_grad": ([vp, C.POINTER(CrossEntropyGradDesc)], C.c_int),
-        "echo_distill": ([vp, C.POINTER(DistillDesc)], C.c_int),
+        "echo_distill": ([vp, vp], C.c_int),
         "echo_distill_grad": ([vp, C.POINTER(DistillGradDesc)], C.c_int),
-        "echo_rotary": ([vp, C.POINTER(RotaryDesc)], C.c_int),
-        "echo_rotary_grad": ([vp, C.POINTER(RotaryDesc)], C.c_int),
+        "echo_rotary": ([vp, vp], C.c_int),
+        "echo_rotary_grad": ([vp, vp], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -367,14 +381,15 @@ def _batch(t, out: bool = False):
 
 def _heads(t, out: bool = False):
     """``t`` [..., heads, dim] as [batch, tokens, heads, dim]: (tensor, batch, tokens, strides of the three)."""
-    if t.stride(-1) == 1 or t.shape[-1] == 1:
-        d = t.dim()
-        if d == 2:
-            return t, 1, 1, (0, 0, t.stride(0))
+    strides = t.stride()
+    if strides[-1] == 1 or t.shape[-1] == 1:
+        d = len(strides)
         if d == 3:
-            return t, 1, t.shape[0], (0, t.stride(0), t.stride(1))
+            return t, 1, t.shape[0], (0, strides[0], strides[1])
         if d == 4:
-            return t, t.shape[0], t.shape[1], t.stride()[:3]
+            return t, t.shape[0], t.shape[1], strides[:3]
+        if d == 2:
+            return t, 1, 1, (0, 0, strides[0])
         try:
             return _heads(t.view(-1, *t.shape[-2:]), out)
         except RuntimeError:
@@ -562,8 +577,9 @@ class Echo:
     def _op(self, call, desc):
         """Enqueues an operator in the order of torch's current stream: where that is not
         the context's, the context's stream waits for it and it for the operator."""
+        at = desc if type(desc) is bytes else C.byref(desc)
         if (_current_stream(self.device) or CUDA_STREAM_LEGACY) == self._stream:
-            rc = call(self.h, C.byref(desc))
+            rc = call(self.h, at)
             if rc:
                 self._check(rc)
             return
@@ -572,7 +588,7 @@ class Echo:
         own = (torch.cuda.default_stream(self.device) if self._stream == CUDA_STREAM_LEGACY
                else torch.cuda.ExternalStream(self._stream, device=self.device))
         own.wait_stream(cur)
-        self._check(call(self.h, C.byref(desc)))
+        self._check(call(self.h, at))
         cur.wait_stream(own)
 
     def wait(self):
@@ -711,13 +727,14 @@ class Echo:
     @staticmethod
     def _head(x, weight):
         """(x, weight, rows of x, of weight, hidden, strides of both, type)"""
+        dtype = x.dtype
         _need(weight.dim() == 2 and x.dim() >= 1, "weight is not a matrix")
-        _need(x.dtype == weight.dtype, "x and weight have different types")
-        h = weight.shape[1]
+        v, h = weight.shape
+        _need(weight.dtype == dtype, "x and weight have different types")
         _need(x.shape[-1] == h, "x and weight have rows of different lengths")
         xm, n, xs = _matrix(x)
         wm, _, ws = _matrix(weight)
-        return xm, wm, n, weight.shape[0], h, xs, ws, _type(x.dtype)
+        return xm, wm, n, v, h, xs, ws, _type(dtype)
 
     @staticmethod
     def _per_token(shape, **given):
@@ -725,10 +742,13 @@ class Echo:
         import torch
         found = []
         for name, t in given.items():
-            _need(t is not None or name in ("dlse", "teacher_lse"), f"{name} is missing")
-            if t is not None:
-                _need(t.dtype == torch.float32 and t.shape == shape, f"{name} is not float32, one of them a token")
-            found.append(None if t is None else t.contiguous())
+            if t is None:
+                _need(name in ("dlse", "teacher_lse"), f"{name} is missing")
+            elif t.dtype != torch.float32 or t.shape != shape:
+                raise EchoError(1, f"{name} is not float32, one of them a token")
+            elif not t.is_contiguous():
+                t = t.contiguous()
+            found.append(t)
         return found
 
     def cross_entropy(self, x, weight, labels, scale: float = 1.0, vocab_start: int = 0):
@@ -739,12 +759,14 @@ class Echo:
         import torch
         bits = self._ids(labels)
         xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
-        _need(labels.shape == x.shape[:-1], "labels have another shape than x without its rows")
+        shape = labels.shape
+        _need(shape == x.shape[:-1], "labels have another shape than x without its rows")
         labels = labels.contiguous()
-        loss, lse, target = out = tuple(torch.empty((3, *labels.shape), dtype=torch.float32, device=x.device).unbind())
-        self._op(self.lib.echo_cross_entropy, CrossEntropyDesc(n, h, v, vocab_start, xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), loss.data_ptr(),
-                                                               lse.data_ptr(), target.data_ptr(), xs, ws, kind, bits, scale))
-        return out
+        out = torch.empty((3, *shape), dtype=torch.float32, device=x.device)
+        at = out.data_ptr()  # (three rows, one behind the other)
+        self._op(self.lib.echo_cross_entropy, _packed(_CROSS_ENTROPY, n, h, v, vocab_start, xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), at, at + 4 * n,
+                                                      at + 8 * n, xs, ws, kind, bits, scale))
+        return out.unbind()
 
     def _head_grads(self, x, weight, dx, dweight, dtype, accumulate):
         import torch
@@ -781,7 +803,8 @@ class Echo:
         bits = self._ids(ids)
         _need(ids.dim() == x.dim() and ids.shape[:-1] == x.shape[:-1], "ids have another shape than x without its rows, and the teacher's entries")
         _need(logits.shape == ids.shape, "logits have another shape than ids")
-        (teacher_lse,) = self._per_token(ids.shape[:-1], teacher_lse=teacher_lse)
+        if teacher_lse is not None:
+            (teacher_lse,) = self._per_token(ids.shape[:-1], teacher_lse=teacher_lse)
         return bits, ids.contiguous(), logits.contiguous(), teacher_lse, ids.shape[-1], _type(logits.dtype)
 
     def distill(self, x, weight, ids, logits, temperature: float = 1.0, teacher_lse=None, scale: float = 1.0, vocab_start: int = 0):
@@ -792,10 +815,11 @@ class Echo:
         import torch
         xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
         bits, ids, logits, teacher_lse, top, lkind = self._teacher(x, ids, logits, teacher_lse)
-        loss, lse, cross = out = tuple(torch.empty((3, *ids.shape[:-1]), dtype=torch.float32, device=x.device).unbind())
-        self._op(self.lib.echo_distill, DistillDesc(n, h, v, vocab_start, top, xm.data_ptr(), wm.data_ptr(), ids.data_ptr(), logits.data_ptr(), _dptr(teacher_lse),
-                                                    loss.data_ptr(), lse.data_ptr(), cross.data_ptr(), xs, ws, kind, bits, lkind, scale, temperature))
-        return out
+        out = torch.empty((3, *ids.shape[:-1]), dtype=torch.float32, device=x.device)
+        at = out.data_ptr()
+        self._op(self.lib.echo_distill, _packed(_DISTILL, n, h, v, vocab_start, top, xm.data_ptr(), wm.data_ptr(), ids.data_ptr(), logits.data_ptr(),
+                                                _dptr(teacher_lse) or 0, at, at + 4 * n, at + 8 * n, xs, ws, kind, bits, lkind, scale, temperature))
+        return out.unbind()
 
     def distill_grad(self, dloss, x, weight, ids, logits, lse, temperature: float = 1.0, teacher_lse=None, scale: float = 1.0, vocab_start: int = 0, dlse=None,
                      dtype=None, dx=None, dweight=None, accumulate: bool = False):
@@ -813,38 +837,46 @@ class Echo:
     # -- rotary positions ----------------------------------------------------------------------
     def _rotary(self, call, q, k, positions, frequencies, interleaved, scale, out):
         import torch
-        bits = self._ids(positions)
-        f = np.ascontiguousarray(frequencies, dtype=np.float64)
-        _need(f.ndim == 1, "frequencies are not one of each pair")
-        one = k is None
-        _need(out is None or one or len(out) == 2, "out is not one of each of q and k")
-        xs = [q] if one else [q, k]
-        outs = [torch.empty_like(x, memory_format=torch.contiguous_format) for x in xs] if out is None else [out] if one else list(out)
-        d = RotaryDesc(dim=q.shape[-1], rot=2 * f.shape[0], type=_type(q.dtype), id_bits=bits, interleaved=1 if interleaved else 0, scale=scale,
-                       frequencies=f.ctypes.data)
-        keep = []
-        for i, (x, y) in enumerate(zip(xs, outs)):
-            _need(x.dim() >= 2 and x.shape[-1] == q.shape[-1] and x.shape[:-2] == q.shape[:-2] and x.dtype == q.dtype,
-                  "q and k have other tokens, lengths of a head or types")
-            _need(y.shape == x.shape and y.dtype == x.dtype, "out has another shape or type than q or k")
-            y, _, _, ys = _heads(y, out=True)
-            if x.dim() > 4 and y.dim() <= 3:
-                x = x.reshape(-1, *x.shape[-2:])
-            x, d.n_batch, d.n_tokens, strides = _heads(x)
-            keep.append(x)
-            d.heads[i], d.x[i], d.out[i] = x.shape[-2], x.data_ptr(), y.data_ptr()
-            d.x_batch_stride[i], d.x_stride[i], d.x_head_stride[i] = strides
-            d.out_batch_stride[i], d.out_stride[i], d.out_head_stride[i] = ys
-        # positions of all batches, or the same ones for each
-        lead = q.shape[:-2]
-        if q.dim() == 4 and positions.shape == lead[1:]:
-            positions = positions.contiguous()
+        lead, dim, dtype = q.shape[:-2], q.shape[-1], q.dtype
+        if type(frequencies) is not np.ndarray or frequencies.dtype != np.float64 or not frequencies.flags.c_contiguous:
+            frequencies = np.ascontiguousarray(frequencies, dtype=np.float64)
+        _need(frequencies.ndim == 1 and q.dim() >= 2, "frequencies are not one of each pair, or q has no heads")
+        if k is None:
+            xs, outs = (q,), None if out is None else (out,)
         else:
-            _need(positions.shape == lead, "positions have another shape than the tokens")
-            positions, d.positions_stride = positions.contiguous(), d.n_tokens
-        d.positions = positions.data_ptr()
-        self._op(call, d)
-        return outs[0] if one else tuple(outs)
+            _need(k.dim() >= 2 and k.shape[-1] == dim and k.shape[:-2] == lead and k.dtype == dtype, "q and k have other tokens, lengths of a head or types")
+            xs, outs = (q, k), out
+            _need(out is None or len(out) == 2, "out is not one of each of q and k")
+        results, parts = [], []
+        batch = tokens = 0
+        for i, x in enumerate(xs):
+            if outs is not None:
+                y = outs[i]
+                _need(y.shape == x.shape and y.dtype == dtype, "out has another shape or type than q or k")
+            elif x.is_contiguous():
+                y = torch.empty_like(x)
+            else:
+                y = torch.empty_like(x, memory_format=torch.contiguous_format)
+            results.append(y)
+            flat, _, _, ys = _heads(y, out=True)
+            if x.dim() > 4:
+                x = x.reshape(-1, *x.shape[-2:])
+            x, batch, tokens, strides = _heads(x)
+            parts.append((x, flat, x.shape[-2], strides, ys))
+        # positions of all batches, or the same ones for each
+        each = tokens
+        if positions.shape != lead:
+            _need(q.dim() == 4 and positions.shape == lead[1:], "positions have another shape than the tokens")
+            each = 0
+        if not positions.is_contiguous():
+            positions = positions.contiguous()
+        (x0, y0, h0, (a0, b0, c0), (d0, e0, f0)) = parts[0]
+        (x1, y1, h1, (a1, b1, c1), (d1, e1, f1)) = parts[1] if k is not None else (None, None, 0, (0, 0, 0), (0, 0, 0))
+        desc = _packed(_ROTARY, batch, tokens, h0, h1, x0.data_ptr(), x1.data_ptr() if h1 else 0, y0.data_ptr(), y1.data_ptr() if h1 else 0,
+                            a0, a1, b0, b1, c0, c1, d0, d1, e0, e1, f0, f1, positions.data_ptr(), each, frequencies.__array_interface__["data"][0], dim,
+                            2 * frequencies.shape[0], _type(dtype), self._ids(positions), 1 if interleaved else 0, scale)
+        self._op(call, desc)
+        return results[0] if k is None else tuple(results)
 
     def rotary(self, q, k, positions, frequencies, interleaved: bool = False, scale: float = 1.0, out=None):
         """``q`` and ``k`` [..., heads, dim] (k may be None) with the first 2 * len(frequencies) elements of each head turned by

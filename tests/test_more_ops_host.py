@@ -40,6 +40,16 @@ def test_descriptors_are_the_header_s(tmp_path):
         assert int(at) == (C.sizeof(py) if field == "size" else getattr(py, field).offset), line
 
 
+def test_the_packed_descriptor_is_the_structure():
+    d = E.RotaryDesc(1, 2, (3, 4), (5, 6), (7, 8), (9, 10), (11, 12), (13, 14), (15, 16), (17, 18), (19, 20), 21, 22, 23, 24, 25, 26, 27, 28, 29.5)
+    assert E._ROTARY.pack(*range(1, 29), 29.5) == bytes(d)
+    for form, kind, n, floats in ((E._CROSS_ENTROPY, E.CrossEntropyDesc, 15, 1), (E._DISTILL, E.DistillDesc, 20, 2)):
+        values = list(range(1, n + 1 - floats)) + [0.5] * floats
+        assert form.pack(*values) == bytes(kind(*values))
+    with pytest.raises(E.EchoError):
+        E._packed(E._CROSS_ENTROPY, 2 ** 70, *range(13), 1.0)
+
+
 def test_heads_of_a_view():
     torch = pytest.importorskip("torch")
     x = torch.arange(2 * 3 * 4 * 6.0).view(2, 3, 4, 6)
