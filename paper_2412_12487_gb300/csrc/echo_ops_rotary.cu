@@ -36,29 +36,37 @@ __device__ __forceinline__ uint32_t divide(uint32_t n, uint32_t by) { return by 
 // are on their way.  Bound by the bytes.
 template <typename T, int W, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_constant__ RotaryArgs a, const RotaryPlan p) {
-  __shared__ float2 angles[kAngles];
+  // cos and sin of pair W j + e, so that neighbouring j are side by side: two e of every j, the next two, ...
+  __shared__ alignas(16) float2 angles[kAngles];
   __shared__ int64_t in_at[2][kTokens], out_at[2][kTokens];
   kernel_begin();
   next_may_start();
   const int half = a.rot / 2;
-  const int64_t all = a.batch * a.tokens, t0 = (int64_t)blockIdx.x * p.tokens_block;
-  const int tokens = (int)min((int64_t)p.tokens_block, all - t0);
+  const uint32_t all = (uint32_t)(a.batch * a.tokens), per_batch = (uint32_t)a.tokens, t0 = blockIdx.x * p.tokens_block;  // (below 2^31)
+  const int tokens = (int)min((uint32_t)p.tokens_block, all - t0);
   const int head0 = blockIdx.y * p.heads_block, heads = min(p.heads_block, (int)(a.heads[0] + a.heads[1]) - head0);
   for (int i = threadIdx.x; i < tokens; i += kThreads) {
-    const int64_t b = (t0 + i) / a.tokens, t = (t0 + i) - b * a.tokens;
+    const uint32_t b = (t0 + i) / per_batch, t = (t0 + i) - b * per_batch;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       in_at[k][i] = b * a.x_batch[k] + t * a.x_token[k];
       out_at[k][i] = b * a.out_batch[k] + t * a.out_token[k];
     }
   }
+  auto position_of = [&](int token) -> int64_t {
+    const uint32_t t = t0 + token, b = t / per_batch;
+    const int64_t at = b * a.positions_batch + (t - b * per_batch);
+    return a.id64 ? static_cast<const int64_t *>(a.positions)[at] : static_cast<const int32_t *>(a.positions)[at];
+  };
+  int64_t position0 = 0;  // of this thread's first angle: on its way with the items
+  if ((int)threadIdx.x < tokens * half) position0 = position_of(threadIdx.x / half);
   __syncthreads();
   const uint32_t per_token = (uint32_t)(heads * p.per_head), items = tokens * per_token;
   const int apart = INTERLEAVED ? W : half;  // the second piece of an item that is turned, from the first
   struct Item {
     Pack<T, W> v[2];
     T *to;
-    int pair;  // of the first element, in the block's angles; or:
+    int pair;  // place of the first pair's angle; or:
   };
   constexpr int kCopied = -1, kCopiedFirst = -2, kNothing = -3;  // both pieces as they are, the first one alone, no item
   auto load = [&](uint32_t i, Item &m) {
@@ -72,7 +80,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_
     int first, second = apart;
     if ((int)j < p.turned) {
       first = INTERLEAVED ? 2 * W * (int)j : W * (int)j;
-      m.pair = (int)token * half + W * (int)j;
+      m.pair = (int)token * half + (W > 1 ? 2 : 1) * (int)j;
     } else {
       first = a.rot + 2 * W * ((int)j - p.turned);
       second = W;
@@ -93,9 +101,19 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_
     float v[2][W];
     unpack<T, W>(m.v[0], v[0]);
     unpack<T, W>(m.v[1], v[1]);
+    float2 angle[W];
+    if constexpr (W == 1) {
+      angle[0] = angles[m.pair];
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; e += 2) {
+        const float4 two = *reinterpret_cast<const float4 *>(angles + m.pair + e * p.turned);
+        angle[e] = make_float2(two.x, two.y), angle[e + 1] = make_float2(two.z, two.w);
+      }
+    }
 #pragma unroll
     for (int e = 0; e < W; ++e) {
-      const float2 c = angles[m.pair + e];
+      const float2 c = angle[e];
       // interleaved: elements 2e and 2e + 1 of the two pieces
       float &x = INTERLEAVED ? v[2 * e / W][2 * e % W] : v[0][e], &y = INTERLEAVED ? v[(2 * e + 1) / W][(2 * e + 1) % W] : v[1][e];
       const float x0 = x;
@@ -110,12 +128,12 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_
   for (int k = 0; k < kItems; ++k) load(threadIdx.x + k * kThreads, m[k]);
   for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
     const int token = i / half, pair = i - token * half;
-    const int64_t t = t0 + token, b = t / a.tokens, at = b * a.positions_batch + (t - b * a.tokens);
-    const int64_t position = a.id64 ? static_cast<const int64_t *>(a.positions)[at] : static_cast<const int32_t *>(a.positions)[at];
+    const int64_t position = i == (int)threadIdx.x ? position0 : position_of(token);
     const int64_t turn = (int64_t)((uint64_t)position * a.turns[pair]);  // of a turn, times 2^64: -1/2 to 1/2
     float s, c;
     sincospif(__ll2float_rn(turn) * 0x1p-63f, &s, &c);
-    angles[i] = make_float2(c * a.scale, (a.back ? -s : s) * a.scale);
+    const int at = W == 1 ? pair : (pair % W / 2 * p.turned + pair / W) * 2 + pair % 2;
+    angles[token * half + at] = make_float2(c * a.scale, (a.back ? -s : s) * a.scale);
   }
   __syncthreads();
   for (uint32_t i0 = threadIdx.x;;) {

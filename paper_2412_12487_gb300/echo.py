@@ -850,19 +850,23 @@ class Echo:
         results, parts = [], []
         batch = tokens = 0
         for i, x in enumerate(xs):
-            if outs is not None:
+            if outs is None and x.is_contiguous():
+                y = torch.empty_like(x)
+                x, batch, tokens, strides = _heads(x)
+                parts.append((x, y, x.shape[-2], strides, strides))
+                results.append(y)
+                continue
+            if outs is None:
+                y = torch.empty_like(x, memory_format=torch.contiguous_format)
+            else:
                 y = outs[i]
                 _need(y.shape == x.shape and y.dtype == dtype, "out has another shape or type than q or k")
-            elif x.is_contiguous():
-                y = torch.empty_like(x)
-            else:
-                y = torch.empty_like(x, memory_format=torch.contiguous_format)
             results.append(y)
-            flat, _, _, ys = _heads(y, out=True)
+            y, _, _, ys = _heads(y, out=True)
             if x.dim() > 4:
                 x = x.reshape(-1, *x.shape[-2:])
             x, batch, tokens, strides = _heads(x)
-            parts.append((x, flat, x.shape[-2], strides, ys))
+            parts.append((x, y, x.shape[-2], strides, ys))
         # positions of all batches, or the same ones for each
         each = tokens
         if positions.shape != lead:
