@@ -231,7 +231,7 @@ int rotary(echo_ctx *c, const echo_rotary_desc *d, bool back, const char *name) 
     }
     a.positions = d->positions, a.positions_batch = d->positions_stride, a.id64 = d->id_bits == 64;
     a.dim = d->dim, a.rot = d->rot, a.type = d->type, a.interleaved = d->interleaved != 0, a.back = back, a.scale = d->scale;
-    RUN(echo::launch_rotary(a, o.stream), name);
+    RUN(echo::launch_rotary(a, o.sms, o.stream), name);
     return (int)ECHO_OK;
   });
 }

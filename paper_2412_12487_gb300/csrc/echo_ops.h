@@ -166,6 +166,6 @@ struct RotaryArgs {
   uint64_t turns[kRotaryPairs];  // of a position, times 2^64
 };
 uint64_t rotary_turns(double frequency);
-cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st);
+cudaError_t launch_rotary(const RotaryArgs &a, int sms, cudaStream_t st);
 
 }  // namespace echo

@@ -17,132 +17,105 @@ namespace echo {
 
 namespace {
 
-constexpr int kThreads = 256, kItems = 4;        // items of a thread in flight
-constexpr int kBlocks = 4;                       // of an SM
-constexpr int kAngles = 1024, kTokens = 128;     // angles and tokens of a block, at most
-static_assert(kRotaryPairs <= kAngles, "a token's angles fit");
+constexpr int kWarps = 4;  // of a block
 
+// An item is two pieces of W elements of a head that are turned together, or copied.  A lane takes the
+// same item j of several heads: a warp has `columns` items of `slots` heads at a time.
 struct RotaryPlan {
-  int per_head, turned;       // items of a head: two pieces of W elements each; those that are turned
-  int heads_block;            // heads of a block (grid.y: groups of them)
-  int tokens_block;
-  uint32_t by_head, by_token; // ceil(2^32 / divisor)
+  int items, turned;   // of a head: all, those that are turned
+  int columns, slots;
+  int column_parts;    // warps for the items of a head
+  int head_parts;      // warps for the heads of a token
 };
 
-// n / d for n * d < 2^32
-__device__ __forceinline__ uint32_t divide(uint32_t n, uint32_t by) { return by ? __umulhi(n, by) : n; }
-
-// A block takes some tokens and heads: their angles once, to shared memory, while the first items
-// are on their way.  Bound by the bytes.
+// A warp takes a token and some of its heads.  Its lanes share the work on the angles: the lanes with
+// the same item compute some of its pairs each and pass them on.  Nothing waits for another warp (with a
+// block's angles in shared memory, and barriers, it took 276 us).  Bound by the bytes where there are many
+// tokens: 65536 tokens of 40 heads of 128 in bf16, 1.3e9 bytes, 213 us, 6.3 TB/s; by latency where there
+// are few: 2048 tokens of 24 heads, 2.5e7 bytes, 6.9 us.
 template <typename T, int W, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads, kBlocks) rotary_kernel(const __grid_constant__ RotaryArgs a, const RotaryPlan p) {
-  // cos and sin of pair W j + e, so that neighbouring j are side by side: two e of every j, the next two, ...
-  __shared__ alignas(16) float2 angles[kAngles];
-  __shared__ int64_t in_at[2][kTokens], out_at[2][kTokens];
+__global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const __grid_constant__ RotaryArgs a, const RotaryPlan p) {
   kernel_begin();
   next_may_start();
-  const int half = a.rot / 2;
-  const uint32_t all = (uint32_t)(a.batch * a.tokens), per_batch = (uint32_t)a.tokens, t0 = blockIdx.x * p.tokens_block;  // (below 2^31)
-  const int tokens = (int)min((uint32_t)p.tokens_block, all - t0);
-  const int head0 = blockIdx.y * p.heads_block, heads = min(p.heads_block, (int)(a.heads[0] + a.heads[1]) - head0);
-  for (int i = threadIdx.x; i < tokens; i += kThreads) {
-    const uint32_t b = (t0 + i) / per_batch, t = (t0 + i) - b * per_batch;
+  const int lane = threadIdx.x & 31, half = a.rot / 2;
+  const uint32_t tokens = (uint32_t)(a.batch * a.tokens), per_token = p.head_parts * p.column_parts;  // (tokens below 2^31)
+  const uint32_t warp = blockIdx.x * kWarps + (threadIdx.x >> 5), n = warp / per_token, in_token = warp - n * per_token;
+  if (n >= tokens) return;
+  const int head_part = in_token / p.column_parts, column_part = in_token - head_part * p.column_parts;
+  const uint32_t b = n / (uint32_t)a.tokens, t = n - b * (uint32_t)a.tokens;
+  const int slot = lane / p.columns, j = column_part * p.columns + lane - slot * p.columns;
+  const bool mine = slot < p.slots && j < p.items, turned = j < p.turned;
+  const int64_t at = b * a.positions_batch + t;
+  const int64_t position = a.id64 ? static_cast<const int64_t *>(a.positions)[at] : static_cast<const int32_t *>(a.positions)[at];
+  const int first = !turned ? a.rot + 2 * W * (j - p.turned) : INTERLEAVED ? 2 * W * j : W * j;
+  const int second = first + (!turned || INTERLEAVED ? W : half);
+  const bool both = second < a.dim;  // (or the first piece alone, which is copied)
+
+  const int all = (int)(a.heads[0] + a.heads[1]), heads0 = (int)a.heads[0];
+  const int head_end = (int)((int64_t)all * (head_part + 1) / p.head_parts);
+  int head = (int)((int64_t)all * head_part / p.head_parts) + slot;
+  const T *from[2];
+  T *to[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      in_at[k][i] = b * a.x_batch[k] + t * a.x_token[k];
-      out_at[k][i] = b * a.out_batch[k] + t * a.out_token[k];
+  for (int k = 0; k < 2; ++k) {
+    from[k] = static_cast<const T *>(a.x[k]) + b * a.x_batch[k] + t * a.x_token[k] + first;
+    to[k] = static_cast<T *>(a.out[k]) + b * a.out_batch[k] + t * a.out_token[k] + first;
+  }
+  Pack<T, W> v[2];  // (one item ahead: two or four leave fewer warps, 224 and 265 us instead of 213)
+  auto load = [&](int h, Pack<T, W> (&x)[2]) {
+    if (!mine || h >= head_end) return;
+    const T *f = h < heads0 ? from[0] + h * a.x_head[0] : from[1] + (h - heads0) * a.x_head[1];
+    x[0] = *reinterpret_cast<const Pack<T, W> *>(f);
+    if (both) x[1] = *reinterpret_cast<const Pack<T, W> *>(f + (second - first));
+  };
+  load(head, v);
+
+  // cos and sin of the item's pairs: this lane computes those whose number is `slot` modulo `slots`
+  float2 angle[W];
+  for (int e0 = 0; e0 < W; e0 += p.slots) {
+    const int pair = W * j + e0 + slot;
+    float2 c = make_float2(1.f, 0.f);
+    if (turned && slot < p.slots && e0 + slot < W) {
+      const int64_t turn = (int64_t)((uint64_t)position * a.turns[pair]);  // of a turn, times 2^64: -1/2 to 1/2
+      float sine, cosine;
+      sincospif(__ll2float_rn(turn) * 0x1p-63f, &sine, &cosine);
+      c = make_float2(cosine * a.scale, (a.back ? -sine : sine) * a.scale);
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const int owner = e - e0;  // (slot that has it)
+      const int source = (owner >= 0 && owner < p.slots ? owner : 0) * p.columns + lane - slot * p.columns;
+      const float x = __shfl_sync(0xFFFFFFFFu, c.x, source), y = __shfl_sync(0xFFFFFFFFu, c.y, source);
+      if (owner >= 0 && owner < p.slots) angle[e] = make_float2(x, y);
     }
   }
-  auto position_of = [&](int token) -> int64_t {
-    const uint32_t t = t0 + token, b = t / per_batch;
-    const int64_t at = b * a.positions_batch + (t - b * per_batch);
-    return a.id64 ? static_cast<const int64_t *>(a.positions)[at] : static_cast<const int32_t *>(a.positions)[at];
-  };
-  int64_t position0 = 0;  // of this thread's first angle: on its way with the items
-  if ((int)threadIdx.x < tokens * half) position0 = position_of(threadIdx.x / half);
-  __syncthreads();
-  const uint32_t per_token = (uint32_t)(heads * p.per_head), items = tokens * per_token;
-  const int apart = INTERLEAVED ? W : half;  // the second piece of an item that is turned, from the first
-  struct Item {
-    Pack<T, W> v[2];
-    T *to;
-    int pair;  // place of the first pair's angle; or:
-  };
-  constexpr int kCopied = -1, kCopiedFirst = -2, kNothing = -3;  // both pieces as they are, the first one alone, no item
-  auto load = [&](uint32_t i, Item &m) {
-    m.pair = kNothing;
-    if (i >= items) return;
-    uint32_t token = 0;
-    if (p.tokens_block > 1) token = heads == p.heads_block ? divide(i, p.by_token) : i / per_token;
-    const uint32_t in_token = i - token * per_token, h = divide(in_token, p.by_head), j = in_token - h * p.per_head;
-    const int head = head0 + (int)h, k = head >= a.heads[0];
-    const int64_t hh = head - (k ? a.heads[0] : 0);
-    int first, second = apart;
-    if ((int)j < p.turned) {
-      first = INTERLEAVED ? 2 * W * (int)j : W * (int)j;
-      m.pair = (int)token * half + (W > 1 ? 2 : 1) * (int)j;
-    } else {
-      first = a.rot + 2 * W * ((int)j - p.turned);
-      second = W;
-      m.pair = first + W < a.dim ? kCopied : kCopiedFirst;
-    }
-    const T *from = static_cast<const T *>(a.x[k]) + in_at[k][token] + hh * a.x_head[k] + first;
-    m.to = static_cast<T *>(a.out[k]) + out_at[k][token] + hh * a.out_head[k] + first;
-    m.v[0] = *reinterpret_cast<const Pack<T, W> *>(from);
-    if (m.pair != kCopiedFirst) m.v[1] = *reinterpret_cast<const Pack<T, W> *>(from + second);
-  };
-  auto finish = [&](const Item &m) {
-    if (m.pair == kNothing) return;
-    if (m.pair < 0) {
-      *reinterpret_cast<Pack<T, W> *>(m.to) = m.v[0];
-      if (m.pair == kCopied) *reinterpret_cast<Pack<T, W> *>(m.to + W) = m.v[1];
+
+  auto finish = [&](int h, const Pack<T, W> (&x)[2]) {
+    if (!mine || h >= head_end) return;
+    T *o = h < heads0 ? to[0] + h * a.out_head[0] : to[1] + (h - heads0) * a.out_head[1];
+    if (!turned) {
+      *reinterpret_cast<Pack<T, W> *>(o) = x[0];
+      if (both) *reinterpret_cast<Pack<T, W> *>(o + (second - first)) = x[1];
       return;
     }
-    float v[2][W];
-    unpack<T, W>(m.v[0], v[0]);
-    unpack<T, W>(m.v[1], v[1]);
-    float2 angle[W];
-    if constexpr (W == 1) {
-      angle[0] = angles[m.pair];
-    } else {
-#pragma unroll
-      for (int e = 0; e < W; e += 2) {
-        const float4 two = *reinterpret_cast<const float4 *>(angles + m.pair + e * p.turned);
-        angle[e] = make_float2(two.x, two.y), angle[e + 1] = make_float2(two.z, two.w);
-      }
-    }
+    float f[2][W];
+    unpack<T, W>(x[0], f[0]);
+    unpack<T, W>(x[1], f[1]);
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       const float2 c = angle[e];
       // interleaved: elements 2e and 2e + 1 of the two pieces
-      float &x = INTERLEAVED ? v[2 * e / W][2 * e % W] : v[0][e], &y = INTERLEAVED ? v[(2 * e + 1) / W][(2 * e + 1) % W] : v[1][e];
-      const float x0 = x;
-      x = fmaf(x0, c.x, -__fmul_rn(y, c.y));  // (one order of roundings for every layout)
-      y = fmaf(x0, c.y, __fmul_rn(y, c.x));
+      float &x0 = INTERLEAVED ? f[2 * e / W][2 * e % W] : f[0][e], &x1 = INTERLEAVED ? f[(2 * e + 1) / W][(2 * e + 1) % W] : f[1][e];
+      const float old = x0;
+      x0 = fmaf(old, c.x, -__fmul_rn(x1, c.y));  // (one order of roundings for every layout)
+      x1 = fmaf(old, c.y, __fmul_rn(x1, c.x));
     }
-    store_piece<W>(m.to, v[0]);
-    store_piece<W>(m.to + apart, v[1]);
+    store_piece<W>(o, f[0]);
+    store_piece<W>(o + (second - first), f[1]);
   };
-  Item m[kItems];
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) load(threadIdx.x + k * kThreads, m[k]);
-  for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
-    const int token = i / half, pair = i - token * half;
-    const int64_t position = i == (int)threadIdx.x ? position0 : position_of(token);
-    const int64_t turn = (int64_t)((uint64_t)position * a.turns[pair]);  // of a turn, times 2^64: -1/2 to 1/2
-    float s, c;
-    sincospif(__ll2float_rn(turn) * 0x1p-63f, &s, &c);
-    const int at = W == 1 ? pair : (pair % W / 2 * p.turned + pair / W) * 2 + pair % 2;
-    angles[token * half + at] = make_float2(c * a.scale, (a.back ? -s : s) * a.scale);
-  }
-  __syncthreads();
-  for (uint32_t i0 = threadIdx.x;;) {
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) finish(m[k]);
-    i0 += kThreads * kItems;
-    if (i0 - threadIdx.x >= items) break;
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) load(i0 + k * kThreads, m[k]);
+  for (; head - slot < head_end; head += p.slots) {
+    finish(head, v);
+    load(head + p.slots, v);
   }
 }
 
@@ -157,7 +130,7 @@ uint64_t rotary_turns(double f) {
   return (uint64_t)((p - std::floor(p)) * 0x1p64) + (uint64_t)std::llrint(rest * 0x1p64);  // (the difference is exact)
 }
 
-cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st) {
+cudaError_t launch_rotary(const RotaryArgs &a, int sms, cudaStream_t st) {
   return with_type(a.type, [&](auto t) {
     using T = decltype(t);
     auto fits = [&](int W) {
@@ -173,16 +146,23 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t st) {
       constexpr int W = decltype(w)::value;
       RotaryPlan p{};
       p.turned = a.rot / 2 / W;
-      p.per_head = p.turned + (a.dim - a.rot + 2 * W - 1) / (2 * W);
-      const int heads = (int)(a.heads[0] + a.heads[1]);
-      p.heads_block = std::min(heads, std::max(1, 2048 / p.per_head));
-      const int per_token = p.heads_block * p.per_head;
-      p.tokens_block = std::max(1, std::min({kThreads * kItems / per_token, kAngles / (a.rot / 2), kTokens}));
-      p.by_head = (uint32_t)((((uint64_t)1 << 32) + p.per_head - 1) / p.per_head);
-      p.by_token = (uint32_t)((((uint64_t)1 << 32) + per_token - 1) / per_token);
-      const dim3 grid((unsigned)((a.batch * a.tokens + p.tokens_block - 1) / p.tokens_block), (unsigned)((heads + p.heads_block - 1) / p.heads_block));
-      if (a.interleaved) return launch_early(rotary_kernel<T, W, true>, grid, kThreads, 0, st, a, p);
-      return launch_early(rotary_kernel<T, W, false>, grid, kThreads, 0, st, a, p);
+      p.items = p.turned + (a.dim - a.rot + 2 * W - 1) / (2 * W);
+      // as many lanes at work as can be, in runs of eight items at least
+      double best = 0;
+      for (int c = std::min(p.items, 32); c >= std::min(p.items, 8); --c) {
+        const double used = (double)p.items / ((p.items + c - 1) / c * c) * (32 / c * c);
+        if (used > best * 1.01) best = used, p.columns = c;
+      }
+      p.slots = 32 / p.columns;
+      p.column_parts = (p.items + p.columns - 1) / p.columns;
+      // few tokens are spread over more warps: up to 16 an SM, as far as there are heads
+      const int64_t heads = a.heads[0] + a.heads[1], tokens = a.batch * a.tokens;
+      p.head_parts = (int)std::clamp<int64_t>(16 * sms / (tokens * p.column_parts), 1, (heads + p.slots - 1) / p.slots);
+      const int64_t warps = tokens * p.head_parts * p.column_parts;
+      if (warps >= (int64_t)1 << 32) return cudaErrorInvalidConfiguration;
+      const unsigned grid = (unsigned)((warps + kWarps - 1) / kWarps);
+      if (a.interleaved) return launch_early(rotary_kernel<T, W, true>, dim3(grid), kWarps * 32, 0, st, a, p);
+      return launch_early(rotary_kernel<T, W, false>, dim3(grid), kWarps * 32, 0, st, a, p);
     };
     constexpr int N = 16 / sizeof(T);
     return fits(N) ? go(Int<N>{}) : fits(2) ? go(Int<2>{}) : go(Int<1>{});
