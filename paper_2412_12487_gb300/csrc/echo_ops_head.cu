@@ -22,8 +22,8 @@
 //     (bf16) of each element, independent of the others, where the results are rounded to the
 //     same.  For an fp32 dW as the sum of two fp16 numbers, with x as fp16 (the same way): a
 //     gradient added up over micro-batches in fp32 would otherwise be 2e-3 off.
-// The tensor core truncates the sums that it adds to, so they are added up in registers, rounding
-// to nearest, every kSet stages.
+// The tensor core truncates the sums that it adds to, which is a bias, so they are added up in
+// registers, rounding to nearest, every few stages (set_of).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -78,16 +78,32 @@ struct Operand {
   Scale scale;
 };
 
+// Up to two matrices for one launch (grid.y): x and the weight.
+struct Source {
+  const void *p;
+  int64_t rows, cols, stride;
+  Scale scale;          // of what it becomes
+  const float *live;    // rows that are not live become zeros; null: all are
+  void *to;
+  int64_t ld, plane;
+  float *amax;
+};
+struct Sources {
+  Source of[2];
+};
+
 // The largest finite element of each block's part of a matrix (without gaps, a single row).
-// Bound by the bytes.
+// Bound by the bytes, or by latency where they are few.
 template <typename T, int W>
-__global__ void __launch_bounds__(256) head_amax_kernel(const T *x, int64_t rows, int64_t cols, int64_t stride, float *part) {
+__global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
   __shared__ float sh[8];
   kernel_begin();
   next_may_start();
-  const int64_t pieces = cols / W, all = rows * pieces;
-  float m = 0.f;
-  constexpr int kFlight = 4;
+  const Source &m = s.of[blockIdx.y];
+  const T *x = static_cast<const T *>(m.p);
+  const int64_t pieces = m.cols / W, all = m.rows * pieces;
+  float most = 0.f;
+  constexpr int kFlight = 8 / (W > 4 ? 2 : 1);
   for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
     float v[kFlight][W];
 #pragma unroll
@@ -95,40 +111,42 @@ __global__ void __launch_bounds__(256) head_amax_kernel(const T *x, int64_t rows
       const int64_t i = i0 + k * 256;
 #pragma unroll
       for (int e = 0; e < W; ++e) v[k][e] = 0.f;
-      if (i < all) load_piece<W>(rows == 1 ? x + i * W : x + i / pieces * stride + i % pieces * W, v[k]);
+      if (i < all) load_piece<W>(m.rows == 1 ? x + i * W : x + i / pieces * m.stride + i % pieces * W, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
 #pragma unroll
-      for (int e = 0; e < W; ++e) m = fmaxf(m, finite_size(v[k][e]));
+      for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[k][e]));
   }
 #pragma unroll
-  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
+  for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = most;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < 8; ++w) m = fmaxf(m, sh[w]);
-    part[blockIdx.x] = m;
+    for (int w = 1; w < 8; ++w) most = fmaxf(most, sh[w]);
+    m.amax[blockIdx.x] = most;
   }
 }
 
 // A matrix as PLANES planes of type D (fp16 ones times 2^exponent); rows that are not live become
 // zeros, so that whatever they hold (padding) meets nothing in a product.  Bound by the bytes.
 template <typename T, typename D, int PLANES, int W>
-__global__ void __launch_bounds__(256) head_pack_kernel(const T *x, int64_t rows, int64_t cols, int64_t stride, Scale scale, const float *live, D *to,
-                                                        int64_t ld, int64_t plane) {
+__global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
   __shared__ int sh;
   kernel_begin();
   next_may_start();
+  const Source &m = s.of[blockIdx.y];
+  const T *x = static_cast<const T *>(m.p);
+  D *to = static_cast<D *>(m.to);
   if (threadIdx.x < 32) {
-    const int e = exponent(scale);
+    const int e = exponent(m.scale);
     if (threadIdx.x == 0) sh = e;
   }
   __syncthreads();
   const float up = ldexpf(1.f, sh);
-  const uint32_t pieces = (uint32_t)(cols / W);
-  const int64_t all = rows * pieces;
-  constexpr int kFlight = 4;
+  const uint32_t pieces = (uint32_t)(m.cols / W);
+  const int64_t all = m.rows * pieces;
+  constexpr int kFlight = 8 / (W > 4 ? 2 : 1);
   for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
     float v[kFlight][W];
     int64_t at[kFlight];
@@ -137,9 +155,9 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T *x, int64_t rows
       const int64_t i = i0 + k * 256;
       if (i >= all) continue;
       const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), c = i - r * pieces;
-      at[k] = r * ld + c * W;
-      if (!live || live[r] != 0.f) {
-        load_piece<W>(x + r * stride + c * W, v[k]);
+      at[k] = r * m.ld + c * W;
+      if (!m.live || m.live[r] != 0.f) {
+        load_piece<W>(x + r * m.stride + c * W, v[k]);
       } else {
 #pragma unroll
         for (int e = 0; e < W; ++e) v[k][e] = 0.f;
@@ -158,7 +176,7 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T *x, int64_t rows
           h.v[e] = from_f<D>(v[k][e]);
           v[k][e] -= to_f(h.v[e]);  // what the next plane holds
         }
-        *reinterpret_cast<Pack<D, W> *>(to + q * plane + at[k]) = h;
+        *reinterpret_cast<Pack<D, W> *>(to + q * m.plane + at[k]) = h;
       }
     }
   }
@@ -308,12 +326,11 @@ static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's r
 constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
 constexpr int kSlots = 2, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
 constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 256 + 1024;
-constexpr int kSet = 16;                         // stages that the tensor core adds up by itself
 
 struct Job {
   int M, N, steps;  // rows, columns; stages of a pair of planes
   int pairs, plane_a[3], plane_b[3];
-  int a_mn, b_mn;
+  int set;          // stages that the tensor core adds up by itself
   uint32_t instr;
   int tiles_n;
   int64_t tiles;
@@ -638,8 +655,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int s = 0, b = 0;
       uint32_t phase = 0, sums_phase = 1;  // (of both sets alike: they take turns)
       bool ok = true;
-      auto multiply = [&](auto a_mn, auto b_mn, uint32_t instr, int steps) {
+      auto multiply = [&](auto a_mn, auto b_mn, const Job &j, int steps) {
         constexpr bool A = decltype(a_mn)::value, B = decltype(b_mn)::value;
+        const uint32_t instr = j.instr;
+        const int set = j.set;
         const uint64_t p0 = operand(ring, A), q0 = operand(ring + kOperandBytes, B);
         for (int left = steps, in_set = 0; left; --left) {
           ok = (in_set || bar_wait(sums_empty + 8 * b, sums_phase, abort, wait)) && bar_wait(full + 8 * s, phase, abort, wait);
@@ -651,7 +670,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(A) * kk, q + step16(B) * kk, instr, kk > 0 || in_set);
           commit_pair(empty + 8 * s);
           if (++s == kStages) s = 0, phase ^= 1;
-          if (++in_set == kSet || left == 1) {
+          if (++in_set == set || left == 1) {
             commit_pair(sums_full + 8 * b);
             in_set = 0;
             b ^= 1;
@@ -661,9 +680,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       };
       Worker worker(a.schedule, pair, pairs);
       for (Share w; ok && worker.next(w);) {
-        if (MODE != kOut) multiply(Int<0>{}, Int<0>{}, a.job[0].instr, w.k1 - w.k0);
-        else if (w.which == 0) multiply(Int<0>{}, Int<1>{}, a.job[0].instr, w.k1 - w.k0);
-        else multiply(Int<1>{}, Int<1>{}, a.job[1].instr, w.k1 - w.k0);
+        if (MODE != kOut) multiply(Int<0>{}, Int<0>{}, a.job[0], w.k1 - w.k0);
+        else if (w.which == 0) multiply(Int<0>{}, Int<1>{}, a.job[0], w.k1 - w.k0);
+        else multiply(Int<1>{}, Int<1>{}, a.job[1], w.k1 - w.k0);
       }
       commit(done);  // nothing is in flight when the block ends
       const long long t0 = clock64();
@@ -709,7 +728,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
       float acc[kParts][32] = {};
-      const int sets = (w.k1 - w.k0 + kSet - 1) / kSet;
+      const int sets = (w.k1 - w.k0 + j.set - 1) / j.set;
       for (int set = 0; set < sets; ++set) {
         const int b = (int)(n & 1);
         ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait);
@@ -797,15 +816,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (in) a.part[(int64_t)(c0 / kHalf) * a.n + row] = make_float2(most, sum[0].a + sum[0].b);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          const int end = c0 + part * 32 + 32;
-          while (__any_sync(0xFFFFFFFFu, at.next < end)) {
-            const bool hit = at.next < end;
-            const int column = hit ? at.next - (end - 32) : -1;
-            float z = 0.f;
+          const int column0 = c0 + part * 32;
+          while (__any_sync(0xFFFFFFFFu, at.next < column0 + 32)) {
+            const bool hit = at.next < column0 + 32;
+            const int column = hit ? at.next - column0 : 0;
+            // the element of that number, a bit of it after the other
+            float z[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) z = column == e ? acc[part][e] : z;
+            for (int e = 0; e < 16; ++e) z[e] = column & 16 ? acc[part][e + 16] : acc[part][e];
+#pragma unroll
+            for (int half = 8; half; half >>= 1)
+#pragma unroll
+              for (int e = 0; e < half; ++e) z[e] = column & half ? z[e + half] : z[e];
             if (hit) {
-              a.picked[row * a.K + at.k] = z * kLn2;
+              a.picked[row * a.K + at.k] = z[0] * kLn2;
               at.step();
             }
           }
@@ -888,38 +912,50 @@ __global__ void __launch_bounds__(256) head_round_kernel(const float *from, int6
 }
 
 // -- the end of the forward pass -------------------------------------------------------------------
-// A block joins the parts of 32 rows: a warp every eighth part of all rows, then a warp a row's
-// targets, in their order.
-__global__ void __launch_bounds__(256) head_join_kernel(HeadArgs a, Targets t, const float2 *part, int64_t chunks, const float *picked) {
-  __shared__ float2 sh[8][32];
-  __shared__ float lses[32];
+// A block joins the parts of 32 rows: a warp every 32nd part of all rows, eight of them on their way,
+// then a warp a row's targets, in their order.  Bound by latency: 2048 rows of 400 parts, 6.6 MB.
+constexpr int kJoinWarps = 32;
+__device__ __forceinline__ float2 joined(float2 x, float2 y) {  // (an empty part has -inf and 0)
+  const float m = fmaxf(x.x, y.x);
+  if (m == -INFINITY) return make_float2(m, x.y + y.y);
+  return make_float2(m, x.y * exp2f(x.x - m) + y.y * exp2f(y.x - m));
+}
+__global__ void __launch_bounds__(kJoinWarps * 32) head_join_kernel(HeadArgs a, Targets t, const float2 *part, int64_t chunks, const float *picked) {
+  __shared__ float2 sh[kJoinWarps][33];
   kernel_begin();
   next_may_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto join = [](float2 x, float2 y) {  // (an empty part has -inf and 0)
-    const float m = fmaxf(x.x, y.x);
-    if (m == -INFINITY) return make_float2(m, x.y + y.y);
-    return make_float2(m, x.y * exp2f(x.x - m) + y.y * exp2f(y.x - m));
-  };
   for (int64_t r0 = (int64_t)blockIdx.x * 32; r0 < a.n; r0 += (int64_t)gridDim.x * 32) {
-    float2 s = make_float2(-INFINITY, 0.f);
-    if (r0 + lane < a.n)
-      for (int64_t k = warp; k < chunks; k += 8) s = join(s, part[k * a.n + r0 + lane]);
-    sh[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0) {
-      for (int w = 1; w < 8; ++w) s = join(s, sh[w][lane]);
-      lses[lane] = s.x == -INFINITY ? s.y == 0.f ? -INFINITY : NAN : fmaf(s.x, kLn2, logf(s.y));
-    }
-    __syncthreads();
-    for (int r = warp; r < 32 && r0 + r < a.n; r += 8) {
-      const int64_t row = r0 + r;
-      float cross = 0.f;
+    // a row's targets, while the parts come
+    const int64_t row = r0 + warp;
+    float cross = 0.f;
+    if (row < a.n)
       for (int k = lane; k < a.K; k += 32)
         if (t.idx[row * a.K + k] != INT_MAX) cross += t.weight[row * a.K + k] * picked[row * a.K + k];
+    float2 s = make_float2(-INFINITY, 0.f);
+    constexpr int kFlight = 8;
+    for (int64_t k0 = warp; k0 < chunks; k0 += kFlight * kJoinWarps) {
+      float2 v[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        v[k] = make_float2(-INFINITY, 0.f);
+        if (k0 + k * kJoinWarps < chunks && r0 + lane < a.n) v[k] = part[(k0 + k * kJoinWarps) * a.n + r0 + lane];
+      }
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) s = joined(s, v[k]);
+    }
+    sh[warp][lane] = s;
+    __syncthreads();
+    if (row < a.n) {
+      s = sh[lane][warp];
+#pragma unroll
+      for (int d = 16; d; d >>= 1) {
+        const float2 other = make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, d), __shfl_xor_sync(0xFFFFFFFFu, s.y, d));
+        s = lane & d ? joined(other, s) : joined(s, other);
+      }
       cross = warp_sum(cross);
       if (lane == 0) {
-        const float lse = lses[r], mass = t.mass[row];
+        const float lse = s.x == -INFINITY ? s.y == 0.f ? -INFINITY : NAN : fmaf(s.x, kLn2, logf(s.y)), mass = t.mass[row];
         if (a.loss) a.loss[row] = mass == 0.f ? 0.f : a.tau * a.tau * (t.entropy[row] + fmaf(mass, lse, -cross));
         if (a.lse) a.lse[row] = lse;
         if (a.part) a.part[row] = cross;
@@ -1063,8 +1099,15 @@ cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type
                  type == ECHO_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16);
 }
 
+// Stages of 64 columns that are summed with truncation.  Taking a set out of tensor memory keeps the
+// tensor core from it for 256 clocks, half a stage: results of 16 bits take 16 stages, of 32 bits eight
+// (2048 tokens of 12288 columns: logits 9.1e-7 off with 16, 4.2e-7 with eight, 2.3e-7 with four), and
+// fp32 matrices, whose stages are summed three times over, four (1003 tokens of 517: 2.5e-6 with 16,
+// 5.9e-7 with four).
+int set_of(bool f32_matrices, bool f32_result) { return f32_matrices ? 4 : f32_result ? 8 : 16; }
+
 // D = A B^T; mn: the operand is held transposed
-Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn) {
+Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, int set) {
   Job j{};
   j.M = (int)(a_mn ? a.cols : a.rows);
   j.N = (int)(b_mn ? b.cols : b.rows);
@@ -1072,7 +1115,7 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn) {
   for (int p = 0; p < a.planes; ++p)
     for (int q = 0; q < b.planes; ++q)
       if (p + q < 2) j.plane_a[j.pairs] = p, j.plane_b[j.pairs++] = q;
-  j.a_mn = a_mn, j.b_mn = b_mn;
+  j.set = set;
   j.instr = instruction(kTile, a_mn, b_mn, a.bf16);
   j.tiles_n = (j.N + kTile - 1) / kTile;
   j.tiles = (int64_t)((j.M + kTile - 1) / kTile) * j.tiles_n;
@@ -1128,34 +1171,46 @@ cudaError_t launch_product(const Maps &m, HeadProduct &g, int sms, cudaStream_t 
     if (_e != cudaSuccess) return _e;            \
   } while (0)
 
-cudaError_t launch_amax(const void *x, int type, int64_t rows, int64_t cols, int64_t stride, float *part, cudaStream_t st) {
+Source source(const void *p, int type, int64_t rows, int64_t cols, int64_t stride) {
+  Source m{};
+  m.p = p, m.rows = rows, m.cols = cols, m.stride = rows == 1 ? cols : stride;
+  return m;
+}
+// The largest elements of `count` matrices.
+cudaError_t launch_amax(Sources s, int count, int type, cudaStream_t st) {
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     constexpr int N = 16 / sizeof(T);
-    const bool one = stride == cols || rows == 1;
-    const int64_t r = one ? 1 : rows, c = one ? rows * cols : cols;
-    if (cols % N == 0 && fits_pieces(x, stride, type, N))
-      return launch_early(head_amax_kernel<T, N>, dim3(kAmaxParts), 256, 0, st, static_cast<const T *>(x), r, c, stride, part);
-    return launch_early(head_amax_kernel<T, 1>, dim3(kAmaxParts), 256, 0, st, static_cast<const T *>(x), r, c, stride, part);
+    bool wide = true;
+    for (int i = 0; i < count; ++i) {
+      Source &m = s.of[i];
+      if (m.stride == m.cols) m.cols *= m.rows, m.rows = 1;
+      wide &= m.cols % N == 0 && fits_pieces(m.p, m.stride, type, N);
+    }
+    return wide ? launch_early(head_amax_kernel<T, N>, dim3(kAmaxParts, count), 256, 0, st, s) : launch_early(head_amax_kernel<T, 1>, dim3(kAmaxParts, count), 256, 0, st, s);
   });
 }
-
-cudaError_t launch_pack(const void *x, int type, int64_t stride, const Operand &o, const float *live, int sms, cudaStream_t st) {
+// `count` matrices of a type as planes, of bf16 numbers or fp16 ones.
+cudaError_t launch_pack(const Sources &s, int count, int type, bool bf16, int sms, cudaStream_t st) {
   return with_type(type, [&](auto t) {
     using T = decltype(t);
+    bool wide = true;
+    int64_t most = 1;
+    for (int i = 0; i < count; ++i) {
+      wide &= s.of[i].cols % 8 == 0 && fits_pieces(s.of[i].p, s.of[i].stride, type, 8);
+      most = std::max(most, s.of[i].rows * s.of[i].cols);
+    }
     auto go = [&](auto d, auto planes) {
-      using D = decltype(d);
       auto with = [&](auto w) {
         constexpr int W = decltype(w)::value;
-        const int64_t blocks = std::min<int64_t>((o.rows * (o.cols / W) + 1023) / 1024, sms * 6);
-        return launch_early(head_pack_kernel<T, D, decltype(planes)::value, W>, dim3((unsigned)blocks), 256, 0, st, static_cast<const T *>(x), o.rows, o.cols,
-                            stride, o.scale, live, static_cast<D *>(const_cast<void *>(o.p)), o.ld, o.plane);
+        const dim3 grid((unsigned)std::min<int64_t>((most / W + 1023) / 1024, sms * 8), count);
+        return launch_early(head_pack_kernel<T, decltype(d), decltype(planes)::value, W>, grid, 256, 0, st, s);
       };
-      return o.cols % 8 == 0 && fits_pieces(x, stride, type, 8) ? with(Int<8>{}) : with(Int<1>{});
+      return wide ? with(Int<8>{}) : with(Int<1>{});
     };
     if constexpr (std::is_same_v<T, float>) return go(__half{}, Int<2>{});
     else if constexpr (std::is_same_v<T, __half>) return go(__half{}, Int<1>{});
-    else return o.bf16 ? go(__nv_bfloat16{}, Int<1>{}) : go(__half{}, Int<1>{});
+    else return bf16 ? go(__nv_bfloat16{}, Int<1>{}) : go(__half{}, Int<1>{});
   });
 }
 
@@ -1170,13 +1225,25 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   const bool f32 = a.type == ECHO_F32;
   TRY(timed("head_targets", [&] { return launch_early(head_targets_kernel, dim3(l.target_blocks), kTargetWarps * 32, 0, st, a, l.targets); }));
   const bool exact_dw = a.grad && a.dw && a.dw_type == ECHO_F32;
-  if (f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16))
-    TRY(timed("head_amax", [&] { return launch_amax(a.x, a.type, a.n, a.H, a.x_stride, l.amax_x, st); }));
-  if (f32 && a.V) TRY(timed("head_amax", [&] { return launch_amax(a.w, a.type, a.V, a.H, a.w_stride, l.amax_w, st); }));
+  const Source sx = source(a.x, a.type, a.n, a.H, a.x_stride), sw = source(a.w, a.type, a.V, a.H, a.w_stride);
+  const bool sized_x = f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16), sized_w = f32 && a.V;
+  Sources s{};
+  int count = 0;
+  if (sized_x) s.of[count] = sx, s.of[count++].amax = l.amax_x;
+  if (sized_w) s.of[count] = sw, s.of[count++].amax = l.amax_w;
+  if (count) TRY(timed("head_amax", [&] { return launch_amax(s, count, a.type, st); }));
   // (backward, the rows of tokens without gradients are zeros in fp32's planes, which both products read)
-  if (l.pack_x) TRY(timed("head_pack", [&] { return launch_pack(a.x, a.type, a.x_stride, l.x, a.grad ? l.targets.live : nullptr, sms, st); }));
-  if (l.pack_w && a.V) TRY(timed("head_pack", [&] { return launch_pack(a.w, a.type, a.w_stride, l.w, nullptr, sms, st); }));
-  if (l.pack_x_dw) TRY(timed("head_pack", [&] { return launch_pack(a.x, a.type, a.x_stride, l.x_dw, l.targets.live, sms, st); }));
+  auto pack = [&](const Source &m, const Operand &o, const float *live) {
+    Source &t = s.of[count++] = m;
+    t.scale = o.scale, t.live = live, t.to = const_cast<void *>(o.p), t.ld = o.ld, t.plane = o.plane;
+  };
+  count = 0;
+  if (l.pack_x) pack(sx, l.x, a.grad && f32 ? l.targets.live : nullptr);
+  if (l.pack_w && a.V) pack(sw, l.w, nullptr);
+  if (count) TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x.bf16, sms, st); }));
+  count = 0;
+  if (l.pack_x_dw) pack(sx, l.x_dw, l.targets.live);
+  if (count) TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x_dw.bf16, sms, st); }));
 
   HeadProduct g{};
   g.wait = {a.status, a.wait_limit}, g.skip = a.skip;
@@ -1187,13 +1254,13 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   if (!a.grad) {
     g.part = l.part, g.picked = l.picked;
     if (a.V) {
-      g.job[0] = job_of(l.x, false, l.w, false);
+      g.job[0] = job_of(l.x, false, l.w, false, set_of(f32, true));
       TRY(stage_map(&m.a[0], l.x, false));
       TRY(stage_map(&m.b[0], l.w, false));
       TRY(timed("head_logits", [&] { return launch_product<kStats>(m, g, sms, st); }));
     }
     return timed("head_join", [&] {
-      return launch_early(head_join_kernel, dim3((unsigned)std::min<int64_t>((a.n + 31) / 32, 8 * sms)), 256, 0, st, a, l.targets, l.part, l.chunks, l.picked);
+      return launch_early(head_join_kernel, dim3((unsigned)std::min<int64_t>((a.n + 31) / 32, 2 * sms)), kJoinWarps * 32, 0, st, a, l.targets, l.part, l.chunks, l.picked);
     });
   }
 
@@ -1214,7 +1281,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     };
     HeadProduct h = g;
     h.v_begin = (int)v;
-    h.job[0] = job_of(l.x, false, w, false);
+    h.job[0] = job_of(l.x, false, w, false, set_of(f32, exact_dw));
     TRY(stage_map(&m.a[0], l.x, false));
     TRY(stage_map(&m.b[0], w, false));
     TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
@@ -1223,7 +1290,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     HeadProduct d = g;
     if (a.dx) {
       const Operand q = planes(a.type == ECHO_BF16, f32 ? 2 : 1);
-      Job &j = d.job[0] = job_of(q, false, w, true);
+      Job &j = d.job[0] = job_of(q, false, w, true, set_of(f32, false));
       TRY(stage_map(&m.a[0], q, false));
       TRY(stage_map(&m.b[0], w, true));
       if (l.dx_sum) TRY(out_to(j, &m.out[0], l.dx_sum, l.dx_ld, ECHO_F32, v > 0));
@@ -1231,7 +1298,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     }
     if (a.dw) {
       const Operand q = planes(l.x_dw.bf16, f32 || exact_dw ? 2 : 1);
-      Job &j = d.job[1] = job_of(q, true, l.x_dw, true);
+      Job &j = d.job[1] = job_of(q, true, l.x_dw, true, set_of(f32, exact_dw));
       TRY(stage_map(&m.a[1], q, true));
       TRY(stage_map(&m.b[1], l.x_dw, true));
       TRY(out_to(j, &m.out[1], static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type), a.dw_stride, a.dw_type, a.accumulate));
