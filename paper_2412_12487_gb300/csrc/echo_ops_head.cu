@@ -330,7 +330,7 @@ constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes
 struct Job {
   int M, N, steps;  // rows, columns; stages of a pair of planes
   int pairs, plane_a[3], plane_b[3];
-  int set;          // stages that the tensor core adds up by itself
+  int lead, set;    // stages that the tensor core adds up by itself: of the first two sets of a tile, of the others
   uint32_t instr;
   int tiles_n;
   int64_t tiles;
@@ -658,9 +658,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       auto multiply = [&](auto a_mn, auto b_mn, const Job &j, int steps) {
         constexpr bool A = decltype(a_mn)::value, B = decltype(b_mn)::value;
         const uint32_t instr = j.instr;
-        const int set = j.set;
+        const int lead = j.lead, set = j.set;
         const uint64_t p0 = operand(ring, A), q0 = operand(ring + kOperandBytes, B);
-        for (int left = steps, in_set = 0; left; --left) {
+        for (int left = steps, in_set = 0, ends = lead, number = 0; left; --left) {
           ok = (in_set || bar_wait(sums_empty + 8 * b, sums_phase, abort, wait)) && bar_wait(full + 8 * s, phase, abort, wait);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -670,9 +670,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < kBK / 16; ++kk) mma(d, p + step16(A) * kk, q + step16(B) * kk, instr, kk > 0 || in_set);
           commit_pair(empty + 8 * s);
           if (++s == kStages) s = 0, phase ^= 1;
-          if (++in_set == set || left == 1) {
+          if (++in_set == ends || left == 1) {
             commit_pair(sums_full + 8 * b);
             in_set = 0;
+            ends = ++number < 2 ? lead : set;
             b ^= 1;
             if (b == 0) sums_phase ^= 1;
           }
@@ -728,7 +729,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
       float acc[kParts][32] = {};
-      const int sets = (w.k1 - w.k0 + j.set - 1) / j.set;
+      const int steps = w.k1 - w.k0, after = steps - 2 * j.lead;  // (stages after the first two sets)
+      const int sets = after > 0 ? 2 + (after + j.set - 1) / j.set : steps > j.lead ? 2 : 1;
       for (int set = 0; set < sets; ++set) {
         const int b = (int)(n & 1);
         ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait);
@@ -865,9 +867,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               }
             } else {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                h[e / 8].v[e % 8] = __float2half_rn(v[e]);
-                v[e] -= __half2float(h[e / 8].v[e % 8]);  // what the next plane holds
+              for (int e = 0; e < 32; e += 2) {  // (two at a time: one element is converted at a quarter of the rate)
+                const __half2 two = __floats2half2_rn(v[e], v[e + 1]);
+                const float2 back = __half22float2(two);
+                memcpy(&h[e / 8].v[e % 8], &two, sizeof two);
+                v[e] -= back.x, v[e + 1] -= back.y;  // what the next plane holds
               }
             }
             unsigned char *slot = slots.next();
@@ -1106,6 +1110,11 @@ cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type
 // 5.9e-7 with four).
 int set_of(bool f32_matrices, bool f32_result) { return f32_matrices ? 4 : f32_result ? 8 : 16; }
 
+// The first two sets of a tile are longer: they are summed while the tile before is finished, or its parts
+// are joined.  A sum of n stages is off by n as a rule, and so is a tile by the mean of its sets' lengths,
+// weighted by them: as long as this leaves it at 11/8 of that of equal sets.
+int lead_of(int set, int64_t stages) { return (int)(0.5 * set + std::sqrt(0.25 * set * set + 0.1875 * set * (double)stages)); }
+
 // D = A B^T; mn: the operand is held transposed
 Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, int set) {
   Job j{};
@@ -1115,7 +1124,7 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, int set) {
   for (int p = 0; p < a.planes; ++p)
     for (int q = 0; q < b.planes; ++q)
       if (p + q < 2) j.plane_a[j.pairs] = p, j.plane_b[j.pairs++] = q;
-  j.set = set;
+  j.set = set, j.lead = lead_of(set, (int64_t)j.steps * j.pairs);
   j.instr = instruction(kTile, a_mn, b_mn, a.bf16);
   j.tiles_n = (j.N + kTile - 1) / kTile;
   j.tiles = (int64_t)((j.M + kTile - 1) / kTile) * j.tiles_n;
