@@ -338,8 +338,8 @@ constexpr int kTile = 256, kHalf = 128, kBK = 64;
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 constexpr int kFewRegs = 88, kManyRegs = 208;    // a thread of warps 0-3 and of 4-11
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
-constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 6;
-constexpr int kSlots = 2, kSlotBytes = 2048;     // a warp's buffers on the way out: 32 rows of 64 bytes each
+constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 5;
+constexpr int kSlots = 2, kSlotBytes = 4096;     // a warp's buffers on the way out: 32 rows of 128 bytes each
 constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 256 + 1024;
 
 struct Job {
@@ -417,7 +417,7 @@ struct Slots {
   unsigned char *base;
   uint32_t turn;
   int lane;
-  // The next one, for the whole warp, 64 bytes a row, pieces of 16 bytes as piece() has them.
+  // The next one, for the whole warp.
   __device__ __forceinline__ unsigned char *next() {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(kSlots - 1) : "memory");
     __syncwarp();
@@ -432,35 +432,41 @@ struct Slots {
     return base;
   }
 };
-// 16 fp32 columns of a slot added to what a matrix holds; what is outside the matrix is dropped.
-__device__ __forceinline__ void add_half(const CUtensorMap *map, const unsigned char *slot, int col, int row) {
+// The 16-byte piece i of a row's 128 bytes, as the copy engine takes them (its 128-byte swizzle): rows
+// would meet in the same banks otherwise.
+template <typename T>
+__device__ __forceinline__ Pack<T, 16 / sizeof(T)> *slot_piece(unsigned char *slot, int row, int i) {
+  return reinterpret_cast<Pack<T, 16 / sizeof(T)> *>(slot + row * 128 + (i ^ (row & 7)) * 16);
+}
+// 32 fp32 columns of a slot added to what a matrix holds; what is outside the matrix is dropped.
+__device__ __forceinline__ void add_slot(const CUtensorMap *map, const unsigned char *slot, int col, int row) {
   asm volatile("cp.reduce.async.bulk.tensor.4d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4, %4}], [%1];\ncp.async.bulk.commit_group;\n" ::"l"(map),
                "r"(smem_u32(slot)), "r"(col), "r"(row), "r"(0)
                : "memory");
 }
 
-// 32 x 32 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
+// 32 rows of 64 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
 // By the copy engine: a 16-byte aligned matrix that is written, or an fp32 one that is added to
 // (each element by one addition, so that the result has one order).
 template <typename T>
-__device__ __forceinline__ void engine_out(const Job &j, const CUtensorMap *map, int row0, int c, const float (&v)[32], Slots &slots) {
-  constexpr int kCols = 64 / sizeof(T), kPiece = 16 / sizeof(T);
+__device__ __forceinline__ void engine_out(const Job &j, const CUtensorMap *map, int row0, int c, const float *v, Slots &slots) {
+  constexpr int kCols = 128 / sizeof(T), kPiece = 16 / sizeof(T);
 #pragma unroll
-  for (int c1 = 0; c1 < 32; c1 += kCols) {
+  for (int c1 = 0; c1 < 64; c1 += kCols) {
+    if (c + c1 >= j.N) return;
     unsigned char *slot = slots.next();
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<Pack<T, kPiece> *>(piece(slot, slots.lane, e)) = pack<T, kPiece>(v + c1 + e * kPiece);
+    for (int e = 0; e < 8; ++e) *slot_piece<T>(slot, slots.lane, e) = pack<T, kPiece>(v + c1 + e * kPiece);
     half_written();
     if (slots.lane == 0) {
-      if (sizeof(T) == 4 && j.add) add_half(map, slot, c + c1, row0);
+      if (sizeof(T) == 4 && j.add) add_slot(map, slot, c + c1, row0);
       else store_half(map, slot, c + c1, row0, 0, 0);
     }
   }
 }
-// By the warp, a row's 32 elements at a time.
+// By the warp, 32 elements of a row at a time.
 template <typename T>
-__device__ __forceinline__ void lanes_out(const Job &j, int row0, int c, const float (&v)[32], Slots &slots) {
+__device__ __forceinline__ void lanes_out(const Job &j, int row0, int c, const float *v, Slots &slots) {
   const int lane = slots.lane;
   float *f = reinterpret_cast<float *>(slots.all());
 #pragma unroll
@@ -482,9 +488,13 @@ __device__ __forceinline__ void lanes_out(const Job &j, int row0, int c, const f
   __syncwarp();
 }
 template <typename T>
-__device__ __forceinline__ void block_out(const Job &j, const CUtensorMap *map, int row0, int c, const float (&v)[32], Slots &slots) {
-  if (j.by_engine) engine_out<T>(j, map, row0, c, v, slots);
-  else lanes_out<T>(j, row0, c, v, slots);
+__device__ __forceinline__ void block_out(const Job &j, const CUtensorMap *map, int row0, int c, const float *v, Slots &slots) {
+  if (j.by_engine) {
+    engine_out<T>(j, map, row0, c, v, slots);
+  } else {
+    lanes_out<T>(j, row0, c, v, slots);
+    lanes_out<T>(j, row0, c + 32, v + 32, slots);
+  }
 }
 
 // What a pair of blocks does, one after the other: stages k0 to k1 of a tile's sum, which is one of
@@ -743,7 +753,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (coef != 0.f && fabsf(rest) < 1.f) coef *= exp2f(-rest);
         }
       }
-      float acc[kParts][32] = {};
+      float acc[kHalf] = {};
       const int steps = w.k1 - w.k0, after = steps - 2 * j.lead;  // (stages after the first two sets)
       const int sets = after > 0 ? 2 + (after + j.set - 1) / j.set : steps > j.lead ? 2 : 1;
       for (int set = 0; set < sets; ++set) {
@@ -761,9 +771,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           pass(s);
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const Pair x{__uint_as_float(s.r[e]), __uint_as_float(s.r[e + 1])}, y{acc[part][e], acc[part][e + 1]};
+            const Pair x{__uint_as_float(s.r[e]), __uint_as_float(s.r[e + 1])}, y{acc[part * 32 + e], acc[part * 32 + e + 1]};
             const Pair sum = MODE == kOut ? add2(x, y) : fma2(x, both(alpha2), y);
-            acc[part][e] = sum.a, acc[part][e + 1] = sum.b;
+            acc[part * 32 + e] = sum.a, acc[part * 32 + e + 1] = sum.b;
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -781,7 +791,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            mine[(part * 8 + e) * 32] = make_float4(acc[part][4 * e], acc[part][4 * e + 1], acc[part][4 * e + 2], acc[part][4 * e + 3]);
+            mine[(part * 8 + e) * 32] = make_float4(acc[part * 32 + 4 * e], acc[part * 32 + 4 * e + 1], acc[part * 32 + 4 * e + 2], acc[part * 32 + 4 * e + 3]);
         __threadfence();
         __syncwarp();
         int32_t *count = a.arrived + w.count * 16 + rank * 8 + warp - 4, before = 0;
@@ -792,7 +802,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[part][e] = 0.f;
+          for (int e = 0; e < 32; ++e) acc[part * 32 + e] = 0.f;
 #pragma unroll 1
         for (int q = 0; q < w.parts; ++q) {
           const float4 *from_part = a.parts + (q ? w.second + (q - 1) * w.step : w.first) * kPart + place;
@@ -801,10 +811,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float4 f = __ldcg(from_part + (part * 8 + e) * 32);
-              acc[part][4 * e] += f.x;
-              acc[part][4 * e + 1] += f.y;
-              acc[part][4 * e + 2] += f.z;
-              acc[part][4 * e + 3] += f.w;
+              acc[part * 32 + 4 * e] += f.x;
+              acc[part * 32 + 4 * e + 1] += f.y;
+              acc[part * 32 + 4 * e + 2] += f.z;
+              acc[part * 32 + 4 * e + 3] += f.w;
             }
         }
       }
@@ -814,19 +824,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (c0 + part * 32 + e >= j.N) acc[part][e] = -INFINITY;
+              if (c0 + part * 32 + e >= j.N) acc[part * 32 + e] = -INFINITY;
         float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], acc[part][e]);
+          for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], acc[part * 32 + e]);
         const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), zero = most == -INFINITY ? 0.f : most;
         Pair sum[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const Pair x = add2({acc[part][e], acc[part][e + 1]}, both(-zero));
+            const Pair x = add2({acc[part * 32 + e], acc[part * 32 + e + 1]}, both(-zero));
             sum[e / 2 & 1] = add2(sum[e / 2 & 1], {exp2_fast(x.a), exp2_fast(x.b)});
           }
         sum[0] = add2(sum[0], sum[1]);
@@ -840,7 +850,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             // the element of that number, a bit of it after the other
             float z[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) z[e] = column & 16 ? acc[part][e + 16] : acc[part][e];
+            for (int e = 0; e < 16; ++e) z[e] = column & 16 ? acc[part * 32 + e + 16] : acc[part * 32 + e];
 #pragma unroll
             for (int half = 8; half; half >>= 1)
 #pragma unroll
@@ -853,60 +863,60 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         continue;
       }
-      // One block after the other, in the registers of the first (unrolled, the code would be long
+      // 64 columns and then the others, in the registers of the first (unrolled, the code would be long
       // and runs once a tile).
-      float (&v)[32] = acc[0];
+      float *v = acc;
       const float f1 = ldexpf(p_down, down[which] / 2), f2 = ldexpf(1.f, down[which] - down[which] / 2);
 #pragma unroll 1
-      for (int c = c0; c < min(j.N, c0 + kHalf); c += 32) {
+      for (int c = c0; c < min(j.N, c0 + kHalf); c += 64) {
         if constexpr (MODE == kGrad) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = coef == 0.f ? 0.f : coef * exp2_fast(v[e] - shift);
-          while (__any_sync(0xFFFFFFFFu, at.next < c + 32)) {
-            const bool hit = at.next < c + 32;
-            const int column = hit ? at.next - c : -1;
-            const float weight = at.w * p_up;
+          for (int e = 0; e < 64; ++e) v[e] = coef == 0.f ? 0.f : coef * exp2_fast(v[e] - shift);
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (column == e) v[e] -= weight;
-            if (hit) at.step();
-          }
-#pragma unroll 1
-          for (int q = 0; q < a.p_bf16 + a.p_half; ++q) {
-            Piece h[4];
-            if (q < a.p_bf16) {
+          for (int e0 = 0; e0 < 64; e0 += 32)
+            while (__any_sync(0xFFFFFFFFu, at.next < c + e0 + 32)) {
+              const bool hit = at.next < c + e0 + 32;
+              const int column = hit ? at.next - c - e0 : -1;
+              const float weight = at.w * p_up;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const Pack<__nv_bfloat16, 8> b = pack<__nv_bfloat16, 8>(v + 8 * e);
-                memcpy(&h[e], &b, sizeof b);
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {  // (two at a time: one element is converted at a quarter of the rate)
-                const __half2 two = __floats2half2_rn(v[e], v[e + 1]);
-                const float2 back = __half22float2(two);
-                memcpy(&h[e / 8].v[e % 8], &two, sizeof two);
-                v[e] -= back.x, v[e + 1] -= back.y;  // what the next plane holds
-              }
+              for (int e = 0; e < 32; ++e)
+                if (column == e) v[e0 + e] -= weight;
+              if (hit) at.step();
             }
+          int plane = 0;
+          if (a.p_bf16) {
             unsigned char *slot = slots.next();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *reinterpret_cast<Piece *>(piece(slot, lane, e)) = h[e];
+            for (int e = 0; e < 8; ++e) *slot_piece<__nv_bfloat16>(slot, lane, e) = pack<__nv_bfloat16, 8>(v + 8 * e);
             half_written();
-            if (lane == 0) store_half(&out0, slot, c, row0, 0, q);
+            if (lane == 0) store_half(&out0, slot, c, row0, 0, plane);
+            ++plane;
+          }
+#pragma unroll 1
+          for (; plane < a.p_bf16 + a.p_half; ++plane) {
+            unsigned char *slot = slots.next();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const Pack<__half, 8> h = pack<__half, 8>(v + 8 * e);
+              float back[8];
+              unpack<__half, 8>(h, back);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[8 * e + i] -= back[i];  // what the next plane holds
+              *slot_piece<__half>(slot, lane, e) = h;
+            }
+            half_written();
+            if (lane == 0) store_half(&out0, slot, c, row0, 0, plane);
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = v[e] * f1 * f2;
+          for (int e = 0; e < 64; ++e) v[e] = v[e] * f1 * f2;
           const CUtensorMap *map = which ? &out1 : &out0;
           if (j.type == ECHO_F32) block_out<float>(j, map, row0, c, v, slots);
           else if (j.type == ECHO_BF16) block_out<__nv_bfloat16>(j, map, row0, c, v, slots);
           else block_out<__half>(j, map, row0, c, v, slots);
         }
 #pragma unroll
-        for (int part = 1; part < kParts; ++part)
-#pragma unroll
-          for (int e = 0; e < 32; ++e) acc[part - 1][e] = acc[part][e];
+        for (int e = 0; e < 64; ++e) acc[e] = acc[e + 64];
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
@@ -1114,7 +1124,7 @@ cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type
   j.out = out, j.out_stride = stride, j.type = type, j.add = add;
   j.by_engine = reinterpret_cast<uintptr_t>(out) % 16 == 0 && stride * size % 16 == 0 && stride < (int64_t)1 << 37 && !(add && type != ECHO_F32);
   if (!j.by_engine) return cudaSuccess;
-  return box_map(map, out, j.M, j.N, stride, 0, 1, 32, 64 / size, CU_TENSOR_MAP_SWIZZLE_64B, size,
+  return box_map(map, out, j.M, j.N, stride, 0, 1, 32, 128 / size, CU_TENSOR_MAP_SWIZZLE_128B, size,
                  type == ECHO_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16);
 }
 
@@ -1307,7 +1317,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     h.job[0] = job_of(l.x, false, w, false, set_of(f32, exact_dw));
     TRY(stage_map(&m.a[0], l.x, false));
     TRY(stage_map(&m.b[0], w, false));
-    TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B));
+    TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 64, CU_TENSOR_MAP_SWIZZLE_128B));
     TRY(timed("head_dlogits", [&] { return launch_product<kGrad>(m, h, sms, st); }));
 
     HeadProduct d = g;
