@@ -326,6 +326,7 @@ def _current_stream(device: int) -> int:
     return _raw_stream(device)
 
 
+_id_bits: Dict[object, int] = {}  # torch dtype -> bits
 _types: Dict[object, int] = {}  # torch dtype -> element type of the C ABI (F32, BF16, F16)
 
 
@@ -598,11 +599,13 @@ class Echo:
 
     @staticmethod
     def _ids(ids) -> int:
-        import torch
-        if ids.dtype == torch.int64:
-            return 64
-        _need(ids.dtype == torch.int32, "ids are neither int32 nor int64")
-        return 32
+        bits = _id_bits.get(ids.dtype)
+        if bits is None:
+            import torch
+            _id_bits.update({torch.int32: 32, torch.int64: 64})
+            bits = _id_bits.get(ids.dtype)
+            _need(bits is not None, "ids are neither int32 nor int64")
+        return bits
 
     def embed(self, ids, table, scale: float = 1.0, vocab_start: int = 0, dtype=None, out=None):
         """``scale * table[ids - vocab_start]`` ([..., hidden] for ids [...]), zeros for ids
@@ -837,10 +840,22 @@ class Echo:
     # -- rotary positions ----------------------------------------------------------------------
     def _rotary(self, call, q, k, positions, frequencies, interleaved, scale, out):
         import torch
-        lead, dim, dtype = q.shape[:-2], q.shape[-1], q.dtype
+        dtype = q.dtype
         if type(frequencies) is not np.ndarray or frequencies.dtype != np.float64 or not frequencies.flags.c_contiguous:
             frequencies = np.ascontiguousarray(frequencies, dtype=np.float64)
         _need(frequencies.ndim == 1 and q.dim() >= 2, "frequencies are not one of each pair, or q has no heads")
+        if out is None and k is not None and q.dim() == 3 and q.is_contiguous() and k.is_contiguous() and positions.is_contiguous():
+            # the usual call, whose strides need no looking for
+            t, h0, dim = q.shape
+            h1 = k.shape[-2] if k.dim() == 3 else 0
+            _need(k.shape == (t, h1, dim) and k.dtype == dtype, "q and k have other tokens, lengths of a head or types")
+            _need(positions.shape == (t,), "positions have another shape than the tokens")
+            y0, y1, a, b = torch.empty_like(q), torch.empty_like(k), h0 * dim, h1 * dim
+            self._op(call, _packed(_ROTARY, 1, t, h0, h1, q.data_ptr(), k.data_ptr(), y0.data_ptr(), y1.data_ptr(), 0, 0, a, b, dim, dim, 0, 0, a, b, dim, dim,
+                                   positions.data_ptr(), t, frequencies.__array_interface__["data"][0], dim, 2 * frequencies.shape[0], _type(dtype),
+                                   self._ids(positions), 1 if interleaved else 0, scale))
+            return y0, y1
+        lead, dim = q.shape[:-2], q.shape[-1]
         if k is None:
             xs, outs = (q,), None if out is None else (out,)
         else:
