@@ -345,7 +345,7 @@ constexpr int kFewRegs = 88, kManyRegs = 208;    // a thread of warps 0-3 and of
 static_assert(128 * kFewRegs + 256 * kManyRegs <= kThreads * 168, "the block's registers");
 constexpr int kOperandBytes = kHalf * kBK * 2, kStageBytes = 2 * kOperandBytes, kStages = 5;
 constexpr int kSlots = 2, kSlotBytes = 4096;     // a warp's buffers on the way out: 32 rows of 128 bytes each
-constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 256 + 1024;
+constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes + 512 + 1024;
 
 struct Job {
   int M, N, steps;  // rows, columns; stages of a pair of planes
@@ -598,6 +598,12 @@ struct Cursor {
   }
 };
 
+// `bytes` contiguous bytes to this block's shared memory.
+__device__ __forceinline__ void copy_bytes(uint32_t to, const void *from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap amap0, const __grid_constant__ CUtensorMap bmap0, const __grid_constant__ CUtensorMap amap1,
@@ -613,7 +619,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;  // (clusters of two along x)
   // `full` and `sums_empty` are used in the first block alone, the others in both
   const uint32_t ring = smem_u32(base), full = smem_u32(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages, sums_empty = sums_full + 16,
-                 done = sums_empty + 16;
+                 done = sums_empty + 16, joins = done + 8;  // (joins: two of each of the eight warps)
   volatile int *abort = &give_up;
   if (threadIdx.x == 0) {
     give_up = 0;
@@ -626,6 +632,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bar_init(sums_empty + 8 * b, 16);
     }
     bar_init(done, 1);
+    for (int i = 0; i < 16; ++i) bar_init(joins + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
   if (threadIdx.x == 32 * 3) asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\n" ::"l"(&amap0), "l"(&bmap0) : "memory");
@@ -728,6 +735,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kManyRegs));
     const int quarter = warp & 3, side = (warp - 4) >> 2;  // (a warp reaches the 32 rows of tensor memory of its number modulo 4)
     Slots slots{buffers + (warp - 4) * kSlots * kSlotBytes, 0, lane};
+    const uint32_t join = joins + 16 * (warp - 4);
     const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + side * kHalf;
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
@@ -808,23 +816,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) *count = 0;
         __threadfence();
 #pragma unroll
-        for (int part = 0; part < kParts; ++part)
-#pragma unroll
-          for (int e = 0; e < 32; ++e) acc[part * 32 + e] = 0.f;
+        for (int e = 0; e < kHalf; ++e) acc[e] = 0.f;
+        // 32 columns of a part at a time come to the warp's buffers, the next ones while these are added
+        // (loads to registers, of which the sums leave few, took 10000 clocks a part)
+        unsigned char *chunk = slots.all();
+        asm volatile("fence.proxy.async;\n" ::: "memory");  // (what other blocks wrote, for the copy engine)
+        auto fetch = [&](int q, int c) {
+          if (lane != 0 || q >= w.parts) return;
+          const float4 *from_part = a.parts + (q ? w.second + (q - 1) * w.step : w.first) * kPart + (place - lane) + c * 256;
+          bar_expect(join + 8 * (c & 1), kSlotBytes);
+          copy_bytes(smem_u32(chunk) + (c & 1) * kSlotBytes, from_part, kSlotBytes, join + 8 * (c & 1));
+        };
+        fetch(0, 0);
 #pragma unroll 1
-        for (int q = 0; q < w.parts; ++q) {
-          const float4 *from_part = a.parts + (q ? w.second + (q - 1) * w.step : w.first) * kPart + place;
+        for (int q = 0; q < w.parts && ok; ++q) {
 #pragma unroll
-          for (int part = 0; part < kParts; ++part)
+          for (int c = 0; c < kParts; ++c) {
+            fetch(c == kParts - 1 ? q + 1 : q, (c + 1) % kParts);
+            ok = ok && bar_wait(join + 8 * (c & 1), c >> 1, abort, a.wait);  // (each has two phases a part)
+            if (ok) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float4 f = __ldcg(from_part + (part * 8 + e) * 32);
-              acc[part * 32 + 4 * e] += f.x;
-              acc[part * 32 + 4 * e + 1] += f.y;
-              acc[part * 32 + 4 * e + 2] += f.z;
-              acc[part * 32 + 4 * e + 3] += f.w;
+              for (int e = 0; e < 8; ++e) {
+                const float4 f = *reinterpret_cast<const float4 *>(chunk + (c & 1) * kSlotBytes + (e * 32 + lane) * 16);
+                acc[c * 32 + 4 * e] += f.x;
+                acc[c * 32 + 4 * e + 1] += f.y;
+                acc[c * 32 + 4 * e + 2] += f.z;
+                acc[c * 32 + 4 * e + 3] += f.w;
+              }
             }
+            __syncwarp();
+          }
         }
+        if (!ok) break;
       }
       if constexpr (MODE == kStats) {
         if (c0 + kHalf > j.N)
@@ -1169,10 +1192,10 @@ struct Maps {
   CUtensorMap a[2], b[2], out[2];
 };
 // The schedule, by an estimate of the pair of blocks that takes longest.  In stages of 560 clocks (512
-// of products at 256 columns): joining the parts of a tile takes about 6000 clocks and 3000 for each part.
+// of products at 256 columns): joining the parts of a tile takes about 3000 clocks and 3000 for each part.
 // Nothing is split where that saves nothing.  Two products have no pool: the first one's operands are
 // long, and are in L2 while its tiles are at the same place of their sums.
-double joining(int64_t parts) { return (6000. + 3000. * parts) / 560; }
+double joining(int64_t parts) { return (3000. + 3000. * parts) / 560; }
 Schedule plan(const Job *j, int pairs) {
   Schedule s{};
   const int64_t tiles = j[0].tiles;
