@@ -40,17 +40,21 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417
 constexpr int kAmaxParts = 304;  // blocks that look for a largest element, at most
 
 // Where the exponent of a matrix's power of two comes from: the largest elements that blocks
-// found.  None: the matrix is as it is.
+// found (none: the matrix is as it is), or, for one of each row, the largest elements of rows.
 struct Scale {
   const float *part;
   int parts;
+  const float *rows;
 };
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+  return v;
+}
 __device__ __forceinline__ float largest(Scale s) {
   float m = 0.f;
   for (int i = threadIdx.x & 31; i < s.parts; i += 32) m = fmaxf(m, s.part[i]);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-  return m;
+  return warp_max(m);
 }
 __device__ __forceinline__ int exponent_of(float m) { return m > 0.f ? max(-110, min(110, 14 - ilogbf(m))) : 0; }
 // By a warp, the same in all lanes: the largest element times 2^exponent is 2^14 to 2^15, if it is
@@ -87,13 +91,14 @@ struct Source {
   void *to;
   int64_t ld, plane;
   float *amax;
+  bool amax_rows;       // of each row
 };
 struct Sources {
   Source of[2];
 };
 
-// The largest finite element of each block's part of a matrix (without gaps, a single row).
-// Bound by the bytes, or by latency where they are few.
+// The largest finite element of each row, by a warp, or of each block's part of a matrix's live rows
+// (without gaps, and all of them live, a single row).  Bound by the bytes, or by latency where they are few.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
   __shared__ float sh[8];
@@ -101,6 +106,16 @@ __global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
   next_may_start();
   const Source &m = s.of[blockIdx.y];
   const T *x = static_cast<const T *>(m.p);
+  if (m.amax_rows) {
+    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < m.rows; r += (int64_t)gridDim.x * 8) {
+      float most = 0.f;
+#pragma unroll 8
+      for (int64_t c = threadIdx.x & 31; c < m.cols; c += 32) most = fmaxf(most, finite_size(to_f(x[r * m.stride + c])));
+      most = warp_max(most);
+      if ((threadIdx.x & 31) == 0) m.amax[r] = most;
+    }
+    return;
+  }
   // (a single row: its 16-byte pieces, and what is before and behind them, by the first block)
   int64_t cols = m.cols;
   float most = 0.f;
@@ -120,7 +135,12 @@ __global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
       const int64_t i = i0 + k * 256;
 #pragma unroll
       for (int e = 0; e < W; ++e) v[k][e] = 0.f;
-      if (i < all) load_piece<W>(m.rows == 1 ? x + i * W : x + i / pieces * m.stride + i % pieces * W, v[k]);
+      if (i < all && m.rows == 1) {
+        load_piece<W>(x + i * W, v[k]);
+      } else if (i < all) {
+        const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / (uint32_t)pieces);
+        if (!m.live || m.live[r] != 0.f) load_piece<W>(x + r * m.stride + (i - r * pieces) * W, v[k]);
+      }
     }
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
@@ -157,19 +177,21 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
   const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   const T *x = static_cast<const T *>(m.p);
   D *to = static_cast<D *>(m.to);
-  const float *live = m.live;
+  const float *live = m.live, *rows = m.scale.rows;
   const int64_t stride = m.stride, ld = m.ld, plane = m.plane, cols = m.cols;
   const uint32_t pieces = (uint32_t)((cols + W - 1) / W);
   const int64_t all = m.rows * pieces;
   for (int64_t i0 = first; i0 < all; i0 += step * kFlight) {
     Pack<T, W> raw[kFlight];
     int64_t at[kFlight];
+    float size[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       const int64_t i = i0 + k * step;
       if (i >= all) continue;
       const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), c = (i - r * pieces) * W;
       at[k] = r * ld + c;
+      size[k] = rows ? rows[r] : 0.f;
 #pragma unroll
       for (int e = 0; e < W; ++e) raw[k].v[e] = from_f<T>(0.f);
       if (live && live[r] == 0.f) continue;
@@ -187,8 +209,9 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
       if (i0 + k * step >= all) continue;
       float v[W];
       unpack<T, W>(raw[k], v);
+      const float by = rows ? ldexpf(1.f, exponent_of(size[k])) : up;
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[e] *= up;
+      for (int e = 0; e < W; ++e) v[e] *= by;
 #pragma unroll
       for (int q = 0; q < PLANES; ++q) {
         const Pack<D, W> h = pack<D, W>(v);
@@ -218,12 +241,6 @@ struct Targets {
 
 constexpr int kTargetWarps = 8;
 constexpr int kMaxTargets = 256;
-
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
-  return v;
-}
 
 __device__ __forceinline__ int64_t id_at(const HeadArgs &a, int64_t i) {
   return a.id64 ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
@@ -740,7 +757,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
     for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
-    const float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
+    float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
     const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
     bool ok = true;
@@ -758,6 +775,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Cursor at;
       at.none();
       float coef = 0.f, shift = 0.f;
+      if (MODE == kStats && a.job[0].scale_a.rows)  // (a factor of each row)
+        alpha2 = ldexpf(a.alpha, down[0] - (in ? exponent_of(a.job[0].scale_a.rows[row]) : 0)) * kLog2e;
       if (MODE != kOut && in) {
         at.start(a.idx + row * a.K, MODE == kGrad ? a.weight + row * a.K : nullptr, a.K, a.v_begin, c0);
         if (MODE == kGrad) {
@@ -1046,7 +1065,7 @@ bool readable(const void *p, int64_t rows, int64_t cols, int64_t stride, int typ
   return type != ECHO_F32 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride % 8 == 0 && stride >= cols && stride < (int64_t)1 << 38));
 }
 Operand in_place(const void *p, int64_t rows, int64_t cols, int64_t stride, int type) {
-  return {p, rows, cols, rows <= 1 ? padded(cols) : stride, 0, 1, type == ECHO_BF16, {nullptr, 0}};
+  return {p, rows, cols, rows <= 1 ? padded(cols) : stride, 0, 1, type == ECHO_BF16, {}};
 }
 
 // Memory of a piece of P at most; a vocabulary whose P is larger is taken in pieces.  Pieces that
@@ -1085,7 +1104,7 @@ Layout layout_of(const HeadArgs &a, int sms) {
   l.targets.n_arrived = sms * 16;
   l.targets.arrived = c.take<int32_t>(l.targets.n_arrived);
   l.parts = c.take<float4>((int64_t)sms / 2 * 2 * kTile * kTile / 4);
-  l.amax_x = c.take<float>(kAmaxParts);
+  l.amax_x = c.take<float>(a.grad ? kAmaxParts : a.n);  // (of blocks' parts, or of rows)
   l.amax_w = c.take<float>(kAmaxParts);
   auto planes = [&](int64_t rows, int64_t cols, int count, bool bf16, Scale scale) {
     const int64_t ld = padded(cols);
@@ -1093,7 +1112,7 @@ Layout layout_of(const HeadArgs &a, int sms) {
   };
   l.pack_x = !readable(a.x, a.n, a.H, a.x_stride, a.type);
   l.pack_w = !readable(a.w, a.V, a.H, a.w_stride, a.type);
-  const Scale sx{l.amax_x, kAmaxParts}, sw{l.amax_w, kAmaxParts}, none{nullptr, 0};
+  const Scale none{}, sw{l.amax_w, kAmaxParts, nullptr}, sx = a.grad ? Scale{l.amax_x, kAmaxParts, nullptr} : Scale{nullptr, 0, l.amax_x};
   l.x = l.pack_x ? planes(a.n, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sx : none) : in_place(a.x, a.n, a.H, a.x_stride, a.type);
   l.w = l.pack_w ? planes(a.V, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sw : none) : in_place(a.w, a.V, a.H, a.w_stride, a.type);
   if (!a.grad) {
@@ -1249,7 +1268,8 @@ cudaError_t launch_amax(Sources s, int count, int type, cudaStream_t st) {
     bool wide = true;
     for (int i = 0; i < count; ++i) {
       Source &m = s.of[i];
-      if (m.stride == m.cols) m.cols *= m.rows, m.rows = 1;
+      if (m.amax_rows) continue;
+      if (m.stride == m.cols && !m.live) m.cols *= m.rows, m.rows = 1;
       wide &= m.rows == 1 || (m.cols % N == 0 && fits_pieces(m.p, m.stride, type, N));
     }
     return wide ? launch_early(head_amax_kernel<T, N>, dim3(kAmaxParts, count), 256, 0, st, s) : launch_early(head_amax_kernel<T, 1>, dim3(kAmaxParts, count), 256, 0, st, s);
@@ -1293,7 +1313,11 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   const bool sized_x = f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16), sized_w = f32 && a.V;
   Sources s{};
   int count = 0;
-  if (sized_x) s.of[count] = sx, s.of[count++].amax = l.amax_x;
+  // (rows that are not live do not count: padding may hold any number.  Forward, each row has its own.)
+  if (sized_x) {
+    Source &m = s.of[count++] = sx;
+    m.amax = l.amax_x, m.amax_rows = !a.grad, m.live = a.grad ? l.targets.live : nullptr;
+  }
   if (sized_w) s.of[count] = sw, s.of[count++].amax = l.amax_w;
   if (count) TRY(timed("head_amax", [&] { return launch_amax(s, count, a.type, st); }));
   // (backward, the rows of tokens without gradients are zeros in fp32's planes, which both products read)
@@ -1329,7 +1353,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     });
   }
 
-  g.p_bf16 = l.p_bf16, g.p_half = l.p_half, g.p_scale = {l.targets.size_part, l.target_blocks};
+  g.p_bf16 = l.p_bf16, g.p_half = l.p_half, g.p_scale = {l.targets.size_part, l.target_blocks, nullptr};
   for (int64_t v = 0; v < a.V; v += l.piece) {
     const int64_t rows = std::min(l.piece, a.V - v);
     Operand w = l.w;
@@ -1337,7 +1361,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     w.rows = rows;
     // the planes of P that dx and dW read
     const int64_t plane = a.n * l.ldp;
-    const Operand p{l.P, a.n, rows, l.ldp, plane, l.p_bf16 + l.p_half, false, {nullptr, 0}};
+    const Operand p{l.P, a.n, rows, l.ldp, plane, l.p_bf16 + l.p_half, false, {}};
     auto planes = [&](bool bf16, int count) {
       Operand o = p;
       o.bf16 = bf16, o.planes = count, o.scale = g.p_scale;

@@ -1,0 +1,205 @@
+"""Losses of a head at the ends of what they take: padding of any content, rows of very different sizes, signs, types and
+layouts that go together, matrices beyond 2^31 elements, two contexts at a time.
+
+Tolerances as in test_gpu_head.py; where a call has to give another call's bits, equality."""
+import math
+
+import pytest
+
+from paper_2412_12487_gb300 import Echo
+
+from .test_gpu_head import BF16, F16, F32, U, Ref, _case, _check_ce, _close, _randint, _randn, _teacher, _teacher_ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def echo():
+    with Echo(0) as e:
+        yield e
+
+
+@pytest.mark.parametrize("dtype,dw_type", [(F32, F32), (BF16, F32), (F16, F16)])
+def test_padding_of_any_size(echo, dtype, dw_type):
+    n, h, v = 50, 72, 400
+    x, w = _case(n, h, v, 0, dtype, 1)
+    labels, dloss = _randint(0, v, (n,), 2), _randn((n,), 3)
+    labels[1::4] = -1
+    live = labels >= 0
+    clean = echo.cross_entropy(x, w, labels)
+    grads = echo.cross_entropy_grad(dloss, x, w, labels, clean[1], dtype=dw_type)
+    y = x.clone()
+    y[~live] = torch.finfo(dtype).max  # what memory may hold
+    got = echo.cross_entropy(y, w, labels)
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1][live], clean[1][live]) and torch.equal(got[2], clean[2])
+    g2 = echo.cross_entropy_grad(dloss, y, w, labels, clean[1], dtype=dw_type)
+    assert torch.equal(g2[0], grads[0]) and torch.equal(g2[1], grads[1])
+
+
+def test_rows_of_different_sizes(echo):
+    """fp32 tokens from 2^-60 to 2^40 times the others, each with the digits of its own size."""
+    n, h, v = 40, 130, 300
+    x, w = _case(n, h, v, 0, F32, 4)
+    by = 2.0 ** torch.linspace(-60, 40, n, device="cuda").round()
+    z = torch.cat([x * by[:, None], torch.zeros((1, h), device="cuda")])
+    labels = _randint(0, v, (n + 1,), 5)
+    loss, lse, target = echo.cross_entropy(z, w, labels, scale=2.0 ** -38)
+    X, W = z.double(), w.double()
+    size = X.abs() @ W.abs().T
+    far = 2.0 ** -37 * (X.abs().amax(1, keepdim=True) * W.abs().sum(1)[None] + W.abs().max() * X.abs().sum(1)[:, None])
+    units = (64 + h / 256) * U + 3 * 2.0 ** -22
+    want = (X @ W.T).gather(1, labels[:, None])[:, 0] * 2.0 ** -38
+    tol = ((units * size + far).gather(1, labels[:, None])[:, 0] + 4 * U * want.abs()) * 2.0 ** -38
+    _close(target, want, tol)
+    assert torch.isfinite(loss).all() and float(lse[n]) == pytest.approx(math.log(v), rel=1e-6)
+
+
+@pytest.mark.parametrize("scale", [-0.5, 0.0])
+def test_signs_and_zero(echo, scale):
+    n, h, v = 90, 40, 333
+    for dtype, dw_type in ((BF16, F32), (F32, F32), (F16, F16)):
+        x, w = _case(n, h, v, 0, dtype, 6)
+        labels, dloss, dlse = _randint(-1, v, (n,), 7), _randn((n,), 8), _randn((n,), 9)
+        lse = _check_ce(echo, x, w, labels, 0, scale)
+        ref = Ref(x, w, scale)
+        dx, dw = echo.cross_entropy_grad(dloss, x, w, labels, lse, scale=scale, dlse=dlse, dtype=dw_type)
+        valid = labels >= 0
+        g = torch.where(valid, dloss.double() * scale, 0.0)
+        coef = g + dlse.double() * scale
+        want = ref.targets(torch.where(valid, labels, -1)[:, None], g[:, None], 0)
+        a, b, ta, tb = ref.grads(coef, g.abs(), want, lse.double(), 1.0, dw_type)
+        more = (4 * U * (g.abs() + (dlse.double() * scale).abs()))[:, None] * torch.exp(ref.z - lse.double()[:, None])  # (the coefficient's sum)
+        _close(dx, a, ta + more @ ref.W.abs())
+        _close(dw, b, tb + more.T @ ref.X.abs())
+
+
+def test_types_that_go_together(echo):
+    """32-bit ids, teachers of another type than the student, a broadcast gradient, one token."""
+    n, h, v, k = 33, 64, 500, 9
+    x, w = _case(n, h, v, 0, BF16, 10)
+    ids, logits = _teacher(n, k, v, 0, F32, 11)
+    want = echo.distill(x, w, ids, logits.to(F16).float(), temperature=1.5)
+    for t in (F32, F16):
+        got = echo.distill(x, w, ids.int(), logits.to(F16).to(t), temperature=1.5)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    one = torch.full((1,), 0.25, device="cuda").expand(n)
+    grads = echo.distill_grad(one.contiguous(), x, w, ids, logits, want[1], temperature=1.5)
+    assert all(torch.equal(a, b) for a, b in zip(grads, echo.distill_grad(one, x, w, ids.int(), logits, want[1], temperature=1.5)))
+    loss, lse, cross = echo.distill(x[0], w, ids[0], logits[0].to(F16), temperature=1.5)
+    assert loss.shape == () and torch.equal(loss, want[0][0]) and torch.equal(lse, want[1][0])
+    dx, dw = echo.distill_grad(one[0], x[0], w, ids[0], logits[0], lse, temperature=1.5)
+    assert dx.shape == (h,) and dw.shape == (v, h)
+    # the same entry many times is one of their summed weight; a missing one in between changes nothing
+    rep = torch.tensor([[7, 7, -1, 7, 7]], device="cuda")
+    same = echo.distill(x[:1], w, rep, torch.zeros((1, 5), device="cuda"))
+    single = echo.cross_entropy(x[:1], w, torch.tensor([7], device="cuda"))
+    assert torch.equal(same[1], single[1])
+    assert abs(float(same[2] - single[2])) <= 8 * U * abs(float(single[2]))
+    assert abs(float(same[0] - (single[0] - math.log(4)))) <= 64 * U * (abs(float(single[1])) + abs(float(single[2])) + 2)
+
+
+@pytest.mark.parametrize("dw_type", [F32, BF16])
+@pytest.mark.parametrize("left", [0, 4, 1])
+def test_sums_into_parts_of_a_matrix(echo, dw_type, left):
+    n, h, v = 70, 96, 300
+    x, w = _case(n, h, v, 0, BF16, 12)
+    labels, dloss = _randint(-1, v, (n,), 13), _randn((n,), 14)
+    lse = echo.cross_entropy(x, w, labels)[1]
+    whole = _randn((v, h + 8), 15, dw_type)
+    old = whole.clone()
+    view = whole[:, left:left + h]
+    tight = view.clone()
+    echo.cross_entropy_grad(dloss, x, w, labels, lse, dweight=tight, accumulate=True)
+    got = echo.cross_entropy_grad(dloss, x, w, labels, lse, dweight=view, accumulate=True)
+    assert got[1] is view
+    assert torch.equal(view, tight) and torch.equal(whole[:, :left], old[:, :left]) and torch.equal(whole[:, left + h:], old[:, left + h:])
+
+
+def test_only_one_of_the_gradients(echo):
+    """dx or dweight alone (NULL for the other, through the C call) are those of both."""
+    import ctypes as C
+
+    from paper_2412_12487_gb300 import echo as E
+    n, h, v = 100, 64, 700
+    for dtype, kind in ((BF16, 1), (F16, 2), (F32, 0)):
+        x, w = _case(n, h, v, 0, dtype, 16)
+        labels, dloss = _randint(-1, v, (n,), 17), _randn((n,), 18)
+        lse = echo.cross_entropy(x, w, labels)[1]
+        dx, dw = echo.cross_entropy_grad(dloss, x, w, labels, lse)
+        for which in (0, 1):
+            a, b = torch.zeros_like(dx), torch.zeros_like(dw)
+            d = E.CrossEntropyGradDesc(n, h, v, 0, dloss.data_ptr(), None, x.data_ptr(), w.data_ptr(), labels.data_ptr(), lse.data_ptr(),
+                                       a.data_ptr() if which == 0 else None, b.data_ptr() if which else None, h, h, h, h, kind, 0, 64, 0, 1.0)
+            assert echo.lib.echo_cross_entropy_grad(echo.h, C.byref(d)) == 0
+            torch.cuda.synchronize()
+            if which:
+                assert torch.equal(b, dw) and not a.any()
+            else:
+                assert not b.any()
+                if dtype == F32:
+                    assert torch.equal(a, dx)
+                else:  # (P is one number then, as in both; tiles are shared out otherwise, and sums of parts rounded otherwise)
+                    assert float((a.double() - dx.double()).abs().max()) <= 2.0 ** -7 * float(dx.double().abs().max())
+
+
+def test_matrices_beyond_32_bits_of_elements(echo):
+    n, h, v = 3, 16384, 135000
+    g = torch.Generator(device="cuda").manual_seed(19)
+    w = torch.randn((v, h), generator=g, device="cuda", dtype=BF16)
+    x = _randn((n, h), 20, BF16, 0.01)
+    labels = torch.tensor([v - 1, 131072, 5], device="cuda")
+    loss, lse, target = echo.cross_entropy(x, w, labels)
+    z = torch.cat([x.double() @ w[i:i + 15000].double().T for i in range(0, v, 15000)], 1)
+    size = torch.cat([x.double().abs() @ w[i:i + 15000].double().abs().T for i in range(0, v, 15000)], 1)
+    tol = (64 + h / 256) * U * size + 4 * U * z.abs()
+    _close(lse, torch.logsumexp(z, 1), tol.amax(1) + 300 * U + 200 * U)
+    _close(target, z.gather(1, labels[:, None])[:, 0], tol.gather(1, labels[:, None])[:, 0])
+    one = torch.ones(n, device="cuda")
+    dx, dw = echo.cross_entropy_grad(one, x, w, labels, lse)
+    p = torch.exp(z - lse.double()[:, None])
+    p[torch.arange(n), labels] -= 1
+    rows = torch.tensor([0, 5, 131071, 131072, v - 2, v - 1], device="cuda")
+    want = p[:, rows].T @ x.double()
+    near = p[:, rows].abs().T @ x.double().abs()
+    _close(dw[rows], want, near * (float(torch.expm1(tol.max() + 600 * U)) + 2.0 ** -19))
+    dx_want = sum(p[:, i:i + 15000] @ w[i:i + 15000].double() for i in range(0, v, 15000))
+    dx_size = sum(p[:, i:i + 15000].abs() @ w[i:i + 15000].double().abs() for i in range(0, v, 15000))
+    _close(dx, dx_want, dx_size * (float(torch.expm1(tol.max() + 600 * U)) + 2.0 ** -8 + 2.0 ** -16))
+
+
+def test_two_contexts_at_a_time():
+    """Calls of two contexts on two streams, without waiting for one another."""
+    x, w = _case(500, 256, 3000, 0, BF16, 21)
+    labels, dloss = _randint(-1, 3000, (500,), 22), _randn((500,), 23)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    contexts = [Echo(0, stream=s) for s in streams]
+    results = [[], []]
+    for _ in range(4):
+        for i, (e, s) in enumerate(zip(contexts, streams)):
+            with torch.cuda.stream(s):
+                out = e.cross_entropy(x, w, labels)
+                results[i].append((*out, *e.cross_entropy_grad(dloss, x, w, labels, out[1])))
+    torch.cuda.synchronize()
+    first = results[0][0]
+    for r in results[0] + results[1]:
+        assert all(torch.equal(a, b) for a, b in zip(r, first))
+    for e in contexts:
+        e.wait()
+        e.close()
+
+
+def test_teacher_without_weight(echo):
+    """Rows whose entries are all missing, have no weight, or an infinite one."""
+    x, w = _case(4, 32, 60, 0, BF16, 24)
+    ids = torch.tensor([[1, 2], [-1, -1], [3, 4], [5, 6]], device="cuda")
+    t = torch.tensor([[0.0, -math.inf], [0.0, 0.0], [-math.inf, -math.inf], [math.nan, 0.0]], device="cuda")
+    loss, lse, cross = echo.distill(x, w, ids, t)
+    label = echo.cross_entropy(x, w, torch.tensor([1, -1, -1, 5], device="cuda"))
+    assert abs(float(loss[0] - label[0][0])) <= 16 * U * float(lse[0].abs() + cross[0].abs()) and torch.equal(lse, label[1])
+    assert loss[1] == 0 and loss[2] == 0 and cross[1] == 0 and cross[2] == 0 and torch.isnan(loss[3])
+    g = torch.tensor([1.0, math.nan, math.inf, 0.0], device="cuda")
+    t[3] = 0
+    dx, dw = echo.distill_grad(g, x, w, ids, t, lse)
+    assert torch.isfinite(dx).all() and torch.isfinite(dw).all() and not dx[1:].any()
