@@ -765,11 +765,11 @@ class Echo:
         shape = labels.shape
         _need(shape == x.shape[:-1], "labels have another shape than x without its rows")
         labels = labels.contiguous()
-        out = torch.empty((3, *shape), dtype=torch.float32, device=x.device)
-        at = out.data_ptr()  # (three rows, one behind the other)
-        self._op(self.lib.echo_cross_entropy, _packed(_CROSS_ENTROPY, n, h, v, vocab_start, xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), at, at + 4 * n,
-                                                      at + 8 * n, xs, ws, kind, bits, scale))
-        return out.unbind()
+        loss = torch.empty(shape, dtype=torch.float32, device=x.device)
+        lse, target = torch.empty_like(loss), torch.empty_like(loss)
+        self._op(self.lib.echo_cross_entropy, _packed(_CROSS_ENTROPY, n, h, v, vocab_start, xm.data_ptr(), wm.data_ptr(), labels.data_ptr(), loss.data_ptr(),
+                                                      lse.data_ptr(), target.data_ptr(), xs, ws, kind, bits, scale))
+        return loss, lse, target
 
     def _head_grads(self, x, weight, dx, dweight, dtype, accumulate):
         import torch
@@ -818,11 +818,12 @@ class Echo:
         import torch
         xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
         bits, ids, logits, teacher_lse, top, lkind = self._teacher(x, ids, logits, teacher_lse)
-        out = torch.empty((3, *ids.shape[:-1]), dtype=torch.float32, device=x.device)
-        at = out.data_ptr()
+        loss = torch.empty(ids.shape[:-1], dtype=torch.float32, device=x.device)
+        lse, cross = torch.empty_like(loss), torch.empty_like(loss)
         self._op(self.lib.echo_distill, _packed(_DISTILL, n, h, v, vocab_start, top, xm.data_ptr(), wm.data_ptr(), ids.data_ptr(), logits.data_ptr(),
-                                                _dptr(teacher_lse) or 0, at, at + 4 * n, at + 8 * n, xs, ws, kind, bits, lkind, scale, temperature))
-        return out.unbind()
+                                                0 if teacher_lse is None else teacher_lse.data_ptr(), loss.data_ptr(), lse.data_ptr(), cross.data_ptr(), xs, ws,
+                                                kind, bits, lkind, scale, temperature))
+        return loss, lse, cross
 
     def distill_grad(self, dloss, x, weight, ids, logits, lse, temperature: float = 1.0, teacher_lse=None, scale: float = 1.0, vocab_start: int = 0, dlse=None,
                      dtype=None, dx=None, dweight=None, accumulate: bool = False):
