@@ -491,9 +491,9 @@ int echo_orthogonalize(echo_ctx *ctx, const echo_orthogonalize_desc *d);
  * Of one shard of many, the loss is not of use: the loss of the whole vocabulary is the
  * logarithm of the sum of the shards' exp(lse) minus the sum of their targets.
  * Each of loss, lse and target may be NULL.  n_tokens and vocab_rows may be 0; hidden is 1
- * to 2^24, n_tokens and vocab_rows at most 2^30.  fp32 elements count with 22 bits down to
- * 2^-14 of the largest finite one of their token (x) or of the matrix (weight), and with an
- * error of 2^-37 of that below. */
+ * to 2^24, n_tokens and vocab_rows at most 2^30.  fp32 elements of more than 16 tokens, and
+ * of the weight with them, count with 22 bits down to 2^-14 of the largest finite one of
+ * their row, and with an error of 2^-37 of that below. */
 typedef struct {
   int64_t n_tokens, hidden, vocab_rows, vocab_start;
   const void *x;      /* [n_tokens][hidden]                                             */
@@ -517,9 +517,10 @@ int echo_cross_entropy(echo_ctx *ctx, const echo_cross_entropy_desc *d);
  * gradient and adds none to dweight, whatever its x holds.
  * dz is rounded to the matrices' 16-bit type where the results have 16 bits, and taken to 22
  * bits for an fp32 dweight or fp32 matrices; fp16: elements of dz below 2^-29 of the largest
- * are rounded to multiples of 2^-40 of it.  fp32 elements of x, and bf16 ones for an fp32
- * dweight, count as above with the largest one of all tokens that have a gradient.  Adding
- * to an fp32 dweight takes subnormal numbers as zeros. */
+ * are rounded to multiples of 2^-40 of it.  fp32 elements of more than 16 tokens and of the
+ * weight with them, and bf16 ones of x for an fp32 dweight, count as above with the largest
+ * one of the matrix, for x of the tokens that have a gradient.  Adding to an fp32 dweight
+ * may take subnormal numbers as zeros. */
 typedef struct {
   int64_t n_tokens, hidden, vocab_rows, vocab_start;
   const float *dloss;       /* [n_tokens]                                               */

@@ -17,11 +17,15 @@
 // Operands are 16-bit numbers on the tensor cores, with sums in fp32:
 //   - bf16 and fp16 matrices as they are; fp32 ones as sums of two fp16 numbers times a power of
 //     two that the largest element sets (22 bits of elements down to 2^-14 of it, an error of
-//     2^-37 of it below), multiplied as high * high + high * low + low * high;
-//   - P, scaled so that its largest element is a power of two, as one number of the matrices' type where the results have 16 bits: an error of 2^-9
-//     (bf16) of each element, independent of the others, where the results are rounded to the
-//     same.  For an fp32 dW as the sum of two fp16 numbers, with x as fp16 (the same way): a
-//     gradient added up over micro-batches in fp32 would otherwise be 2e-3 off.
+//     2^-37 of it below), multiplied as high * high + high * low + low * high.  Forward each row
+//     has its own power of two, backward x and the weight have one each, as the sums then run over
+//     rows;
+//   - P, scaled so that its largest element is a power of two, as one number of the matrices' type
+//     where the results have 16 bits: an error of up to 2^-8 (bf16) of each element, independent
+//     of the others', where the results are rounded to the same (2.4e-3 from 64 bits at the most,
+//     1.7e-3 of which is the result's rounding).  For an fp32 dW as the sum of two fp16 numbers,
+//     with x as fp16 (scaled in the same way): a gradient added up over micro-batches in fp32
+//     would otherwise be 2e-3 off.  That takes dW's products twice.
 // The tensor core truncates the sums that it adds to, which is a bias, so they are added up in
 // registers, rounding to nearest, every few stages (set_of).
 #include <algorithm>
@@ -91,14 +95,14 @@ struct Source {
   void *to;
   int64_t ld, plane;
   float *amax;
-  bool amax_rows;       // of each row
+  bool down;            // what takes a row back, instead of its largest element
 };
 struct Sources {
   Source of[2];
 };
 
-// The largest finite element of each row, by a warp, or of each block's part of a matrix's live rows
-// (without gaps, and all of them live, a single row).  Bound by the bytes, or by latency where they are few.
+// The largest finite element of each block's part of a matrix's live rows (without gaps, and all of
+// them live, a single row).  Bound by the bytes, or by latency where they are few.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
   __shared__ float sh[8];
@@ -106,16 +110,6 @@ __global__ void __launch_bounds__(256) head_amax_kernel(Sources s) {
   next_may_start();
   const Source &m = s.of[blockIdx.y];
   const T *x = static_cast<const T *>(m.p);
-  if (m.amax_rows) {
-    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < m.rows; r += (int64_t)gridDim.x * 8) {
-      float most = 0.f;
-#pragma unroll 8
-      for (int64_t c = threadIdx.x & 31; c < m.cols; c += 32) most = fmaxf(most, finite_size(to_f(x[r * m.stride + c])));
-      most = warp_max(most);
-      if ((threadIdx.x & 31) == 0) m.amax[r] = most;
-    }
-    return;
-  }
   // (a single row: its 16-byte pieces, and what is before and behind them, by the first block)
   int64_t cols = m.cols;
   float most = 0.f;
@@ -177,21 +171,19 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
   const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   const T *x = static_cast<const T *>(m.p);
   D *to = static_cast<D *>(m.to);
-  const float *live = m.live, *rows = m.scale.rows;
+  const float *live = m.live;
   const int64_t stride = m.stride, ld = m.ld, plane = m.plane, cols = m.cols;
   const uint32_t pieces = (uint32_t)((cols + W - 1) / W);
   const int64_t all = m.rows * pieces;
   for (int64_t i0 = first; i0 < all; i0 += step * kFlight) {
     Pack<T, W> raw[kFlight];
     int64_t at[kFlight];
-    float size[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
       const int64_t i = i0 + k * step;
       if (i >= all) continue;
       const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), c = (i - r * pieces) * W;
       at[k] = r * ld + c;
-      size[k] = rows ? rows[r] : 0.f;
 #pragma unroll
       for (int e = 0; e < W; ++e) raw[k].v[e] = from_f<T>(0.f);
       if (live && live[r] == 0.f) continue;
@@ -209,9 +201,8 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
       if (i0 + k * step >= all) continue;
       float v[W];
       unpack<T, W>(raw[k], v);
-      const float by = rows ? ldexpf(1.f, exponent_of(size[k])) : up;
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[e] *= by;
+      for (int e = 0; e < W; ++e) v[e] *= up;
 #pragma unroll
       for (int q = 0; q < PLANES; ++q) {
         const Pack<D, W> h = pack<D, W>(v);
@@ -221,6 +212,56 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
         for (int e = 0; e < W; ++e) v[e] -= back[e];  // what the next plane holds
         *reinterpret_cast<Pack<D, W> *>(to + q * plane + at[k]) = h;
       }
+    }
+  }
+}
+
+// fp32 rows as two planes of fp16 each, a warp a row: scaled by its own largest finite element, which it
+// leaves (x), or by the power of two that takes it back (the weight's `down`).  Bound by the bytes: a row's
+// second pass finds it in L1 or L2.
+template <bool WIDE>
+__global__ void __launch_bounds__(256) head_pack_rows_kernel(Sources s) {
+  kernel_begin();
+  next_may_start();
+  constexpr int W = 8;
+  const Source &m = s.of[blockIdx.y];
+  const int lane = threadIdx.x & 31;
+  const int64_t pieces = (m.cols + W - 1) / W;
+  __half *to = static_cast<__half *>(m.to);
+  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < m.rows; r += (int64_t)gridDim.x * 8) {
+    const float *x = static_cast<const float *>(m.p) + r * m.stride;
+    auto load = [&](int64_t piece, float (&v)[W]) {
+      if (WIDE) {
+        load_piece<W>(x + piece * W, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] = piece * W + e < m.cols ? x[piece * W + e] : 0.f;
+      }
+    };
+    float most = 0.f;
+#pragma unroll 4
+    for (int64_t i = lane; i < pieces; i += 32) {
+      float v[W];
+      load(i, v);
+#pragma unroll
+      for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[e]));
+    }
+    most = warp_max(most);
+    const int up = exponent_of(most);
+    if (lane == 0) m.amax[r] = m.down ? ldexpf(1.f, -up) : most;
+    const float by = ldexpf(1.f, up);
+#pragma unroll 4
+    for (int64_t i = lane; i < pieces; i += 32) {
+      float v[W], back[W];
+      load(i, v);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] *= by;
+      const Pack<__half, W> high = pack<__half, W>(v);
+      unpack<__half, W>(high, back);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] -= back[e];
+      *reinterpret_cast<Pack<__half, W> *>(to + r * m.ld + i * W) = high;
+      *reinterpret_cast<Pack<__half, W> *>(to + m.plane + r * m.ld + i * W) = pack<__half, W>(v);
     }
   }
 }
@@ -355,7 +396,24 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 // -- products --------------------------------------------------------------------------------------
 // D = A B^T on tiles of 256 x 256 by persistent pairs of blocks (echo_tensor.cuh).  The sum may run
 // along the rows of an operand in memory (K-major) or down its columns (MN-major), and over several
-// pairs of planes.  A launch has up to two products, whose tiles follow one another.
+// pairs of planes.  A launch has up to two products (dx and dW), whose tiles are shared out together.
+//
+// In each block one thread copies stages into a ring, a thread of the pair's first block issues the
+// products, and eight warps take the sums out of tensor memory, which holds two sets of them, add
+// them up, and finish the tile while the next one is summed.  What bounds it, at 2048 tokens:
+//   - logits, 12288 columns, 6400 rows, bf16: 187 us, 1.73 PFLOP/s, tensor pipe busy 74% of the time.
+//     A stage takes 660 to 700 clocks, of which the products are 512: operands come from L2 at 64 bytes
+//     a clock and SM, and a copy of half of them (other results wrong) saved 5% only.
+//   - logits, 2048 columns, 51200 rows, 64 targets a token: 262 us; 22 rounds where 21.05 would do.
+//   - P, 2048 columns, 25600 rows, three planes: 160 us, 10000 clocks a tile to finish beside the 20000
+//     of its products, which go slower meanwhile.
+//   - dx and dW, 25600 x 2048, fp32 dW (3.2e11 operations on 16-bit numbers twice for dW): 377 us; with a
+//     16-bit dW 6400 x 12288: 359 us, 1.80 PFLOP/s.
+// What counted: 32-bit counters and nothing looked up in a stage's way, which single threads take (a
+// stage of 64-bit counters and arguments read from memory: 20% slower); results through the copy engine
+// (1236 us for dx and dW with stores by lanes, 451 so); tiles split where rounds are not full, and joined
+// through shared memory; longer first sets (lead_of).  Five stages and 64 KB on the way out are as fast
+// as six and 32 KB; four are 4% slower.
 constexpr int kTile = 256, kHalf = 128, kBK = 64;
 constexpr int kThreads = 384;                    // warp 0: copies, 1: products, 4-11: tiles out
 constexpr int kFewRegs = 88, kManyRegs = 208;    // a thread of warps 0-3 and of 4-11
@@ -406,6 +464,7 @@ struct HeadProduct {
   float alpha;       // scale / tau
   const int32_t *idx;
   const float *weight, *coef, *lse;
+  const float *w_down;  // forward, fp32: factors of the weight's rows
   float2 *part;      // [columns / 128][n] largest element (times log2 e) and sum of exponentials
   float *picked;     // [n][K] z of the targets
   int p_bf16, p_half;  // planes of P: one of bf16, of fp16
@@ -677,8 +736,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       uint32_t phase = 1;
       bool ok = true;
       auto copy = [&](auto a_mn, auto b_mn, const CUtensorMap *amap, const CUtensorMap *bmap, const Job &j, const Share &w) {
-        const int steps = j.steps;
-        int r0, c0, p = w.k0 / steps, k = w.k0 - p * steps;
+        // (the pairs of planes of a stage follow one another, so that a plane that two of them read is in L2)
+        const int planes = j.pairs;
+        int r0, c0, k = w.k0 / planes, p = w.k0 - k * planes;
         tile_place(j, w.tile, r0, c0);
         r0 += rank * kHalf, c0 += rank * kHalf;
         int plane_a = j.plane_a[p], plane_b = j.plane_b[p];
@@ -690,8 +750,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           copy_rows(at, amap, decltype(a_mn)::value, r0, k * kBK, plane_a, bar);
           copy_rows(at + kOperandBytes, bmap, decltype(b_mn)::value, c0, k * kBK, plane_b, bar);
           if (++s == kStages) s = 0, phase ^= 1;
-          if (++k == steps && left > 1) {
-            k = 0, ++p;
+          if (planes == 1) {
+            ++k;
+          } else {
+            if (++p == planes) p = 0, ++k;
             plane_a = j.plane_a[p], plane_b = j.plane_b[p];
           }
         }
@@ -869,6 +931,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
       }
       if constexpr (MODE == kStats) {
+        if (a.w_down)  // (fp32: a power of two of each row of the weight; the array is as long as the tiles)
+#pragma unroll
+          for (int e = 0; e < kHalf; e += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(a.w_down + c0 + e);
+            acc[e] *= f.x, acc[e + 1] *= f.y, acc[e + 2] *= f.z, acc[e + 3] *= f.w;
+          }
         if (c0 + kHalf > j.N)
 #pragma unroll
           for (int part = 0; part < kParts; ++part)
@@ -1044,6 +1112,222 @@ __global__ void __launch_bounds__(kJoinWarps * 32) head_join_kernel(HeadArgs a, 
   }
 }
 
+// -- few tokens of fp32 matrices ---------------------------------------------------------------------
+// Planes of the weight are read, written and read again before the tensor cores have them, for tiles of
+// 256 tokens: with 51200 x 4096 a call takes 559 us forward and 1388 backward from 17 tokens on, whose
+// products alone would be 170.  Up to kFew tokens the products are made in fp32 from the weight as it is,
+// read once for the logits (149 us with one token, 206 with eight, 371 with 16; its 839 MB take 124) and
+// once for dx, and dW is written once (420, 535 and 880 us, of 371).  Above eight tokens their arithmetic
+// is what bounds them: 32 would take 957 us forward.
+constexpr int kFew = 16, kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kFewColumns = 512;   // of x in shared memory at a time
+constexpr int few_rows(int tokens, bool many) { return tokens > 8 ? 4 : many ? 8 : 2; }  // of the weight, of a warp
+
+// Where x and weight are 16-byte rows, a lane takes four neighbouring columns, else every 32nd.
+template <bool WIDE>
+__device__ __forceinline__ int few_column(int lane, int e) { return WIDE ? 4 * lane + e : lane + 32 * e; }
+
+// Logits of a block's rows of the weight and all tokens; then the parts and targets of the forward pass, or P.
+template <int TOKENS, int R, bool WIDE, bool GRAD>
+__global__ void __launch_bounds__(kFewThreads) head_few_kernel(HeadArgs a, Targets t, float2 *part, float *picked, float *P, int64_t ldp) {
+  constexpr int kRowsBlock = R * kFewWarps, kAhead = 8 / R;  // (of R rows, 128 columns each are on their way)
+  __shared__ alignas(16) float xs[TOKENS][kFewColumns];
+  __shared__ float zs[TOKENS][kRowsBlock];
+  kernel_begin();
+  next_may_start();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)a.n;
+  const float *x = static_cast<const float *>(a.x);
+  const int64_t v0 = (int64_t)blockIdx.x * kRowsBlock, first = v0 + warp * R;
+  const float *w = static_cast<const float *>(a.w) + first * a.w_stride;
+  float acc[R][TOKENS] = {};
+  for (int64_t h0 = 0; h0 < a.H; h0 += kFewColumns) {
+    for (int i = threadIdx.x; i < TOKENS * kFewColumns; i += kFewThreads) {
+      const int row = i / kFewColumns, c = i % kFewColumns;
+      xs[row][c] = row < n && h0 + c < a.H ? x[row * a.x_stride + h0 + c] : 0.f;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int c0 = 0; c0 < kFewColumns && h0 + c0 < a.H; c0 += 128 * kAhead) {
+      float f[kAhead][R][4];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int64_t c = h0 + c0 + 128 * u;
+          const float *at = w + r * a.w_stride + c;
+          const bool row = first + r < a.V;
+          if (WIDE) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row && c + 4 * lane < a.H) v = __ldcs(reinterpret_cast<const float4 *>(at + 4 * lane));
+            f[u][r][0] = v.x, f[u][r][1] = v.y, f[u][r][2] = v.z, f[u][r][3] = v.w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[u][r][e] = row && c + few_column<WIDE>(lane, e) < a.H ? __ldcs(at + few_column<WIDE>(lane, e)) : 0.f;
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int k = 0; k < TOKENS; ++k) {
+          const float *at = &xs[k][c0 + 128 * u];
+          float g[4];
+          if (WIDE) {
+            const float4 v = *reinterpret_cast<const float4 *>(at + 4 * lane);
+            g[0] = v.x, g[1] = v.y, g[2] = v.z, g[3] = v.w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[e] = at[few_column<WIDE>(lane, e)];
+          }
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[r][k] = fmaf(f[u][r][e], g[e], acc[r][k]);
+        }
+    }
+    __syncthreads();
+  }
+  const float alpha = a.scale / a.tau;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int k = 0; k < TOKENS; ++k) {
+      const float z = warp_sum(acc[r][k]) * alpha;
+      if (lane == 0) zs[k][warp * R + r] = z;
+    }
+  __syncthreads();
+  // a warp a token
+  const int rows = (int)min((int64_t)kRowsBlock, a.V - v0);
+  for (int k = warp; k < n; k += kFewWarps) {
+    const int32_t *idx = t.idx + (int64_t)k * a.K;
+    if (!GRAD) {
+      float most = -INFINITY, sum = 0.f;
+      for (int r = lane; r < rows; r += 32) most = fmaxf(most, zs[k][r] * kLog2e);
+      most = warp_max(most);
+      const float zero = most == -INFINITY ? 0.f : most;
+      for (int r = lane; r < rows; r += 32) sum += exp2f(fmaf(zs[k][r], kLog2e, -zero));
+      sum = warp_sum(sum);
+      if (lane == 0) part[blockIdx.x * a.n + k] = make_float2(most, sum);
+      for (int i = lane; i < a.K; i += 32)
+        if (idx[i] >= v0 && idx[i] - v0 < rows) picked[(int64_t)k * a.K + i] = zs[k][idx[i] - v0];
+    } else {
+      const float coef = t.coef[k], lse = a.lse_in[k];
+      for (int r = lane; r < rows; r += 32) {
+        float p = coef == 0.f ? 0.f : coef * expf(zs[k][r] - lse);
+        for (int i = 0; i < a.K; ++i)
+          if (idx[i] - v0 == r) p -= t.weight[(int64_t)k * a.K + i];
+        P[k * ldp + v0 + r] = p;
+      }
+    }
+  }
+}
+
+// dx's part of a range of the weight's rows, for 1024 columns: [range][token][column].
+template <int TOKENS, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads) head_few_dx_kernel(HeadArgs a, const float *P, int64_t ldp, float *parts, int64_t rows_range) {
+  constexpr int kRowsAt = 64;
+  __shared__ alignas(16) float ps[kRowsAt][TOKENS];
+  kernel_begin();
+  next_may_start();
+  const int64_t c0 = (int64_t)blockIdx.x * 4 * kFewThreads, begin = blockIdx.y * rows_range, end = min(a.V, begin + rows_range);
+  const float *w = static_cast<const float *>(a.w);
+  auto column = [&](int e) { return c0 + (WIDE ? 4 * (int)threadIdx.x + e : (int)threadIdx.x + kFewThreads * e); };
+  float acc[TOKENS][4] = {};
+  for (int64_t v0 = begin; v0 < end; v0 += kRowsAt) {
+    for (int i = threadIdx.x; i < kRowsAt * TOKENS; i += kFewThreads) {
+      const int r = i % kRowsAt, k = i / kRowsAt;
+      ps[r][k] = k < a.n && v0 + r < end ? P[k * ldp + v0 + r] : 0.f;
+    }
+    __syncthreads();
+    const int rows = (int)min((int64_t)kRowsAt, end - v0);
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+      const float *at = w + (v0 + r) * a.w_stride;
+      float f[4] = {};
+      if (WIDE) {
+        if (column(0) < a.H) load_piece<4>(at + column(0), f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (column(e) < a.H) f[e] = at[column(e)];
+      }
+#pragma unroll
+      for (int k = 0; k < TOKENS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[k][e] = fmaf(ps[r][k], f[e], acc[k][e]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int k = 0; k < TOKENS; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (k < a.n && column(e) < a.H) parts[(blockIdx.y * a.n + k) * a.H + column(e)] = acc[k][e];
+}
+// The parts' sum, in their order.
+__global__ void __launch_bounds__(256) head_few_dx_join_kernel(HeadArgs a, const float *parts, int ranges) {
+  kernel_begin();
+  next_may_start();
+  const int64_t all = a.n * a.H;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int q = 0; q < ranges; ++q) s += parts[q * all + i];
+    static_cast<float *>(a.dx)[i / a.H * a.dx_stride + i % a.H] = s;
+  }
+}
+
+// dW: a block has 1024 columns of 64 rows.
+template <int TOKENS, typename T, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads) head_few_dw_kernel(HeadArgs a, const float *live, const float *P, int64_t ldp) {
+  constexpr int kRowsAt = 64;
+  __shared__ alignas(16) float ps[kRowsAt][TOKENS];
+  kernel_begin();
+  next_may_start();
+  const int64_t c0 = (int64_t)blockIdx.x * 4 * kFewThreads, v0 = (int64_t)blockIdx.y * kRowsAt;
+  auto column = [&](int e) { return c0 + (WIDE ? 4 * (int)threadIdx.x + e : (int)threadIdx.x + kFewThreads * e); };
+  float x[TOKENS][4] = {};
+#pragma unroll
+  for (int k = 0; k < TOKENS; ++k)
+    if (k < a.n && live[k] != 0.f)  // (what other tokens hold meets nothing)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (column(e) < a.H) x[k][e] = static_cast<const float *>(a.x)[k * a.x_stride + column(e)];
+  for (int i = threadIdx.x; i < kRowsAt * TOKENS; i += kFewThreads) {
+    const int r = i % kRowsAt, k = i / kRowsAt;
+    ps[r][k] = k < a.n && v0 + r < a.V ? P[k * ldp + v0 + r] : 0.f;
+  }
+  __syncthreads();
+  const int rows = (int)min((int64_t)kRowsAt, a.V - v0);
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r) {
+    T *to = static_cast<T *>(a.dw) + (v0 + r) * a.dw_stride;
+    float f[4] = {};
+    if (a.accumulate) {
+      if (WIDE) {
+        if (column(0) < a.H) load_piece<4>(to + column(0), f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (column(e) < a.H) f[e] = to_f(to[column(e)]);
+      }
+    }
+    float s[4] = {};
+#pragma unroll
+    for (int k = 0; k < TOKENS; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = fmaf(ps[r][k], x[k][e], s[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] += s[e];
+    if (WIDE) {
+      if (column(0) < a.H) store_piece<4>(to + column(0), f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (column(e) < a.H) to[column(e)] = from_f<T>(f[e]);
+    }
+  }
+}
+
 // -- host -------------------------------------------------------------------------------------------
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 int64_t padded(int64_t x) { return (x + 63) / 64 * 64; }
@@ -1088,10 +1372,23 @@ struct Layout {
   int p_bf16, p_half;
   int64_t piece, ldp;
   uint16_t *P;
-  float *dx_sum;      // fp32, where dx is added up over pieces
+  float *few_p;       // few tokens: P in fp32
+  float *dx_sum;      // fp32, where dx is added up over pieces (few tokens: its parts)
   int64_t dx_ld;
   size_t bytes;
 };
+
+bool few_tokens(const HeadArgs &a) { return a.type == ECHO_F32 && a.n <= kFew; }
+int few_count(int64_t n) { return n > 8 ? 16 : n > 4 ? 8 : n > 1 ? 4 : 1; }
+// Rows of a block: as many as share an x, but four blocks an SM.
+int few_block(const HeadArgs &a, int sms) {
+  const int n = few_count(a.n), most = few_rows(n, true) * kFewWarps;
+  return a.V >= (int64_t)4 * sms * most ? most : few_rows(n, false) * kFewWarps;
+}
+int64_t few_ranges(const HeadArgs &a, int sms) {  // of the weight's rows, for dx: as many as fill the SMs four times
+  const int64_t tiles = (a.H + 4 * kFewThreads - 1) / (4 * kFewThreads);
+  return std::clamp<int64_t>(4 * sms / tiles, 1, (a.V + 63) / 64);
+}
 
 Layout layout_of(const HeadArgs &a, int sms) {
   Layout l{};
@@ -1100,19 +1397,37 @@ Layout layout_of(const HeadArgs &a, int sms) {
   l.target_blocks = (int)std::min<int64_t>((a.n + kTargetWarps - 1) / kTargetWarps, 2 * sms);
   l.targets.idx = c.take<int32_t>(a.n * a.K);
   l.targets.weight = c.take<float>(a.n * a.K);
+  if (few_tokens(a)) {
+    if (!a.grad) {
+      l.chunks = (a.V + few_block(a, sms) - 1) / few_block(a, sms);
+      l.targets.entropy = c.take<float>(a.n);
+      l.targets.mass = c.take<float>(a.n);
+      l.part = c.take<float2>(l.chunks * a.n);
+      l.picked = c.take<float>(a.n * a.K);
+    } else {
+      l.targets.coef = c.take<float>(a.n);
+      l.targets.live = c.take<float>(a.n);
+      l.targets.size_part = c.take<float>(l.target_blocks);
+      l.ldp = padded(a.V);
+      l.few_p = c.take<float>(a.n * l.ldp);
+      if (a.dx) l.dx_sum = c.take<float>(few_ranges(a, sms) * a.n * a.H);
+    }
+    l.bytes = c.at;
+    return l;
+  }
   // (split tiles have two parts for each pair of blocks at most, and are no more than that)
   l.targets.n_arrived = sms * 16;
   l.targets.arrived = c.take<int32_t>(l.targets.n_arrived);
   l.parts = c.take<float4>((int64_t)sms / 2 * 2 * kTile * kTile / 4);
-  l.amax_x = c.take<float>(a.grad ? kAmaxParts : a.n);  // (of blocks' parts, or of rows)
-  l.amax_w = c.take<float>(kAmaxParts);
+  l.amax_x = c.take<float>(a.grad ? kAmaxParts : f32 ? a.n : 0);  // (of blocks' parts, or of rows)
+  l.amax_w = c.take<float>(a.grad ? kAmaxParts : f32 ? (a.V + kTile - 1) / kTile * kTile : 0);  // (or of rows, what takes them back)
   auto planes = [&](int64_t rows, int64_t cols, int count, bool bf16, Scale scale) {
     const int64_t ld = padded(cols);
     return Operand{c.take<uint16_t>(count * rows * ld), rows, cols, ld, rows * ld, count, bf16, scale};
   };
   l.pack_x = !readable(a.x, a.n, a.H, a.x_stride, a.type);
   l.pack_w = !readable(a.w, a.V, a.H, a.w_stride, a.type);
-  const Scale none{}, sw{l.amax_w, kAmaxParts, nullptr}, sx = a.grad ? Scale{l.amax_x, kAmaxParts, nullptr} : Scale{nullptr, 0, l.amax_x};
+  const Scale none{}, sw = a.grad ? Scale{l.amax_w, kAmaxParts, nullptr} : none, sx = a.grad ? Scale{l.amax_x, kAmaxParts, nullptr} : Scale{nullptr, 0, l.amax_x};
   l.x = l.pack_x ? planes(a.n, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sx : none) : in_place(a.x, a.n, a.H, a.x_stride, a.type);
   l.w = l.pack_w ? planes(a.V, a.H, f32 ? 2 : 1, a.type == ECHO_BF16, f32 ? sw : none) : in_place(a.w, a.V, a.H, a.w_stride, a.type);
   if (!a.grad) {
@@ -1268,7 +1583,6 @@ cudaError_t launch_amax(Sources s, int count, int type, cudaStream_t st) {
     bool wide = true;
     for (int i = 0; i < count; ++i) {
       Source &m = s.of[i];
-      if (m.amax_rows) continue;
       if (m.stride == m.cols && !m.live) m.cols *= m.rows, m.rows = 1;
       wide &= m.rows == 1 || (m.cols % N == 0 && fits_pieces(m.p, m.stride, type, N));
     }
@@ -1298,6 +1612,74 @@ cudaError_t launch_pack(const Sources &s, int count, int type, bool bf16, int sm
   });
 }
 
+// f(Int<the number of tokens that the kernels for few of them are made for>, Int<whether rows are 16-byte ones>)
+template <typename F>
+cudaError_t with_few(int64_t n, bool wide, F &&f) {
+  auto with = [&](auto w) {
+    switch (few_count(n)) {
+      case 1: return f(Int<1>{}, w);
+      case 4: return f(Int<4>{}, w);
+      case 8: return f(Int<8>{}, w);
+      default: return f(Int<16>{}, w);
+    }
+  };
+  return wide ? with(Int<1>{}) : with(Int<0>{});
+}
+cudaError_t launch_few_dw(const HeadArgs &a, const Layout &l, const OpTimer &timed, cudaStream_t st) {
+  const bool wide = a.H % 4 == 0 && fits_pieces(a.dw, a.dw_stride, a.dw_type, 4);
+  const dim3 grid((unsigned)((a.H + 4 * kFewThreads - 1) / (4 * kFewThreads)), (unsigned)((a.V + 63) / 64));
+  return timed("head_few_dw", [&] {
+    return with_type(a.dw_type, [&](auto t) {
+      return with_few(a.n, wide, [&](auto tokens, auto w) {
+        return launch_early(head_few_dw_kernel<decltype(tokens)::value, decltype(t), decltype(w)::value>, grid, kFewThreads, 0, st, a,
+                            (const float *)l.targets.live, (const float *)l.few_p, l.ldp);
+      });
+    });
+  });
+}
+cudaError_t launch_few(const HeadArgs &a, const Layout &l, int sms, const OpTimer &timed, cudaStream_t st) {
+  const bool wide = a.H % 4 == 0 && fits_pieces(a.w, a.w_stride, a.type, 4);
+  const unsigned tiles = (unsigned)((a.H + 4 * kFewThreads - 1) / (4 * kFewThreads));
+  if (a.V)
+    TRY(timed("head_few", [&] {
+      return with_few(a.n, wide, [&](auto tokens, auto w) {
+        constexpr int N = decltype(tokens)::value;
+        constexpr bool W = decltype(w)::value;
+        const int block = few_block(a, sms);
+        const dim3 grid((unsigned)((a.V + block - 1) / block));
+        auto go = [&](auto rows) {
+          constexpr int R = decltype(rows)::value;
+          if (a.grad) return launch_early(head_few_kernel<N, R, W, true>, grid, kFewThreads, 0, st, a, l.targets, l.part, l.picked, l.few_p, l.ldp);
+          return launch_early(head_few_kernel<N, R, W, false>, grid, kFewThreads, 0, st, a, l.targets, l.part, l.picked, l.few_p, l.ldp);
+        };
+        return block == few_rows(N, true) * kFewWarps ? go(Int<few_rows(N, true)>{}) : go(Int<few_rows(N, false)>{});
+      });
+    }));
+  if (a.dx) {
+    const int64_t ranges = few_ranges(a, sms), rows = (a.V + ranges - 1) / ranges;
+    TRY(timed("head_few_dx", [&] {
+      return with_few(a.n, wide, [&](auto tokens, auto w) {
+        return launch_early(head_few_dx_kernel<decltype(tokens)::value, decltype(w)::value>, dim3(tiles, (unsigned)ranges), kFewThreads, 0, st, a,
+                            (const float *)l.few_p, l.ldp, l.dx_sum, rows);
+      });
+    }));
+    TRY(timed("head_few_dx", [&] {
+      return launch_early(head_few_dx_join_kernel, dim3((unsigned)std::min<int64_t>((a.n * a.H + 255) / 256, 8 * sms)), 256, 0, st, a, (const float *)l.dx_sum,
+                          (int)ranges);
+    }));
+  }
+  constexpr int64_t kMost = 65535 * 64;  // rows of a launch (a grid's second dimension)
+  for (int64_t v = 0; a.dw && v < a.V; v += kMost) {
+    HeadArgs b = a;
+    Layout m = l;
+    b.V = std::min(kMost, a.V - v);
+    b.dw = static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type);
+    m.few_p = l.few_p + v;
+    TRY(launch_few_dw(b, m, timed, st));
+  }
+  return cudaSuccess;
+}
+
 }  // namespace
 
 int64_t head_piece_bytes() { return kPieceBytes; }
@@ -1308,16 +1690,24 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   const Layout l = layout_of(a, sms);
   const bool f32 = a.type == ECHO_F32;
   TRY(timed("head_targets", [&] { return launch_early(head_targets_kernel, dim3(l.target_blocks), kTargetWarps * 32, 0, st, a, l.targets); }));
+  auto join = [&] {
+    return timed("head_join", [&] {
+      return launch_early(head_join_kernel, dim3((unsigned)std::min<int64_t>((a.n + 31) / 32, 2 * sms)), kJoinWarps * 32, 0, st, a, l.targets, l.part, l.chunks,
+                          l.picked);
+    });
+  };
+  if (few_tokens(a)) {
+    const cudaError_t e = launch_few(a, l, sms, timed, st);
+    return e != cudaSuccess || a.grad ? e : join();
+  }
   const bool exact_dw = a.grad && a.dw && a.dw_type == ECHO_F32;
+  HeadProduct g{};
   const Source sx = source(a.x, a.type, a.n, a.H, a.x_stride), sw = source(a.w, a.type, a.V, a.H, a.w_stride);
-  const bool sized_x = f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16), sized_w = f32 && a.V;
+  const bool sized_x = a.grad && (f32 || (l.pack_x_dw && exact_dw && a.type == ECHO_BF16)), sized_w = a.grad && f32;
   Sources s{};
   int count = 0;
-  // (rows that are not live do not count: padding may hold any number.  Forward, each row has its own.)
-  if (sized_x) {
-    Source &m = s.of[count++] = sx;
-    m.amax = l.amax_x, m.amax_rows = !a.grad, m.live = a.grad ? l.targets.live : nullptr;
-  }
+  // (rows that are not live do not count: padding may hold any number)
+  if (sized_x) s.of[count] = sx, s.of[count].live = l.targets.live, s.of[count++].amax = l.amax_x;
   if (sized_w) s.of[count] = sw, s.of[count++].amax = l.amax_w;
   if (count) TRY(timed("head_amax", [&] { return launch_amax(s, count, a.type, st); }));
   // (backward, the rows of tokens without gradients are zeros in fp32's planes, which both products read)
@@ -1328,13 +1718,22 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   count = 0;
   if (l.pack_x) pack(sx, l.x, a.grad && f32 ? l.targets.live : nullptr);
   if (l.pack_w && a.V) pack(sw, l.w, nullptr);
-  if (count) TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x.bf16, sms, st); }));
+  if (count && f32 && !a.grad) {  // (each row has its own scale)
+    s.of[0].amax = l.amax_x, s.of[1].amax = l.amax_w, s.of[1].down = true;
+    const bool wide = a.H % 8 == 0 && fits_pieces(a.x, s.of[0].stride, a.type, 8) && fits_pieces(a.w, s.of[1].stride, a.type, 8);
+    const dim3 grid((unsigned)std::min<int64_t>((std::max(a.n, a.V) + 7) / 8, 8 * sms), count);
+    TRY(timed("head_pack", [&] {
+      return wide ? launch_early(head_pack_rows_kernel<true>, grid, 256, 0, st, s) : launch_early(head_pack_rows_kernel<false>, grid, 256, 0, st, s);
+    }));
+    g.w_down = l.amax_w;
+  } else if (count) {
+    TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x.bf16, sms, st); }));
+  }
   // (a launch of its own: done by warps of the product that have nothing else to do, it held up the others
   // by more, 60 us instead of 22 for 2048 x 12288 in bf16)
   count = 0;
   if (l.pack_x_dw) pack(sx, l.x_dw, l.targets.live);
   if (count) TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x_dw.bf16, sms, st); }));
-  HeadProduct g{};
   g.wait = {a.status, a.wait_limit}, g.skip = a.skip;
   g.parts = l.parts, g.arrived = l.targets.arrived;
   g.n = a.n, g.K = a.K, g.alpha = a.scale / a.tau;
@@ -1348,9 +1747,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
       TRY(stage_map(&m.b[0], l.w, false));
       TRY(timed("head_logits", [&] { return launch_product<kStats>(m, g, sms, st); }));
     }
-    return timed("head_join", [&] {
-      return launch_early(head_join_kernel, dim3((unsigned)std::min<int64_t>((a.n + 31) / 32, 2 * sms)), kJoinWarps * 32, 0, st, a, l.targets, l.part, l.chunks, l.picked);
-    });
+    return join();
   }
 
   g.p_bf16 = l.p_bf16, g.p_half = l.p_half, g.p_scale = {l.targets.size_part, l.target_blocks, nullptr};

@@ -53,6 +53,15 @@ def test_rows_of_different_sizes(echo):
     tol = ((units * size + far).gather(1, labels[:, None])[:, 0] + 4 * U * want.abs()) * 2.0 ** -38
     _close(target, want, tol)
     assert torch.isfinite(loss).all() and float(lse[n]) == pytest.approx(math.log(v), rel=1e-6)
+    # and rows of the weight
+    by = 2.0 ** torch.linspace(-60, 40, v, device="cuda").round()
+    big = w * by[:, None]
+    target = echo.cross_entropy(x, big, labels[:n], scale=2.0 ** -38)[2]
+    X, W = x.double(), big.double()
+    want = (X @ W.T).gather(1, labels[:n, None])[:, 0] * 2.0 ** -38
+    far = 2.0 ** -37 * (X.abs().amax(1, keepdim=True) * W.abs().sum(1)[None] + W.abs().amax(1)[None] * X.abs().sum(1)[:, None])
+    tol = ((units * (X.abs() @ W.abs().T) + far).gather(1, labels[:n, None])[:, 0] * 2.0 ** -38 + 4 * U * want.abs())
+    _close(target, want, tol)
 
 
 @pytest.mark.parametrize("scale", [-0.5, 0.0])
@@ -203,3 +212,42 @@ def test_teacher_without_weight(echo):
     t[3] = 0
     dx, dw = echo.distill_grad(g, x, w, ids, t, lse)
     assert torch.isfinite(dx).all() and torch.isfinite(dw).all() and not dx[1:].any()
+
+
+@pytest.mark.parametrize("n", [2, 7, 8, 9, 16, 17])
+@pytest.mark.parametrize("h,left", [(516, 0), (517, 0), (1030, 3), (2052, 4)])
+def test_few_tokens_in_full_precision(echo, n, h, left):
+    """Up to 16 fp32 tokens take kernels of their own; one more does not.  Sums of up to 20 terms a lane and a tree: within
+    the bounds of the others."""
+    v, v0 = 333 if n != 7 else 40000, 11  # (many rows: more of them a block)
+    x = _randn((n, h), 30)
+    w = _randn((v, h + 8), 31, F32, 2.0 / math.sqrt(h))[:, left:left + h]
+    labels, dloss = _randint(-1, v0 + v + 20, (n,), 32), _randn((n,), 33)
+    lse = _check_ce(echo, x, w, labels, v0, 0.75)
+    ids, logits = _teacher(n, 12, v, v0, F32, 34)
+    ids[0, :3] = v0 + 5
+    q, _, eq = _teacher_ref(ids, logits, 2.0)
+    loss, lse2, cross = echo.distill(x, w, ids, logits, temperature=2.0, vocab_start=v0)
+    ref = Ref(x, w, 1.0, 2.0)
+    mine = (ids >= v0) & (ids < v0 + v)
+    row = torch.where(mine, ids - v0, 0)
+    zk, ek = torch.where(mine, ref.z.gather(1, row), 0.0), torch.where(mine, ref.ez.gather(1, row), 0.0)
+    _close(lse2, ref.lse, ref.elast)
+    _close(cross, (q * zk).sum(1), (q * ek + eq * zk.abs()).sum(1) + 20 * U * (q * zk).abs().sum(1))
+    for dw_type in (F32, BF16):
+        up = dloss.double()[:, None] * 2.0
+        a, b, ta, tb = ref.grads((up * q).sum(1), (up * q).abs().sum(1), ref.targets(ids, up * q, v0), lse2.double(), 1.0, dw_type)
+        eP = ref.targets(ids, (up * eq).abs(), v0) + ((up * eq).abs().sum(1) + 16 * U * (up * q).abs().sum(1))[:, None] * torch.exp(ref.z - lse2.double()[:, None])
+        old = _randn((v, h + 8), 35, dw_type)
+        out = old.clone()
+        dx, dw = echo.distill_grad(dloss, x, w, ids, logits, lse2, temperature=2.0, vocab_start=v0, dweight=out[:, left:left + h], accumulate=True)
+        _close(dx, a, ta + eP @ ref.W.abs())
+        total = b + old[:, left:left + h].double()
+        _close(dw, total, tb + eP.T @ ref.X.abs() + 2 * U * total.abs())
+        assert torch.equal(out[:, :left], old[:, :left]) and torch.equal(out[:, left + h:], old[:, left + h:])
+    y, m = x.clone(), labels.clone()
+    m[0] = -1
+    clean = echo.cross_entropy_grad(dloss, y, w, m, lse, scale=0.75, vocab_start=v0)
+    y[0] = math.nan
+    got = echo.cross_entropy_grad(dloss, y, w, m, lse, scale=0.75, vocab_start=v0)
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1]) and not got[0][0].any()
