@@ -430,11 +430,7 @@ struct Job {
   int tiles_n;
   int64_t tiles;
   Scale scale_a, scale_b;
-  // D, times 2^-(both exponents), plus what `out` holds
-  void *out;
-  int64_t out_stride;
-  int type, add;
-  int by_engine;    // the TMA engine writes (or adds, in fp32) it
+  int type, add;    // D, times 2^-(both exponents), is written as that type, or added
 };
 // Who computes what, of two products whose tiles take steps0 and steps1 stages.
 //   - Of the first one `whole` tiles, each in `split` parts of (almost) equal length along its sum, a
@@ -527,8 +523,8 @@ __device__ __forceinline__ void add_slot(const CUtensorMap *map, const unsigned 
 }
 
 // 32 rows of 64 elements out, by a warp: lane r has those of row row0 + r in v, from column c.
-// By the copy engine: a 16-byte aligned matrix that is written, or an fp32 one that is added to
-// (each element by one addition, so that the result has one order).
+// By the copy engine, which writes it, or adds it to an fp32 matrix (each element by one addition, so
+// that the result has one order).
 template <typename T>
 __device__ __forceinline__ void engine_out(const Job &j, const CUtensorMap *map, int row0, int c, const float *v, Slots &slots) {
   constexpr int kCols = 128 / sizeof(T), kPiece = 16 / sizeof(T);
@@ -545,39 +541,6 @@ __device__ __forceinline__ void engine_out(const Job &j, const CUtensorMap *map,
     }
   }
 }
-// By the warp, 32 elements of a row at a time.
-template <typename T>
-__device__ __forceinline__ void lanes_out(const Job &j, int row0, int c, const float *v, Slots &slots) {
-  const int lane = slots.lane;
-  float *f = reinterpret_cast<float *>(slots.all());
-#pragma unroll
-  for (int i = 0; i < 32; ++i) f[lane * 32 + (i ^ lane)] = v[i];
-  __syncwarp();
-  if (c + lane < j.N) {
-    T *o = static_cast<T *>(j.out) + (int64_t)row0 * j.out_stride + c + lane;
-    const int rows = min(32, j.M - row0);
-#pragma unroll 1
-    for (int r0 = 0; r0 < rows; r0 += 16) {
-      float x[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = j.add && r0 + r < rows ? to_f(o[(int64_t)(r0 + r) * j.out_stride]) : 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (r0 + r < rows) o[(int64_t)(r0 + r) * j.out_stride] = from_f<T>(f[(r0 + r) * 32 + (lane ^ (r0 + r))] + x[r]);
-    }
-  }
-  __syncwarp();
-}
-template <typename T>
-__device__ __forceinline__ void block_out(const Job &j, const CUtensorMap *map, int row0, int c, const float *v, Slots &slots) {
-  if (j.by_engine) {
-    engine_out<T>(j, map, row0, c, v, slots);
-  } else {
-    lanes_out<T>(j, row0, c, v, slots);
-    lanes_out<T>(j, row0, c + 32, v + 32, slots);
-  }
-}
-
 // What a pair of blocks does, one after the other: stages k0 to k1 of a tile's sum, which is one of
 // several parts of it or all.
 struct Share {
@@ -1029,9 +992,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 64; ++e) v[e] = v[e] * f1 * f2;
           const CUtensorMap *map = which ? &out1 : &out0;
-          if (j.type == ECHO_F32) block_out<float>(j, map, row0, c, v, slots);
-          else if (j.type == ECHO_BF16) block_out<__nv_bfloat16>(j, map, row0, c, v, slots);
-          else block_out<__half>(j, map, row0, c, v, slots);
+          if (j.type == ECHO_F32) engine_out<float>(j, map, row0, c, v, slots);
+          else if (j.type == ECHO_BF16) engine_out<__nv_bfloat16>(j, map, row0, c, v, slots);
+          else engine_out<__half>(j, map, row0, c, v, slots);
         }
 #pragma unroll
         for (int e = 0; e < 64; ++e) acc[e] = acc[e + 64];
@@ -1049,13 +1012,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-// dx from its sum over pieces.
-template <typename T>
-__global__ void __launch_bounds__(256) head_round_kernel(const float *from, int64_t ld, int64_t rows, int64_t cols, T *to, int64_t stride) {
+// A result from its fp32 sums, written or added, in pieces of W elements, four of a thread on their way.
+// Bound by the bytes.
+template <typename T, int W>
+__global__ void __launch_bounds__(256) head_round_kernel(const float *from, int64_t ld, int64_t rows, int64_t cols, T *to, int64_t stride, int add) {
   kernel_begin();
   next_may_start();
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256)
-    to[i / cols * stride + i % cols] = from_f<T>(from[i / cols * ld + i % cols]);
+  const uint32_t pieces = (uint32_t)(cols / W);
+  const int64_t all = rows * pieces;
+  constexpr int kFlight = 4;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 * kFlight + threadIdx.x; i0 < all; i0 += (int64_t)gridDim.x * 256 * kFlight) {
+    float v[kFlight][W];
+    Pack<T, W> old[kFlight];
+    T *at[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const int64_t i = i0 + k * 256;
+      at[k] = nullptr;
+      if (i >= all) continue;
+      const int64_t r = all >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), c = (i - r * pieces) * W;
+      at[k] = to + r * stride + c;
+      load_piece<W>(from + r * ld + c, v[k]);
+      if (add) old[k] = *reinterpret_cast<const Pack<T, W> *>(at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      if (!at[k]) continue;
+      if (add) {
+        float x[W];
+        unpack<T, W>(old[k], x);
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[k][e] += x[e];
+      }
+      store_piece<W>(at[k], v[k]);
+    }
+  }
 }
 
 // -- the end of the forward pass -------------------------------------------------------------------
@@ -1348,6 +1339,13 @@ struct Carver {
 bool readable(const void *p, int64_t rows, int64_t cols, int64_t stride, int type) {
   return type != ECHO_F32 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride % 8 == 0 && stride >= cols && stride < (int64_t)1 << 38));
 }
+// Whether the copy engine can write a result: rows of 16-byte pieces at 16-byte addresses; sums of 16-bit
+// matrices are rounded once, so it does not add to those.  Other results go to fp32 scratch, and from there
+// by a kernel of their own.
+bool writable(const void *p, int64_t rows, int64_t cols, int64_t stride, int type, bool add) {
+  const int size = type_bytes(type);
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride * size % 16 == 0 && stride < (int64_t)1 << 37)) && !(add && type != ECHO_F32);
+}
 Operand in_place(const void *p, int64_t rows, int64_t cols, int64_t stride, int type) {
   return {p, rows, cols, rows <= 1 ? padded(cols) : stride, 0, 1, type == ECHO_BF16, {}};
 }
@@ -1374,7 +1372,8 @@ struct Layout {
   uint16_t *P;
   float *few_p;       // few tokens: P in fp32
   float *dx_sum;      // fp32, where dx is added up over pieces (few tokens: its parts)
-  int64_t dx_ld;
+  float *dw_sum;      // fp32, of a piece, where dW cannot be written at once
+  int64_t sum_ld;
   size_t bytes;
 };
 
@@ -1451,14 +1450,16 @@ Layout layout_of(const HeadArgs &a, int sms) {
     } else {
       l.x_dw = l.x;
     }
-    const int64_t row_bytes = std::max<int64_t>(1, a.n) * 2 * (l.p_bf16 + l.p_half);
+    const bool dw_sum = a.dw && !writable(a.dw, a.V, a.H, a.dw_stride, a.dw_type, a.accumulate);
+    l.sum_ld = padded(a.H);
+    const int64_t row_bytes = std::max<int64_t>(1, a.n) * 2 * (l.p_bf16 + l.p_half) + (dw_sum ? 4 * l.sum_ld : 0);
     const int64_t columns = std::max<int64_t>(kTile, a.piece_bytes / row_bytes / kTile * kTile);
     const int64_t pieces = (a.V + columns - 1) / columns;  // of equal size
     l.piece = pieces <= 1 ? a.V : ((a.V + pieces - 1) / pieces + kTile - 1) / kTile * kTile;
     l.ldp = padded(l.piece);
     l.P = c.take<uint16_t>((l.p_bf16 + l.p_half) * a.n * l.ldp);
-    l.dx_ld = padded(a.H);
-    if (a.dx && l.piece < a.V) l.dx_sum = c.take<float>(a.n * l.dx_ld);
+    if (a.dx && (l.piece < a.V || !writable(a.dx, a.n, a.H, a.dx_stride, a.type, false))) l.dx_sum = c.take<float>(a.n * l.sum_ld);
+    if (dw_sum) l.dw_sum = c.take<float>(l.piece * l.sum_ld);
   }
   l.bytes = c.at;
   return l;
@@ -1481,24 +1482,28 @@ cudaError_t stage_map(CUtensorMap *map, const Operand &o, bool mn) {
   return box_map(map, o.p, o.rows, o.cols, o.ld, o.plane, o.planes, mn ? kBK : kHalf, kBK, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// Where a product's result goes: by the copy engine where its rows are 16-byte ones at 16-byte
-// addresses, but for sums of 16-bit matrices, which are rounded once.
 cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type, bool add) {
   const int size = type_bytes(type);
   if (j.M <= 1) stride = (j.N + 7) / 8 * 8;
-  j.out = out, j.out_stride = stride, j.type = type, j.add = add;
-  j.by_engine = reinterpret_cast<uintptr_t>(out) % 16 == 0 && stride * size % 16 == 0 && stride < (int64_t)1 << 37 && !(add && type != ECHO_F32);
-  if (!j.by_engine) return cudaSuccess;
+  j.type = type, j.add = add;
   return box_map(map, out, j.M, j.N, stride, 0, 1, 32, 128 / size, CU_TENSOR_MAP_SWIZZLE_128B, size,
                  type == ECHO_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16);
 }
 
-// Stages of 64 columns that are summed with truncation.  Taking a set out of tensor memory keeps the
-// tensor core from it for 256 clocks, half a stage: results of 16 bits take 16 stages, of 32 bits eight
-// (2048 tokens of 12288 columns: logits 9.1e-7 off with 16, 4.2e-7 with eight, 2.3e-7 with four), and
-// fp32 matrices, whose stages are summed three times over, four (1003 tokens of 517: 2.5e-6 with 16,
-// 5.9e-7 with four).
-int set_of(bool f32_matrices, bool f32_result) { return f32_matrices ? 4 : f32_result ? 8 : 16; }
+// Stages of 64 columns that are summed with truncation: the result is off by about n 2^-25 of its usual size
+// for n additions, four a stage.  Taking a set out of tensor memory keeps the tensor core from it for 256
+// clocks, half a stage.  So results of 16 bits take 16 stages, those of 32 bits eight (2048 tokens of 12288
+// columns: logits 9.1e-7 off with 16, 4.2e-7 with eight; 300 us with four instead of 275 for 51200 rows).
+// P for an fp32 dW takes five, as a logit's error is as large a part of it (3% more time).  Short sums, and up
+// to 256 tokens, which do not wait for the tensor cores, take three: among few numbers one near zero, off by
+// the usual, counts (48 tokens: 1.7e-5 with eight, 5e-6 in fp32).  fp32 matrices, whose stages are summed three
+// times over, take three, or two (1003 tokens of 517: 2.5e-6 off with 16, 8.9e-7 with four).
+enum { kResult16, kResult32, kExactP };
+int set_of(bool f32_matrices, int result, int64_t stages, int64_t tokens) {
+  const bool few = tokens <= kTile;
+  if (f32_matrices) return few ? 2 : 3;
+  return result == kResult16 ? 16 : few || (result == kResult32 && stages <= 12) ? 3 : result == kExactP ? 5 : 8;
+}
 
 // The first two sets of a tile are longer: they are summed while the tile before is finished, or its parts
 // are joined.  A sum of n stages is off by n as a rule, and so is a tile by the mean of its sets' lengths,
@@ -1506,7 +1511,7 @@ int set_of(bool f32_matrices, bool f32_result) { return f32_matrices ? 4 : f32_r
 int lead_of(int set, int64_t stages) { return (int)(0.5 * set + std::sqrt(0.25 * set * set + 0.1875 * set * (double)stages)); }
 
 // D = A B^T; mn: the operand is held transposed
-Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, int set) {
+Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, bool f32_matrices, int result, int64_t tokens) {
   Job j{};
   j.M = (int)(a_mn ? a.cols : a.rows);
   j.N = (int)(b_mn ? b.cols : b.rows);
@@ -1514,7 +1519,8 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, int set) {
   for (int p = 0; p < a.planes; ++p)
     for (int q = 0; q < b.planes; ++q)
       if (p + q < 2) j.plane_a[j.pairs] = p, j.plane_b[j.pairs++] = q;
-  j.set = set, j.lead = lead_of(set, (int64_t)j.steps * j.pairs);
+  const int64_t stages = (int64_t)j.steps * j.pairs;
+  j.set = set_of(f32_matrices, result, stages, tokens), j.lead = lead_of(j.set, stages);
   j.instr = instruction(kTile, a_mn, b_mn, a.bf16);
   j.tiles_n = (j.N + kTile - 1) / kTile;
   j.tiles = (int64_t)((j.M + kTile - 1) / kTile) * j.tiles_n;
@@ -1609,6 +1615,20 @@ cudaError_t launch_pack(const Sources &s, int count, int type, bool bf16, int sm
     if constexpr (std::is_same_v<T, float>) return go(__half{}, Int<2>{});
     else if constexpr (std::is_same_v<T, __half>) return go(__half{}, Int<1>{});
     else return bf16 ? go(__nv_bfloat16{}, Int<1>{}) : go(__half{}, Int<1>{});
+  });
+}
+
+cudaError_t launch_round(const float *from, int64_t ld, int64_t rows, int64_t cols, void *to, int64_t stride, int type, bool add, int sms, cudaStream_t st) {
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    auto go = [&](auto w) {
+      constexpr int W = decltype(w)::value;
+      const int64_t blocks = std::min<int64_t>((rows * (cols / W) + 1023) / 1024, sms * 8);
+      return launch_early(head_round_kernel<T, W>, dim3((unsigned)blocks), 256, 0, st, from, ld, rows, cols, static_cast<T *>(to), stride, (int)add);
+    };
+    constexpr int N = 16 / sizeof(T);
+    if (cols % N == 0 && fits_pieces(to, stride, type, N)) return go(Int<N>{});
+    return cols % 2 == 0 && fits_pieces(to, stride, type, 2) ? go(Int<2>{}) : go(Int<1>{});
   });
 }
 
@@ -1742,7 +1762,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   if (!a.grad) {
     g.part = l.part, g.picked = l.picked;
     if (a.V) {
-      g.job[0] = job_of(l.x, false, l.w, false, set_of(f32, true));
+      g.job[0] = job_of(l.x, false, l.w, false, f32, kResult32, a.n);
       TRY(stage_map(&m.a[0], l.x, false));
       TRY(stage_map(&m.b[0], l.w, false));
       TRY(timed("head_logits", [&] { return launch_product<kStats>(m, g, sms, st); }));
@@ -1751,6 +1771,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   }
 
   g.p_bf16 = l.p_bf16, g.p_half = l.p_half, g.p_scale = {l.targets.size_part, l.target_blocks, nullptr};
+  auto piece_of_dw = [&](int64_t v) -> void * { return static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type); };
   for (int64_t v = 0; v < a.V; v += l.piece) {
     const int64_t rows = std::min(l.piece, a.V - v);
     Operand w = l.w;
@@ -1767,7 +1788,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     };
     HeadProduct h = g;
     h.v_begin = (int)v;
-    h.job[0] = job_of(l.x, false, w, false, set_of(f32, exact_dw));
+    h.job[0] = job_of(l.x, false, w, false, f32, exact_dw ? kExactP : kResult16, a.n);
     TRY(stage_map(&m.a[0], l.x, false));
     TRY(stage_map(&m.b[0], w, false));
     TRY(box_map(&m.out[0], l.P, a.n, rows, l.ldp, plane, p.planes, 32, 64, CU_TENSOR_MAP_SWIZZLE_128B));
@@ -1776,29 +1797,25 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
     HeadProduct d = g;
     if (a.dx) {
       const Operand q = planes(a.type == ECHO_BF16, f32 ? 2 : 1);
-      Job &j = d.job[0] = job_of(q, false, w, true, set_of(f32, false));
+      Job &j = d.job[0] = job_of(q, false, w, true, f32, kResult16, a.n);
       TRY(stage_map(&m.a[0], q, false));
       TRY(stage_map(&m.b[0], w, true));
-      if (l.dx_sum) TRY(out_to(j, &m.out[0], l.dx_sum, l.dx_ld, ECHO_F32, v > 0));
+      if (l.dx_sum) TRY(out_to(j, &m.out[0], l.dx_sum, l.sum_ld, ECHO_F32, v > 0));
       else TRY(out_to(j, &m.out[0], a.dx, a.dx_stride, a.type, false));
     }
     if (a.dw) {
       const Operand q = planes(l.x_dw.bf16, f32 || exact_dw ? 2 : 1);
-      Job &j = d.job[1] = job_of(q, true, l.x_dw, true, set_of(f32, exact_dw));
+      Job &j = d.job[1] = job_of(q, true, l.x_dw, true, f32, exact_dw ? kResult32 : kResult16, a.n);
       TRY(stage_map(&m.a[1], q, true));
       TRY(stage_map(&m.b[1], l.x_dw, true));
-      TRY(out_to(j, &m.out[1], static_cast<char *>(a.dw) + v * a.dw_stride * type_bytes(a.dw_type), a.dw_stride, a.dw_type, a.accumulate));
+      if (l.dw_sum) TRY(out_to(j, &m.out[1], l.dw_sum, l.sum_ld, ECHO_F32, false));
+      else TRY(out_to(j, &m.out[1], piece_of_dw(v), a.dw_stride, a.dw_type, a.accumulate));
     }
     TRY(timed("head_grads", [&] { return launch_product<kOut>(m, d, sms, st); }));
+    if (l.dw_sum) TRY(timed("head_round", [&] { return launch_round(l.dw_sum, l.sum_ld, rows, a.H, piece_of_dw(v), a.dw_stride, a.dw_type, a.accumulate, sms, st); }));
   }
   if (!l.dx_sum) return cudaSuccess;
-  return timed("head_round", [&] {
-    return with_type(a.type, [&](auto t) {
-      using T = decltype(t);
-      const int64_t blocks = std::min<int64_t>((a.n * a.H + 255) / 256, sms * 8);
-      return launch_early(head_round_kernel<T>, dim3((unsigned)blocks), 256, 0, st, (const float *)l.dx_sum, l.dx_ld, a.n, a.H, static_cast<T *>(a.dx), a.dx_stride);
-    });
-  });
+  return timed("head_round", [&] { return launch_round(l.dx_sum, l.sum_ld, a.n, a.H, a.dx, a.dx_stride, a.type, false, sms, st); });
 }
 
 }  // namespace echo
