@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 //     A stage takes 660 to 700 clocks, of which the products are 512: operands come from L2 at 64 bytes
 //     a clock and SM, and a copy of half of them (other results wrong) saved 5% only.
 //   - logits, 2048 columns, 51200 rows, 64 targets a token: 262 us; 22 rounds where 21.05 would do.
-//   - P, 2048 columns, 25600 rows, three planes: 160 us, 10000 clocks a tile to finish beside the 20000
+//   - P, 2048 columns, 25600 rows, three planes: 165 us, 10000 clocks a tile to finish beside the 20000
 //     of its products, which go slower meanwhile.
 //   - dx and dW, 25600 x 2048, fp32 dW (3.2e11 operations on 16-bit numbers twice for dW): 377 us; with a
 //     16-bit dW 6400 x 12288: 359 us, 1.80 PFLOP/s.
@@ -818,7 +818,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int sets = after > 0 ? 2 + (after + j.set - 1) / j.set : steps > j.lead ? 2 : 1;
       for (int set = 0; set < sets; ++set) {
         const int b = (int)(n & 1);
-        ok = bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait);
+        ok = __all_sync(0xFFFFFFFFu, bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait));  // (a warp gives up as one)
         if (!ok) break;
         ++n;
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -877,7 +877,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int c = 0; c < kParts; ++c) {
             fetch(c == kParts - 1 ? q + 1 : q, (c + 1) % kParts);
-            ok = ok && bar_wait(join + 8 * (c & 1), c >> 1, abort, a.wait);  // (each has two phases a part)
+            ok = ok && __all_sync(0xFFFFFFFFu, bar_wait(join + 8 * (c & 1), c >> 1, abort, a.wait));  // (each has two phases a part)
             if (ok) {
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
