@@ -230,38 +230,46 @@ __global__ void __launch_bounds__(256) head_pack_rows_kernel(Sources s) {
   __half *to = static_cast<__half *>(m.to);
   for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < m.rows; r += (int64_t)gridDim.x * 8) {
     const float *x = static_cast<const float *>(m.p) + r * m.stride;
-    auto load = [&](int64_t piece, float (&v)[W]) {
-      if (WIDE) {
-        load_piece<W>(x + piece * W, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < W; ++e) v[e] = piece * W + e < m.cols ? x[piece * W + e] : 0.f;
-      }
-    };
     float most = 0.f;
+    if (WIDE) {
 #pragma unroll 4
-    for (int64_t i = lane; i < pieces; i += 32) {
-      float v[W];
-      load(i, v);
+      for (int64_t i = lane; i < pieces; i += 32) {
+        float v[W];
+        load_piece<W>(x + i * W, v);
 #pragma unroll
-      for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[e]));
+        for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[e]));
+      }
+    } else {
+#pragma unroll 8
+      for (int64_t c = lane; c < m.cols; c += 32) most = fmaxf(most, finite_size(x[c]));
     }
     most = warp_max(most);
     const int up = exponent_of(most);
     if (lane == 0) m.amax[r] = m.down ? ldexpf(1.f, -up) : most;
     const float by = ldexpf(1.f, up);
+    __half *high = to + r * m.ld, *low = high + m.plane;
+    if (WIDE) {
 #pragma unroll 4
-    for (int64_t i = lane; i < pieces; i += 32) {
-      float v[W], back[W];
-      load(i, v);
+      for (int64_t i = lane; i < pieces; i += 32) {
+        float v[W], back[W];
+        load_piece<W>(x + i * W, v);
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[e] *= by;
-      const Pack<__half, W> high = pack<__half, W>(v);
-      unpack<__half, W>(high, back);
+        for (int e = 0; e < W; ++e) v[e] *= by;
+        const Pack<__half, W> h = pack<__half, W>(v);
+        unpack<__half, W>(h, back);
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[e] -= back[e];
-      *reinterpret_cast<Pack<__half, W> *>(to + r * m.ld + i * W) = high;
-      *reinterpret_cast<Pack<__half, W> *>(to + m.plane + r * m.ld + i * W) = pack<__half, W>(v);
+        for (int e = 0; e < W; ++e) v[e] -= back[e];
+        *reinterpret_cast<Pack<__half, W> *>(high + i * W) = h;
+        store_piece<W>(low + i * W, v);
+      }
+    } else {  // (an element a lane: rows at any address are read and written in runs of 32)
+#pragma unroll 8
+      for (int64_t c = lane; c < m.cols; c += 32) {
+        const float v = x[c] * by;
+        const __half h = __float2half_rn(v);
+        high[c] = h;
+        low[c] = __float2half_rn(v - __half2float(h));
+      }
     }
   }
 }
