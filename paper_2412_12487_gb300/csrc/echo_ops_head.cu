@@ -216,55 +216,81 @@ __global__ void __launch_bounds__(256) head_pack_kernel(Sources s) {
   }
 }
 
-// fp32 rows as two planes of fp16 each, a warp a row: scaled by its own largest finite element, which it
-// leaves (x), or by the power of two that takes it back (the weight's `down`).  Bound by the bytes: a row's
-// second pass finds it in L1 or L2.
-template <bool WIDE>
+// fp32 rows as two planes of fp16 each: a row is scaled by its own largest finite element, which is left
+// (x), or by the power of two that takes it back (the weight's `down`).  A warp takes a short row, a block a
+// longer one: its pieces stay in registers (HELD of a lane; further ones are read again, from L2).  With a warp
+// a row of any length the rows on their way are more than L2 holds, and were read twice from memory: 51200 x
+// 4096, 1.7e9 bytes, 365 us instead of 280.
+template <bool WIDE, int WARPS, int HELD>
 __global__ void __launch_bounds__(256) head_pack_rows_kernel(Sources s) {
+  __shared__ float of_warps[2][8];
   kernel_begin();
   next_may_start();
-  constexpr int W = 8;
+  constexpr int W = 8, kLanes = 32 * WARPS, kRows = 8 / WARPS;
   const Source &m = s.of[blockIdx.y];
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x % kLanes, warp = threadIdx.x >> 5;
   const int64_t pieces = (m.cols + W - 1) / W;
   __half *to = static_cast<__half *>(m.to);
-  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < m.rows; r += (int64_t)gridDim.x * 8) {
+  int turn = 0;
+  for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; r < m.rows; r += (int64_t)gridDim.x * kRows, turn ^= 1) {
     const float *x = static_cast<const float *>(m.p) + r * m.stride;
-    float most = 0.f;
+    float most = 0.f, held[HELD][W];
+    auto largest_of = [&](const float (&v)[W]) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[e]));
+    };
     if (WIDE) {
-#pragma unroll 4
-      for (int64_t i = lane; i < pieces; i += 32) {
+#pragma unroll
+      for (int k = 0; k < HELD; ++k)
+        if (lane + k * kLanes < pieces) load_piece<W>(x + (lane + k * kLanes) * W, held[k]);
+#pragma unroll
+      for (int k = 0; k < HELD; ++k)
+        if (lane + k * kLanes < pieces) largest_of(held[k]);
+#pragma unroll 2
+      for (int64_t i = lane + HELD * kLanes; i < pieces; i += kLanes) {
         float v[W];
         load_piece<W>(x + i * W, v);
-#pragma unroll
-        for (int e = 0; e < W; ++e) most = fmaxf(most, finite_size(v[e]));
+        largest_of(v);
       }
     } else {
 #pragma unroll 8
-      for (int64_t c = lane; c < m.cols; c += 32) most = fmaxf(most, finite_size(x[c]));
+      for (int64_t c = lane; c < m.cols; c += kLanes) most = fmaxf(most, finite_size(x[c]));
     }
     most = warp_max(most);
+    if (WARPS > 1) {  // (by turns, so that one wait a row is enough)
+      if (threadIdx.x % 32 == 0) of_warps[turn][warp] = most;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) most = fmaxf(most, of_warps[turn][k]);
+    }
     const int up = exponent_of(most);
     if (lane == 0) m.amax[r] = m.down ? ldexpf(1.f, -up) : most;
     const float by = ldexpf(1.f, up);
     __half *high = to + r * m.ld, *low = high + m.plane;
+    auto leave = [&](int64_t i, float (&v)[W]) {
+      float back[W];
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] *= by;
+      const Pack<__half, W> h = pack<__half, W>(v);
+      unpack<__half, W>(h, back);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] -= back[e];
+      *reinterpret_cast<Pack<__half, W> *>(high + i * W) = h;
+      store_piece<W>(low + i * W, v);
+    };
     if (WIDE) {
-#pragma unroll 4
-      for (int64_t i = lane; i < pieces; i += 32) {
-        float v[W], back[W];
+#pragma unroll
+      for (int k = 0; k < HELD; ++k)
+        if (lane + k * kLanes < pieces) leave(lane + k * kLanes, held[k]);
+#pragma unroll 2
+      for (int64_t i = lane + HELD * kLanes; i < pieces; i += kLanes) {
+        float v[W];
         load_piece<W>(x + i * W, v);
-#pragma unroll
-        for (int e = 0; e < W; ++e) v[e] *= by;
-        const Pack<__half, W> h = pack<__half, W>(v);
-        unpack<__half, W>(h, back);
-#pragma unroll
-        for (int e = 0; e < W; ++e) v[e] -= back[e];
-        *reinterpret_cast<Pack<__half, W> *>(high + i * W) = h;
-        store_piece<W>(low + i * W, v);
+        leave(i, v);
       }
     } else {  // (an element a lane: rows at any address are read and written in runs of 32)
 #pragma unroll 8
-      for (int64_t c = lane; c < m.cols; c += 32) {
+      for (int64_t c = lane; c < m.cols; c += kLanes) {
         const float v = x[c] * by;
         const __half h = __float2half_rn(v);
         high[c] = h;
@@ -1113,7 +1139,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) head_join_kernel(HeadArgs a, 
 
 // -- few tokens of fp32 matrices ---------------------------------------------------------------------
 // Planes of the weight are read, written and read again before the tensor cores have them, for tiles of
-// 256 tokens: with 51200 x 4096 a call takes 559 us forward and 1388 backward from 17 tokens on, whose
+// 256 tokens: with 51200 x 4096 a call takes 485 us forward and 1060 backward from 17 tokens on, whose
 // products alone would be 170.  Up to kFew tokens the products are made in fp32 from the weight as it is,
 // read once for the logits (149 us with one token, 206 with eight, 371 with 16; its 839 MB take 124) and
 // once for dx, and dW is written once (420, 535 and 880 us, of 371).  Above eight tokens their arithmetic
@@ -1544,19 +1570,27 @@ struct Maps {
 // Nothing is split where that saves nothing.  Two products have no pool: the first one's operands are
 // long, and are in L2 while its tiles are at the same place of their sums.
 double joining(int64_t parts) { return (3000. + 3000. * parts) / 560; }
+// A tile of few stages takes longer than they do: its results leave in the time of 10 stages in fp32, 6 in 16
+// bits, of which only the next tile's lead is hidden (32 tokens, 51200 x 4096, dx and dW: 736 us in fp32 where
+// the pairs that take tiles of dW early counted stages only, 368 so; bf16 551 and 200).
+double tile_of(const Job &j) {
+  const int stages = j.steps * j.pairs;
+  return stages + std::max(0., (j.type == ECHO_F32 ? 10. : 6.) - std::min(j.lead, stages));
+}
 Schedule plan(const Job *j, int pairs) {
   Schedule s{};
   const int64_t tiles = j[0].tiles;
   s.whole = tiles, s.tiles1 = j[1].tiles, s.split = 1;
   s.steps0 = j[0].steps * j[0].pairs, s.steps1 = j[1].steps * j[1].pairs;
+  const double tile1 = tile_of(j[1]);
   double least = 0;
   for (int64_t split = 1; split <= std::max<int64_t>(1, s.steps0 / 4) && (split == 1 || tiles * split <= 2 * pairs); ++split) {
     const int64_t n = tiles * split, extra = n % pairs;
     const double length = (double)((s.steps0 + split - 1) / split);
-    const int early = extra && s.tiles1 ? (int)std::min<double>(length / s.steps1 + 0.5, (double)(s.tiles1 / (pairs - extra))) : 0;
+    const int early = extra && s.tiles1 ? (int)std::min<double>(length / tile1 + 0.5, (double)(s.tiles1 / (pairs - extra))) : 0;
     const int64_t late = s.tiles1 - (extra ? early * (pairs - extra) : 0);
     const int64_t most = (late + pairs - 1) / pairs;  // (of a pair; the first ones have it)
-    const double clocks = std::max((double)(n / pairs + (extra > 0)) * length, (double)(n / pairs) * length + (double)early * s.steps1) + (double)most * s.steps1 +
+    const double clocks = std::max((double)(n / pairs + (extra > 0)) * length, (double)(n / pairs) * length + (double)early * tile1) + (double)most * tile1 +
                           (split > 1 ? joining(split) : 0);
     if (split == 1 || clocks < least) least = clocks, s.split = (int)split, s.early = early;
   }
@@ -1624,6 +1658,17 @@ cudaError_t launch_pack(const Sources &s, int count, int type, bool bf16, int sm
     else if constexpr (std::is_same_v<T, __half>) return go(__half{}, Int<1>{});
     else return bf16 ? go(__nv_bfloat16{}, Int<1>{}) : go(__half{}, Int<1>{});
   });
+}
+
+// Matrices of rows with a scale each; a lane holds two pieces of 8 columns at least where it can.
+cudaError_t launch_pack_rows(const Sources &s, int count, bool wide, int64_t cols, int64_t rows, int sms, cudaStream_t st) {
+  auto go = [&](auto kernel, int64_t rows_block) {
+    const dim3 grid((unsigned)std::min<int64_t>((rows + rows_block - 1) / rows_block, 8 * sms), count);
+    return launch_early(kernel, grid, 256, 0, st, s);
+  };
+  if (cols <= 1024) return wide ? go(head_pack_rows_kernel<true, 1, 4>, 8) : go(head_pack_rows_kernel<false, 1, 1>, 8);
+  if (!wide) return go(head_pack_rows_kernel<false, 8, 1>, 1);
+  return cols <= 4096 ? go(head_pack_rows_kernel<true, 8, 2>, 1) : go(head_pack_rows_kernel<true, 8, 6>, 1);
 }
 
 cudaError_t launch_round(const float *from, int64_t ld, int64_t rows, int64_t cols, void *to, int64_t stride, int type, bool add, int sms, cudaStream_t st) {
@@ -1749,10 +1794,7 @@ cudaError_t launch_head(const HeadArgs &a, int sms, const OpTimer &timed, cudaSt
   if (count && f32 && !a.grad) {  // (each row has its own scale)
     s.of[0].amax = l.amax_x, s.of[1].amax = l.amax_w, s.of[1].down = true;
     const bool wide = a.H % 8 == 0 && fits_pieces(a.x, s.of[0].stride, a.type, 8) && fits_pieces(a.w, s.of[1].stride, a.type, 8);
-    const dim3 grid((unsigned)std::min<int64_t>((std::max(a.n, a.V) + 7) / 8, 8 * sms), count);
-    TRY(timed("head_pack", [&] {
-      return wide ? launch_early(head_pack_rows_kernel<true>, grid, 256, 0, st, s) : launch_early(head_pack_rows_kernel<false>, grid, 256, 0, st, s);
-    }));
+    TRY(timed("head_pack", [&] { return launch_pack_rows(s, count, wide, a.H, std::max(a.n, a.V), sms, st); }));
     g.w_down = l.amax_w;
   } else if (count) {
     TRY(timed("head_pack", [&] { return launch_pack(s, count, a.type, l.x.bf16, sms, st); }));

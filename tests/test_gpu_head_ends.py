@@ -251,3 +251,39 @@ def test_few_tokens_in_full_precision(echo, n, h, left):
     y[0] = math.nan
     got = echo.cross_entropy_grad(dloss, y, w, m, lse, scale=0.75, vocab_start=v0)
     assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1]) and not got[0][0].any()
+
+
+@pytest.mark.parametrize("h", [1024, 1032, 1033, 4096, 4104, 12296])
+def test_long_rows_of_full_precision(echo, h):
+    """Rows that a warp, a block's registers, and neither can hold; more of them than blocks; each of its own size, which its
+    last column may set alone."""
+    n, v = 20, 2500
+    x, w = _randn((n, h), 40), _randn((v, h), 41, F32, 1.0 / math.sqrt(h))
+    x *= torch.pow(2.0, (torch.arange(n, device="cuda") % 5 - 2).float())[:, None]
+    w *= torch.pow(2.0, -(torch.arange(v, device="cuda") % 13).float())[:, None]
+    w[::3, -1] *= 64.0
+    x[1::4, -1] *= 64.0
+    labels = _randint(0, v, (n,), 42)
+    labels[4] = v - 1
+    first = echo.cross_entropy(x, w, labels)
+    _check_ce(echo, x, w, labels, 0, 1.0, first)
+    assert all(torch.equal(a, b) for a, b in zip(first, echo.cross_entropy(x, w, labels)))
+
+
+@pytest.mark.parametrize("dtype,dw_type", [(F32, F32), (BF16, F32), (BF16, BF16), (F16, F16)])
+@pytest.mark.parametrize("n,h,v", [(17, 512, 9000), (200, 1024, 5000)])
+def test_gradients_of_few_tokens_and_many_tiles(echo, dtype, dw_type, n, h, v):
+    """Tiles of dW of a few stages, taken early by the pairs that have less of dx."""
+    x, w = _case(n, h, v, 0, dtype, 43)
+    labels, dloss = _randint(-1, v, (n,), 44), _randn((n,), 45, F32, 0.1)
+    ref = Ref(x, w, 1.0)
+    lse = echo.cross_entropy(x, w, labels)[1]
+    up = torch.where(labels >= 0, dloss.double(), 0.0)
+    a, b, ta, tb = ref.grads(up, up.abs(), ref.targets(labels[:, None], up[:, None], 0), lse.double(), 1.0, dw_type)
+    old = _randn((v, h), 46, dw_type)
+    for accumulate in (False, True):
+        out = old.clone()
+        dx, dw = echo.cross_entropy_grad(dloss, x, w, labels, lse, dweight=out, accumulate=accumulate)
+        _close(dx, a, ta)
+        total = b + old.double() if accumulate else b
+        _close(dw, total, tb + 2 * U * total.abs())
