@@ -435,14 +435,14 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 // In each block one thread copies stages into a ring, a thread of the pair's first block issues the
 // products, and eight warps take the sums out of tensor memory, which holds two sets of them, add
 // them up, and finish the tile while the next one is summed.  What bounds it, at 2048 tokens:
-//   - logits, 12288 columns, 6400 rows, bf16: 187 us, 1.73 PFLOP/s, tensor pipe busy 74% of the time.
-//     A stage takes 660 to 700 clocks, of which the products are 512: operands come from L2 at 64 bytes
+//   - logits, 12288 columns, 6400 rows, bf16: 180 us, 1.79 PFLOP/s, tensor pipe busy 78% of the time.
+//     A stage takes 640 to 660 clocks, of which the products are 512: operands come from L2 at 64 bytes
 //     a clock and SM, and a copy of half of them (other results wrong) saved 5% only.
-//   - logits, 2048 columns, 51200 rows, 64 targets a token: 262 us; 22 rounds where 21.05 would do.
-//   - P, 2048 columns, 25600 rows, three planes: 165 us, 10000 clocks a tile to finish beside the 20000
+//   - logits, 2048 columns, 51200 rows, 64 targets a token: 247 us; 22 rounds where 21.05 would do.
+//   - P, 2048 columns, 25600 rows, three planes: 162 us, 10000 clocks a tile to finish beside the 20000
 //     of its products, which go slower meanwhile.
-//   - dx and dW, 25600 x 2048, fp32 dW (3.2e11 operations on 16-bit numbers twice for dW): 377 us; with a
-//     16-bit dW 6400 x 12288: 359 us, 1.80 PFLOP/s.
+//   - dx and dW, 25600 x 2048, fp32 dW (3.2e11 operations on 16-bit numbers twice for dW): 357 us; with a
+//     16-bit dW 6400 x 12288: 342 us, 1.88 PFLOP/s.
 // What counted: 32-bit counters and nothing looked up in a stage's way, which single threads take (a
 // stage of 64-bit counters and arguments read from memory: 20% slower); results through the copy engine
 // (1236 us for dx and dW with stores by lanes, 451 so); tiles split where rounds are not full, and joined
@@ -1527,7 +1527,7 @@ cudaError_t out_to(Job &j, CUtensorMap *map, void *out, int64_t stride, int type
 // Stages of 64 columns that are summed with truncation: the result is off by about n 2^-25 of its usual size
 // for n additions, four a stage.  Taking a set out of tensor memory keeps the tensor core from it for 256
 // clocks, half a stage.  So results of 16 bits take 16 stages, those of 32 bits eight (2048 tokens of 12288
-// columns: logits 9.1e-7 off with 16, 4.2e-7 with eight; 300 us with four instead of 275 for 51200 rows).
+// columns: logits 9.1e-7 off with 16, 4.2e-7 with eight; 290 us with four instead of 263 for 51200 rows).
 // P for an fp32 dW takes five, as a logit's error is as large a part of it (3% more time).  Short sums, and up
 // to 256 tokens, which do not wait for the tensor cores, take three: among few numbers one near zero, off by
 // the usual, counts (48 tokens: 1.7e-5 with eight, 5e-6 in fp32).  fp32 matrices, whose stages are summed three
