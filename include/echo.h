@@ -493,7 +493,8 @@ int echo_orthogonalize(echo_ctx *ctx, const echo_orthogonalize_desc *d);
  * Each of loss, lse and target may be NULL.  n_tokens and vocab_rows may be 0; hidden is 1
  * to 2^24, n_tokens and vocab_rows at most 2^30.  fp32 elements of more than 16 tokens, and
  * of the weight with them, count with 22 bits down to 2^-14 of the largest finite one of
- * their row, and with an error of 2^-37 of that below. */
+ * their row, and with an error of 2^-37 of that below; with fewer bits where that one is
+ * below 2^-112. */
 typedef struct {
   int64_t n_tokens, hidden, vocab_rows, vocab_start;
   const void *x;      /* [n_tokens][hidden]                                             */

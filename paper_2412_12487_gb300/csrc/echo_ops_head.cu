@@ -60,9 +60,10 @@ __device__ __forceinline__ float largest(Scale s) {
   for (int i = threadIdx.x & 31; i < s.parts; i += 32) m = fmaxf(m, s.part[i]);
   return warp_max(m);
 }
-__device__ __forceinline__ int exponent_of(float m) { return m > 0.f ? max(-110, min(110, 14 - ilogbf(m))) : 0; }
+// (-113 to 126: powers of two whose inverses are normal numbers too)
+__device__ __forceinline__ int exponent_of(float m) { return m > 0.f ? min(126, 14 - ilogbf(m)) : 0; }
 // By a warp, the same in all lanes: the largest element times 2^exponent is 2^14 to 2^15, if it is
-// within 2^-96 and 2^124.
+// 2^-112 at least (below that it has fewer digits).
 __device__ __forceinline__ int exponent(Scale s) { return exponent_of(largest(s)); }
 // The same for P, whose largest element becomes 2^15 itself: tokens have the same weight as a rule,
 // and 1 is what its targets then round to, not all of them up or down (that left dx 3.0e-3 off in bf16
@@ -816,7 +817,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
     for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
-    float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
+    const float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
     const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
     bool ok = true;
@@ -834,8 +835,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Cursor at;
       at.none();
       float coef = 0.f, shift = 0.f;
-      if (MODE == kStats && a.job[0].scale_a.rows)  // (a factor of each row)
-        alpha2 = ldexpf(a.alpha, down[0] - (in ? exponent_of(a.job[0].scale_a.rows[row]) : 0)) * kLog2e;
+      const int row_down = MODE == kStats && in && a.w_down ? -exponent_of(a.job[0].scale_a.rows[row]) : 0;  // (a power of two of each row)
       if (MODE != kOut && in) {
         at.start(a.idx + row * a.K, MODE == kGrad ? a.weight + row * a.K : nullptr, a.K, a.v_begin, c0);
         if (MODE == kGrad) {
@@ -928,12 +928,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
       }
       if constexpr (MODE == kStats) {
-        if (a.w_down)  // (fp32: a power of two of each row of the weight; the array is as long as the tiles)
+        if (a.w_down) {  // (fp32: a power of two of each row of the weight; the array is as long as the tiles)
+          // Half of the token's power, the weight's, the other half: the two powers may be far from one
+          // where their product is not, and sums (2^54 at most) meet neither end of fp32's range on the way.
+          const float r1 = ldexpf(1.f, row_down / 2), r2 = ldexpf(1.f, row_down - row_down / 2);
 #pragma unroll
           for (int e = 0; e < kHalf; e += 4) {
             const float4 f = *reinterpret_cast<const float4 *>(a.w_down + c0 + e);
+            acc[e] *= r1, acc[e + 1] *= r1, acc[e + 2] *= r1, acc[e + 3] *= r1;
             acc[e] *= f.x, acc[e + 1] *= f.y, acc[e + 2] *= f.z, acc[e + 3] *= f.w;
+            acc[e] *= r2, acc[e + 1] *= r2, acc[e + 2] *= r2, acc[e + 3] *= r2;
           }
+        }
         if (c0 + kHalf > j.N)
 #pragma unroll
           for (int part = 0; part < kParts; ++part)
