@@ -460,7 +460,7 @@ constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * kSlots * kSlotBytes
 struct Job {
   int M, N, steps;  // rows, columns; stages of a pair of planes
   int pairs, plane_a[3], plane_b[3];
-  int lead, set;    // stages that the tensor core adds up by itself: of the first two sets of a tile, of the others
+  int lead, lead_part, set;  // stages that the tensor core adds up by itself: of the first two sets of a tile, of a part of one, of the others
   uint32_t instr;
   int tiles_n;
   int64_t tiles;
@@ -772,12 +772,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int s = 0, b = 0;
       uint32_t phase = 0, sums_phase = 1;  // (of both sets alike: they take turns)
       bool ok = true;
-      auto multiply = [&](auto a_mn, auto b_mn, const Job &j, int steps) {
+      auto multiply = [&](auto a_mn, auto b_mn, const Job &j, const Share &w) {
         constexpr bool A = decltype(a_mn)::value, B = decltype(b_mn)::value;
         const uint32_t instr = j.instr;
-        const int lead = j.lead, set = j.set;
+        const int lead = w.parts > 1 ? j.lead_part : j.lead, set = j.set;
         const uint64_t p0 = operand(ring, A), q0 = operand(ring + kOperandBytes, B);
-        for (int left = steps, in_set = 0, ends = lead, number = 0; left; --left) {
+        for (int left = w.k1 - w.k0, in_set = 0, ends = lead, number = 0; left; --left) {
           ok = (in_set || bar_wait(sums_empty + 8 * b, sums_phase, abort, wait)) && bar_wait(full + 8 * s, phase, abort, wait);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -798,9 +798,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       };
       Worker worker(a.schedule, pair, pairs);
       for (Share w; ok && worker.next(w);) {
-        if (MODE != kOut) multiply(Int<0>{}, Int<0>{}, a.job[0], w.k1 - w.k0);
-        else if (w.which == 0) multiply(Int<0>{}, Int<1>{}, a.job[0], w.k1 - w.k0);
-        else multiply(Int<1>{}, Int<1>{}, a.job[1], w.k1 - w.k0);
+        if (MODE != kOut) multiply(Int<0>{}, Int<0>{}, a.job[0], w);
+        else if (w.which == 0) multiply(Int<0>{}, Int<1>{}, a.job[0], w);
+        else multiply(Int<1>{}, Int<1>{}, a.job[1], w);
       }
       commit(done);  // nothing is in flight when the block ends
       const long long t0 = clock64();
@@ -848,8 +848,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
       float acc[kHalf] = {};
-      const int steps = w.k1 - w.k0, after = steps - 2 * j.lead;  // (stages after the first two sets)
-      const int sets = after > 0 ? 2 + (after + j.set - 1) / j.set : steps > j.lead ? 2 : 1;
+      const int lead = w.parts > 1 ? j.lead_part : j.lead, steps = w.k1 - w.k0, after = steps - 2 * lead;  // (stages after the first two sets)
+      const int sets = after > 0 ? 2 + (after + j.set - 1) / j.set : steps > lead ? 2 : 1;
       for (int set = 0; set < sets; ++set) {
         const int b = (int)(n & 1);
         ok = __all_sync(0xFFFFFFFFu, bar_wait(sums_full + 8 * b, (uint32_t)(n / 2) & 1, abort, a.wait));  // (a warp gives up as one)
@@ -1545,10 +1545,14 @@ int set_of(bool f32_matrices, int result, int64_t stages, int64_t tokens) {
   return result == kResult16 ? 16 : few || (result == kResult32 && stages <= 12) ? 3 : result == kExactP ? 5 : 8;
 }
 
-// The first two sets of a tile are longer: they are summed while the tile before is finished, or its parts
-// are joined.  A sum of n stages is off by n as a rule, and so is a tile by the mean of its sets' lengths,
-// weighted by them: as long as this leaves it at 11/8 of that of equal sets.
-int lead_of(int set, int64_t stages) { return (int)(0.5 * set + std::sqrt(0.25 * set * set + 0.1875 * set * (double)stages)); }
+// The first two sets of a tile, or of each of its parts, are longer: they are summed while the tile before
+// is finished, or its parts are joined.  A sum of n stages is off by n as a rule, and so is a tile by the
+// mean of its sets' lengths, weighted by them: as long as this leaves it at 11/8 of that of equal sets, and
+// no set at more than 32 stages.  (Parts with the lead of a whole sum had means of up to 23 stages where 3 is
+// usual, and left fp32 dx of 200 tokens x 256, 51200 rows, 3.1e-6 too small.)
+int lead_of(int set, int64_t stages, int64_t parts) {
+  return std::min(32, (int)(0.5 * set + std::sqrt(0.25 * set * set + 0.1875 * set * (double)(stages / parts))));
+}
 
 // D = A B^T; mn: the operand is held transposed
 Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, bool f32_matrices, int result, int64_t tokens) {
@@ -1560,7 +1564,7 @@ Job job_of(const Operand &a, bool a_mn, const Operand &b, bool b_mn, bool f32_ma
     for (int q = 0; q < b.planes; ++q)
       if (p + q < 2) j.plane_a[j.pairs] = p, j.plane_b[j.pairs++] = q;
   const int64_t stages = (int64_t)j.steps * j.pairs;
-  j.set = set_of(f32_matrices, result, stages, tokens), j.lead = lead_of(j.set, stages);
+  j.set = set_of(f32_matrices, result, stages, tokens), j.lead = j.lead_part = lead_of(j.set, stages, 1);
   j.instr = instruction(kTile, a_mn, b_mn, a.bf16);
   j.tiles_n = (j.N + kTile - 1) / kTile;
   j.tiles = (int64_t)((j.M + kTile - 1) / kTile) * j.tiles_n;
@@ -1607,11 +1611,19 @@ Schedule plan(const Job *j, int pairs) {
   if (clocks < least) s.whole = tiles - rest, s.split = 1, s.pool = pool, s.pool_pairs = pool_pairs;
   return s;
 }
+// The parts of a tile of the first product that has several, at most (Worker's).
+int64_t most_parts(const Schedule &s) {
+  int64_t most = s.split;
+  for (int64_t base = 0; base < s.pool; base += s.steps0)
+    most = std::max(most, ((base + s.steps0) * s.pool_pairs - 1) / s.pool - ((base + 1) * s.pool_pairs - 1) / s.pool + 1);
+  return most;
+}
 template <int MODE>
 cudaError_t launch_product(const Maps &m, HeadProduct &g, int sms, cudaStream_t st) {
   auto kernel = head_product_kernel<MODE>;
   const int pairs = sms / 2;
   g.schedule = plan(g.job, pairs);
+  g.job[0].lead_part = lead_of(g.job[0].set, g.schedule.steps0, most_parts(g.schedule));
   const int64_t busy = std::max<int64_t>(g.schedule.pool_pairs, g.schedule.whole * g.schedule.split + g.schedule.tiles1);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (e != cudaSuccess) return e;
