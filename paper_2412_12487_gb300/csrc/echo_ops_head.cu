@@ -762,11 +762,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         else if (w.which == 0) copy(Int<0>{}, Int<1>{}, &amap0, &bmap0, a.job[0], w);
         else copy(Int<1>{}, Int<1>{}, &amap1, &bmap1, a.job[1], w);
       }
-      if (!ok) {  // what is still being copied lands long before this
-        const long long t0 = clock64();
-        while (clock64() - t0 < 1000000) {
-        }
-      }
     } else if (warp == 1 && lane == 0 && rank == 0) {
       const WaitLimit wait = a.wait;
       int s = 0, b = 0;
@@ -1045,6 +1040,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
+  if (give_up) {  // stages and parts of tiles that nobody has waited for may be on their way to this block: they land long before this
+    const long long t0 = clock64();
+    while (clock64() - t0 < 1000000) {
+    }
+  }
   cluster_sync();  // (the other block's products read this one's stages, and signal its barriers)
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
