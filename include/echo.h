@@ -582,8 +582,9 @@ int echo_distill_grad(echo_ctx *ctx, const echo_distill_grad_desc *d);
  * arrays of heads in one pass.  In each head the pairs i of the first `rot` of its `dim`
  * elements, elements (i, i + rot / 2) or, interleaved, (2 i, 2 i + 1), become
  *   a' = scale * (a * cos(w) - b * sin(w)),  b' = scale * (a * sin(w) + b * cos(w)),
- * with w = positions[b][t] * frequencies[i] in radians, exact to fp32's last bits for every
- * position; the other elements are copied.  out has x's type and may be x itself (same
+ * with w = positions[b][t] * frequencies[i] in radians, exact to fp32's last bits for
+ * positions of up to 2^37 either way (beyond, within 2^-62.3 radians a position: 1.9e-7 at
+ * 2^40); the other elements are copied.  out has x's type and may be x itself (same
  * strides).  echo_rotary_grad turns back (w negative): given the gradients of out it
  * returns those of x.
  * Strides are those of a batch, a token and a head; elements of a head are contiguous.  An

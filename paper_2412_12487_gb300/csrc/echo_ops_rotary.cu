@@ -4,9 +4,10 @@
 // the angle position * frequency of the pair; the gradient is the turn back.  Pairs are
 // neighbours, or an element and the one half of `rot` further on.
 //
-// An angle matters modulo a turn.  Frequencies are held as fractions of a turn times 2^64, so
-// the low 64 bits of position * frequency are the angle, for every position, without the digits
-// that 32 bits lose far into a context and without 64-bit floating point.
+// An angle matters modulo a turn.  Frequencies are held as fractions of a turn times 2^64, rounded,
+// so the low 64 bits of position * frequency are the angle, without the digits that 32 bits lose far
+// into a context and without 64-bit floating point.  The half unit that a frequency is off by grows
+// with the position: pi 2^-64 |position| radians, fp32's last bits from 2^38 on (1.9e-7 at 2^40).
 #include <algorithm>
 #include <cmath>
 
@@ -121,13 +122,14 @@ __global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const __grid_consta
 
 }  // namespace
 
-// A frequency in radians as the fraction of a turn, times 2^64; with 1 / (2 pi) in two doubles, so
+// A frequency in radians as the fraction of a turn, times 2^64, rounded; with 1 / (2 pi) in two doubles, so
 // that far positions find all of its bits.
 uint64_t rotary_turns(double f) {
   const double high = 0x1.45f306dc9c883p-3, low = -0x1.6b01ec5417056p-57;
   if (f < 0) return -rotary_turns(-f);
   const double p = f * high, rest = std::fma(f, high, -p) + f * low;
-  return (uint64_t)((p - std::floor(p)) * 0x1p64) + (uint64_t)std::llrint(rest * 0x1p64);  // (the difference is exact)
+  const double at = (p - std::floor(p)) * 0x1p64, whole = std::floor(at);  // (exact, as is their difference)
+  return (uint64_t)whole + (uint64_t)std::llrint(rest * 0x1p64 + (at - whole));
 }
 
 cudaError_t launch_rotary(const RotaryArgs &a, int sms, cudaStream_t st) {
