@@ -392,7 +392,7 @@ def _heads(t, out: bool = False):
         if d == 2:
             return t, 1, 1, (0, 0, strides[0])
         try:
-            return _heads(t.view(-1, *t.shape[-2:]), out)
+            return _heads(t.view(t.shape[:-2].numel(), *t.shape[-2:]), out)
         except RuntimeError:
             pass
     _need(not out, "an output's heads are not contiguous, or its tokens not a fixed distance apart")
@@ -880,7 +880,7 @@ class Echo:
             results.append(y)
             y, _, _, ys = _heads(y, out=True)
             if x.dim() > 4:
-                x = x.reshape(-1, *x.shape[-2:])
+                x = x.reshape(lead.numel(), *x.shape[-2:])
             x, batch, tokens, strides = _heads(x)
             parts.append((x, y, x.shape[-2], strides, ys))
         # positions of all batches, or the same ones for each
