@@ -545,7 +545,11 @@ int echo_cross_entropy_grad(echo_ctx *ctx, const echo_cross_entropy_grad_desc *d
  *   lse = log(sum over the shard's rows of exp(z / T)),
  *   cross = sum of q[k] * z[t][id[k] - vocab_start] / T over the entries of the shard's rows,
  *   loss = T^2 * (sum of q log q + (sum of q) * lse - cross), 0 without entries.
- * Entries with the same id add up.  Shards are put together as for the cross entropy.
+ * Entries with the same id add up.  The loss of the whole vocabulary, from one of its shards
+ * (with rows) that has lse, cross and loss, the logarithm l of the sum of all shards'
+ * exp(lse) and the sum c of all shards' cross, is
+ *   loss + T^2 * (Q * (l - lse) + cross - c),  Q = sum of q: 1 without teacher_lse, else the
+ * sum of exp(logit / T - teacher_lse) over the entries; 0 without entries.
  * n_top is 1 to 256. */
 typedef struct {
   int64_t n_tokens, hidden, vocab_rows, vocab_start, n_top;

@@ -814,7 +814,9 @@ class Echo:
         """(loss, lse, cross), float32 [...], of a student with logits ``scale * x @ weight.T`` against a teacher's top
         ``logits`` [..., top] of tokens ``ids`` (below 0: no entry).  The teacher's probabilities are those among its entries,
         or with ``teacher_lse`` [...] (of all of its logits over the temperature) their own.  ``lse`` is the student's, over the
-        temperature; ``loss`` is temperature^2 times the divergence from the teacher.  Shards as for ``cross_entropy``."""
+        temperature; ``loss`` is temperature^2 times the divergence from the teacher.  Of a shard, the whole vocabulary's is
+        ``loss + temperature^2 * (Q * (l - lse) + cross - c)``, with l and c of all shards (the logarithm of the sum of exp(lse),
+        the sum of cross) and Q the sum of the teacher's probabilities: 1 without ``teacher_lse``, 0 without entries."""
         import torch
         xm, wm, n, v, h, xs, ws, kind = self._head(x, weight)
         bits, ids, logits, teacher_lse, top, lkind = self._teacher(x, ids, logits, teacher_lse)
