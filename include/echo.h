@@ -516,12 +516,17 @@ int echo_cross_entropy(echo_ctx *ctx, const echo_cross_entropy_desc *d);
  * over shards.  dweight is written (accumulate = 0; zeros without tokens) or added to (1).
  * Each of dx and dweight may be NULL.  A token whose dloss (or label) and dlse are 0 has no
  * gradient and adds none to dweight, whatever its x holds.
- * dz is rounded to the matrices' 16-bit type where the results have 16 bits, and taken to 22
- * bits for an fp32 dweight or fp32 matrices; fp16: elements of dz below 2^-29 of the largest
- * are rounded to multiples of 2^-40 of it.  fp32 elements of more than 16 tokens and of the
- * weight with them, and bf16 ones of x for an fp32 dweight, count as above with the largest
- * one of the matrix, for x of the tokens that have a gradient.  Adding to an fp32 dweight
- * may take subnormal numbers as zeros. */
+ * dz, with m the largest bound of any token's (twice its |dloss|, and |dlse|), is taken
+ *   - bf16 matrices, for dx and a 16-bit dweight: as a bf16 number, off by up to 2^-8 of itself;
+ *   - fp16 matrices, the same: as an fp16 number, off by up to 2^-11 of itself or 2^-40 of m;
+ *   - for an fp32 dweight, and with fp32 matrices of more than 16 tokens: as two fp16 numbers,
+ *     off by up to 2^-22 of itself or 2^-40 of m, so that an element of 2^-30 of m has 10 bits
+ *     and one of 2^-40 of m none;
+ *   - with fp32 matrices of up to 16 tokens: in fp32.
+ * fp32 elements of more than 16 tokens and of the weight with them count as above with the
+ * largest one of the matrix instead of the row's, for x of the tokens that have a gradient.
+ * bf16 elements of x for an fp32 dweight are exact down to 2^-31 of that one, and off by up to
+ * 2^-39 of it below.  Adding to an fp32 dweight may take subnormal numbers as zeros. */
 typedef struct {
   int64_t n_tokens, hidden, vocab_rows, vocab_start;
   const float *dloss;       /* [n_tokens]                                               */

@@ -25,7 +25,10 @@
 //     of the others', where the results are rounded to the same (2.4e-3 from 64 bits at the most,
 //     1.7e-3 of which is the result's rounding).  For an fp32 dW as the sum of two fp16 numbers,
 //     with x as fp16 (scaled in the same way): a gradient added up over micro-batches in fp32
-//     would otherwise be 2e-3 off.  That takes dW's products twice.
+//     would otherwise be 2e-3 off.  That takes dW's products twice.  The two have 22 bits down to
+//     2^-18 of P's largest element and an error of 2^-40 of that below: fp16's smallest step is the
+//     same for both, so the rows of tokens that hardly any context expects keep fewer bits (2^-30: 10),
+//     which no error over the whole of dW shows.
 // The tensor core truncates the sums that it adds to, which is a bias, so they are added up in
 // registers, rounding to nearest, every few stages (set_of).
 #include <algorithm>
@@ -67,7 +70,7 @@ __device__ __forceinline__ int exponent_of(float m) { return m > 0.f ? min(126, 
 __device__ __forceinline__ int exponent(Scale s) { return exponent_of(largest(s)); }
 // The same for P, whose largest element becomes 2^15 itself: tokens have the same weight as a rule,
 // and 1 is what its targets then round to, not all of them up or down (that left dx 3.0e-3 off in bf16
-// where a token's weight is 1 / 1984, and 2.4e-3 so).  What P is multiplied by is 2^exponent times this.
+// where a token's weight is 1 / 1984, and 2.0e-3 so).  What P is multiplied by is 2^exponent times this.
 __device__ __forceinline__ float fraction(Scale s) {
   const float m = largest(s), at = ldexpf(m, exponent_of(m));
   return at >= 16384.f && at < 32768.f ? 32768.f / at : 1.f;
@@ -442,7 +445,7 @@ __global__ void __launch_bounds__(kTargetWarps * 32) head_targets_kernel(HeadArg
 //   - logits, 2048 columns, 51200 rows, 64 targets a token: 247 us; 22 rounds where 21.05 would do.
 //   - P, 2048 columns, 25600 rows, three planes: 162 us, 10000 clocks a tile to finish beside the 20000
 //     of its products, which go slower meanwhile.
-//   - dx and dW, 25600 x 2048, fp32 dW (3.2e11 operations on 16-bit numbers twice for dW): 357 us; with a
+//   - dx and dW, 25600 x 2048, fp32 dW (2.15e11 operations on 16-bit numbers for dx, twice that for dW): 357 us; with a
 //     16-bit dW 6400 x 12288: 342 us, 1.88 PFLOP/s.
 // What counted: 32-bit counters and nothing looked up in a stage's way, which single threads take (a
 // stage of 64-bit counters and arguments read from memory: 20% slower); results through the copy engine
@@ -1148,8 +1151,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) head_join_kernel(HeadArgs a, 
 // 256 tokens: with 51200 x 4096 a call takes 485 us forward and 1060 backward from 17 tokens on, whose
 // products alone would be 170.  Up to kFew tokens the products are made in fp32 from the weight as it is,
 // read once for the logits (149 us with one token, 206 with eight, 371 with 16; its 839 MB take 124) and
-// once for dx, and dW is written once (420, 535 and 880 us, of 371).  Above eight tokens their arithmetic
-// is what bounds them: 32 would take 957 us forward.
+// once for dx, and dW is written once (420, 535 and 880 us, of 371).  Above eight tokens it is neither bytes
+// nor arithmetic that bounds them (16: DRAM 28%, the fma pipe 29%): with 128 registers a thread there are 16
+// warps an SM, which issue in half of the cycles and wait for the weight in a third of their time.  32 tokens
+// would take 957 us forward.
 constexpr int kFew = 16, kFewThreads = 256, kFewWarps = kFewThreads / 32;
 constexpr int kFewColumns = 512;   // of x in shared memory at a time
 constexpr int few_rows(int tokens, bool many) { return tokens > 8 ? 4 : many ? 8 : 2; }  // of the weight, of a warp
