@@ -815,7 +815,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     constexpr int kParts = kHalf / 32;
     int down[2] = {0, 0};
     for (int w = 0; w < (MODE == kOut ? 2 : 1); ++w) down[w] = -exponent(a.job[w].scale_a) - exponent(a.job[w].scale_b);
-    const float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
+    float alpha2 = MODE == kOut ? 1.f : ldexpf(a.alpha, down[0]) * kLog2e;  // (sums become logits over ln 2)
     const float p_up = MODE == kGrad ? ldexpf(fraction(a.p_scale), exponent(a.p_scale)) : 1.f, p_down = MODE == kOut ? 1.f / fraction(a.p_scale) : 1.f;
     int64_t n = 0;
     bool ok = true;
@@ -833,7 +833,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       Cursor at;
       at.none();
       float coef = 0.f, shift = 0.f;
-      const int row_down = MODE == kStats && in && a.w_down ? -exponent_of(a.job[0].scale_a.rows[row]) : 0;  // (a power of two of each row)
+      // (fp32: a power of two of each row, one of each row of the weight.  Half of the row's, the weight's, the other half: the two
+      // may be far from one where their product is not, and sums, 2^54 at most, meet neither end of fp32's range on the way)
+      const int row_down = MODE == kStats && in && a.w_down ? -exponent_of(a.job[0].scale_a.rows[row]) : 0;
+      if (MODE == kStats && a.w_down) alpha2 = ldexpf(a.alpha, row_down / 2) * kLog2e;
       if (MODE != kOut && in) {
         at.start(a.idx + row * a.K, MODE == kGrad ? a.weight + row * a.K : nullptr, a.K, a.v_begin, c0);
         if (MODE == kGrad) {
@@ -926,16 +929,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
       }
       if constexpr (MODE == kStats) {
-        if (a.w_down) {  // (fp32: a power of two of each row of the weight; the array is as long as the tiles)
-          // Half of the token's power, the weight's, the other half: the two powers may be far from one
-          // where their product is not, and sums (2^54 at most) meet neither end of fp32's range on the way.
-          const float r1 = ldexpf(1.f, row_down / 2), r2 = ldexpf(1.f, row_down - row_down / 2);
+        if (a.w_down) {  // (the array is as long as the tiles)
+          const float rest = ldexpf(1.f, row_down - row_down / 2);
 #pragma unroll
           for (int e = 0; e < kHalf; e += 4) {
             const float4 f = *reinterpret_cast<const float4 *>(a.w_down + c0 + e);
-            acc[e] *= r1, acc[e + 1] *= r1, acc[e + 2] *= r1, acc[e + 3] *= r1;
-            acc[e] *= f.x, acc[e + 1] *= f.y, acc[e + 2] *= f.z, acc[e + 3] *= f.w;
-            acc[e] *= r2, acc[e + 1] *= r2, acc[e + 2] *= r2, acc[e + 3] *= r2;
+            acc[e] = acc[e] * f.x * rest, acc[e + 1] = acc[e + 1] * f.y * rest;
+            acc[e + 2] = acc[e + 2] * f.z * rest, acc[e + 3] = acc[e + 3] * f.w * rest;
           }
         }
         if (c0 + kHalf > j.N)
